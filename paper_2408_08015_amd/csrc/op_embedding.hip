@@ -41,47 +41,305 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const int32_t* __res
 // ids outside the table sort behind every row
 __device__ __forceinline__ uint32_t sort_key(int32_t id, uint32_t rows) { return min((uint32_t)id, rows); }
 
-__global__ __launch_bounds__(256) void embedding_zero_kernel(float4* __restrict__ p, size_t n4, float* __restrict__ tail, int rest) {
-  for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n4; i += (size_t)gridDim.x * 256)
+// The gradient of a large table is mostly zeros, and writing them takes longer than the sort: they are written by blocks of
+// their own beside the blocks of the sort's launches, a share with each.
+struct ZeroShare {
+  float* p;         // 16-byte aligned
+  size_t n4;        // groups of four
+  float* edge[2];   // what is left in front of and behind the aligned part: single values
+  int edges[2];
+};
+
+__device__ __forceinline__ void zero_share(const ZeroShare& z, unsigned block, unsigned blocks) {
+  float4* const p = reinterpret_cast<float4*>(z.p);
+  for (size_t i = (size_t)block * blockDim.x + threadIdx.x; i < z.n4; i += (size_t)blocks * blockDim.x)
     p[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (blockIdx.x == 0 && (int)threadIdx.x < rest) tail[threadIdx.x] = 0.f;
+  if (block == 0)
+    for (int e = 0; e < 2; ++e)
+      if ((int)threadIdx.x < z.edges[e]) z.edge[e][threadIdx.x] = 0.f;
 }
 
-// Place of every token in the order: the number of tokens in front of it, counted.
-__global__ __launch_bounds__(256) void embedding_rank_kernel(const int32_t* __restrict__ ids, int64_t tokens, uint32_t rows,
-                                                             uint32_t* __restrict__ key, uint32_t* __restrict__ order) {
-  __shared__ uint32_t sk[1024];
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const uint32_t mine = t < tokens ? sort_key(ids[t], rows) : 0xffffffffu;
-  uint32_t rank = 0;
-  for (int64_t u0 = 0; u0 < tokens; u0 += 1024) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < 1024; i += 256) sk[i] = u0 + i < tokens ? sort_key(ids[u0 + i], rows) : 0xffffffffu;
-    __syncthreads();
-    const int n = (int)min((int64_t)1024, tokens - u0);
-    for (int i = 0; i < n; ++i) rank += sk[i] < mine || (sk[i] == mine && u0 + i < t);
+// Order of few tokens: the place of a token is the number of tokens in front of it, counted.  A block places 64 tokens; each
+// of its 16 wavefronts counts over its share of all tokens, whose ids are the same for every lane (scalar loads: two
+// vector instructions a comparison).
+constexpr int RANK_WAVES = 16;
+__global__ __launch_bounds__(64 * RANK_WAVES) void embedding_rank_kernel(const int32_t* __restrict__ ids, int tokens,
+                                                                         uint32_t rows, uint32_t* __restrict__ key,
+                                                                         uint32_t* __restrict__ order, unsigned sort_blocks,
+                                                                         ZeroShare z) {
+  if (blockIdx.x >= sort_blocks) {
+    zero_share(z, blockIdx.x - sort_blocks, gridDim.x - sort_blocks);
+    return;
   }
-  if (t < tokens) {
+  __shared__ uint32_t part[RANK_WAVES][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t0 = blockIdx.x * 64, t = t0 + lane;
+  const uint32_t mine = t < tokens ? sort_key(ids[t], rows) : 0;
+  uint32_t rank = 0;
+  // shares of whole groups of 64, so that one of them is exactly the block's own tokens
+  const int groups = (tokens + 63) / 64, per = (groups + RANK_WAVES - 1) / RANK_WAVES;
+  for (int g = wave * per; g < min((wave + 1) * per, groups); ++g) {
+    const int u0 = g * 64, n = min(64, tokens - u0);
+    const uint32_t limit = mine + (u0 < t0 ? 1 : 0);  // an equal id in front counts
+    if (u0 == t0) {
+      for (int i = 0; i < n; ++i) rank += sort_key(ids[u0 + i], rows) < mine + (i < lane ? 1u : 0u);
+    } else if (n == 64) {
+#pragma unroll 16
+      for (int i = 0; i < 64; ++i) rank += sort_key(ids[u0 + i], rows) < limit;
+    } else {
+      for (int i = 0; i < n; ++i) rank += sort_key(ids[u0 + i], rows) < limit;
+    }
+  }
+  part[wave][lane] = rank;
+  __syncthreads();
+  if (wave == 0 && t < tokens) {
+    rank = 0;
+#pragma unroll
+    for (int w = 0; w < RANK_WAVES; ++w) rank += part[w][lane];
     key[rank] = mine;
     order[rank] = (uint32_t)t;
   }
 }
 
-// One wavefront per run of equal ids.
-template <typename T>
-__global__ __launch_bounds__(256) void embedding_runs_kernel(const uint32_t* __restrict__ key, const uint32_t* __restrict__ order,
-                                                             int64_t tokens, uint32_t rows, int width, const T* __restrict__ dy,
-                                                             float scale, int accumulate, float* __restrict__ dtable) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < tokens; i += (int64_t)gridDim.x * 4) {
-    const uint32_t k = key[i];
-    if (k >= rows || (i > 0 && key[i - 1] == k)) continue;
-    for (int c = lane; c < width; c += 64) {
-      double s = 0;
-      for (int64_t j = i; j < tokens && key[j] == k; ++j) s += load1(dy + (size_t)order[j] * width + c);
-      float* out = dtable + (size_t)k * width + c;
-      *out = (accumulate ? *out : 0.f) + (float)s * scale;
+// Order of many tokens: passes over digits of up to nine bits, from the lowest, each stable.  A tile of tokens is one block's;
+// a pass counts the digits of every tile and then places the tiles' tokens.
+constexpr int RADIX_BITS = 9, RADIX_BINS = 1 << RADIX_BITS;
+constexpr int RADIX_STEP = 2048;  // tokens of a tile at a time: 8 of a thread
+constexpr int RADIX_TILES = 256;  // at most
+
+struct RadixArgs {
+  const int32_t* ids;                          // first pass
+  const uint32_t *key_in, *order_in;           // later ones
+  uint32_t *key, *order;
+  uint32_t* count;                             // [tiles][bins]
+  int64_t tokens, tile;
+  uint32_t rows;
+  int shift, bits;
+  unsigned tiles;
+};
+
+__device__ __forceinline__ uint32_t radix_key(const RadixArgs& a, int64_t i) {
+  return a.ids ? sort_key(a.ids[i], a.rows) : a.key_in[i];
+}
+
+__global__ __launch_bounds__(256) void embedding_count_kernel(const RadixArgs a, ZeroShare z) {
+  if (blockIdx.x >= a.tiles) {
+    zero_share(z, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+    return;
+  }
+  __shared__ uint32_t bin[RADIX_BINS];
+  const int bins = 1 << a.bits;
+  for (int b = threadIdx.x; b < bins; b += 256) bin[b] = 0;
+  __syncthreads();
+  const int64_t lo = blockIdx.x * a.tile, hi = min(lo + a.tile, a.tokens);
+  for (int64_t i = lo + threadIdx.x; i < hi; i += 256) atomicAdd(&bin[(radix_key(a, i) >> a.shift) & (bins - 1)], 1u);
+  __syncthreads();
+  for (int b = threadIdx.x; b < bins; b += 256) a.count[(size_t)blockIdx.x * bins + b] = bin[b];
+}
+
+__global__ __launch_bounds__(256) void embedding_place_kernel(const RadixArgs a, ZeroShare z) {
+  if (blockIdx.x >= a.tiles) {
+    zero_share(z, blockIdx.x - a.tiles, gridDim.x - a.tiles);
+    return;
+  }
+  __shared__ uint32_t next[RADIX_BINS];          // where the next token of a digit goes
+  __shared__ uint32_t seen[4][RADIX_BINS];       // tokens of a digit that each wavefront holds of this step
+  __shared__ uint32_t wsum[4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int bins = 1 << a.bits;
+  {  // first place of a digit in this tile: all smaller digits, and this digit in the tiles in front
+    uint32_t before[2] = {0, 0}, all[2] = {0, 0};
+    for (int k = 0; k < 2; ++k) {
+      const int b = 2 * tid + k;
+      if (b < bins)
+        for (unsigned t = 0; t < a.tiles; ++t) {
+          const uint32_t c = a.count[(size_t)t * bins + b];
+          if (t < blockIdx.x) before[k] += c;
+          all[k] += c;
+        }
     }
+    uint32_t sum = all[0] + all[1];  // inclusive prefix over the threads
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t v = __shfl_up(sum, o, 64);
+      if (lane >= o) sum += v;
+    }
+    if (lane == 63) wsum[wave] = sum;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) sum += wsum[w];
+    const uint32_t start = sum - all[0] - all[1];
+    if (2 * tid < bins) next[2 * tid] = start + before[0];
+    if (2 * tid + 1 < bins) next[2 * tid + 1] = start + all[0] + before[1];
+  }
+  const int64_t lo = blockIdx.x * a.tile, hi = min(lo + a.tile, a.tokens);
+  for (int64_t s = lo; s < hi; s += RADIX_STEP) {
+    __syncthreads();
+    for (int b = tid; b < 4 * RADIX_BINS; b += 256) (&seen[0][0])[b] = 0;
+    __syncthreads();
+    // a wavefront holds 512 consecutive tokens, 64 at a time; tokens of equal digit are numbered in their order
+    uint32_t k[8], o[8], at[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const int64_t i = s + wave * 512 + r * 64 + lane;
+      const bool on = i < hi;
+      k[r] = on ? radix_key(a, i) : 0;
+      o[r] = on ? (a.ids ? (uint32_t)i : a.order_in[i]) : 0;
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      const bool on = s + wave * 512 + r * 64 + lane < hi;
+      const uint32_t d = (k[r] >> a.shift) & (bins - 1);
+      uint64_t same = __ballot(on);
+      for (int b = 0; b < a.bits; ++b) {
+        const uint64_t bit = __ballot((d >> b) & 1);
+        same &= (d >> b) & 1 ? bit : ~bit;
+      }
+      const uint64_t below = same & ((1ull << lane) - 1);
+      at[r] = 0;
+      if (on) {
+        at[r] = seen[wave][d] + (uint32_t)__popcll(below);
+        if (below == 0) seen[wave][d] += (uint32_t)__popcll(same);  // (behind every lane's read: a wavefront's LDS accesses are in order)
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      if (s + wave * 512 + r * 64 + lane >= hi) continue;
+      const uint32_t d = (k[r] >> a.shift) & (bins - 1);
+      uint32_t p = next[d] + at[r];
+      for (int w = 0; w < wave; ++w) p += seen[w][d];
+      a.key[p] = k[r];
+      a.order[p] = o[r];
+    }
+    __syncthreads();
+    for (int b = tid; b < bins; b += 256) next[b] += seen[0][b] + seen[1][b] + seen[2][b] + seen[3][b];
+  }
+}
+
+// Sums over the sorted tokens.  A wavefront takes `chunk` of them and 512 columns, eight a lane, and adds up runs of equal
+// ids; a run that lies inside the chunk is a row's gradient, one that crosses its border leaves a partial: part[c][0] where it
+// began in front of the chunk, part[c][1] where it begins in it.
+struct SumArgs {
+  const uint32_t *key, *order;
+  int64_t tokens;
+  uint32_t rows;
+  int width, chunk, accumulate;
+  float scale;
+  float* dtable;
+  float* part;  // [chunks][2][width]
+};
+
+constexpr int SUM_COLS = 512;
+
+__device__ __forceinline__ void put_row(const SumArgs& g, uint32_t k, int c, const double (&v)[8]) {
+  float* p = g.dtable + (size_t)k * g.width + c;
+  const int n = g.width - c;
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = 0.f;
+  if (g.accumulate) {
+    if (n >= 8) load8(p, f);
+    else load8_part(p, n, f);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = fmaf((float)v[i], g.scale, f[i]);
+  if (n >= 8) store8(p, f);
+  else store8_part(p, n, f);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(const SumArgs g, const T* __restrict__ dy) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t chunk_id = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t lo = chunk_id * g.chunk, hi = min(lo + g.chunk, g.tokens);
+  if (lo >= hi) return;
+  const int c = blockIdx.y * SUM_COLS + lane * 8, n = g.width - c;
+  if (g.key[lo] >= g.rows) return;  // behind the last row: padding
+  const bool began = lo > 0 && g.key[lo - 1] == g.key[lo];
+  const uint32_t next = hi < g.tokens ? g.key[hi] : 0xffffffffu;
+  float acc[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+  uint32_t cur = g.key[lo];
+  bool first = true;
+  auto flush = [&](bool last) __attribute__((always_inline)) {
+    if (n <= 0 || cur >= g.rows) return;
+    const bool open = first && began;
+    if (open || (last && next == cur)) {
+      float* p = g.part + ((size_t)chunk_id * 2 + (open ? 0 : 1)) * g.width + c;
+      if (n >= 8) store8(p, acc);
+      else store8_part(p, n, acc);
+    } else {
+      double v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = acc[i];
+      put_row(g, cur, c, v);
+    }
+  };
+  for (int64_t i = lo; i < hi; i += 8) {
+    float v[8][8];
+    uint32_t k[8];
+    const int m = (int)min((int64_t)8, hi - i);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      k[r] = r < m ? g.key[i + r] : 0xffffffffu;
+      const T* src = dy + (size_t)(r < m ? g.order[i + r] : 0) * g.width + c;
+      if (r < m && n >= 8) load8(src, v[r]);
+      else load8_part(src, r < m ? n : 0, v[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      if (r >= m) break;
+      if (k[r] != cur) {
+        flush(false);
+        first = false;
+        cur = k[r];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += v[r][e];
+    }
+  }
+  flush(true);
+}
+
+// Runs that cross chunks: the block of the chunk in which one begins adds up its partials, each wavefront every eighth, in 64
+// bits, and the wavefronts' sums in their order.
+__global__ __launch_bounds__(512) void embedding_join_kernel(const SumArgs g) {
+  __shared__ double sh[8][SUM_COLS];
+  const int64_t c0 = blockIdx.x;
+  const int64_t lo = c0 * g.chunk, hi = lo + g.chunk;  // (the last chunk has no block)
+  const uint32_t k = g.key[hi - 1];
+  if (k >= g.rows || g.key[hi] != k) return;                                      // nothing goes on behind this chunk
+  if (g.key[lo] == k && lo > 0 && g.key[lo - 1] == k) return;                     // it began in front of it
+  // last chunk of the run: the first place behind it, by bisection
+  int64_t a = hi, b = g.tokens;
+  while (a < b) {
+    const int64_t m = (a + b) / 2;
+    if (g.key[m] == k) a = m + 1; else b = m;
+  }
+  const int64_t last = (a - 1) / g.chunk;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int c = blockIdx.y * SUM_COLS + lane * 8, n = g.width - c;
+  double v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = 0;
+  for (int64_t j = c0 + wave; j <= last; j += 8) {
+    const float* p = g.part + ((size_t)j * 2 + (j == c0 ? 1 : 0)) * g.width + c;
+    float f[8];
+    if (n >= 8) load8(p, f);
+    else load8_part(p, n, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += f[i];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sh[wave][i * 64 + lane] = v[i];
+  __syncthreads();
+  if (wave == 0 && n > 0) {
+    for (int w = 1; w < 8; ++w)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += sh[w][i * 64 + lane];
+    put_row(g, k, c, v);
   }
 }
 
@@ -109,31 +367,127 @@ void embedding_fwd(hipStream_t st, const int32_t* ids, int64_t tokens, const voi
 #undef LAUNCH
 }
 
-size_t embedding_bwd_ws_bytes(int64_t tokens, int64_t, int64_t) { return ((size_t)tokens * 8 + 15) / 16 * 16; }
+namespace {
+
+constexpr int64_t RANK_MOST = 16384;  // tokens that are placed by counting
+
+int chunk_of(int64_t tokens) {  // tokens of a wavefront: the chip filled, and no more than 8192 partials
+  int c = 8;
+  while (c < 32 && tokens / c >= 2048) c *= 2;
+  while ((tokens + c - 1) / c > 8192) c *= 2;
+  return c;
+}
+int64_t chunks_of(int64_t tokens) { return (tokens + chunk_of(tokens) - 1) / chunk_of(tokens); }
+size_t align16(size_t v) { return (v + 15) / 16 * 16; }
+
+int radix_passes(int64_t rows, int* bits) {  // digits of equal size for the keys 0 .. rows
+  int b = 1;
+  while (((int64_t)1 << b) <= rows) ++b;
+  const int passes = (b + RADIX_BITS - 1) / RADIX_BITS;
+  *bits = (b + passes - 1) / passes;
+  return passes;
+}
+int64_t radix_tile(int64_t tokens) {
+  const int64_t per = (tokens + RADIX_TILES - 1) / RADIX_TILES;
+  return (per + RADIX_STEP - 1) / RADIX_STEP * RADIX_STEP;
+}
+
+}  // namespace
+
+// key and order, for the radix passes twice, the digit counts; then the partials
+size_t embedding_bwd_ws_bytes(int64_t tokens, int64_t, int64_t width) {
+  if (tokens <= 0) return 0;
+  const size_t lists = align16((size_t)tokens * 4) * (tokens > RANK_MOST ? 4 : 2);
+  const size_t counts = tokens > RANK_MOST ? (size_t)RADIX_TILES * RADIX_BINS * 4 : 0;
+  return lists + counts + align16((size_t)chunks_of(tokens) * 2 * width * 4);
+}
 
 void embedding_bwd(hipStream_t st, const int32_t* ids, int64_t tokens, const void* dy, bool dy_bf16, int64_t rows,
                    int64_t width, float scale, bool accumulate, float* dtable, void* ws) {
-  uint32_t* key = static_cast<uint32_t*>(ws);
-  uint32_t* order = key + tokens;
-  if (!accumulate) {
-    const size_t n = (size_t)rows * width;
-    // (16-byte writes from the first address that allows them)
-    size_t head = std::min<size_t>((16 - (reinterpret_cast<uintptr_t>(dtable) & 15)) / 4 % 4, n);
-    const size_t n4 = (n - head) / 4;
-    const unsigned blocks = (unsigned)std::min<size_t>(n4 / 256 + 1, 8192);
-    KLAUNCH(embedding_zero_kernel, dim3(blocks), dim3(256), 0, st, reinterpret_cast<float4*>(dtable + head), n4,
-            dtable + head + 4 * n4, (int)(n - head - 4 * n4));
-    if (head) KLAUNCH(embedding_zero_kernel, dim3(1), dim3(256), 0, st, nullptr, 0, dtable, (int)head);
+  char* at = static_cast<char*>(ws);
+  auto take = [&](size_t bytes) { char* p = at; at += align16(bytes); return p; };
+  const bool radix = tokens > RANK_MOST;
+  int bits = 0;
+  const int passes = radix ? radix_passes(rows, &bits) : 0;
+  const int shares = tokens <= 0 ? 1 : radix ? 2 * passes : 1;
+
+  // zeros: a 16-byte aligned middle in equal shares, the edges with the first
+  const size_t n = accumulate ? 0 : (size_t)rows * width;
+  const size_t head = std::min<size_t>((16 - (reinterpret_cast<uintptr_t>(dtable) & 15)) / 4 % 4, n);
+  const size_t n4 = (n - head) / 4;
+  auto share = [&](int i) {
+    ZeroShare z = {};
+    const size_t lo = n4 * i / shares, hi = n4 * (i + 1) / shares;
+    z.p = dtable + head + 4 * lo;
+    z.n4 = hi - lo;
+    if (i == 0) {
+      z.edge[0] = dtable;
+      z.edges[0] = (int)head;
+      z.edge[1] = dtable + head + 4 * n4;
+      z.edges[1] = (int)(n - head - 4 * n4);
+    }
+    return z;
+  };
+  auto zero_blocks = [&](const ZeroShare& z, unsigned threads) {
+    if (!z.n4 && !z.edges[0] && !z.edges[1]) return 0u;
+    return (unsigned)std::min<size_t>(z.n4 / (4 * threads) + 1, 4096);
+  };
+
+  if (tokens <= 0) {
+    const ZeroShare z = share(0);
+    const unsigned zb = zero_blocks(z, 64 * RANK_WAVES);
+    if (zb) KLAUNCH(embedding_rank_kernel, dim3(zb), dim3(64 * RANK_WAVES), 0, st, ids, 0, 0u, nullptr, nullptr, 0u, z);
+    return;
   }
-  if (tokens <= 0) return;
-  KLAUNCH(embedding_rank_kernel, dim3((unsigned)((tokens + 255) / 256)), dim3(256), 0, st, ids, tokens, (uint32_t)rows, key, order);
-  const unsigned blocks = (unsigned)std::min<int64_t>((tokens + 3) / 4, 1 << 16);
-  if (dy_bf16)
-    KLAUNCH(embedding_runs_kernel<bf16_t>, dim3(blocks), dim3(256), 0, st, key, order, tokens, (uint32_t)rows, (int)width,
-            static_cast<const bf16_t*>(dy), scale, (int)accumulate, dtable);
-  else
-    KLAUNCH(embedding_runs_kernel<float>, dim3(blocks), dim3(256), 0, st, key, order, tokens, (uint32_t)rows, (int)width,
-            static_cast<const float*>(dy), scale, (int)accumulate, dtable);
+  uint32_t* key = reinterpret_cast<uint32_t*>(take((size_t)tokens * 4));
+  uint32_t* order = reinterpret_cast<uint32_t*>(take((size_t)tokens * 4));
+  if (!radix) {
+    const ZeroShare z = share(0);
+    const unsigned sort = (unsigned)((tokens + 63) / 64);
+    KLAUNCH(embedding_rank_kernel, dim3(sort + zero_blocks(z, 64 * RANK_WAVES)), dim3(64 * RANK_WAVES), 0, st, ids, (int)tokens,
+            (uint32_t)rows, key, order, sort, z);
+  } else {
+    RadixArgs a = {};
+    uint32_t* key2 = reinterpret_cast<uint32_t*>(take((size_t)tokens * 4));
+    uint32_t* order2 = reinterpret_cast<uint32_t*>(take((size_t)tokens * 4));
+    a.count = reinterpret_cast<uint32_t*>(take((size_t)RADIX_TILES * RADIX_BINS * 4));
+    a.tokens = tokens;
+    a.tile = radix_tile(tokens);
+    a.tiles = (unsigned)((tokens + a.tile - 1) / a.tile);
+    a.rows = (uint32_t)rows;
+    a.bits = bits;
+    uint32_t *ka = key2, *oa = order2;
+    for (int p = 0; p < passes; ++p) {
+      a.ids = p == 0 ? ids : nullptr;
+      a.key_in = key;
+      a.order_in = order;
+      a.key = ka;
+      a.order = oa;
+      a.shift = p * bits;
+      const ZeroShare z0 = share(2 * p), z1 = share(2 * p + 1);
+      KLAUNCH(embedding_count_kernel, dim3(a.tiles + zero_blocks(z0, 256)), dim3(256), 0, st, a, z0);
+      KLAUNCH(embedding_place_kernel, dim3(a.tiles + zero_blocks(z1, 256)), dim3(256), 0, st, a, z1);
+      std::swap(ka, key);
+      std::swap(oa, order);
+    }
+  }
+  SumArgs g = {};
+  g.key = key;
+  g.order = order;
+  g.tokens = tokens;
+  g.rows = (uint32_t)rows;
+  g.width = (int)width;
+  g.chunk = chunk_of(tokens);
+  g.accumulate = accumulate;
+  g.scale = scale;
+  g.dtable = dtable;
+  const int64_t chunks = chunks_of(tokens);
+  g.part = reinterpret_cast<float*>(take((size_t)chunks * 2 * width * 4));
+  const unsigned cols = (unsigned)((width + SUM_COLS - 1) / SUM_COLS);
+  const dim3 grid((unsigned)((chunks + 3) / 4), cols);
+  if (dy_bf16) KLAUNCH(embedding_sum_kernel<bf16_t>, grid, dim3(256), 0, st, g, static_cast<const bf16_t*>(dy));
+  else KLAUNCH(embedding_sum_kernel<float>, grid, dim3(256), 0, st, g, static_cast<const float*>(dy));
+  if (chunks > 1) KLAUNCH(embedding_join_kernel, dim3((unsigned)(chunks - 1), cols), dim3(512), 0, st, g);
 }
 
 }  // namespace ast
