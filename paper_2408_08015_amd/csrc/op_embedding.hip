@@ -60,8 +60,8 @@ __device__ __forceinline__ void zero_share(const ZeroShare& z, unsigned block, u
 }
 
 // Order of few tokens: the place of a token is the number of tokens in front of it, counted.  A block places 64 tokens; each
-// of its 16 wavefronts counts over its share of all tokens, whose ids are the same for every lane (scalar loads: two
-// vector instructions a comparison).
+// of its 16 wavefronts counts over its share of all tokens, 64 of them in a register of the wavefront, handed out one by one
+// to all lanes (three vector instructions a comparison, and no memory access among them).
 constexpr int RANK_WAVES = 16;
 __global__ __launch_bounds__(64 * RANK_WAVES) void embedding_rank_kernel(const int32_t* __restrict__ ids, int tokens,
                                                                          uint32_t rows, uint32_t* __restrict__ key,
@@ -74,21 +74,26 @@ __global__ __launch_bounds__(64 * RANK_WAVES) void embedding_rank_kernel(const i
   __shared__ uint32_t part[RANK_WAVES][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t0 = blockIdx.x * 64, t = t0 + lane;
-  const uint32_t mine = t < tokens ? sort_key(ids[t], rows) : 0;
-  uint32_t rank = 0;
   // shares of whole groups of 64, so that one of them is exactly the block's own tokens
   const int groups = (tokens + 63) / 64, per = (groups + RANK_WAVES - 1) / RANK_WAVES;
-  for (int g = wave * per; g < min((wave + 1) * per, groups); ++g) {
-    const int u0 = g * 64, n = min(64, tokens - u0);
-    const uint32_t limit = mine + (u0 < t0 ? 1 : 0);  // an equal id in front counts
-    if (u0 == t0) {
-      for (int i = 0; i < n; ++i) rank += sort_key(ids[u0 + i], rows) < mine + (i < lane ? 1u : 0u);
-    } else if (n == 64) {
-#pragma unroll 16
-      for (int i = 0; i < 64; ++i) rank += sort_key(ids[u0 + i], rows) < limit;
+  const int g0 = wave * per, g1 = min(g0 + per, groups);
+  // (behind the last token: a key that is in front of no token)
+  auto load = [&](int g) { const int u = g * 64 + lane; return g < g1 && u < tokens ? sort_key(ids[u], rows) : 0xffffffffu; };
+  uint32_t cur = load(g0), next = load(g0 + 1);
+  const uint32_t mine = t < tokens ? sort_key(ids[t], rows) : 0;
+  uint32_t rank = 0;
+  for (int g = g0; g < g1; ++g) {
+    const uint32_t after = load(g + 2);
+    if (g * 64 == t0) {
+#pragma unroll
+      for (int i = 0; i < 64; ++i) rank += (uint32_t)__builtin_amdgcn_readlane(cur, i) < mine + (i < lane ? 1u : 0u);
     } else {
-      for (int i = 0; i < n; ++i) rank += sort_key(ids[u0 + i], rows) < limit;
+      const uint32_t limit = mine + (g * 64 < t0 ? 1 : 0);  // an equal id in front counts
+#pragma unroll
+      for (int i = 0; i < 64; ++i) rank += (uint32_t)__builtin_amdgcn_readlane(cur, i) < limit;
     }
+    cur = next;
+    next = after;
   }
   part[wave][lane] = rank;
   __syncthreads();
@@ -149,14 +154,16 @@ __global__ __launch_bounds__(256) void embedding_place_kernel(const RadixArgs a,
   const int bins = 1 << a.bits;
   {  // first place of a digit in this tile: all smaller digits, and this digit in the tiles in front
     uint32_t before[2] = {0, 0}, all[2] = {0, 0};
-    for (int k = 0; k < 2; ++k) {
-      const int b = 2 * tid + k;
-      if (b < bins)
-        for (unsigned t = 0; t < a.tiles; ++t) {
-          const uint32_t c = a.count[(size_t)t * bins + b];
-          if (t < blockIdx.x) before[k] += c;
-          all[k] += c;
-        }
+    if (2 * tid < bins) {
+      const uint2* const c = reinterpret_cast<const uint2*>(a.count) + tid;  // (two digits, of one tile after the other)
+#pragma unroll 16
+      for (unsigned t = 0; t < a.tiles; ++t) {
+        const uint2 v = c[(size_t)t * (bins / 2)];
+        before[0] += t < blockIdx.x ? v.x : 0;
+        before[1] += t < blockIdx.x ? v.y : 0;
+        all[0] += v.x;
+        all[1] += v.y;
+      }
     }
     uint32_t sum = all[0] + all[1];  // inclusive prefix over the threads
     for (int o = 1; o < 64; o <<= 1) {
@@ -324,13 +331,19 @@ __global__ __launch_bounds__(512) void embedding_join_kernel(const SumArgs g) {
   double v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 0;
-  for (int64_t j = c0 + wave; j <= last; j += 8) {
-    const float* p = g.part + ((size_t)j * 2 + (j == c0 ? 1 : 0)) * g.width + c;
-    float f[8];
-    if (n >= 8) load8(p, f);
-    else load8_part(p, n, f);
+  for (int64_t j0 = c0 + wave; j0 <= last; j0 += 32) {  // four loads at a time
+    float f[4][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += f[i];
+    for (int q = 0; q < 4; ++q) {
+      const int64_t j = j0 + 8 * q;
+      const float* p = g.part + ((size_t)j * 2 + (j == c0 ? 1 : 0)) * g.width + c;
+      if (j <= last && n >= 8) load8(p, f[q]);
+      else load8_part(p, j <= last ? n : 0, f[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += f[q][i];
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) sh[wave][i * 64 + lane] = v[i];

@@ -18,30 +18,31 @@ namespace ast {
 
 namespace {
 
-struct HeadsIn { const void* p; int64_t ts, hs; };
-struct HeadsOut { void* p; int64_t ts, hs; };
+struct HeadsAt { const void* p; int64_t ts, hs; };
 
 struct QkArgs {
-  HeadsIn x[2], dy[2];  // queries, keys
-  HeadsOut y[2];        // y, or dx
+  HeadsAt x[2], dy[2], y[2];  // queries, keys; y: the result, or dx
   const float* gain[2];
   const int32_t* pos;
-  float* part;          // backward: [blocks][2][head_dim] sums of du * n
+  float* part;                // backward: [blocks][head_dim] sums of du * n
   int64_t tokens;
   double log2_theta;
-  float eps, inv_dim;
+  float eps, inv_dim, inv_heads[2];
   int period, heads[2], dim, rotary;
-  int units, rot_units; // units (a lane's places) of a head, and how many of them rotate
-  int ls;               // log2 of the lanes of a head
-  int tb;               // tokens a block takes at a time
+  int units, rot_units;       // units (a lane's places) of a head, and how many of them rotate
+  int ls;                     // log2 of the lanes of a head
+  int tb[2];                  // tokens a block takes at a time
+  unsigned blocks_q;          // the first blocks take queries, the others keys
 };
 
 constexpr int QK_TRIG = 2048;  // pairs (cos, sin) of a block's tokens
+constexpr int QK_ROWS = 4;     // heads that a lane has in flight
 
+// VEC consecutive values: as they are loaded, and as numbers
 template <typename T, int VEC> struct Vec;
 template <> struct Vec<bf16_t, 8> {
-  static __device__ __forceinline__ void load(const bf16_t* p, float (&v)[8]) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
+  typedef uint4 Raw;
+  static __device__ __forceinline__ void expand(const Raw& a, float (&v)[8]) {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -54,16 +55,15 @@ template <> struct Vec<bf16_t, 8> {
   }
 };
 template <> struct Vec<float, 4> {
-  static __device__ __forceinline__ void load(const float* p, float (&v)[4]) {
-    const float4 a = *reinterpret_cast<const float4*>(p);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-  }
+  typedef float4 Raw;
+  static __device__ __forceinline__ void expand(const Raw& a, float (&v)[4]) { v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; }
   static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   }
 };
 template <typename T> struct Vec<T, 1> {
-  static __device__ __forceinline__ void load(const T* p, float (&v)[1]) { v[0] = load1(p); }
+  typedef T Raw;
+  static __device__ __forceinline__ void expand(const Raw& a, float (&v)[1]) { v[0] = load1(&a); }
   static __device__ __forceinline__ void store(T* p, const float (&v)[1]) { store1(p, v[0]); }
 };
 
@@ -81,14 +81,20 @@ __device__ __forceinline__ float head_sum(float v, int ls) {
 // One lane's share of a head: IT units of 2 x VEC values.
 template <typename T, int VEC, int IT, bool INTER, bool BWD>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
+  typedef Vec<T, VEC> V;
   __shared__ __attribute__((aligned(16))) float2 trig[QK_TRIG];
   __shared__ float red[BWD ? 4 * 256 : 1];
   const int tid = threadIdx.x, lane = tid & ((1 << g.ls) - 1), group = tid >> g.ls, groups = 256 >> g.ls;
   const int half = g.rotary / 2;
+  const int w = blockIdx.x >= g.blocks_q;
+  const unsigned block = blockIdx.x - (w ? g.blocks_q : 0), blocks = w ? gridDim.x - g.blocks_q : g.blocks_q;
+  const int H = g.heads[w], tb = g.tb[w];
+  const HeadsAt X = g.x[w], D = g.dy[w], Y = g.y[w];
 
-  // this lane's places in a head
+  // this lane's places in a head, and their gains
   int pa[IT], pb[IT], pair[IT];
   bool on_a[IT], on_b[IT], rot[IT];
+  float gain[IT][2][VEC], acc[IT][2][VEC];
 #pragma unroll
   for (int i = 0; i < IT; ++i) {
     const int u = lane + (i << g.ls);
@@ -103,6 +109,12 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
     }
     on_a[i] = u < g.units;  // (a unit's first place always exists)
     on_b[i] = on_a[i] && pb[i] < g.dim;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      gain[i][0][e] = on_a[i] ? g.gain[w][pa[i] + e] : 0.f;
+      gain[i][1][e] = on_b[i] ? g.gain[w][pb[i] + e] : 0.f;
+      acc[i][0][e] = acc[i][1][e] = 0.f;
+    }
   }
   // this thread's share of the angles: one pair of every few tokens
   double turn = 0;
@@ -110,18 +122,38 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
   const int ti = half ? tid / half : 0, tp = half ? tid - ti * half : 0;
   if (half) turn = exp2(-(double)(2 * tp) / (double)g.rotary * g.log2_theta) * 0.15915494309189533577;
 
-  float acc[2][BWD ? IT : 1][BWD ? 2 * VEC : 1];
-  if (BWD) {
+  for (int64_t t0 = (int64_t)block * tb; t0 < g.tokens; t0 += (int64_t)blocks * tb) {
+    const int nt = (int)min((int64_t)tb, g.tokens - t0);
+    const int rows = nt * H;
+    typename V::Raw xr[QK_ROWS][IT][2], dr[BWD ? QK_ROWS : 1][IT][2];
+    int token[QK_ROWS];
+    int64_t head[QK_ROWS];
+    auto place = [&](int base) __attribute__((always_inline)) {
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
+      for (int k = 0; k < QK_ROWS; ++k) {
+        const int row = base + k * groups + group;
+        token[k] = row < rows ? (int)(((float)row + 0.5f) * g.inv_heads[w]) : -1;  // row / H (tb * H < 2^20)
+        head[k] = row - token[k] * H;
+      }
+    };
+    // every load of the rows at hand is requested before the first is used
+    auto load = [&]() __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < IT; ++i)
+      for (int k = 0; k < QK_ROWS; ++k) {
+        if (token[k] < 0) continue;
+        const T* src = static_cast<const T*>(X.p) + (t0 + token[k]) * X.ts + head[k] * X.hs;
+        const T* dsrc = static_cast<const T*>(D.p) + (t0 + token[k]) * D.ts + head[k] * D.hs;
 #pragma unroll
-        for (int e = 0; e < 2 * VEC; ++e) acc[w][BWD ? i : 0][BWD ? e : 0] = 0.f;
-  }
-
-  for (int64_t t0 = (int64_t)blockIdx.x * g.tb; t0 < g.tokens; t0 += (int64_t)gridDim.x * g.tb) {
-    const int nt = (int)min((int64_t)g.tb, g.tokens - t0);
+        for (int i = 0; i < IT; ++i) {
+          if (on_a[i]) xr[k][i][0] = *reinterpret_cast<const typename V::Raw*>(src + pa[i]);
+          if (on_b[i]) xr[k][i][1] = *reinterpret_cast<const typename V::Raw*>(src + pb[i]);
+          if (BWD && on_a[i]) dr[BWD ? k : 0][i][0] = *reinterpret_cast<const typename V::Raw*>(dsrc + pa[i]);
+          if (BWD && on_b[i]) dr[BWD ? k : 0][i][1] = *reinterpret_cast<const typename V::Raw*>(dsrc + pb[i]);
+        }
+      }
+    };
+    place(0);
+    load();
     if (half) {
       __syncthreads();  // the last tokens' angles have been read
       if (ti < tpass)
@@ -135,49 +167,30 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
         }
       __syncthreads();
     }
+    for (int base = 0; base < rows;) {
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {  // queries, keys
-      const int H = g.heads[w];
-      float gain[IT][2 * VEC];
-#pragma unroll
-      for (int i = 0; i < IT; ++i)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          gain[i][e] = on_a[i] ? g.gain[w][pa[i] + e] : 0.f;
-          gain[i][VEC + e] = on_b[i] ? g.gain[w][pb[i] + e] : 0.f;
-        }
-      int t = group / H, h = group - t * H;
-      const int dt = groups / H, dh = groups - dt * H;
-      while (t < nt) {
-        const T* src = static_cast<const T*>(g.x[w].p) + (t0 + t) * g.x[w].ts + h * g.x[w].hs;
-        float x[IT][2][VEC], d[BWD ? IT : 1][2][VEC];
+      for (int k = 0; k < QK_ROWS; ++k) {
+        if (token[k] < 0) continue;
+        float x[IT][2][VEC], d[IT][2][VEC];
         float ss = 0.f, dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < IT; ++i) {
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) x[i][0][e] = x[i][1][e] = 0.f;
-          if (on_a[i]) Vec<T, VEC>::load(src + pa[i], x[i][0]);
-          if (on_b[i]) Vec<T, VEC>::load(src + pb[i], x[i][1]);
-        }
-        if (BWD) {
-          const T* dsrc = static_cast<const T*>(g.dy[w].p) + (t0 + t) * g.dy[w].ts + h * g.dy[w].hs;
-#pragma unroll
-          for (int i = 0; i < IT; ++i) {
-            const int k = BWD ? i : 0;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) d[k][0][e] = d[k][1][e] = 0.f;
-            if (on_a[i]) Vec<T, VEC>::load(dsrc + pa[i], d[k][0]);
-            if (on_b[i]) Vec<T, VEC>::load(dsrc + pb[i], d[k][1]);
-          }
-        }
 #pragma unroll
         for (int i = 0; i < IT; ++i)
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) ss += x[i][0][e] * x[i][0][e] + x[i][1][e] * x[i][1][e];
+          for (int z = 0; z < 2; ++z) {
+            V::expand(xr[k][i][z], x[i][z]);
+            if (BWD) V::expand(dr[BWD ? k : 0][i][z], d[i][z]);
+            const bool on = z ? on_b[i] : on_a[i];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              x[i][z][e] = on ? x[i][z][e] : 0.f;
+              if (BWD) d[i][z][e] = on ? d[i][z][e] : 0.f;
+              ss += x[i][z][e] * x[i][z][e];
+            }
+          }
         // the rotation of the pairs (u, v) in place, forwards or (BWD) backwards
         auto rotate = [&](int i, float (&a)[VEC], float (&b)[VEC]) __attribute__((always_inline)) {
           if (!rot[i]) return;
-          const float2* cs = trig + t * half + pair[i];
+          const float2* cs = trig + token[k] * half + pair[i];
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
             // (a head that ends inside a unit has no second place: nothing there turns)
@@ -194,49 +207,48 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
         if (BWD) {
 #pragma unroll
           for (int i = 0; i < IT; ++i) {
-            const int k = BWD ? i : 0;
-            rotate(i, d[k][0], d[k][1]);
+            rotate(i, d[i][0], d[i][1]);
 #pragma unroll
             for (int z = 0; z < 2; ++z)
 #pragma unroll
-              for (int e = 0; e < VEC; ++e) dot += d[k][z][e] * gain[i][z * VEC + e] * x[i][z][e];
+              for (int e = 0; e < VEC; ++e) dot += d[i][z][e] * gain[i][z][e] * x[i][z][e];
           }
           dot = head_sum(dot, g.ls);
         }
         ss = head_sum(ss, g.ls);
         const float r = rsqrtf(ss * g.inv_dim + g.eps);
-        T* dst = static_cast<T*>(g.y[w].p) + (t0 + t) * g.y[w].ts + h * g.y[w].hs;
         if (BWD) {
           const float m = r * r * dot * g.inv_dim;  // r mean(h n) = r^2 mean(h x)
 #pragma unroll
-          for (int i = 0; i < IT; ++i) {
-            const int k = BWD ? i : 0;
+          for (int i = 0; i < IT; ++i)
 #pragma unroll
             for (int z = 0; z < 2; ++z)
 #pragma unroll
               for (int e = 0; e < VEC; ++e) {
-                acc[w][k][BWD ? z * VEC + e : 0] += d[k][z][e] * (x[i][z][e] * r);
-                x[i][z][e] = r * (d[k][z][e] * gain[i][z * VEC + e] - x[i][z][e] * m);
+                acc[i][z][e] += d[i][z][e] * (x[i][z][e] * r);
+                x[i][z][e] = r * (d[i][z][e] * gain[i][z][e] - x[i][z][e] * m);
               }
-          }
         } else {
 #pragma unroll
           for (int i = 0; i < IT; ++i) {
 #pragma unroll
             for (int z = 0; z < 2; ++z)
 #pragma unroll
-              for (int e = 0; e < VEC; ++e) x[i][z][e] = x[i][z][e] * r * gain[i][z * VEC + e];
+              for (int e = 0; e < VEC; ++e) x[i][z][e] = x[i][z][e] * r * gain[i][z][e];
             rotate(i, x[i][0], x[i][1]);
           }
         }
+        T* dst = static_cast<T*>(const_cast<void*>(Y.p)) + (t0 + token[k]) * Y.ts + head[k] * Y.hs;
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
-          if (on_a[i]) Vec<T, VEC>::store(dst + pa[i], x[i][0]);
-          if (on_b[i]) Vec<T, VEC>::store(dst + pb[i], x[i][1]);
+          if (on_a[i]) V::store(dst + pa[i], x[i][0]);
+          if (on_b[i]) V::store(dst + pb[i], x[i][1]);
         }
-        t += dt;
-        h += dh;
-        if (h >= H) { h -= H; ++t; }
+      }
+      base += QK_ROWS * groups;
+      if (base < rows) {
+        place(base);
+        load();
       }
     }
   }
@@ -244,63 +256,94 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
   if (BWD) {  // sums of the gains' gradients: over the heads of a wavefront, then over the wavefronts, in a fixed order
     const int wave = tid >> 6;
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-      __syncthreads();
+    for (int i = 0; i < IT; ++i)
 #pragma unroll
-      for (int i = 0; i < IT; ++i)
+      for (int z = 0; z < 2; ++z)
 #pragma unroll
-        for (int e = 0; e < 2 * VEC; ++e) {
-          float v = acc[w][BWD ? i : 0][BWD ? e : 0];
+        for (int e = 0; e < VEC; ++e) {
+          float v = acc[i][z][e];
           for (int o = 1 << g.ls; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
-          const int place = e < VEC ? pa[i] + e : pb[i] + e - VEC;
-          if ((tid & 63) >> g.ls == 0 && (e < VEC ? on_a[i] : on_b[i])) red[wave * 256 + place] = v;
+          if ((tid & 63) >> g.ls == 0 && (z ? on_b[i] : on_a[i])) red[wave * 256 + (z ? pb[i] : pa[i]) + e] = v;
         }
-      __syncthreads();
-      if (tid < g.dim)
-        g.part[((int64_t)blockIdx.x * 2 + w) * g.dim + tid] = red[tid] + red[256 + tid] + red[512 + tid] + red[768 + tid];
-    }
+    __syncthreads();
+    if (tid < g.dim) g.part[(int64_t)blockIdx.x * g.dim + tid] = red[tid] + red[256 + tid] + red[512 + tid] + red[768 + tid];
   }
 }
 
-// dgain[i] (+)= sum over the blocks, in 64 bits: 16 columns a block, 16 rows of it at a time
-__global__ __launch_bounds__(256) void qk_gain_sum_kernel(const float* __restrict__ part, int blocks, int dim, float* dq,
-                                                          float* dk, int accumulate) {
-  __shared__ double sh[16][17];
-  const int col = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+// dgain[i] (+)= sum over the blocks, in 64 bits: 16 columns a block, 64 rows of it at a time
+__global__ __launch_bounds__(1024) void qk_gain_sum_kernel(const float* __restrict__ part, int blocks_q, int blocks_k, int dim,
+                                                           float* dq, float* dk, int accumulate) {
+  __shared__ double sh[64][17];
+  const int col = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4, w = blockIdx.y;
+  const float* p = part + (w ? (int64_t)blocks_q * dim : 0) + col;
+  const int blocks = w ? blocks_k : blocks_q;
   double s = 0;
-  if (col < 2 * dim)
-    for (int b = row; b < blocks; b += 16) s += part[(int64_t)b * 2 * dim + col];
+  if (col < dim) {
+#pragma unroll 8
+    for (int b = row; b < blocks; b += 64) s += p[(int64_t)b * dim];
+  }
   sh[row][threadIdx.x & 15] = s;
   __syncthreads();
-  if (row == 0 && col < 2 * dim) {
-    for (int r = 1; r < 16; ++r) s += sh[r][threadIdx.x];
-    float* out = col < dim ? dq + col : dk + (col - dim);
+  if (row < 8) {
+    for (int r = row + 8; r < 64; r += 8) s += sh[r][threadIdx.x & 15];
+    sh[row][threadIdx.x & 15] = s;
+  }
+  __syncthreads();
+  if (row == 0 && col < dim) {
+    for (int r = 1; r < 8; ++r) s += sh[r][threadIdx.x];
+    float* out = (w ? dk : dq) + col;
     *out = (accumulate ? *out : 0.f) + (float)s;
   }
 }
 
-bool wide(const ast_heads& h, int vec_bytes, int esize) {
-  return (reinterpret_cast<uintptr_t>(h.dev) % vec_bytes) == 0 && (h.token_stride * esize) % vec_bytes == 0 &&
-         (h.head_stride * esize) % vec_bytes == 0;
+bool wide(const ast_heads& h, int esize) {
+  return (reinterpret_cast<uintptr_t>(h.dev) % 16) == 0 && (h.token_stride * esize) % 16 == 0 && (h.head_stride * esize) % 16 == 0;
 }
 
-constexpr int QK_MOST_BLOCKS = 1024;  // of a backward pass: partial sums of the gains' gradients
+constexpr int QK_MOST_BLOCKS = 1024;  // of a backward pass and of queries or keys: partial sums of the gains' gradients
 
-int backward_blocks(int64_t tokens) { return (int)std::min<int64_t>(std::max<int64_t>(tokens, 1), QK_MOST_BLOCKS); }
+struct Shape { int vec, ls, units, rot_units, tb[2]; unsigned blocks[2]; };
+
+// Lanes and blocks of a call.  A block takes as many tokens as keep QK_ROWS heads of every lane in flight, fewer where the
+// chip would not be filled.
+Shape shape_of(const ast_qk_cfg& c, const int heads[2], bool vec, bool bwd) {
+  Shape s = {};
+  s.vec = !vec ? 1 : c.dtype == AST_BF16_F32ACC ? 8 : 4;
+  if (c.interleaved) {
+    s.units = (c.head_dim + 2 * s.vec - 1) / (2 * s.vec);
+    s.rot_units = (c.rotary + 2 * s.vec - 1) / (2 * s.vec);
+  } else {
+    s.rot_units = c.rotary / 2 / s.vec;
+    s.units = s.rot_units + ((c.head_dim - c.rotary) / s.vec + 1) / 2;
+  }
+  while (s.ls < 6 && (1 << s.ls) < s.units) ++s.ls;
+  const int groups = 256 >> s.ls;
+  for (int w = 0; w < 2; ++w) {
+    int64_t tb = std::max(1, QK_ROWS * groups / heads[w]);
+    if (c.rotary) tb = std::min<int64_t>(tb, QK_TRIG / (c.rotary / 2));
+    tb = std::max<int64_t>(1, std::min<int64_t>(tb, c.tokens / 256));
+    s.tb[w] = (int)tb;
+    const int64_t need = (c.tokens + tb - 1) / tb;
+    s.blocks[w] = (unsigned)std::min<int64_t>(need, bwd ? QK_MOST_BLOCKS : 1 << 20);
+  }
+  return s;
+}
 
 void launch(hipStream_t st, const ast_qk_cfg& c, const ast_heads* dy, const ast_heads* x, const float* gq, const float* gk,
-            const ast_heads* y, float* part) {
+            const ast_heads* y, float* part, unsigned* blocks) {
   const bool bwd = dy != nullptr, bf = c.dtype == AST_BF16_F32ACC;
   QkArgs g = {};
-  const int full = bf ? 8 : 4;
+  const int full = bf ? 8 : 4, esize = bf ? 2 : 4;
   bool vec = c.head_dim % full == 0 && (c.interleaved ? c.rotary % (2 * full) == 0 || c.rotary == c.head_dim : c.rotary / 2 % full == 0);
   for (int w = 0; w < 2; ++w) {
     g.x[w] = {x[w].dev, x[w].token_stride, x[w].head_stride};
-    g.y[w] = {const_cast<void*>(y[w].dev), y[w].token_stride, y[w].head_stride};
+    g.y[w] = {y[w].dev, y[w].token_stride, y[w].head_stride};
     if (bwd) g.dy[w] = {dy[w].dev, dy[w].token_stride, dy[w].head_stride};
     g.heads[w] = x[w].heads;
-    vec = vec && wide(x[w], 16, bf ? 2 : 4) && wide(y[w], 16, bf ? 2 : 4) && (!bwd || wide(dy[w], 16, bf ? 2 : 4));
+    g.inv_heads[w] = 1.f / (float)x[w].heads;
+    vec = vec && wide(x[w], esize) && wide(y[w], esize) && (!bwd || wide(dy[w], esize));
   }
+  const Shape s = shape_of(c, g.heads, vec, bwd);
   g.gain[0] = gq;
   g.gain[1] = gk;
   g.pos = c.positions_dev;
@@ -312,28 +355,23 @@ void launch(hipStream_t st, const ast_qk_cfg& c, const ast_heads* dy, const ast_
   g.inv_dim = 1.f / (float)c.head_dim;
   g.dim = c.head_dim;
   g.rotary = c.rotary;
-  const int V = vec ? full : 1;
-  if (c.interleaved) {
-    g.units = (c.head_dim + 2 * V - 1) / (2 * V);
-    g.rot_units = (c.rotary + 2 * V - 1) / (2 * V);
-  } else {
-    g.rot_units = c.rotary / 2 / V;
-    g.units = g.rot_units + ((c.head_dim - c.rotary) / V + 1) / 2;
+  g.units = s.units;
+  g.rot_units = s.rot_units;
+  g.ls = s.ls;
+  for (int w = 0; w < 2; ++w) {
+    g.tb[w] = s.tb[w];
+    blocks[w] = s.blocks[w];
   }
-  while (g.ls < 6 && (1 << g.ls) < g.units) ++g.ls;
-  g.tb = 1;
-  const int most = std::min(16, c.rotary ? QK_TRIG / (c.rotary / 2) : 16);
-  while (2 * g.tb <= most && (int64_t)g.tb * 2 * 1024 <= c.tokens) g.tb *= 2;
-  const int64_t need = (c.tokens + g.tb - 1) / g.tb;
-  const unsigned blocks = bwd ? (unsigned)backward_blocks(need) : (unsigned)std::min<int64_t>(need, 1 << 20);
+  g.blocks_q = s.blocks[0];
+  const dim3 grid(s.blocks[0] + s.blocks[1]);
 #define GO(T, VEC, IT)                                                                                                        \
   do {                                                                                                                        \
     if (bwd) {                                                                                                                \
-      if (c.interleaved) KLAUNCH((qk_norm_rope_kernel<T, VEC, IT, true, true>), dim3(blocks), dim3(256), 0, st, g);           \
-      else KLAUNCH((qk_norm_rope_kernel<T, VEC, IT, false, true>), dim3(blocks), dim3(256), 0, st, g);                        \
+      if (c.interleaved) KLAUNCH((qk_norm_rope_kernel<T, VEC, IT, true, true>), grid, dim3(256), 0, st, g);                   \
+      else KLAUNCH((qk_norm_rope_kernel<T, VEC, IT, false, true>), grid, dim3(256), 0, st, g);                                \
     } else {                                                                                                                  \
-      if (c.interleaved) KLAUNCH((qk_norm_rope_kernel<T, VEC, IT, true, false>), dim3(blocks), dim3(256), 0, st, g);          \
-      else KLAUNCH((qk_norm_rope_kernel<T, VEC, IT, false, false>), dim3(blocks), dim3(256), 0, st, g);                       \
+      if (c.interleaved) KLAUNCH((qk_norm_rope_kernel<T, VEC, IT, true, false>), grid, dim3(256), 0, st, g);                  \
+      else KLAUNCH((qk_norm_rope_kernel<T, VEC, IT, false, false>), grid, dim3(256), 0, st, g);                               \
     }                                                                                                                         \
   } while (0)
   if (bf) {
@@ -350,11 +388,12 @@ void qk_norm_rope_fwd(hipStream_t st, const ast_qk_cfg& c, const ast_heads& q, c
                       const float* gk, const ast_heads& yq, const ast_heads& yk) {
   if (c.tokens <= 0) return;
   const ast_heads x[2] = {q, k}, y[2] = {yq, yk};
-  launch(st, c, nullptr, x, gq, gk, y, nullptr);
+  unsigned blocks[2];
+  launch(st, c, nullptr, x, gq, gk, y, nullptr, blocks);
 }
 
-size_t qk_norm_rope_bwd_ws_bytes(int64_t tokens, int head_dim) {
-  return (size_t)backward_blocks(tokens) * 2 * head_dim * sizeof(float);
+size_t qk_norm_rope_bwd_ws_bytes(int64_t tokens, int head_dim) {  // (whatever the blocks' shape: at most one block a token)
+  return (size_t)std::min<int64_t>(std::max<int64_t>(tokens, 1), QK_MOST_BLOCKS) * 2 * head_dim * sizeof(float);
 }
 
 void qk_norm_rope_bwd(hipStream_t st, const ast_qk_cfg& c, const ast_heads& dyq, const ast_heads& dyk, const ast_heads& q,
@@ -362,16 +401,10 @@ void qk_norm_rope_bwd(hipStream_t st, const ast_qk_cfg& c, const ast_heads& dyq,
                       float* dgq, float* dgk, bool accumulate, void* ws) {
   const ast_heads dy[2] = {dyq, dyk}, x[2] = {q, k}, y[2] = {dq, dk};
   float* part = static_cast<float*>(ws);
-  int blocks = 0;
-  if (c.tokens > 0) {
-    launch(st, c, dy, x, gq, gk, y, part);
-    int tb = 1;
-    const int most = std::min(16, c.rotary ? QK_TRIG / (c.rotary / 2) : 16);
-    while (2 * tb <= most && (int64_t)tb * 2 * 1024 <= c.tokens) tb *= 2;
-    blocks = backward_blocks((c.tokens + tb - 1) / tb);
-  }
-  KLAUNCH(qk_gain_sum_kernel, dim3((unsigned)((2 * c.head_dim + 15) / 16)), dim3(256), 0, st, part, blocks, c.head_dim, dgq, dgk,
-          (int)accumulate);
+  unsigned blocks[2] = {0, 0};
+  if (c.tokens > 0) launch(st, c, dy, x, gq, gk, y, part, blocks);
+  KLAUNCH(qk_gain_sum_kernel, dim3((unsigned)((c.head_dim + 15) / 16), 2), dim3(1024), 0, st, part, (int)blocks[0], (int)blocks[1],
+          c.head_dim, dgq, dgk, (int)accumulate);
 }
 
 }  // namespace ast

@@ -11,6 +11,7 @@ import torch
 from .binding import _check, load_library
 
 _DT = {torch.float32: 0, torch.bfloat16: 1}
+_F32, _I32 = (torch.float32,), (torch.int32,)
 
 
 class ast_heads(C.Structure):
@@ -51,33 +52,32 @@ def _lib():
     return _LIB
 
 
-class _On:
-    """Makes the tensors' device current (the calls launch on the current one) and gives its stream."""
+def _device(t, *others):
+    """The GPU that holds the tensors."""
+    d = t.get_device()
+    if d < 0:
+        raise ValueError("tensors must be on a GPU, got %s" % t.device)
+    for o in others:
+        if o is not None and o.get_device() != d:
+            raise ValueError("tensors on different devices: %s and %s" % (t.device, o.device))
+    return d
 
-    def __init__(self, *tensors):
-        dev = tensors[0].device
-        if dev.type != "cuda":
-            raise ValueError("tensors must be on a GPU, got %s" % dev)
-        for t in tensors:
-            if t is not None and t.device != dev:
-                raise ValueError("tensors on different devices: %s and %s" % (dev, t.device))
-        self.dev, self.guard = dev, None
 
-    def __enter__(self):
-        if torch.cuda.current_device() != self.dev.index:
-            self.guard = torch.cuda.device(self.dev)
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.dev).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _call(d, fn, *args):
+    """fn(*args, stream) with device d current (the calls launch on the current one) and its current stream."""
+    if torch.cuda.current_device() == d:
+        st = fn(*args, torch.cuda.current_stream(d).cuda_stream)
+    else:
+        with torch.cuda.device(d):
+            st = fn(*args, torch.cuda.current_stream(d).cuda_stream)
+    if st:
+        _check(_LIB, st)
 
 
 def _is(t, name, dtypes, shape):
     if not isinstance(t, torch.Tensor) or t.dtype not in dtypes:
         raise ValueError("%s must be a tensor of %s" % (name, " or ".join(str(d) for d in dtypes)))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
@@ -93,7 +93,7 @@ def _matrix(t, name, dtypes=(torch.float32, torch.bfloat16)):
 def _vector_i32(t, name, n=None):
     if not isinstance(t, torch.Tensor) or t.dim() != 1:
         raise ValueError("%s must be a vector" % name)
-    return _is(t, name, (torch.int32,), t.shape if n is None else (n,))
+    return _is(t, name, _I32, t.shape if n is None else (n,))
 
 
 def _empty(n, device):
@@ -120,9 +120,8 @@ def embedding_forward(ids, table, scale=1.0, dtype=None, out=None):
         out = torch.empty((T, D), dtype=dtype or table.dtype, device=table.device)
     _is(out, "out", (dtype,) if dtype else tuple(_DT), (T, D))
     lib = _lib()
-    with _On(table, ids, out) as st:
-        _check(lib, lib.asteroid_embedding_forward(ids.data_ptr(), T, table.data_ptr(), _DT[table.dtype], V, D, scale,
-                                                   out.data_ptr(), _DT[out.dtype], st))
+    _call(_device(table, ids, out), lib.asteroid_embedding_forward, ids.data_ptr(), T, table.data_ptr(), _DT[table.dtype],
+          V, D, scale, out.data_ptr(), _DT[out.dtype])
     return out
 
 
@@ -145,24 +144,25 @@ def embedding_backward(ids, dy, rows, scale=1.0, out=None, accumulate=False, wor
         if accumulate:
             raise ValueError("accumulate needs the tensor to add to")
         out = torch.empty((rows, D), dtype=torch.float32, device=dy.device)
-    _is(out, "out", (torch.float32,), (rows, D))
+    _is(out, "out", _F32, (rows, D))
     lib = _lib()
-    with _On(dy, ids, out) as st:
-        need = embedding_backward_workspace(T, rows, D)
-        ws = _workspace(workspace, need, dy.device)
-        _check(lib, lib.asteroid_embedding_backward(ids.data_ptr(), T, dy.data_ptr(), _DT[dy.dtype], rows, D, scale,
-                                                    int(bool(accumulate)), out.data_ptr(), ws.data_ptr(), ws.numel(), st))
+    d = _device(dy, ids, out)
+    ws = _workspace(workspace, embedding_backward_workspace(T, rows, D), dy.device)
+    _call(d, lib.asteroid_embedding_backward, ids.data_ptr(), T, dy.data_ptr(), _DT[dy.dtype], rows, D, scale,
+          bool(accumulate), out.data_ptr(), ws.data_ptr(), ws.numel())
     return out
 
 
 # ------------------------------------------------------------------------------------------------ queries and keys
 
 def _heads(t, name, T, d, dtype):
-    if not isinstance(t, torch.Tensor) or t.dim() != 3 or t.dtype != dtype or t.shape[0] != T or t.shape[2] != d:
+    shape = t.shape if isinstance(t, torch.Tensor) else ()
+    if len(shape) != 3 or t.dtype != dtype or shape[0] != T or shape[2] != d:
         raise ValueError("%s must be a %s tensor [%d, heads, %d]" % (name, dtype, T, d))
-    if d > 1 and t.stride(2) != 1:
+    ts, hs, unit = t.stride()
+    if unit != 1 and d > 1:
         raise ValueError("%s must have unit stride inside a head" % name)
-    return ast_heads(t.data_ptr(), t.stride(0), t.stride(1), t.shape[1])
+    return ast_heads(t.data_ptr(), ts, hs, shape[1])
 
 
 def _qk_cfg(q, positions, period, rotary, theta, interleaved, eps):
@@ -188,12 +188,12 @@ def qk_norm_rope_forward(q, k, q_gain, k_gain, positions=None, period=0, rotary=
     T, d = q.shape[0], q.shape[2]
     yq, yk = out if out is not None else (torch.empty(q.shape, dtype=q.dtype, device=q.device),
                                           torch.empty(k.shape, dtype=q.dtype, device=q.device))
-    _is(q_gain, "q_gain", (torch.float32,), (d,))
-    _is(k_gain, "k_gain", (torch.float32,), (d,))
+    _is(q_gain, "q_gain", _F32, (d,))
+    _is(k_gain, "k_gain", _F32, (d,))
     a = [_heads(t, n, T, d, q.dtype) for t, n in ((q, "q"), (k, "k"), (yq, "yq"), (yk, "yk"))]
     lib = _lib()
-    with _On(q, k, yq, yk, q_gain, k_gain, positions) as st:
-        _check(lib, lib.asteroid_qk_norm_rope_forward(cfg, a[0], a[1], q_gain.data_ptr(), k_gain.data_ptr(), a[2], a[3], st))
+    _call(_device(q, k, yq, yk, q_gain, k_gain, positions), lib.asteroid_qk_norm_rope_forward, cfg, a[0], a[1],
+          q_gain.data_ptr(), k_gain.data_ptr(), a[2], a[3])
     return yq, yk
 
 
@@ -220,14 +220,13 @@ def qk_norm_rope_backward(dyq, dyk, q, k, q_gain, k_gain, positions=None, period
         gain_out = torch.empty((2, d), dtype=torch.float32, device=q.device).unbind(0)
     gq, gk = gain_out
     for t, n in ((q_gain, "q_gain"), (k_gain, "k_gain"), (gq, "dq_gain"), (gk, "dk_gain")):
-        _is(t, n, (torch.float32,), (d,))
+        _is(t, n, _F32, (d,))
     a = [_heads(t, n, T, d, q.dtype) for t, n in ((dyq, "dyq"), (dyk, "dyk"), (q, "q"), (k, "k"), (dq, "dq"), (dk, "dk"))]
     lib = _lib()
-    with _On(q, k, dyq, dyk, dq, dk, q_gain, k_gain, gq, gk, positions) as st:
-        ws = _workspace(workspace, qk_norm_rope_backward_workspace(T, d), q.device)
-        _check(lib, lib.asteroid_qk_norm_rope_backward(cfg, a[0], a[1], a[2], a[3], q_gain.data_ptr(), k_gain.data_ptr(), a[4],
-                                                       a[5], gq.data_ptr(), gk.data_ptr(), int(bool(accumulate)),
-                                                       ws.data_ptr(), ws.numel(), st))
+    on = _device(q, k, dyq, dyk, dq, dk, q_gain, k_gain, gq, gk, positions)
+    ws = _workspace(workspace, qk_norm_rope_backward_workspace(T, d), q.device)
+    _call(on, lib.asteroid_qk_norm_rope_backward, cfg, a[0], a[1], a[2], a[3], q_gain.data_ptr(), k_gain.data_ptr(), a[4], a[5],
+          gq.data_ptr(), gk.data_ptr(), bool(accumulate), ws.data_ptr(), ws.numel())
     return dq, dk, gq, gk
 
 
@@ -264,8 +263,7 @@ def stash8_pack(x, out=None):
     if (s.rows, s.cols) != tuple(x.shape):
         raise ValueError("the stash keeps [%d, %d], x is %s" % (s.rows, s.cols, tuple(x.shape)))
     lib = _lib()
-    with _On(x, s.data) as st:
-        _check(lib, lib.asteroid_stash8_pack(x.data_ptr(), _DT[x.dtype], s.rows, s.cols, s.data.data_ptr(), st))
+    _call(_device(x, s.data), lib.asteroid_stash8_pack, x.data_ptr(), _DT[x.dtype], s.rows, s.cols, s.data.data_ptr())
     return s
 
 
@@ -276,8 +274,7 @@ def stash8_unpack(stash, dtype=torch.bfloat16, out=None):
         out = torch.empty((s.rows, s.cols), dtype=dtype, device=s.data.device)
     _is(out, "out", tuple(_DT), (s.rows, s.cols))
     lib = _lib()
-    with _On(s.data, out) as st:
-        _check(lib, lib.asteroid_stash8_unpack(s.data.data_ptr(), s.rows, s.cols, out.data_ptr(), _DT[out.dtype], st))
+    _call(_device(s.data, out), lib.asteroid_stash8_unpack, s.data.data_ptr(), s.rows, s.cols, out.data_ptr(), _DT[out.dtype])
     return out
 
 
@@ -301,17 +298,16 @@ def linear_wgrad_stash8(dy, stash, bias=True, out=None, bias_out=None, accumulat
         raise ValueError("accumulate needs the tensors to add to")
     if out is None:
         out = torch.empty((N, K), dtype=torch.float32, device=dy.device)
-    _is(out, "out", (torch.float32,), (N, K))
+    _is(out, "out", _F32, (N, K))
     db = None
     if bias:
         db = torch.empty((N,), dtype=torch.float32, device=dy.device) if bias_out is None else bias_out
-        _is(db, "bias_out", (torch.float32,), (N,))
+        _is(db, "bias_out", _F32, (N,))
     lib = _lib()
-    with _On(dy, s.data, out, db) as st:
-        ws = _workspace(workspace, linear_wgrad_stash8_workspace(s.rows, K, N), dy.device)
-        _check(lib, lib.asteroid_linear_wgrad_stash8(dy.data_ptr(), s.data.data_ptr(), s.rows, K, N, out.data_ptr(),
-                                                     None if db is None else db.data_ptr(), int(bool(accumulate)),
-                                                     ws.data_ptr(), ws.numel(), st))
+    d = _device(dy, s.data, out, db)
+    ws = _workspace(workspace, linear_wgrad_stash8_workspace(s.rows, K, N), dy.device)
+    _call(d, lib.asteroid_linear_wgrad_stash8, dy.data_ptr(), s.data.data_ptr(), s.rows, K, N, out.data_ptr(),
+          None if db is None else db.data_ptr(), bool(accumulate), ws.data_ptr(), ws.numel())
     return out, db
 
 
@@ -323,7 +319,6 @@ def gelu_backward_stash8(dy, stash, out=None):
         out = torch.empty_like(dy)
     _is(out, "out", (dy.dtype,), (s.rows, s.cols))
     lib = _lib()
-    with _On(dy, s.data, out) as st:
-        _check(lib, lib.asteroid_gelu_backward_stash8(dy.data_ptr(), _DT[dy.dtype], s.data.data_ptr(), s.rows, s.cols,
-                                                      out.data_ptr(), st))
+    _call(_device(dy, s.data, out), lib.asteroid_gelu_backward_stash8, dy.data_ptr(), _DT[dy.dtype], s.data.data_ptr(), s.rows,
+          s.cols, out.data_ptr())
     return out
