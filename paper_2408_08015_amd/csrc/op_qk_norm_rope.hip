@@ -36,7 +36,6 @@ struct QkArgs {
 };
 
 constexpr int QK_TRIG = 2048;  // pairs (cos, sin) of a block's tokens
-constexpr int QK_ROWS = 4;     // heads that a lane has in flight
 
 // VEC consecutive values: as they are loaded, and as numbers
 template <typename T, int VEC> struct Vec;
@@ -80,7 +79,7 @@ __device__ __forceinline__ float head_sum(float v, int ls) {
 
 // One lane's share of a head: IT units of 2 x VEC values.
 template <typename T, int VEC, int IT, bool INTER, bool BWD>
-__global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
+__global__ __launch_bounds__(256, 4) void qk_norm_rope_kernel(const QkArgs g) {
   typedef Vec<T, VEC> V;
   __shared__ __attribute__((aligned(16))) float2 trig[QK_TRIG];
   __shared__ float red[BWD ? 4 * 256 : 1];
@@ -125,35 +124,31 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
   for (int64_t t0 = (int64_t)block * tb; t0 < g.tokens; t0 += (int64_t)blocks * tb) {
     const int nt = (int)min((int64_t)tb, g.tokens - t0);
     const int rows = nt * H;
-    typename V::Raw xr[QK_ROWS][IT][2], dr[BWD ? QK_ROWS : 1][IT][2];
-    int token[QK_ROWS];
-    int64_t head[QK_ROWS];
-    auto place = [&](int base) __attribute__((always_inline)) {
-#pragma unroll
-      for (int k = 0; k < QK_ROWS; ++k) {
-        const int row = base + k * groups + group;
-        token[k] = row < rows ? (int)(((float)row + 0.5f) * g.inv_heads[w]) : -1;  // row / H (tb * H < 2^20)
-        head[k] = row - token[k] * H;
-      }
+    struct Row {  // a head: where it lies, and its values as they were loaded
+      int token, head;
+      typename V::Raw x[IT][2], d[BWD ? IT : 1][2];
     };
-    // every load of the rows at hand is requested before the first is used
-    auto load = [&]() __attribute__((always_inline)) {
+    auto fetch = [&](int row, Row& r) __attribute__((always_inline)) {
+      r.token = row < rows ? (int)(((float)row + 0.5f) * g.inv_heads[w]) : -1;  // row / H (exact: tb * H <= 2^20)
+      r.head = row - r.token * H;
+      if (r.token < 0) return;
+      const T* src = static_cast<const T*>(X.p) + (t0 + r.token) * X.ts + r.head * X.hs;
+      const T* dsrc = static_cast<const T*>(D.p) + (t0 + r.token) * D.ts + r.head * D.hs;
 #pragma unroll
-      for (int k = 0; k < QK_ROWS; ++k) {
-        if (token[k] < 0) continue;
-        const T* src = static_cast<const T*>(X.p) + (t0 + token[k]) * X.ts + head[k] * X.hs;
-        const T* dsrc = static_cast<const T*>(D.p) + (t0 + token[k]) * D.ts + head[k] * D.hs;
+      for (int i = 0; i < IT; ++i)
 #pragma unroll
-        for (int i = 0; i < IT; ++i) {
-          if (on_a[i]) xr[k][i][0] = *reinterpret_cast<const typename V::Raw*>(src + pa[i]);
-          if (on_b[i]) xr[k][i][1] = *reinterpret_cast<const typename V::Raw*>(src + pb[i]);
-          if (BWD && on_a[i]) dr[BWD ? k : 0][i][0] = *reinterpret_cast<const typename V::Raw*>(dsrc + pa[i]);
-          if (BWD && on_b[i]) dr[BWD ? k : 0][i][1] = *reinterpret_cast<const typename V::Raw*>(dsrc + pb[i]);
+        for (int z = 0; z < 2; ++z) {
+          const int place = z ? pb[i] : pa[i];
+          r.x[i][z] = typename V::Raw{};
+          if (BWD) r.d[BWD ? i : 0][z] = typename V::Raw{};
+          if (z ? on_b[i] : on_a[i]) {
+            r.x[i][z] = *reinterpret_cast<const typename V::Raw*>(src + place);
+            if (BWD) r.d[BWD ? i : 0][z] = *reinterpret_cast<const typename V::Raw*>(dsrc + place);
+          }
         }
-      }
     };
-    place(0);
-    load();
+    Row cur;
+    fetch(group, cur);
     if (half) {
       __syncthreads();  // the last tokens' angles have been read
       if (ti < tpass)
@@ -167,89 +162,78 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs g) {
         }
       __syncthreads();
     }
-    for (int base = 0; base < rows;) {
+    for (int row = group; row < rows; row += groups) {
+      Row next;  // requested before this head is worked on
+      fetch(row + groups, next);
+      float x[IT][2][VEC], d[IT][2][VEC];
+      float ss = 0.f, dot = 0.f;
 #pragma unroll
-      for (int k = 0; k < QK_ROWS; ++k) {
-        if (token[k] < 0) continue;
-        float x[IT][2][VEC], d[IT][2][VEC];
-        float ss = 0.f, dot = 0.f;
+      for (int i = 0; i < IT; ++i)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          V::expand(cur.x[i][z], x[i][z]);
+          if (BWD) V::expand(cur.d[BWD ? i : 0][z], d[i][z]);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) ss += x[i][z][e] * x[i][z][e];
+        }
+      // the rotation of the pairs (u, v) in place, forwards or (BWD) backwards
+      auto rotate = [&](int i, float (&a)[VEC], float (&b)[VEC]) __attribute__((always_inline)) {
+        if (!rot[i]) return;
+        const float2* cs = trig + cur.token * half + pair[i];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          // (a head that ends inside a unit has no second place: nothing there turns)
+          const float2 f = !INTER || 2 * e < VEC || on_b[i] ? cs[e] : make_float2(1.f, 0.f);
+          const float s = BWD ? -f.y : f.y;
+          // pair e: (a_e, b_e), or neighbours: pairs 0 .. VEC/2 - 1 in a, the others in b
+          float& p = INTER && VEC > 1 ? (2 * e < VEC ? a[(2 * e) % VEC] : b[(2 * e) % VEC]) : a[e];
+          float& q = INTER && VEC > 1 ? (2 * e < VEC ? a[(2 * e + 1) % VEC] : b[(2 * e + 1) % VEC]) : b[e];
+          const float u = p, v = q;
+          p = u * f.x - v * s;
+          q = u * s + v * f.x;
+        }
+      };
+      if (BWD) {
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+          rotate(i, d[i][0], d[i][1]);
+#pragma unroll
+          for (int z = 0; z < 2; ++z)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) dot += d[i][z][e] * gain[i][z][e] * x[i][z][e];
+        }
+        dot = head_sum(dot, g.ls);
+      }
+      ss = head_sum(ss, g.ls);
+      const float r = rsqrtf(ss * g.inv_dim + g.eps);
+      if (BWD) {
+        const float m = r * r * dot * g.inv_dim;  // r mean(h n) = r^2 mean(h x)
 #pragma unroll
         for (int i = 0; i < IT; ++i)
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            V::expand(xr[k][i][z], x[i][z]);
-            if (BWD) V::expand(dr[BWD ? k : 0][i][z], d[i][z]);
-            const bool on = z ? on_b[i] : on_a[i];
+          for (int z = 0; z < 2; ++z)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-              x[i][z][e] = on ? x[i][z][e] : 0.f;
-              if (BWD) d[i][z][e] = on ? d[i][z][e] : 0.f;
-              ss += x[i][z][e] * x[i][z][e];
+              acc[i][z][e] += d[i][z][e] * (x[i][z][e] * r);
+              x[i][z][e] = r * (d[i][z][e] * gain[i][z][e] - x[i][z][e] * m);
             }
-          }
-        // the rotation of the pairs (u, v) in place, forwards or (BWD) backwards
-        auto rotate = [&](int i, float (&a)[VEC], float (&b)[VEC]) __attribute__((always_inline)) {
-          if (!rot[i]) return;
-          const float2* cs = trig + token[k] * half + pair[i];
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            // (a head that ends inside a unit has no second place: nothing there turns)
-            const float2 f = !INTER || 2 * e < VEC || on_b[i] ? cs[e] : make_float2(1.f, 0.f);
-            const float s = BWD ? -f.y : f.y;
-            // pair e: (a_e, b_e), or neighbours: pairs 0 .. VEC/2 - 1 in a, the others in b
-            float& p = INTER && VEC > 1 ? (2 * e < VEC ? a[(2 * e) % VEC] : b[(2 * e) % VEC]) : a[e];
-            float& q = INTER && VEC > 1 ? (2 * e < VEC ? a[(2 * e + 1) % VEC] : b[(2 * e + 1) % VEC]) : b[e];
-            const float u = p, v = q;
-            p = u * f.x - v * s;
-            q = u * s + v * f.x;
-          }
-        };
-        if (BWD) {
-#pragma unroll
-          for (int i = 0; i < IT; ++i) {
-            rotate(i, d[i][0], d[i][1]);
-#pragma unroll
-            for (int z = 0; z < 2; ++z)
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) dot += d[i][z][e] * gain[i][z][e] * x[i][z][e];
-          }
-          dot = head_sum(dot, g.ls);
-        }
-        ss = head_sum(ss, g.ls);
-        const float r = rsqrtf(ss * g.inv_dim + g.eps);
-        if (BWD) {
-          const float m = r * r * dot * g.inv_dim;  // r mean(h n) = r^2 mean(h x)
-#pragma unroll
-          for (int i = 0; i < IT; ++i)
-#pragma unroll
-            for (int z = 0; z < 2; ++z)
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) {
-                acc[i][z][e] += d[i][z][e] * (x[i][z][e] * r);
-                x[i][z][e] = r * (d[i][z][e] * gain[i][z][e] - x[i][z][e] * m);
-              }
-        } else {
-#pragma unroll
-          for (int i = 0; i < IT; ++i) {
-#pragma unroll
-            for (int z = 0; z < 2; ++z)
-#pragma unroll
-              for (int e = 0; e < VEC; ++e) x[i][z][e] = x[i][z][e] * r * gain[i][z][e];
-            rotate(i, x[i][0], x[i][1]);
-          }
-        }
-        T* dst = static_cast<T*>(const_cast<void*>(Y.p)) + (t0 + token[k]) * Y.ts + head[k] * Y.hs;
+      } else {
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
-          if (on_a[i]) V::store(dst + pa[i], x[i][0]);
-          if (on_b[i]) V::store(dst + pb[i], x[i][1]);
+#pragma unroll
+          for (int z = 0; z < 2; ++z)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) x[i][z][e] = x[i][z][e] * r * gain[i][z][e];
+          rotate(i, x[i][0], x[i][1]);
         }
       }
-      base += QK_ROWS * groups;
-      if (base < rows) {
-        place(base);
-        load();
+      T* dst = static_cast<T*>(const_cast<void*>(Y.p)) + (t0 + cur.token) * Y.ts + cur.head * Y.hs;
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        if (on_a[i]) V::store(dst + pa[i], x[i][0]);
+        if (on_b[i]) V::store(dst + pb[i], x[i][1]);
       }
+      cur = next;
     }
   }
 
@@ -304,8 +288,10 @@ constexpr int QK_MOST_BLOCKS = 1024;  // of a backward pass and of queries or ke
 
 struct Shape { int vec, ls, units, rot_units, tb[2]; unsigned blocks[2]; };
 
-// Lanes and blocks of a call.  A block takes as many tokens as keep QK_ROWS heads of every lane in flight, fewer where the
-// chip would not be filled.
+// Lanes and blocks of a call.  About 2048 blocks of queries and as many of keys forward, 1024 backward (whose blocks each leave
+// partial sums): a block forms its angles and waits for its first loads once.  us, forward of 32768 tokens, 32 + 8 heads of
+// 128, and backward of 10007 tokens, 12 + 3 fp32 heads of 80: 1024 blocks 145 and 38.4, 2048 blocks 140 and 42.2, blocks that
+// take a token of every lane group 199 and 46.7.
 Shape shape_of(const ast_qk_cfg& c, const int heads[2], bool vec, bool bwd) {
   Shape s = {};
   s.vec = !vec ? 1 : c.dtype == AST_BF16_F32ACC ? 8 : 4;
@@ -317,11 +303,12 @@ Shape shape_of(const ast_qk_cfg& c, const int heads[2], bool vec, bool bwd) {
     s.units = s.rot_units + ((c.head_dim - c.rotary) / s.vec + 1) / 2;
   }
   while (s.ls < 6 && (1 << s.ls) < s.units) ++s.ls;
-  const int groups = 256 >> s.ls;
+  const int groups = 256 >> s.ls;  // heads at a time
   for (int w = 0; w < 2; ++w) {
-    int64_t tb = std::max(1, QK_ROWS * groups / heads[w]);
+    const int most = bwd ? QK_MOST_BLOCKS : 2048;
+    int64_t tb = std::max<int64_t>((c.tokens + most - 1) / most, std::min<int64_t>((groups + heads[w] - 1) / heads[w], c.tokens / 256));
     if (c.rotary) tb = std::min<int64_t>(tb, QK_TRIG / (c.rotary / 2));
-    tb = std::max<int64_t>(1, std::min<int64_t>(tb, c.tokens / 256));
+    tb = std::max<int64_t>(1, std::min<int64_t>({tb, 64, (1 << 20) / heads[w]}));
     s.tb[w] = (int)tb;
     const int64_t need = (c.tokens + tb - 1) / tb;
     s.blocks[w] = (unsigned)std::min<int64_t>(need, bwd ? QK_MOST_BLOCKS : 1 << 20);

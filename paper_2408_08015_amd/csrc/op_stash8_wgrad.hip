@@ -2,8 +2,12 @@
 //   dW[n][c] = sum_t dy[t][n] * x'[t][c],   db[n] = sum_t dy[t][n]
 // on the bf16 matrix cores (a restored value is exact in bf16, so its product with dy is exact and only the fp32 sum rounds).
 // The contraction index is the row of both operands: the tiles lie in LDS as [row][channel] and the operands are read with the
-// transposing LDS read (four rows of 16 channels -> lane i gets the four rows of channel i).  Kept values are restored on
-// their way into LDS: every one of them once per block.
+// transposing LDS read (four rows of 16 channels -> lane i gets the four rows of channel i).
+//
+// A block computes a tile of 32 TM WM outputs x 32 TN WN inputs over a range of rows, 64 at a time, with two LDS stages.  The
+// next stage is filled while this one is multiplied, a quarter (16 rows) behind each of its four 16-row steps: 16 bytes of dy
+// and 8 kept values a thread, requested one stage earlier and restored on the way into LDS, each once per block (a conversion, a
+// multiplication, half a byte permutation).
 #include <algorithm>
 
 #include "ops.h"
@@ -14,10 +18,13 @@ namespace ast {
 
 namespace {
 
-constexpr int SW_BN = 128, SW_BC = 128, SW_BK = 32;  // outputs, inputs, rows of a block's step
+constexpr int SW_BK = 64;  // rows of a stage
+constexpr unsigned SW_OOB = 0x80000000u;  // an offset behind every buffer: zeros, and no memory access
 
 typedef short sw_short4 __attribute__((ext_vector_type(4)));
 typedef short sw_short8 __attribute__((ext_vector_type(8)));
+typedef unsigned int sw_u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int sw_u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) sw_short4 sw_lds_short4;
 
 struct SwArgs {
@@ -31,32 +38,54 @@ struct SwArgs {
   int add;          // out and bias_out are added to (one split only)
 };
 
-// [row][128 channels] bf16 tile, 16-byte chunks swizzled so that the four rows of a transposed read lie in different banks
-__device__ __forceinline__ int sw_off(int row, int chunk) { return row * 256 + ((chunk ^ ((row & 3) << 2)) << 4); }
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t sw_rsrc(const void* p, unsigned bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
 
+// [row][CH channels] bf16 tile, 16-byte chunks swizzled so that the four rows of a transposed read lie in different banks
+template <int CH>
+__device__ __forceinline__ int sw_off(int row, int chunk) { return row * (CH * 2) + ((chunk ^ ((row & 3) << 2)) << 4); }
+
+template <int CH>
 __device__ __forceinline__ bf16x8 sw_frag(const unsigned char* tile, int off) {
   const sw_short4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((sw_lds_short4*)(tile + off));
-  const sw_short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((sw_lds_short4*)(tile + off + 4 * 256));
+  const sw_short4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((sw_lds_short4*)(tile + off + 4 * CH * 2));
   const sw_short8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
   return __builtin_bit_cast(bf16x8, v);
 }
 
-__global__ __launch_bounds__(256) void stash8_wgrad_kernel(const SwArgs g) {
-  __shared__ __attribute__((aligned(16))) unsigned char sa[SW_BK * 256], sb[SW_BK * 256];
+// four kept values (the bytes of w) restored: bf16 pairs (exact, so the upper halves of the fp32 values)
+__device__ __forceinline__ void sw_restore4(uint32_t w, float s, uint32_t& lo, uint32_t& hi) {
+  float v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (float)(int)(int8_t)(w >> (8 * i)) * s;
+  lo = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302u);
+  hi = __builtin_amdgcn_perm(__float_as_uint(v[3]), __float_as_uint(v[2]), 0x07060302u);
+}
+
+// EVEN: rows of dy start at 16-byte addresses
+template <int WM, int WN, int TM, int TN, bool EVEN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void stash8_wgrad_kernel(const SwArgs g) {
+  constexpr int BN = 32 * TM * WM, BC = 32 * TN * WN, NT = 64 * WM * WN;
+  static_assert(16 * BN / 8 == NT && 16 * BC / 8 == NT, "a thread fills one chunk of each operand per quarter");
+  constexpr int A_BYTES = SW_BK * BN * 2, STAGE = A_BYTES + SW_BK * BC * 2;
+  extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wm = wave >> 1, wn = wave & 1;
-  int bid = blockIdx.x;
+  const int wm = wave / WN, wn = wave % WN;
+  // neighbouring tiles on one XCD: they share their rows of dy, or the kept values, in its L2
+  int bid = (int)xcd_grouped(blockIdx.x, gridDim.x);
   const int tc = bid % g.tiles_c; bid /= g.tiles_c;
   const int tn = bid % g.tiles_n;
   const int split = bid / g.tiles_n;
-  const int n0 = tn * SW_BN, c0 = tc * SW_BC;
+  const int n0 = tn * BN, c0 = tc * BC;
   const int64_t r_begin = split * g.rows_per_split, r_end = min(r_begin + g.rows_per_split, g.rows);
+  const int nk = (int)((r_end - r_begin + SW_BK - 1) / SW_BK);
 
-  floatx16 acc[2][2];
+  floatx16 acc[TM][TN];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   const bool bias = g.bias_out && tc == 0;
@@ -64,91 +93,157 @@ __global__ __launch_bounds__(256) void stash8_wgrad_kernel(const SwArgs g) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) bsum[e] = 0.f;
 
-  // this thread copies chunk `ch` (8 channels) of rows r0 and r0 + 16
-  const int ch = tid & 15, r0 = tid >> 4;
-  const int n = n0 + ch * 8, c = c0 + ch * 8;
-  const int j16 = lane & 15, blk = lane >> 4;
-  const int krow = 8 * (blk >> 1) + (j16 >> 2);
-  int ao[2], bo[2];
+  // ---- what this thread copies: one chunk of eight channels of each operand, of row `trow` of every quarter
+  const int chunk = tid % (BN / 8), trow = tid / (BN / 8);
+  const int n = n0 + chunk * 8, c = c0 + chunk * 8;
+  const int sp = g.pitch / kStash8Block;
+  unsigned a_voff[4], q_voff[4], s_voff[4];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int ca = wm * 64 + i * 32 + 16 * (blk & 1) + 4 * (j16 & 3), cb = wn * 64 + i * 32 + 16 * (blk & 1) + 4 * (j16 & 3);
-    ao[i] = sw_off(krow, ca >> 3) + (ca & 7) * 2;
-    bo[i] = sw_off(krow, cb >> 3) + (cb & 7) * 2;
+  for (int h = 0; h < 4; ++h) {
+    a_voff[h] = n < g.N ? (unsigned)((16 * h + trow) * g.N + n) * 2u : SW_OOB;
+    q_voff[h] = c < g.pitch ? (unsigned)((16 * h + trow) * g.pitch + c) : SW_OOB;
+    s_voff[h] = c < g.pitch ? (unsigned)((16 * h + trow) * sp + c / kStash8Block) : SW_OOB;
   }
-
-  for (int64_t r = r_begin; r < r_end; r += SW_BK) {
-    __syncthreads();
+  uint32_t ra[4][4], rq[4][2], rs[4];
+  // Rows behind the range come back as zeros (the buffers end with it).  A chunk that reaches behind its row reads values of the
+  // next one: they belong to outputs or inputs that do not exist, and are never written.
+  struct Stage { const bf16_t* dy; __amdgpu_buffer_rsrc_t a, q, s; unsigned left; };
+  auto stage_of = [&](int kt) __attribute__((always_inline)) {
+    const int64_t r = r_begin + (int64_t)kt * SW_BK;
+    const unsigned left = (unsigned)max((int64_t)0, min((int64_t)SW_BK, r_end - r));
+    return Stage{g.dy + r * g.N, sw_rsrc(g.dy + r * g.N, left * (unsigned)g.N * 2u), sw_rsrc(g.q + r * g.pitch, left * (unsigned)g.pitch),
+                 sw_rsrc(g.sc + r * sp, left * (unsigned)sp), left};
+  };
+  auto request = [&](const Stage& t, int h) __attribute__((always_inline)) {
+    if (EVEN) {
+      const sw_u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(t.a, a_voff[h], 0, 0);
+      ra[h][0] = v.x; ra[h][1] = v.y; ra[h][2] = v.z; ra[h][3] = v.w;
+    } else {
+      ra[h][0] = ra[h][1] = ra[h][2] = ra[h][3] = 0;
+      const bf16_t* src = t.dy + (int64_t)(16 * h + trow) * g.N + n;
+      if ((unsigned)(16 * h + trow) < t.left) {
+        if (n + 8 <= g.N) {
+          const Raw16 v = *reinterpret_cast<const Raw16*>(src);
 #pragma unroll
-    for (int p = 0; p < 2; ++p) {
-      const int rr = r0 + 16 * p;
-      const int64_t row = r + rr;
-      float v[8], w[8];
+          for (int e = 0; e < 4; ++e) ra[h][e] = v.w[e];
+        } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = w[e] = 0.f;
-      if (row < r_end) {
-        if (n + 8 <= g.N) load8(g.dy + row * g.N + n, v);
-        else if (n < g.N) load8_part(g.dy + row * g.N + n, g.N - n, v);
-        if (c < g.pitch) {
-          const uint2 q = *reinterpret_cast<const uint2*>(g.q + row * g.pitch + c);
-          const float s = __uint_as_float((uint32_t)g.sc[row * (g.pitch / kStash8Block) + c / kStash8Block] << 23);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            w[e] = (float)(int)(int8_t)(q.x >> (8 * e)) * s;
-            w[4 + e] = (float)(int)(int8_t)(q.y >> (8 * e)) * s;
-          }
+          for (int e = 0; e < 8; ++e)
+            if (n + e < g.N) ra[h][e / 2] |= (uint32_t)src[e] << (16 * (e & 1));
         }
       }
-      if (bias) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) bsum[e] += v[e];
-      }
-      *reinterpret_cast<uint4*>(sa + sw_off(rr, ch)) = make_uint4(f2bf_pk(v[0], v[1]), f2bf_pk(v[2], v[3]), f2bf_pk(v[4], v[5]), f2bf_pk(v[6], v[7]));
-      *reinterpret_cast<uint4*>(sb + sw_off(rr, ch)) = make_uint4(f2bf_pk(w[0], w[1]), f2bf_pk(w[2], w[3]), f2bf_pk(w[4], w[5]), f2bf_pk(w[6], w[7]));
     }
-    __syncthreads();
+    const sw_u32x2 q = __builtin_amdgcn_raw_buffer_load_b64(t.q, q_voff[h], 0, 0);
+    rq[h][0] = q.x; rq[h][1] = q.y;
+    rs[h] = __builtin_amdgcn_raw_buffer_load_b8(t.s, s_voff[h], 0, 0);
+  };
+  const int w_off = sw_off<BN>(trow, chunk), w_off_c = A_BYTES + sw_off<BC>(trow, chunk);
+  auto fill = [&](int h, int stage) __attribute__((always_inline)) {
+    if (bias) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8 fa[2], fb[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fa[i] = sw_frag(sa, ao[i] + ks * 16 * 256);
-        fb[i] = sw_frag(sb, bo[i] + ks * 16 * 256);
+      for (int e = 0; e < 4; ++e) {
+        bsum[2 * e] += __uint_as_float(ra[h][e] << 16);
+        bsum[2 * e + 1] += __uint_as_float(ra[h][e] & 0xffff0000u);
       }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
     }
+    *reinterpret_cast<uint4*>(smem + stage + w_off + h * 16 * BN * 2) = make_uint4(ra[h][0], ra[h][1], ra[h][2], ra[h][3]);
+    const float s = __uint_as_float(rs[h] << 23);
+    uint4 v;
+    sw_restore4(rq[h][0], s, v.x, v.y);
+    sw_restore4(rq[h][1], s, v.z, v.w);
+    *reinterpret_cast<uint4*>(smem + stage + w_off_c + h * 16 * BC * 2) = v;
+  };
+
+  // ---- operand fragments: lane l of a transposed read gives the address of four channels of one row
+  const int j16 = lane & 15, blk = lane >> 4;
+  const int krow = 8 * (blk >> 1) + (j16 >> 2);
+  int ao[TM], bo[TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int ch = wm * (32 * TM) + i * 32 + 16 * (blk & 1) + 4 * (j16 & 3);
+    ao[i] = sw_off<BN>(krow, ch >> 3) + (ch & 7) * 2;
+  }
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int ch = wn * (32 * TN) + j * 32 + 16 * (blk & 1) + 4 * (j16 & 3);
+    bo[j] = A_BYTES + sw_off<BC>(krow, ch >> 3) + (ch & 7) * 2;
+  }
+  bf16x8 fa[2][TM], fb[2][TN];  // of two steps: the next one's are read while this one's are multiplied
+  auto read = [&](int stage, int ks) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) fa[ks & 1][i] = sw_frag<BN>(smem, stage + ao[i] + ks * 16 * BN * 2);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) fb[ks & 1][j] = sw_frag<BC>(smem, stage + bo[j] + ks * 16 * BC * 2);
+  };
+  // every LDS access of the wavefront has been made; loads from memory stay in flight (__syncthreads() would wait for them)
+  auto barrier = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  {
+    const Stage t0 = stage_of(0), t1 = stage_of(1);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) request(t0, h);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      fill(h, 0);
+      request(t1, h);
+    }
+  }
+  barrier();
+  read(0, 0);
+  for (int kt = 0; kt < nk; ++kt) {
+    const int cur = (kt & 1) * STAGE, nxt = STAGE - cur;
+    const Stage t2 = stage_of(kt + 2);
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      if (ks < 3) read(cur, ks + 1);
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[ks & 1][i], fb[ks & 1][j], acc[i][j], 0, 0, 0);
+      fill(ks, nxt);
+      request(t2, ks);
+    }
+    barrier();
+    read(nxt, 0);  // (behind the last stage: zeros that nothing is made of)
   }
 
   if (bias) {  // 16 groups of rows, added in order
-    float* const sum = reinterpret_cast<float*>(sa);  // [16][128]
-    __syncthreads();
+    barrier();
+    float* const sum = reinterpret_cast<float*>(smem);  // [16][BN]
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum[r0 * 128 + ch * 8 + e] = bsum[e];
+    for (int e = 0; e < 8; ++e) sum[trow * BN + chunk * 8 + e] = bsum[e];
     __syncthreads();
-    if (tid < SW_BN && n0 + tid < g.N) {
+    if (tid < BN && n0 + tid < g.N) {
       float t = 0.f;
-      for (int k = 0; k < 16; ++k) t += sum[k * 128 + tid];
+      for (int k = 0; k < 16; ++k) t += sum[k * BN + tid];
       float* out = g.bias_out + (int64_t)split * g.N + n0 + tid;
       *out = (g.add ? *out : 0.f) + t;
     }
   }
-  // accumulator register r of lane l: row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32
-  float* out = g.out + (int64_t)split * g.N * g.C;
+  // Accumulator register r of lane l: row 8 (r / 4) + 4 (l / 32) + r % 4, column l % 32.  What lies outside the matrix goes to
+  // an offset behind the buffer, where a store is dropped.
+  const unsigned rows_here = (unsigned)min(BN, g.N - n0);
+  float* const tile = g.out + ((int64_t)split * g.N + n0) * g.C;
+  const __amdgpu_buffer_rsrc_t ro = sw_rsrc(tile, rows_here * (unsigned)g.C * 4u);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int cc = c0 + wn * 64 + j * 32 + (lane & 31);
-      if (cc >= g.C) continue;
+    for (int j = 0; j < TN; ++j) {
+      const int cc = c0 + wn * (32 * TN) + j * 32 + (lane & 31);
+      const unsigned row = wm * (32 * TM) + i * 32 + 4 * (lane >> 5);
+      const unsigned at = cc < g.C ? (row * (unsigned)g.C + (unsigned)cc) * 4u : SW_OOB;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int nn = n0 + wm * 64 + i * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-        if (nn >= g.N) continue;
-        float* p = out + (int64_t)nn * g.C + cc;
-        *p = (g.add ? *p : 0.f) + acc[i][j][r];
+        const unsigned off = at + (unsigned)(8 * (r >> 2) + (r & 3)) * (unsigned)g.C * 4u;
+        float v = acc[i][j][r];
+        if (g.add) v += __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(ro, off, 0, 0));
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), ro, off, 0, 0);
       }
     }
 }
@@ -169,22 +264,42 @@ __global__ __launch_bounds__(256) void stash8_wgrad_sum_kernel(const float* __re
   }
 }
 
-// shares of the rows: enough blocks for the chip, none of fewer than 256 rows
-int wgrad_splits(int64_t rows, int64_t in, int64_t out) {
-  const int64_t tiles = ((out + SW_BN - 1) / SW_BN) * ((in + SW_BC - 1) / SW_BC);
-  return (int)std::max<int64_t>(1, std::min<int64_t>({(512 + tiles - 1) / tiles, (rows + 255) / 256, 64}));
+// Tile and shares of the rows.
+struct WgradShape { bool big; int64_t tiles_n, tiles_c; int splits; };
+WgradShape wgrad_shape(int64_t rows, int64_t in, int64_t out) {
+  auto tiles = [&](int b) { return ((out + b - 1) / b) * ((in + b - 1) / b); };
+  WgradShape s = {};
+  s.big = tiles(256) >= 192;
+  const int b = s.big ? 256 : 128;
+  s.tiles_n = (out + b - 1) / b;
+  s.tiles_c = (in + b - 1) / b;
+  const int64_t t = s.tiles_n * s.tiles_c;
+  s.splits = s.big ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({256 / t, (rows + 255) / 256, 64}));
+  return s;
+}
+
+template <int WM, int WN, int TM, int TN>
+void launch(hipStream_t st, const SwArgs& g, unsigned blocks, bool even) {
+  constexpr int lds = 2 * SW_BK * 2 * (32 * TM * WM + 32 * TN * WN);
+  auto go = [&](auto kernel) {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    KLAUNCH_NAMED("stash8_wgrad_kernel", kernel, dim3(blocks), dim3(64 * WM * WN), lds, st, g);
+  };
+  if (even) go(stash8_wgrad_kernel<WM, WN, TM, TN, true>);
+  else go(stash8_wgrad_kernel<WM, WN, TM, TN, false>);
 }
 
 }  // namespace
 
 size_t linear_wgrad_stash8_ws_bytes(int64_t rows, int64_t in, int64_t out) {
-  const int s = wgrad_splits(rows, in, out);
+  const int s = wgrad_shape(rows, in, out).splits;
   return s > 1 ? (size_t)s * (size_t)(out * in + out) * sizeof(float) : 0;
 }
 
 void linear_wgrad_stash8(hipStream_t st, const void* dy, const void* stash, int64_t rows, int64_t in, int64_t out, float* dw,
                          float* db, bool accumulate, void* ws) {
-  const int splits = wgrad_splits(rows, in, out);
+  const WgradShape s = wgrad_shape(rows, in, out);
+  const int splits = s.splits;
   SwArgs g = {};
   g.dy = static_cast<const bf16_t*>(dy);
   g.q = static_cast<const uint8_t*>(stash);
@@ -194,14 +309,17 @@ void linear_wgrad_stash8(hipStream_t st, const void* dy, const void* stash, int6
   g.N = (int)out;
   g.C = (int)in;
   g.pitch = (int)stash8_pitch(in);
-  g.tiles_n = (int)((out + SW_BN - 1) / SW_BN);
-  g.tiles_c = (int)((in + SW_BC - 1) / SW_BC);
+  g.tiles_n = (int)s.tiles_n;
+  g.tiles_c = (int)s.tiles_c;
   float* part = static_cast<float*>(ws);
   float* bias_part = part + (size_t)splits * out * in;
   g.out = splits > 1 ? part : dw;
   g.bias_out = !db ? nullptr : splits > 1 ? bias_part : db;
   g.add = splits == 1 && accumulate;
-  KLAUNCH(stash8_wgrad_kernel, dim3((unsigned)(g.tiles_n * g.tiles_c * splits)), dim3(256), 0, st, g);
+  const bool even = out % 8 == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0;
+  const unsigned blocks = (unsigned)(g.tiles_n * g.tiles_c * splits);
+  if (s.big) launch<4, 2, 2, 4>(st, g, blocks, even);
+  else launch<2, 2, 2, 2>(st, g, blocks, even);
   if (splits > 1) {
     const int64_t n = out * in;
     KLAUNCH(stash8_wgrad_sum_kernel, dim3((unsigned)std::min<int64_t>((n + out + 255) / 256, 1 << 16)), dim3(256), 0, st, part, n, dw,
