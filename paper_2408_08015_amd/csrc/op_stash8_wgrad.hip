@@ -104,9 +104,12 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void stash8_wgrad_kernel(const SwA
     q_voff[h] = c < g.pitch ? (unsigned)((16 * h + trow) * g.pitch + c) : SW_OOB;
     s_voff[h] = c < g.pitch ? (unsigned)((16 * h + trow) * sp + c / kStash8Block) : SW_OOB;
   }
+  // A last chunk that would reach behind its row is read from `over` values further in front, and shifted when it is used.
+  const int over = !EVEN && g.N >= 8 && n < g.N ? max(n + 8 - g.N, 0) : 0;
+  const bool ragged = !EVEN && g.N >= 8 && n0 + BN > g.N;
   uint32_t ra[4][4], rq[4][2], rs[4];
-  // Rows behind the range come back as zeros (the buffers end with it).  A chunk that reaches behind its row reads values of the
-  // next one: they belong to outputs or inputs that do not exist, and are never written.
+  // Rows behind the range come back as zeros (the buffers end with it).  Kept values behind a row's are the next row's: they belong
+  // to inputs that do not exist, and are never written.
   struct Stage { const bf16_t* dy; __amdgpu_buffer_rsrc_t a, q, s; unsigned left; };
   auto stage_of = [&](int kt) __attribute__((always_inline)) {
     const int64_t r = r_begin + (int64_t)kt * SW_BK;
@@ -120,16 +123,16 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void stash8_wgrad_kernel(const SwA
       ra[h][0] = v.x; ra[h][1] = v.y; ra[h][2] = v.z; ra[h][3] = v.w;
     } else {
       ra[h][0] = ra[h][1] = ra[h][2] = ra[h][3] = 0;
-      const bf16_t* src = t.dy + (int64_t)(16 * h + trow) * g.N + n;
-      if ((unsigned)(16 * h + trow) < t.left) {
-        if (n + 8 <= g.N) {
-          const Raw16 v = *reinterpret_cast<const Raw16*>(src);
+      if (n < g.N && (unsigned)(16 * h + trow) < t.left) {
+        const bf16_t* src = t.dy + (unsigned)((16 * h + trow) * g.N + n);
+        if (g.N >= 8) {
+          const Raw16 v = *reinterpret_cast<const Raw16*>(src - over);
 #pragma unroll
           for (int e = 0; e < 4; ++e) ra[h][e] = v.w[e];
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (n + e < g.N) ra[h][e / 2] |= (uint32_t)src[e] << (16 * (e & 1));
+          for (int e = 0; e < 7; ++e)
+            if (e < g.N) ra[h][e / 2] |= (uint32_t)src[e] << (16 * (e & 1));
         }
       }
     }
@@ -139,6 +142,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void stash8_wgrad_kernel(const SwA
   };
   const int w_off = sw_off<BN>(trow, chunk), w_off_c = A_BYTES + sw_off<BC>(trow, chunk);
   auto fill = [&](int h, int stage) __attribute__((always_inline)) {
+    if (ragged) {
+      uint64_t lo = ra[h][0] | (uint64_t)ra[h][1] << 32, hi = ra[h][2] | (uint64_t)ra[h][3] << 32;
+      const int by = 16 * (over & 3);
+      if (over >= 4) lo = hi, hi = 0;
+      lo = by ? lo >> by | hi << (64 - by) : lo;
+      hi >>= by;
+      ra[h][0] = (uint32_t)lo; ra[h][1] = (uint32_t)(lo >> 32); ra[h][2] = (uint32_t)hi; ra[h][3] = (uint32_t)(hi >> 32);
+    }
     if (bias) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -264,18 +275,29 @@ __global__ __launch_bounds__(256) void stash8_wgrad_sum_kernel(const float* __re
   }
 }
 
-// Tile and shares of the rows.
+// Tile and shares of the rows: the cheapest by a model in us of what was measured - 64 rows of a 256 x 256 tile take 1.85, of a
+// 128 x 128 tile 0.85 (one block a compute unit), a launch's ends 8 and 6, and shares write and read partials of 4 bytes
+// (6 TB/s) and cost a second launch, 5.  2048 -> 512 of 4096 rows in small tiles and 4 shares 28 us, in big ones 42 by the model;
+// 4096 -> 4096 of 16384 rows in big tiles 472 us, in small ones 870.
 struct WgradShape { bool big; int64_t tiles_n, tiles_c; int splits; };
 WgradShape wgrad_shape(int64_t rows, int64_t in, int64_t out) {
-  auto tiles = [&](int b) { return ((out + b - 1) / b) * ((in + b - 1) / b); };
-  WgradShape s = {};
-  s.big = tiles(256) >= 192;
-  const int b = s.big ? 256 : 128;
-  s.tiles_n = (out + b - 1) / b;
-  s.tiles_c = (in + b - 1) / b;
-  const int64_t t = s.tiles_n * s.tiles_c;
-  s.splits = s.big ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>({256 / t, (rows + 255) / 256, 64}));
-  return s;
+  WgradShape best = {};
+  double least = 0;
+  for (const bool big : {false, true}) {
+    const int b = big ? 256 : 128;
+    const int64_t tn = (out + b - 1) / b, tc = (in + b - 1) / b;
+    for (const int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+      if (s > 1 && rows < (int64_t)s * 128) break;
+      const double steps = (double)((rows + s - 1) / s + SW_BK - 1) / SW_BK, rounds = (double)((tn * tc * s + 255) / 256);
+      double us = rounds * steps * (big ? 1.85 : 0.85) + (big ? 8 : 6);
+      if (s > 1) us += 5 + (double)s * (double)in * (double)out * 8 / 6e6;
+      if (!best.splits || us < least) {
+        least = us;
+        best = {big, tn, tc, s};
+      }
+    }
+  }
+  return best;
 }
 
 template <int WM, int WN, int TM, int TN>
