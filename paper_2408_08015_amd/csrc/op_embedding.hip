@@ -13,28 +13,76 @@ namespace ast {
 
 namespace {
 
-// Forward: L = 2^ls lanes per row, eight values each at a time.
-template <typename TW, typename TY>
+// Forward: bound by its bytes, so the output is taken as one run of values, eight of a thread at 16-byte addresses whatever the
+// row length, U times a thread with all ids, then all rows requested before the first is used.  A group of eight that goes on
+// in the next row takes the last eight values of its row and the first eight of the next one.  (width >= 8)
+template <typename TW, typename TY, int U, bool EVEN>  // EVEN: rows of the table start at 16-byte addresses
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(const int32_t* __restrict__ ids, int64_t tokens,
                                                             const TW* __restrict__ table, uint32_t rows, int width,
-                                                            float scale, TY* __restrict__ y, int ls) {
-  const int lane = threadIdx.x & ((1 << ls) - 1);
-  const int per = 256 >> ls;  // rows of a block at a time
-  for (int64_t t = (int64_t)blockIdx.x * per + (threadIdx.x >> ls); t < tokens; t += (int64_t)gridDim.x * per) {
-    const uint32_t id = (uint32_t)ids[t];
-    const bool live = id < rows;
-    const TW* src = table + (size_t)(live ? id : 0) * width;
-    TY* dst = y + (size_t)t * width;
-    for (int c = lane * 8; c < width; c += 8 << ls) {
-      float v[8];
-      const int n = width - c;
-      if (n >= 8) load8(src + c, v);
-      else load8_part(src + c, n, v);
+                                                            float inv_width, float scale, TY* __restrict__ y) {
+  constexpr int SPAN = 256 * 8 * U;  // values of a block
+  const int64_t total = tokens * width;
+  for (int64_t base = (int64_t)blockIdx.x * SPAN; base < total; base += (int64_t)gridDim.x * SPAN) {
+    // (base < 2^51: exact, but for the last bit of the quotient)
+    int64_t t0 = (int64_t)((double)base / (double)width);
+    int64_t in_row = base - t0 * width;
+    if (in_row < 0) --t0, in_row += width;
+    if (in_row >= width) ++t0, in_row -= width;
+    int c[U], over[U];  // place in the row, and values that lie in the next one
+    uint32_t k0[U], k1[U];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = live ? v[i] * scale : 0.f;
-      if (n >= 8) store8(dst + c, v);
-      else store8_part(dst + c, n, v);
+    for (int u = 0; u < U; ++u) {
+      const int off = (int)in_row + (u * 256 + (int)threadIdx.x) * 8;  // (< 2^21)
+      int q = (int)((float)off * inv_width), r = off - q * width;
+      if (r < 0) --q, r += width;
+      if (r >= width) ++q, r -= width;
+      over[u] = max(r + 8 - width, 0);
+      c[u] = r - over[u];
+      k0[u] = (uint32_t)ids[min(t0 + q, tokens - 1)];
+      k1[u] = (uint32_t)ids[min(t0 + q + 1, tokens - 1)];
     }
+    Eight<TW, EVEN> a[U], b[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      a[u].load(table + (size_t)(k0[u] < rows ? k0[u] : 0) * width + c[u]);
+      b[u] = a[u];
+      if (over[u]) b[u].load(table + (size_t)(k1[u] < rows ? k1[u] : 0) * width);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      constexpr int W = Eight<TW, EVEN>::W;
+      uint32_t w[W];
+      a[u].words(w);
+#pragma unroll
+      for (int i = 0; i < W; ++i) w[i] = k0[u] < rows ? w[i] : 0;
+      if (__any(over[u])) {
+        uint32_t x[W];
+        b[u].words(x);
+#pragma unroll
+        for (int i = 0; i < W; ++i) x[i] = k1[u] < rows ? x[i] : 0;
+        funnel<W>(w, x, (uint32_t)over[u] * (uint32_t)sizeof(TW));
+      }
+      float v[8];
+      eight_values<TW>(w, v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] *= scale;
+      const int64_t f = base + (u * 256 + (int)threadIdx.x) * 8;
+      if (f + 8 <= total) store8(y + f, v);
+      else if (f < total) store8_part(y + f, (int)(total - f), v);
+    }
+  }
+}
+
+// ... and rows of fewer than eight values: one value a thread
+template <typename TW, typename TY>
+__global__ __launch_bounds__(256) void embedding_fwd_narrow_kernel(const int32_t* __restrict__ ids, int64_t tokens,
+                                                                   const TW* __restrict__ table, uint32_t rows, int width,
+                                                                   float scale, TY* __restrict__ y) {
+  const int64_t total = tokens * width;
+  for (int64_t f = (int64_t)blockIdx.x * 256 + threadIdx.x; f < total; f += (int64_t)gridDim.x * 256) {
+    const int64_t t = f / width;
+    const uint32_t k = (uint32_t)ids[t];
+    store1(y + f, k < rows ? load1(table + (size_t)k * width + (f - t * width)) * scale : 0.f);
   }
 }
 
@@ -316,17 +364,25 @@ __global__ __launch_bounds__(512) void embedding_join_kernel(const SumArgs g) {
   __shared__ double sh[8][SUM_COLS];
   const int64_t c0 = blockIdx.x;
   const int64_t lo = c0 * g.chunk, hi = lo + g.chunk;  // (the last chunk has no block)
-  const uint32_t k = g.key[hi - 1];
-  if (k >= g.rows || g.key[hi] != k) return;                                      // nothing goes on behind this chunk
-  if (g.key[lo] == k && lo > 0 && g.key[lo - 1] == k) return;                     // it began in front of it
-  // last chunk of the run: the first place behind it, by bisection
-  int64_t a = hi, b = g.tokens;
-  while (a < b) {
-    const int64_t m = (a + b) / 2;
-    if (g.key[m] == k) a = m + 1; else b = m;
-  }
-  const int64_t last = (a - 1) / g.chunk;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t chunks = (g.tokens + g.chunk - 1) / g.chunk;
+  const uint32_t k = g.key[hi - 1], behind = g.key[hi], first = g.key[lo], before = lo > 0 ? g.key[lo - 1] : 0xffffffffu;
+  // does the run go on in a chunk (its first key)?  Every wavefront looks at 64 chunks at a time
+  auto goes_on = [&](int64_t j) { return j < chunks && g.key[j * g.chunk] == k; };
+  uint64_t on = __ballot(goes_on(c0 + 1 + lane));
+  if (k >= g.rows || behind != k) return;     // nothing goes on behind this chunk
+  if (first == k && before == k) return;      // it began in front of it
+  int64_t last = c0 + (~on ? __builtin_ctzll(~on) : 64);
+  if (!~on) {  // a long one: 64 steps of 64 chunks, then the chunks of the last step
+    for (;;) {
+      on = __ballot(goes_on(last + 64 * (lane + 1)));
+      if (~on) break;
+      last += 64 * 64;
+    }
+    last += 64 * __builtin_ctzll(~on);
+    on = __ballot(goes_on(last + 1 + lane));
+    last += ~on ? __builtin_ctzll(~on) : 64;
+  }
   const int c = blockIdx.y * SUM_COLS + lane * 8, n = g.width - c;
   double v[8];
 #pragma unroll
@@ -356,28 +412,38 @@ __global__ __launch_bounds__(512) void embedding_join_kernel(const SumArgs g) {
   }
 }
 
-int row_lanes_log2(int64_t width) {  // lanes that share a row's chunks of eight
-  int ls = 0;
-  while (ls < 8 && (8 << ls) < width) ++ls;
-  return ls;
-}
-
 }  // namespace
 
 void embedding_fwd(hipStream_t st, const int32_t* ids, int64_t tokens, const void* table, bool table_bf16, int64_t rows,
                    int64_t width, float scale, void* y, bool y_bf16) {
   if (tokens <= 0) return;
-  const int ls = row_lanes_log2(width), per = 256 >> ls;
-  const unsigned blocks = (unsigned)std::min<int64_t>((tokens + per - 1) / per, 1 << 20);
-#define LAUNCH(TW, TY)                                                                                                        \
-  KLAUNCH((embedding_fwd_kernel<TW, TY>), dim3(blocks), dim3(256), 0, st, ids, tokens, static_cast<const TW*>(table), (uint32_t)rows, \
-          (int)width, scale, static_cast<TY*>(y), ls)
+  const int64_t total = tokens * width;
+  const unsigned most = 1 << 20;
+#define NARROW(TW, TY)                                                                                                       \
+  KLAUNCH((embedding_fwd_narrow_kernel<TW, TY>), dim3((unsigned)std::min<int64_t>((total + 255) / 256, most)), dim3(256), 0, st, ids, \
+          tokens, static_cast<const TW*>(table), (uint32_t)rows, (int)width, scale, static_cast<TY*>(y))
+#define LAUNCH(TW, TY, U, EVEN)                                                                                              \
+  KLAUNCH((embedding_fwd_kernel<TW, TY, U, EVEN>), dim3((unsigned)std::min<int64_t>((total + 2048 * U - 1) / (2048 * U), most)), \
+          dim3(256), 0, st, ids, tokens, static_cast<const TW*>(table), (uint32_t)rows, (int)width, 1.f / (float)width, scale,  \
+          static_cast<TY*>(y))
+  // (four groups a thread where that leaves the chip full)
+  const bool wide = total >= 8 * 256 * 4 * 1024;
+  const bool even = width * (table_bf16 ? 2 : 4) % 16 == 0 && reinterpret_cast<uintptr_t>(table) % 16 == 0;
+#define PICK(TW, TY)                            \
+  do {                                          \
+    if (width < 8) NARROW(TW, TY);              \
+    else if (wide && even) LAUNCH(TW, TY, 4, true);  \
+    else if (wide) LAUNCH(TW, TY, 4, false);    \
+    else LAUNCH(TW, TY, 1, false);              \
+  } while (0)
   if (table_bf16) {
-    if (y_bf16) LAUNCH(bf16_t, bf16_t); else LAUNCH(bf16_t, float);
+    if (y_bf16) PICK(bf16_t, bf16_t); else PICK(bf16_t, float);
   } else {
-    if (y_bf16) LAUNCH(float, bf16_t); else LAUNCH(float, float);
+    if (y_bf16) PICK(float, bf16_t); else PICK(float, float);
   }
+#undef PICK
 #undef LAUNCH
+#undef NARROW
 }
 
 namespace {
@@ -386,7 +452,6 @@ constexpr int64_t RANK_MOST = 16384;  // tokens that are placed by counting
 
 int chunk_of(int64_t tokens) {  // tokens of a wavefront: the chip filled, and no more than 8192 partials
   int c = 8;
-  while (c < 32 && tokens / c >= 2048) c *= 2;
   while ((tokens + c - 1) / c > 8192) c *= 2;
   return c;
 }
