@@ -4,6 +4,7 @@
 // last), so that the tokens of a row lie next to each other and one wavefront adds them in their order: no atomics, equal
 // calls give equal bits.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 #include "ops_device.h"
@@ -285,29 +286,44 @@ struct SumArgs {
 
 constexpr int SUM_COLS = 512;
 
-__device__ __forceinline__ void put_row(const SumArgs& g, uint32_t k, int c, const double (&v)[8]) {
+// How the columns are read and written: eight at 16-byte addresses; eight at any address, where the last lane of a row takes its
+// last eight and so some of its neighbour's (both write the same values); or what there is of rows of fewer than eight.
+enum : int { COLS_EVEN = 0, COLS_ANY = 1, COLS_NARROW = 2 };
+template <int COLS>
+__device__ __forceinline__ int first_col(int width, int lane) {
+  const int c = blockIdx.y * SUM_COLS + lane * 8;
+  return COLS == COLS_ANY && c < width ? min(c, width - 8) : c;
+}
+template <int COLS>
+__device__ __forceinline__ void put8(float* p, int n, const float (&v)[8]) {
+  if (COLS == COLS_NARROW) store8_part(p, n, v);
+  else store8(p, v);
+}
+template <int COLS>
+__device__ __forceinline__ void put_row(const SumArgs& g, uint32_t k, int c, const float (&v)[8]) {
   float* p = g.dtable + (size_t)k * g.width + c;
-  const int n = g.width - c;
   float f[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = 0.f;
   if (g.accumulate) {
-    if (n >= 8) load8(p, f);
-    else load8_part(p, n, f);
-  }
+    if (COLS == COLS_NARROW) load8_part(p, g.width - c, f);
+    else load8(p, f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = fmaf((float)v[i], g.scale, f[i]);
-  if (n >= 8) store8(p, f);
-  else store8_part(p, n, f);
+    for (int i = 0; i < 8; ++i) f[i] = fmaf(v[i], g.scale, f[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = v[i] * g.scale;
+  }
+  put8<COLS>(p, g.width - c, f);
 }
 
-template <typename T>
+template <typename T, int COLS>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const SumArgs g, const T* __restrict__ dy) {
+  constexpr int B = COLS == COLS_EVEN ? 8 : 4;  // tokens whose rows are requested at a time
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t chunk_id = (int64_t)blockIdx.x * 4 + wave;
   const int64_t lo = chunk_id * g.chunk, hi = min(lo + g.chunk, g.tokens);
   if (lo >= hi) return;
-  const int c = blockIdx.y * SUM_COLS + lane * 8, n = g.width - c;
+  const int c = first_col<COLS>(g.width, lane);
+  const bool live = c < g.width;
   if (g.key[lo] >= g.rows) return;  // behind the last row: padding
   const bool began = lo > 0 && g.key[lo - 1] == g.key[lo];
   const uint32_t next = hi < g.tokens ? g.key[hi] : 0xffffffffu;
@@ -317,32 +333,29 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const SumArgs g, con
   uint32_t cur = g.key[lo];
   bool first = true;
   auto flush = [&](bool last) __attribute__((always_inline)) {
-    if (n <= 0 || cur >= g.rows) return;
+    if (cur >= g.rows) return;
     const bool open = first && began;
     if (open || (last && next == cur)) {
-      float* p = g.part + ((size_t)chunk_id * 2 + (open ? 0 : 1)) * g.width + c;
-      if (n >= 8) store8(p, acc);
-      else store8_part(p, n, acc);
-    } else {
-      double v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = acc[i];
-      put_row(g, cur, c, v);
+      if (live) put8<COLS>(g.part + ((size_t)chunk_id * 2 + (open ? 0 : 1)) * g.width + c, g.width - c, acc);
+    } else if (live) {
+      put_row<COLS>(g, cur, c, acc);
     }
   };
-  for (int64_t i = lo; i < hi; i += 8) {
-    float v[8][8];
-    uint32_t k[8];
-    const int m = (int)min((int64_t)8, hi - i);
+  for (int64_t i = lo; i < hi; i += B) {
+    Eight<T, COLS == COLS_EVEN> raw[B];
+    float part[COLS == COLS_NARROW ? B : 1][8];
+    uint32_t k[B];
+    const int m = (int)min((int64_t)B, hi - i);
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      k[r] = r < m ? g.key[i + r] : 0xffffffffu;
-      const T* src = dy + (size_t)(r < m ? g.order[i + r] : 0) * g.width + c;
-      if (r < m && n >= 8) load8(src, v[r]);
-      else load8_part(src, r < m ? n : 0, v[r]);
+    for (int r = 0; r < B; ++r) {  // (behind the end: the last row once more)
+      const int64_t at = i + min(r, m - 1);
+      k[r] = g.key[at];
+      const T* src = dy + (size_t)g.order[at] * g.width + (live ? c : 0);
+      if (COLS == COLS_NARROW) load8_part(src, live ? g.width - c : 0, part[COLS == COLS_NARROW ? r : 0]);
+      else raw[r].load(src);
     }
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
+    for (int r = 0; r < B; ++r) {
       if (r >= m) break;
       if (k[r] != cur) {
         flush(false);
@@ -351,8 +364,10 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const SumArgs g, con
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = 0.f;
       }
+      float v[8];
+      if (COLS != COLS_NARROW) raw[r].values(v);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += v[r][e];
+      for (int e = 0; e < 8; ++e) acc[e] += COLS == COLS_NARROW ? part[COLS == COLS_NARROW ? r : 0][e] : v[e];
     }
   }
   flush(true);
@@ -360,7 +375,8 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const SumArgs g, con
 
 // Runs that cross chunks: the block of the chunk in which one begins adds up its partials, each wavefront every eighth, in 64
 // bits, and the wavefronts' sums in their order.
-__global__ __launch_bounds__(512) void embedding_join_kernel(const SumArgs g) {
+template <int COLS>
+__global__ __launch_bounds__(512, 6) void embedding_join_kernel(const SumArgs g) {
   __shared__ double sh[8][SUM_COLS];
   const int64_t c0 = blockIdx.x;
   const int64_t lo = c0 * g.chunk, hi = lo + g.chunk;  // (the last chunk has no block)
@@ -383,32 +399,36 @@ __global__ __launch_bounds__(512) void embedding_join_kernel(const SumArgs g) {
     on = __ballot(goes_on(last + 1 + lane));
     last += ~on ? __builtin_ctzll(~on) : 64;
   }
-  const int c = blockIdx.y * SUM_COLS + lane * 8, n = g.width - c;
+  const int c = first_col<COLS>(g.width, lane), n = g.width - c;
   double v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 0;
-  for (int64_t j0 = c0 + wave; j0 <= last; j0 += 32) {  // four loads at a time
-    float f[4][8];
+  if (n > 0)
+    for (int64_t j0 = c0 + wave; j0 <= last; j0 += 16) {  // two at a time
+      float f[2][8];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int64_t j = j0 + 8 * q;
-      const float* p = g.part + ((size_t)j * 2 + (j == c0 ? 1 : 0)) * g.width + c;
-      if (j <= last && n >= 8) load8(p, f[q]);
-      else load8_part(p, j <= last ? n : 0, f[q]);
+      for (int q = 0; q < 2; ++q) {
+        const int64_t j = min(j0 + 8 * q, last);
+        const float* p = g.part + ((size_t)j * 2 + (j == c0 ? 1 : 0)) * g.width + c;
+        if (COLS == COLS_NARROW) load8_part(p, n, f[q]);
+        else load8(p, f[q]);
+      }
+#pragma unroll
+      for (int q = 0; q < 2; ++q)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += j0 + 8 * q <= last ? f[q][i] : 0.f;
     }
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] += f[q][i];
-  }
 #pragma unroll
   for (int i = 0; i < 8; ++i) sh[wave][i * 64 + lane] = v[i];
   __syncthreads();
   if (wave == 0 && n > 0) {
+    float f[8];
     for (int w = 1; w < 8; ++w)
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += sh[w][i * 64 + lane];
-    put_row(g, k, c, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (float)v[i];
+    put_row<COLS>(g, k, c, f);
   }
 }
 
@@ -452,6 +472,7 @@ constexpr int64_t RANK_MOST = 16384;  // tokens that are placed by counting
 
 int chunk_of(int64_t tokens) {  // tokens of a wavefront: the chip filled, and no more than 8192 partials
   int c = 8;
+  while (c < 32 && tokens / c >= 2048) c *= 2;
   while ((tokens + c - 1) / c > 8192) c *= 2;
   return c;
 }
@@ -561,11 +582,18 @@ void embedding_bwd(hipStream_t st, const int32_t* ids, int64_t tokens, const voi
   g.dtable = dtable;
   const int64_t chunks = chunks_of(tokens);
   g.part = reinterpret_cast<float*>(take((size_t)chunks * 2 * width * 4));
-  const unsigned cols = (unsigned)((width + SUM_COLS - 1) / SUM_COLS);
-  const dim3 grid((unsigned)((chunks + 3) / 4), cols);
-  if (dy_bf16) KLAUNCH(embedding_sum_kernel<bf16_t>, grid, dim3(256), 0, st, g, static_cast<const bf16_t*>(dy));
-  else KLAUNCH(embedding_sum_kernel<float>, grid, dim3(256), 0, st, g, static_cast<const float*>(dy));
-  if (chunks > 1) KLAUNCH(embedding_join_kernel, dim3((unsigned)(chunks - 1), cols), dim3(512), 0, st, g);
+  const unsigned cols_blocks = (unsigned)((width + SUM_COLS - 1) / SUM_COLS);
+  const dim3 grid((unsigned)((chunks + 3) / 4), cols_blocks);
+  const bool even = width % 8 == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0 && reinterpret_cast<uintptr_t>(dtable) % 16 == 0;
+  auto go = [&](auto cols) {
+    constexpr int C = decltype(cols)::value;
+    if (dy_bf16) KLAUNCH_NAMED("embedding_sum_kernel", (embedding_sum_kernel<bf16_t, C>), grid, dim3(256), 0, st, g, static_cast<const bf16_t*>(dy));
+    else KLAUNCH_NAMED("embedding_sum_kernel", (embedding_sum_kernel<float, C>), grid, dim3(256), 0, st, g, static_cast<const float*>(dy));
+    if (chunks > 1) KLAUNCH_NAMED("embedding_join_kernel", (embedding_join_kernel<C>), dim3((unsigned)(chunks - 1), cols_blocks), dim3(512), 0, st, g);
+  };
+  if (even) go(std::integral_constant<int, COLS_EVEN>());
+  else if (width >= 8) go(std::integral_constant<int, COLS_ANY>());
+  else go(std::integral_constant<int, COLS_NARROW>());
 }
 
 }  // namespace ast
