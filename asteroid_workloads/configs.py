@@ -13,9 +13,11 @@ Layer dictionaries (keys are plain ints/floats/bools):
   se_begin ... se_scale   squeeze-and-excitation: the layers in between (global_avgpool, linear,
                swish, linear, sigmoid) turn the tensor at se_begin into one gate per sample and
                channel; se_scale multiplies that tensor by its gate
-  linear       cin cout bias
+  linear       cin cout bias (keep8: its input is kept in 8 bits for the backward pass)
   layernorm    d eps
-  mha          d heads
+  mha          d heads (qk_norm rotary theta interleaved eps: norm and rotation of queries and keys; keep8)
+  gelu         (keep8)
+  embedding    rows d scale: the first layer of a stage whose input is token ids
 """
 from dataclasses import dataclass, field
 from typing import List, Tuple
@@ -156,6 +158,17 @@ def encoder_layer(d, heads, ffn, eps=1e-5):
             simple("res_add"), dict(kind="layernorm", d=d, eps=eps)]
 
 
+def lm_encoder_layer(d, heads, ffn, eps=1e-5, keep8=True, theta=10000):
+    """The encoder layer with norm and rotation of queries and keys, its dense layers' inputs and GELU's
+    pre-activation kept in 8 bits."""
+    k8 = int(keep8)
+    return [simple("res_begin"),
+            dict(kind="mha", d=d, heads=heads, qk_norm=1, rotary=d // heads, theta=theta, eps=1e-6, keep8=k8),
+            simple("res_add"), dict(kind="layernorm", d=d, eps=eps),
+            simple("res_begin"), dict(linear(d, ffn), keep8=k8), dict(simple("gelu"), keep8=k8),
+            dict(linear(ffn, d), keep8=k8), simple("res_add"), dict(kind="layernorm", d=d, eps=eps)]
+
+
 def vgg_layers(cin, c):
     return [conv(cin, c, 3, 1, 1, bias=True), simple("relu"),
             conv(c, c, 3, 1, 1, bias=True), simple("relu"),
@@ -230,6 +243,15 @@ def cfg7(B=32, M=4, hw=56, seed=1008, cin=64, mid=64, blocks=3):
     return StageConfig("cfg7_resnet50_stage", L, B, M, (cin, hw, hw), "f32", "nchw", True, seed)
 
 
+def lm_stage(B=32, M=4, S=128, d=512, heads=8, ffn=2048, nlayers=6, rows=32768, keep8=True, seed=1010):
+    """The first stage of a language model: token embedding, then encoder layers whose queries and keys are
+    normalised and rotated; what the backward pass needs of the dense layers is kept in 8 bits."""
+    L = [dict(kind="embedding", rows=rows, d=d, scale=float(d) ** 0.5)]
+    for _ in range(nlayers):
+        L += lm_encoder_layer(d, heads, ffn, keep8=keep8)
+    return StageConfig("lm_stage_bf16", L, B, M, (S, 1), "bf16", "bsd", False, seed, init="normal0.02")
+
+
 def effnetb1(B=8, M=8, hw=240, seed=1007, num_classes=1000):
     """The whole EfficientNet-B1 as one stage (profiler tables; no stored full-size oracle samples)."""
     return StageConfig("effnetb1_full", efficientnet_b1_layers(num_classes), B, M, (3, hw, hw),
@@ -244,7 +266,7 @@ def resnet50(B=8, M=8, hw=224, seed=1009, num_classes=1000):
 
 CONFIGS = {
     "cfg1": cfg1, "cfg2": cfg2, "cfg3": cfg3, "cfg4": cfg4, "cfg5": cfg5, "cfg6": cfg6,
-    "cfg7": cfg7, "effnetb1": effnetb1, "resnet50": resnet50,
+    "cfg7": cfg7, "effnetb1": effnetb1, "resnet50": resnet50, "lm": lm_stage,
 }
 
 

@@ -3,7 +3,8 @@
 Draw order for a config with seed s, from numpy Generator(PCG64(s)):
 x (boundary layout), then labels or dy, then the parameters in flat order.
 Flat parameter order = layer order; inside a layer weight then bias
-(BatchNorm / LayerNorm: gamma then beta; MHA: W_qkv[3D][D], b_qkv[3D], W_o[D][D], b_o[D]).
+(BatchNorm / LayerNorm: gamma then beta; MHA: W_qkv[3D][D], b_qkv[3D], W_o[D][D], b_o[D], with
+qk_norm q_gain, k_gain; embedding: its table [rows][d]).
 Conv weights are logically [Cout][Cin/groups][kh][kw], linear weights [out][in].
 """
 import numpy as np
@@ -36,6 +37,11 @@ def param_specs(layers):
             specs.append((i, "b_qkv", (3 * d,), 0, "bias"))
             specs.append((i, "w_o", (d, d), d, "weight"))
             specs.append((i, "b_o", (d,), 0, "bias"))
+            if L.get("qk_norm"):
+                specs.append((i, "q_gain", (d // L["heads"],), 0, "gamma"))
+                specs.append((i, "k_gain", (d // L["heads"],), 0, "gamma"))
+        elif k == "embedding":
+            specs.append((i, "table", (L["rows"], L["d"]), L["d"], "weight"))
     return specs
 
 
@@ -109,6 +115,8 @@ def layer_shapes(layers, in_shape):
             s = (s[0],)
         elif k == "linear":
             s = s[:-1] + (L["cout"],)
+        elif k == "embedding":
+            s = s[:-1] + (L["d"],)
         shapes.append(s)
     return shapes
 
@@ -125,7 +133,13 @@ def make_inputs(cfg, randomize_affine=False):
     to bf16-representable values so every consumer sees identical numbers."""
     rng = np.random.Generator(np.random.PCG64(cfg.seed))
     n = cfg.B * cfg.M
-    x = rng.standard_normal(boundary_shape(cfg.layout, cfg.in_shape, n)).astype(np.float32)
+    tokens = cfg.layers[0]["kind"] == "embedding"
+    if tokens:   # ids as text has them (the k-th commonest in proportion to 1 / k), a few of them padding
+        u = rng.random((n, cfg.in_shape[0]))
+        x = np.minimum(np.exp(u * np.log(cfg.layers[0]["rows"] + 1.0)).astype(np.int32) - 1, cfg.layers[0]["rows"] - 1)
+        x[rng.random(x.shape) < 0.05] = -1
+    else:
+        x = rng.standard_normal(boundary_shape(cfg.layout, cfg.in_shape, n)).astype(np.float32)
     out = dict()
     if cfg.loss_tail:
         ncls = out_shape(cfg.layers, cfg.in_shape)[0]
@@ -134,6 +148,6 @@ def make_inputs(cfg, randomize_affine=False):
         osh = out_shape(cfg.layers, cfg.in_shape)
         dy = rng.standard_normal(boundary_shape(cfg.layout, osh, n)).astype(np.float32)
         out["dy"] = round_to_bf16(dy) if cfg.dtype == "bf16" else dy
-    out["x"] = round_to_bf16(x) if cfg.dtype == "bf16" else x
+    out["x"] = round_to_bf16(x) if cfg.dtype == "bf16" and not tokens else x
     out["params"] = make_params(cfg.layers, rng, cfg.init, randomize_affine)
     return out

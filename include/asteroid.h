@@ -70,12 +70,16 @@ typedef enum {
   AST_RES_BEGIN = 4,   /* remembers the current activation as the skip input                  */
   AST_RES_ADD = 5,     /* adds the remembered skip input                                      */
   AST_GLOBAL_AVGPOOL = 6,
-  AST_LINEAR = 7,      /* p = {in, out, has_bias}; y = x W^T + b on the last dimension        */
+  AST_LINEAR = 7,      /* p = {in, out, has_bias, keep8}; y = x W^T + b on the last dimension; keep8: see
+                          "8-bit stash" below                                                   */
   AST_SOFTMAX_CE = 8,  /* loss tail: mean over the whole mini-batch (divides by M*B)          */
   AST_MAXPOOL2X2 = 9,  /* 2x2 window, stride 2; gradient to the first maximum in row-major order */
   AST_LAYERNORM = 10,  /* p = {D}; eps; over the last dimension                               */
-  AST_MHA = 11,        /* p = {D, heads}; self-attention, no mask, no dropout                 */
-  AST_GELU = 12,       /* x * Phi(x) with the exact erf form                                  */
+  AST_MHA = 11,        /* p = {D, heads, qk_norm, rotary, theta, interleaved, keep8}; self-attention, no mask, no
+                          dropout.  qk_norm: every query and key head is normalised (RMS, eps) and
+                          scaled by a gain, and its first `rotary` values are rotated by the
+                          position in the sequence (asteroid_qk_norm_rope_forward), before the scores */
+  AST_GELU = 12,       /* p = {keep8}; x * Phi(x) with the exact erf form                     */
   AST_SWISH = 13,      /* x * sigmoid(x)  (fp32 stages; the EfficientNet workload of Table 4)  */
   AST_SIGMOID = 14,    /* 1 / (1 + exp(-x))  (fp32 stages)                                     */
   AST_SE_BEGIN = 15,   /* squeeze-and-excitation: remembers the current image tensor x; must be
@@ -89,9 +93,20 @@ typedef enum {
                           workload).  The layers from here to AST_RES_ADD are the shortcut branch:
                           they run on the tensor AST_RES_BEGIN remembered, and AST_RES_ADD adds
                           the main branch's result to theirs                                    */
-  AST_MAXPOOL3X3S2 = 18 /* 3x3 window, stride 2, padding 1 (padding never wins); fp32 stages; gradient
+  AST_MAXPOOL3X3S2 = 18, /* 3x3 window, stride 2, padding 1 (padding never wins); fp32 stages; gradient
                           to the first maximum in row-major order                               */
+  AST_EMBEDDING = 19   /* p = {rows, D}, eps = the scale: y = eps * table[id], zeros for ids outside
+                          [0, rows); the first layer of a bf16 AST_BSD stage whose x is int32
+                          [B][S] (in_shape {S, 1}); D % 8 == 0, needs_input_grad == 0; the table
+                          stays fp32, the result is rounded once                                */
 } ast_layer_kind;
+
+/* 8-bit stash (bf16 stages).  keep8 = 1 keeps a layer's input (AST_MHA: the input of its query, key and
+ * value projection) between the forward and the backward pass in the 8-bit form of asteroid_ops.h, and
+ * the weight gradient (AST_GELU: the input gradient) is formed from the restored values; the forward
+ * pass and the input gradients of dense layers are those of keep8 = 0.  An activation that no other
+ * layer's backward pass needs leaves the stash - act_per_mb falls by what it held - and lives in the
+ * workspace during a forward pass.  Entries of p that a kind does not list are 0. */
 
 typedef struct {
   int32_t kind;  /* ast_layer_kind */
@@ -112,12 +127,13 @@ typedef struct {
 /* Flat parameter vector (set/get_params, get_grads, set/get_velocity), fp32:
  * layer order; inside a layer weight then bias.  CONV2D weight is logically
  * [Cout][Cin/groups][kh][kw]; LINEAR weight [out][in]; BATCHNORM2D / LAYERNORM
- * gamma then beta; MHA: W_qkv[3D][D] (rows Q, K, V), b_qkv[3D], W_o[D][D], b_o[D].
+ * gamma then beta; MHA: W_qkv[3D][D] (rows Q, K, V), b_qkv[3D], W_o[D][D], b_o[D], with qk_norm
+ * query gain[64], key gain[64] (which start at 1); EMBEDDING: table [rows][D].
  * These orders are independent of `layout`. */
 
 /* Build a stage (Sec. 3.2: the stage model a device takes charge of).
  * `layers` (host) is copied.  `hip_stream` is a hipStream_t (NULL = default stream).
- * Parameters start at 0 (BatchNorm/LayerNorm gamma at 1), gradients and velocity at 0.
+ * Parameters start at 0 (BatchNorm/LayerNorm gamma and query / key gains at 1), gradients and velocity at 0.
  * Errors: AST_EINVAL (bad sizes, unbalanced RES_BEGIN/RES_ADD, shapes that do not
  * chain), AST_EUNSUPPORTED, AST_ENOMEM, AST_EHIP.  On error *out is NULL. */
 ast_status asteroid_stage_create(const ast_layer* layers, int32_t n_layers,

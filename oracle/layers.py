@@ -15,6 +15,8 @@ import math
 import numpy as np
 from scipy.special import erf as _erf     # library erf (vectorised libm erf)
 
+from . import lm_ops
+
 F = np.float64
 
 
@@ -244,29 +246,51 @@ def softmax_ce_bwd(p, labels, denom):
 
 
 # --------------------------------------------------------------------------- attention
-def mha_fwd(x, w_qkv, b_qkv, w_o, b_o, heads):
+def _rotated(t, gain, args):
+    """Heads [n][heads][s][d] normalised, scaled by the gain and rotated by their position."""
+    n, h, s, d = t.shape
+    y = lm_ops.norm_rope_forward(t.transpose(0, 2, 1, 3).reshape(n * s, h, d), gain, np.tile(args[0], n), *args[1:])[0]
+    return y.reshape(n, s, h, d).transpose(0, 2, 1, 3)
+
+
+def _rotated_bwd(g, t, gain, args):
+    n, h, s, d = t.shape
+    flat = lambda a: a.transpose(0, 2, 1, 3).reshape(n * s, h, d)
+    dx, dgain, _, _ = lm_ops.norm_rope_backward(flat(g), flat(t), gain, np.tile(args[0], n), *args[1:])
+    return dx.reshape(n, s, h, d).transpose(0, 2, 1, 3), dgain
+
+
+def mha_fwd(x, w_qkv, b_qkv, w_o, b_o, heads, gains=None, args=None, stored=lambda a: a):
     """Multi-head self-attention, no mask, no dropout.
     [Q;K;V] = x W_qkv^T + b_qkv; per head S = Q K^T / sqrt(d); P = softmax_rows(S);
-    O = P V; y = concat_heads(O) W_o^T + b_o."""
+    O = P V; y = concat_heads(O) W_o^T + b_o.  With gains, queries and keys are normalised and rotated before the
+    scores; `stored` is then the rounding of the tensors that stand between the layer's steps (the projection, the
+    rotated heads, O)."""
     n, s, dm = x.shape
     d = dm // heads
     qkv = np.matmul(x, w_qkv.T) + b_qkv
     q, k, v = [qkv[..., i * dm:(i + 1) * dm].reshape(n, s, heads, d).transpose(0, 2, 1, 3)
                for i in range(3)]
+    if gains is not None:
+        raw = q, k = stored(q), stored(k)
+        v = stored(v)
+        q, k = stored(_rotated(q, gains[0], args)), stored(_rotated(k, gains[1], args))
     sc = np.matmul(q, k.transpose(0, 1, 3, 2)) / math.sqrt(d)
     sc = sc - sc.max(axis=-1, keepdims=True)
     e = np.exp(sc)
     p = e / e.sum(axis=-1, keepdims=True)
     o = np.matmul(p, v)
     oc = o.transpose(0, 2, 1, 3).reshape(n, s, dm)
+    if gains is not None:
+        oc = stored(oc)
     y = np.matmul(oc, w_o.T) + b_o
-    return y, (q, k, v, p, oc)
+    return y, (q, k, v, p, oc) + ((raw,) if gains is not None else ())
 
 
-def mha_bwd(x, w_qkv, w_o, g, saved, heads):
+def mha_bwd(x, w_qkv, w_o, g, saved, heads, gains=None, args=None, stored=None):
     """dV = P^T dO; dP = dO V^T; dS = P*(dP - rowsum(dP*P)); dQ = dS K/sqrt(d);
     dK = dS^T Q/sqrt(d); then linear backward through both projections."""
-    q, k, v, p, oc = saved
+    q, k, v, p, oc = saved[:5]
     n, s, dm = x.shape
     d = dm // heads
     g2 = g.reshape(-1, dm)
@@ -279,9 +303,15 @@ def mha_bwd(x, w_qkv, w_o, g, saved, heads):
     ds = p * (dp - (dp * p).sum(axis=-1, keepdims=True))
     dq = np.matmul(ds, k) / math.sqrt(d)
     dk = np.matmul(ds.transpose(0, 1, 3, 2), q) / math.sqrt(d)
+    more = []
+    if gains is not None:
+        raw = saved[5]
+        dq, dgq = _rotated_bwd(dq, raw[0], gains[0], args)
+        dk, dgk = _rotated_bwd(dk, raw[1], gains[1], args)
+        more = [dgq, dgk]
     dqkv = np.concatenate([t.transpose(0, 2, 1, 3).reshape(n, s, dm) for t in (dq, dk, dv)], axis=-1)
     d2 = dqkv.reshape(-1, 3 * dm)
     dw_qkv = np.matmul(d2.T, x.reshape(-1, dm))
     db_qkv = d2.sum(axis=0)
     dx = np.matmul(dqkv, w_qkv)
-    return dx, [dw_qkv, db_qkv, dw_o, db_o]
+    return dx, [dw_qkv, db_qkv, dw_o, db_o] + more

@@ -27,6 +27,7 @@ It imports nothing from the HIP package.
 import numpy as np
 
 from . import layers as L
+from . import lm_ops
 
 F = np.float64
 
@@ -53,7 +54,9 @@ def _param_shapes(layer):
         return [(layer["d"],), (layer["d"],)]
     if k == "mha":
         d = layer["d"]
-        return [(3 * d, d), (3 * d,), (d, d), (d,)]
+        return [(3 * d, d), (3 * d,), (d, d), (d,)] + ([(d // layer["heads"],)] * 2 if layer.get("qk_norm") else [])
+    if k == "embedding":
+        return [(layer["rows"], layer["d"])]
     return []
 
 
@@ -119,6 +122,18 @@ class OracleStage:
         """In-place accumulation G += grad_m (Sec. 3.2)."""
         for o, s, g in zip(self.offsets[i], self.shapes[i], grads):
             self.G[o:o + g.size] += g.ravel()
+
+    @staticmethod
+    def _kept(l, a):
+        """What the backward pass sees of a layer's input: with keep8 its 8-bit form."""
+        return lm_ops.stash8(a.reshape(-1, a.shape[-1]))[0].reshape(a.shape) if l.get("keep8") else a
+
+    def _qk(self, l, P, S):
+        """Norm and rotation of queries and keys: () or (gains, arguments of lm_ops.norm_rope_forward)."""
+        if not l.get("qk_norm"):
+            return ()
+        return ((P[4], P[5]), (np.arange(S), l.get("rotary", 0), float(l.get("theta", 0) or 1), bool(l.get("interleaved", 0)), l["eps"]),
+                round_bf16 if self.storage == "bf16" else lambda a: a)
 
     # ---- layout at the boundary
     def _to_logical(self, a):
@@ -206,9 +221,13 @@ class OracleStage:
                 saved.append(a)
                 a = L.linear_fwd(a, P[0], P[1] if l["bias"] else None)
             elif k == "mha":
-                y, sv = L.mha_fwd(a, P[0], P[1], P[2], P[3], l["heads"])
+                y, sv = L.mha_fwd(a, P[0], P[1], P[2], P[3], l["heads"], *self._qk(l, P, a.shape[1]))
                 saved.append((a, sv))
                 a = y
+            elif k == "embedding":
+                ids = np.asarray(x).reshape(self.B, -1)
+                saved.append(ids)
+                a = lm_ops.embedding_forward(ids.ravel(), P[0], l["scale"]).reshape(ids.shape + (l["d"],))
             elif k == "softmax_ce":
                 logits = a
                 loss, p = L.softmax_ce_fwd(a, np.asarray(labels), self.M * self.B)
@@ -251,7 +270,7 @@ class OracleStage:
             elif k == "relu6":
                 g = L.relu6_bwd(g, sv)
             elif k == "gelu":
-                g = L.gelu_bwd(g, sv)
+                g = L.gelu_bwd(g, self._kept(l, sv))
             elif k == "swish":
                 g = L.swish_bwd(g, sv)
             elif k == "sigmoid":
@@ -277,11 +296,14 @@ class OracleStage:
             elif k == "maxpool3x3s2":
                 g = L.maxpool3x3s2_bwd(g, sv[0], sv[1][2], sv[1][3])
             elif k == "linear":
-                g, grads = L.linear_bwd(sv, P[0], g, l["bias"])
+                g, grads = L.linear_bwd(self._kept(l, sv), P[0], g, l["bias"])
                 self._acc(i, grads)
             elif k == "mha":
-                g, grads = L.mha_bwd(sv[0], P[0], P[2], g, sv[1], l["heads"])
+                g, grads = L.mha_bwd(self._kept(l, sv[0]), P[0], P[2], g, sv[1], l["heads"], *self._qk(l, P, g.shape[1]))
                 self._acc(i, grads)
+            elif k == "embedding":
+                self._acc(i, [lm_ops.embedding_backward(sv.ravel(), g.reshape(-1, l["d"]), l["rows"], l["scale"])[0]])
+                g = None
         return self._to_boundary(g) if self.needs_input_grad else None
 
     # ---- weight update, once per HPP-Round

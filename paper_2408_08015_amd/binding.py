@@ -11,7 +11,8 @@ STATUS = {0: "AST_OK", -1: "AST_EINVAL", -2: "AST_ESTATE", -3: "AST_ENOMEM", -4:
           -5: "AST_EUNSUPPORTED"}
 KINDS = {"conv2d": 0, "batchnorm2d": 1, "relu": 2, "relu6": 3, "res_begin": 4, "res_add": 5,
          "global_avgpool": 6, "linear": 7, "softmax_ce": 8, "maxpool2x2": 9, "layernorm": 10,
-         "mha": 11, "gelu": 12, "swish": 13, "sigmoid": 14, "se_begin": 15, "se_scale": 16, "res_swap": 17, "maxpool3x3s2": 18}
+         "mha": 11, "gelu": 12, "swish": 13, "sigmoid": 14, "se_begin": 15, "se_scale": 16, "res_swap": 17, "maxpool3x3s2": 18,
+         "embedding": 19}
 DTYPES = {"f32": 0, "bf16": 1}
 LAYOUTS = {"nchw": 0, "nhwc": 1, "bsd": 2}
 
@@ -93,13 +94,19 @@ def _marshal_layers(layers):
         if k == "conv2d":
             vals = [L["cin"], L["cout"], L["k"], L["stride"], L["pad"], L["groups"], int(L["bias"])]
         elif k == "linear":
-            vals = [L["cin"], L["cout"], int(L["bias"])]
+            vals = [L["cin"], L["cout"], int(L["bias"]), int(L.get("keep8", 0))]
         elif k == "batchnorm2d":
             vals = [L["c"]]
         elif k == "layernorm":
             vals = [L["d"]]
         elif k == "mha":
-            vals = [L["d"], L["heads"]]
+            vals = [L["d"], L["heads"], int(L.get("qk_norm", 0)), L.get("rotary", 0), L.get("theta", 0),
+                    int(L.get("interleaved", 0)), int(L.get("keep8", 0))]
+        elif k == "gelu":
+            vals = [int(L.get("keep8", 0))]
+        elif k == "embedding":
+            vals = [L["rows"], L["d"]]
+            a.eps = float(L.get("scale", 1.0))
         else:
             vals = []
         for i, v in enumerate(vals):

@@ -103,12 +103,15 @@ void free_stage(ast::Stage& s) {
   s.ws = nullptr;
 }
 
-// initial parameter values: 0, with BatchNorm / LayerNorm gamma at 1
+// initial parameter values: 0, with BatchNorm / LayerNorm gamma and the gains of queries and keys at 1
 std::vector<float> initial_params(const ast::Stage& s) {
   std::vector<float> w(s.nparams, 0.f);
   for (const ast::Op& op : s.ops)
     if (op.kind == ast::OP_BN || op.kind == ast::OP_LAYERNORM)
       for (int c = 0; c < op.cin; ++c) w[op.w_off + c] = 1.f;
+  for (const ast::Op& op : s.ops)
+    if (op.kind == ast::OP_MHA && op.qk_norm)
+      for (int c = 0; c < 2 * 64; ++c) w[op.w_off + (size_t)4 * op.cin * op.cin + 4 * op.cin + c] = 1.f;
   return w;
 }
 

@@ -1,5 +1,5 @@
 // Self-attention core (no mask, head size 64, S % 32 == 0, S <= 256) on packed
-// qkv [B][S][3D]: forward with online softmax, and backward as two kernels
+// qkv [B][S][3D] (queries and keys also from a tensor of their own, of rows `ldqk`): forward with online softmax, and backward as two kernels
 // (dK/dV parallel over keys, dQ parallel over queries).  The S x S score matrix never
 // leaves the chip: bytes moved are Q, K, V, O (+ dO, dQ, dK, dV) only.
 //
@@ -87,8 +87,8 @@ __device__ __forceinline__ void stage_pair(bf16_t* rows0, bf16_t* tr0, const bf1
 __device__ __forceinline__ int acc_row(int r, int g) { return 8 * (r >> 2) + 4 * g + (r & 3); }
 
 // ------------------------------------------------------------------ forward
-__global__ __launch_bounds__(256) void attention_fwd_kernel(const bf16_t* __restrict__ qkv,
-                                                            bf16_t* __restrict__ o, float* __restrict__ lse,
+__global__ __launch_bounds__(256) void attention_fwd_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ qk,
+                                                            int ldqk, bf16_t* __restrict__ o, float* __restrict__ lse,
                                                             int S, int D, int H) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   bf16_t* sK = reinterpret_cast<bf16_t*>(smem);  // [S][RS]
@@ -98,15 +98,16 @@ __global__ __launch_bounds__(256) void attention_fwd_kernel(const bf16_t* __rest
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 31, g = lane >> 5;
   const long ld = 3L * D;
-  const bf16_t* base = qkv + (long)b * S * ld + h * HD;
+  const bf16_t* base = qk + (long)b * S * ldqk + h * HD;
+  const bf16_t* vbase = qkv + (long)b * S * ld + 2 * D + h * HD;
   // everything this wavefront reads from global memory is requested before the staging copies wait for theirs
   const int q0 = blockIdx.x * 128 + wave * 32;
   const bool live = q0 < S;
   const int q = live ? q0 + col : 0;
   bf16x8 qf[4];
 #pragma unroll
-  for (int t = 0; t < 4; ++t) qf[t] = ld_frag(base + (long)q * ld + 16 * t + 8 * g);
-  stage_pair<true, false, false, true>(sK, nullptr, base + D, ld, nullptr, sVt, base + 2 * D, ld, S);
+  for (int t = 0; t < 4; ++t) qf[t] = ld_frag(base + (long)q * ldqk + 16 * t + 8 * g);
+  stage_pair<true, false, false, true>(sK, nullptr, base + D, ldqk, nullptr, sVt, vbase, ld, S);
   __syncthreads();
   if (!live) return;
 
@@ -202,7 +203,7 @@ __device__ __forceinline__ float dsum_half(const bf16_t* __restrict__ po, const 
 }
 
 // dK, dV: a wavefront owns 32 keys (lane = key), loops over query tiles.
-__device__ __forceinline__ void attention_bwd_dkv_body(const bf16_t* __restrict__ qkv,
+__device__ __forceinline__ void attention_bwd_dkv_body(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ qk, int ldqk,
                                                        const bf16_t* __restrict__ d_o,
                                                        const float* __restrict__ lse,
                                                        const bf16_t* __restrict__ o,
@@ -219,7 +220,8 @@ __device__ __forceinline__ void attention_bwd_dkv_body(const bf16_t* __restrict_
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 31, g = lane >> 5;
   const long ld = 3L * D;
-  const bf16_t* base = qkv + (long)b * S * ld + h * HD;
+  const bf16_t* base = qk + (long)b * S * ldqk + h * HD;
+  const bf16_t* vbase = qkv + (long)b * S * ld + 2 * D + h * HD;
   const bf16_t* dobase = d_o + (long)b * S * D + h * HD;
   // Everything read from global memory is requested before the staging copies wait for theirs: this wavefront's
   // K and V fragments, the log-sum-exp values, and the words of the first round of row sums of dO * O.
@@ -229,8 +231,8 @@ __device__ __forceinline__ void attention_bwd_dkv_body(const bf16_t* __restrict_
   bf16x8 kf[4], vf[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    kf[t] = ld_frag(base + D + (long)key * ld + 16 * t + 8 * g);
-    vf[t] = ld_frag(base + 2 * D + (long)key * ld + 16 * t + 8 * g);
+    kf[t] = ld_frag(base + D + (long)key * ldqk + 16 * t + 8 * g);
+    vf[t] = ld_frag(vbase + (long)key * ld + 16 * t + 8 * g);
   }
   const int tid = threadIdx.x;
   const float lse_mine = tid < S ? lse[((long)b * H + h) * S + tid] : 0.f;  // blockDim.x = 256 >= S
@@ -240,7 +242,7 @@ __device__ __forceinline__ void attention_bwd_dkv_body(const bf16_t* __restrict_
     const long at = ((long)b * S + (tid >> 1)) * D + h * HD;
     dsum_load(o + at, d_o + at, tid & 1, w0);
   }
-  stage_pair<true, true, true, true>(sQ, sQt, base, ld, sdO, sdOt, dobase, D, S);
+  stage_pair<true, true, true, true>(sQ, sQt, base, ldqk, sdO, sdOt, dobase, D, S);
   if (tid < S) sL[tid] = lse_mine;
   if (has0) {
     const float half = dsum_math(w0);
@@ -314,7 +316,7 @@ __device__ __forceinline__ void attention_bwd_dkv_body(const bf16_t* __restrict_
 }
 
 // dQ: a wavefront owns 32 queries (lane = query), loops over key tiles.
-__device__ __forceinline__ void attention_bwd_dq_body(const bf16_t* __restrict__ qkv,
+__device__ __forceinline__ void attention_bwd_dq_body(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ qk, int ldqk,
                                                       const bf16_t* __restrict__ d_o,
                                                       const float* __restrict__ lse,
                                                       const bf16_t* __restrict__ o,
@@ -328,7 +330,8 @@ __device__ __forceinline__ void attention_bwd_dq_body(const bf16_t* __restrict__
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 31, g = lane >> 5;
   const long ld = 3L * D;
-  const bf16_t* base = qkv + (long)b * S * ld + h * HD;
+  const bf16_t* base = qk + (long)b * S * ldqk + h * HD;
+  const bf16_t* vbase = qkv + (long)b * S * ld + 2 * D + h * HD;
   // (all global reads of this wavefront are requested before the staging copies wait for theirs)
   const int q0 = bx * 128 + wave * 32;
   const bool live = q0 < S;
@@ -336,7 +339,7 @@ __device__ __forceinline__ void attention_bwd_dq_body(const bf16_t* __restrict__
   bf16x8 qf[4], dof[4];
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    qf[t] = ld_frag(base + (long)q * ld + 16 * t + 8 * g);
+    qf[t] = ld_frag(base + (long)q * ldqk + 16 * t + 8 * g);
     dof[t] = ld_frag(d_o + ((long)b * S + q) * D + h * HD + 16 * t + 8 * g);
   }
   const float lq = lse[((long)b * H + h) * S + q];
@@ -345,7 +348,7 @@ __device__ __forceinline__ void attention_bwd_dq_body(const bf16_t* __restrict__
     const long at = ((long)b * S + q) * D + h * HD;
     dsum_load(o + at, d_o + at, g, wq);
   }
-  stage_pair<true, true, true, false>(sK, sKt, base + D, ld, sV, nullptr, base + 2 * D, ld, S);
+  stage_pair<true, true, true, false>(sK, sKt, base + D, ldqk, sV, nullptr, vbase, ld, S);
   __syncthreads();
   if (!live) return;
   float dq_sum;
@@ -402,14 +405,15 @@ size_t lds_dq(int S) { return ((size_t)2 * S * RS + (size_t)HD * (S + 8)) * 2; }
 // dK/dV and dQ in ONE launch: the two are independent and each alone is a short latency-bound
 // chain, so their blocks are dealt from one grid: block ids [0, nx) of the x dimension are the
 // key tiles of the dK/dV role, [nx, 2 nx) the query tiles of the dQ role.
-__global__ __launch_bounds__(256) void attention_bwd_kernel(const bf16_t* __restrict__ qkv,
+__global__ __launch_bounds__(256) void attention_bwd_kernel(const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ qk,
+                                                            int ldqk,
                                                             const bf16_t* __restrict__ d_o,
                                                             const float* __restrict__ lse,
                                                             const bf16_t* __restrict__ o,
                                                             bf16_t* __restrict__ dqkv, int S, int D, int H, int nx) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  if ((int)blockIdx.x < nx) attention_bwd_dkv_body(qkv, d_o, lse, o, dqkv, S, D, H, (int)blockIdx.x, smem);  // uniform
-  else attention_bwd_dq_body(qkv, d_o, lse, o, dqkv, S, D, H, (int)blockIdx.x - nx, smem);
+  if ((int)blockIdx.x < nx) attention_bwd_dkv_body(qkv, qk, ldqk, d_o, lse, o, dqkv, S, D, H, (int)blockIdx.x, smem);  // uniform
+  else attention_bwd_dq_body(qkv, qk, ldqk, d_o, lse, o, dqkv, S, D, H, (int)blockIdx.x - nx, smem);
 }
 
 void allow_lds(const void* fn, size_t bytes) {
@@ -423,20 +427,20 @@ size_t mha_bf16_ws_bytes(int B, int S, int D, int heads) {
   return (size_t)B * heads * S * sizeof(float) + 256;  // Dsum
 }
 
-void attention_fwd_bf16(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, int B, int S, int D, int heads) {
+void attention_fwd_bf16(hipStream_t st, const bf16_t* qkv, const bf16_t* qk, int ldqk, bf16_t* o, float* lse, int B, int S, int D, int heads) {
   size_t lds = lds_fwd(S);
   allow_lds((const void*)attention_fwd_kernel, lds);
-  KLAUNCH(attention_fwd_kernel, dim3((S + 127) / 128, heads, B), dim3(256), lds, st, qkv, o, lse, S, D, heads);
+  KLAUNCH(attention_fwd_kernel, dim3((S + 127) / 128, heads, B), dim3(256), lds, st, qkv, qk, ldqk, o, lse, S, D, heads);
 }
 
-void attention_bwd_bf16(hipStream_t st, const bf16_t* qkv, const bf16_t* o, const bf16_t* d_o, const float* lse,
+void attention_bwd_bf16(hipStream_t st, const bf16_t* qkv, const bf16_t* qk, int ldqk, const bf16_t* o, const bf16_t* d_o, const float* lse,
                         bf16_t* dqkv, float* dsum, int B, int S, int D, int heads) {
   (void)dsum;  // the row sums of dO * O are formed inside the kernel (they were a launch of their own)
   const size_t l1 = lds_dkv(S), l2 = lds_dq(S), lds = l1 > l2 ? l1 : l2;
   allow_lds((const void*)attention_bwd_kernel, lds);
   const int nx = (S + 127) / 128;
   dim3 grid(2 * nx, heads, B);
-  KLAUNCH(attention_bwd_kernel, grid, dim3(256), lds, st, qkv, d_o, lse, o, dqkv, S, D, heads, nx);
+  KLAUNCH(attention_bwd_kernel, grid, dim3(256), lds, st, qkv, qk, ldqk, d_o, lse, o, dqkv, S, D, heads, nx);
 }
 
 }  // namespace ast

@@ -7,6 +7,7 @@
 
 #include "kernels.h"
 #include "kernels_bf16.h"
+#include "ops.h"
 #include "stage.h"
 #include "static_scratch.h"
 
@@ -27,8 +28,10 @@ inline int final_act_of(const Stage& s) { return s.final_act; }
 
 inline void* act_ptr(Ctx& c, int id) {
   if (id == c.final_act && !c.s.loss_tail && id != 0 && !c.s.final_in_slot) return c.s.cur_y;
+  if (c.s.acts[id].passing) return id == 0 ? const_cast<void*>(c.s.cur_x) : c.s.ws + c.s.fscratch_off + c.s.acts[id].fwd_off;
   return c.slot + c.s.acts[id].slot_off;
 }
+inline char* act8_ptr(Ctx& c, int id) { return c.slot + c.s.acts[id].slot8_off; }  // an activation kept in 8 bits
 inline void* grad_ptr(Ctx& c, int id) {
   while (c.s.acts[id].grad_alias >= 0) id = c.s.acts[id].grad_alias;
   if (id == 0) return c.s.cur_dx;  // may be NULL: the input gradient is not wanted
@@ -55,6 +58,12 @@ inline hipStream_t fork_side(Ctx& c) {
   return s.side;
 }
 inline size_t align256(size_t v) { return (v + 255) / 256 * 256; }
+inline int64_t act_rows(const Act& a) { return (int64_t)(a.elems / a.c); }
+// the norm and rotation of an attention's queries and keys: rows of `ld` from `qk` on, keys D behind the queries
+inline ast_qk_cfg qk_cfg(const Op& op, const Act& I) {
+  return {(int64_t)I.n * I.h, AST_BF16_F32ACC, 64, op.rotary, op.interleaved, op.eps, op.theta, nullptr, I.h};
+}
+inline ast_heads qk_heads(const bf16_t* qk, int64_t ld, const Op& op) { return {qk, ld, 64, op.heads}; }
 // attention scratch: [d_o, dqkv][row sums of dO*O][weight-gradient partials ...]
 inline size_t mha_lw_offset(int B, int S, int D, int heads) {
   return align256((size_t)B * S * 4 * D * sizeof(bf16_t)) + align256(mha_bf16_ws_bytes(B, S, D, heads));
@@ -224,12 +233,28 @@ void fwd_op(Ctx& c, const Op& op, const int32_t* labels, float* loss) {
       const float* bq = s.W + op.w_off + (size_t)3 * D * D;
       const float* bo = bq + 3 * D + (size_t)D * D;
       linear_bf16_fwd(st, (cb)act_ptr(c, op.in), s.shadow + op.sh_off, bq, qkv, nullptr, nullptr, R, D, 3 * D, 0);
-      attention_fwd_bf16(st, qkv, o, lse, I.n, I.h, D, op.heads);
+      bf16_t* qk = qkv;
+      if (op.qk_norm) {  // (the raw ones stay for the backward pass)
+        qk = reinterpret_cast<bf16_t*>(c.slot + op.aux_off + op.qk_off);
+        qk_norm_rope_fwd(st, qk_cfg(op, I), qk_heads(qkv, 3 * D, op), qk_heads(qkv + D, 3 * D, op), bo + D, bo + D + 64,
+                         qk_heads(qk, 2 * D, op), qk_heads(qk + D, 2 * D, op));
+      }
+      attention_fwd_bf16(st, qkv, qk, op.qk_norm ? 2 * D : 3 * D, o, lse, I.n, I.h, D, op.heads);
       linear_bf16_fwd(st, o, s.shadow + op.sh_off + (size_t)3 * D * D, bo, (bf16_t*)act_ptr(c, op.out), nullptr,
                       op.res_in >= 0 ? (cb)act_ptr(c, op.res_in) : nullptr, R, D, D, 0);
       break;
     }
+    case OP_EMBEDDING:
+      embedding_fwd(st, static_cast<const int32_t*>(act_ptr(c, op.in)), (int64_t)I.n * I.h, s.W + op.w_off, false, op.cin, op.cout,
+                    op.scale, act_ptr(c, op.out), true);
+      break;
   }
+}
+
+// the 8-bit form of an activation that a forward op has just written
+void keep8_act(Ctx& c, int id) {
+  if (id < 0 || !c.s.acts[id].kept8) return;
+  stash8_pack(c.st, act_ptr(c, id), true, act_rows(c.s.acts[id]), c.s.acts[id].c, act8_ptr(c, id));
 }
 
 void bwd_op(Ctx& c, const Op& op) {
@@ -385,7 +410,9 @@ void bwd_op(Ctx& c, const Op& op) {
     }
     case OP_ACT:
       if (!gin || op.act_bwd_done) break;
-      if (s.bf16)
+      if (op.keep8)
+        gelu_bwd_stash8(st, grad_ptr(c, op.out), true, act8_ptr(c, op.in), act_rows(I), I.c, gin);
+      else if (s.bf16)
         act_bwd_bf16(st, (cb)grad_ptr(c, op.out), op.act == 3 ? (cb)act_ptr(c, op.in) : (cb)act_ptr(c, op.out),
                      (bf16_t*)gin, I.elems, op.act);
       else
@@ -428,16 +455,20 @@ void bwd_op(Ctx& c, const Op& op) {
         char* sc = scratch(c, op);  // [GELU-masked upstream gradient][weight-gradient partials]
         if (op.act == 3 && !op.gelu_bwd_fused) {
           bf16_t* gp = reinterpret_cast<bf16_t*>(sc);
-          act_bwd_bf16(st, g, (cb)act_ptr(c, op.skip), gp, O.elems, 3);
+          if (s.acts[op.skip].kept8) gelu_bwd_stash8(st, g, true, act8_ptr(c, op.skip), (int64_t)R, op.cout, gp);
+          else act_bwd_bf16(st, g, (cb)act_ptr(c, op.skip), gp, O.elems, 3);
           g = gp;
         }
         sc += align256(O.bytes);
-        hipStream_t sw = op.wg_grouped ? st : fork_side(c);
+        hipStream_t sw = op.wg_grouped || op.keep8 ? st : fork_side(c);
         if (gin)
           linear_bf16_dgrad(st, g, s.shadow + op.sh2_off, (bf16_t*)gin,
                             op.gelu_from >= 0 ? (cb)act_ptr(c, op.gelu_from) : nullptr,
                             op.dgrad_add >= 0 ? (cb)grad_ptr(c, op.dgrad_add) : nullptr, R, op.cin, op.cout);
-        if (!op.wg_grouped)  // else: part of the grouped launch at the end of the pass
+        if (op.keep8)
+          linear_wgrad_stash8(st, g, act8_ptr(c, op.in), (int64_t)R, op.cin, op.cout, s.G + op.w_off,
+                              op.has_bias ? s.G + op.b_off : nullptr, true, sc);
+        else if (!op.wg_grouped)  // else: part of the grouped launch at the end of the pass
           linear_bf16_wgrad(sw, g, (cb)act_ptr(c, op.in), s.G + op.w_off, s.G + op.b_off, op.has_bias != 0,
                             s.red_nblocks != 0, sc, R, op.cin, op.cout);
       } else {
@@ -485,14 +516,28 @@ void bwd_op(Ctx& c, const Op& op) {
       hipStream_t sw = op.wg_grouped ? st : fork_side(c);
       linear_bf16_dgrad(st, g, s.shadow + op.sh2_off + (size_t)3 * D * D, d_o, nullptr, nullptr, R, D, D);
       if (!op.wg_grouped) linear_bf16_wgrad(sw, g, o, Go, Gbo, true, defer, lw_o, R, D, D);
-      attention_bwd_bf16(st, qkv, o, d_o, lse, dqkv, dsum, I.n, I.h, D, op.heads);
-      if (!op.wg_grouped) sw = fork_side(c);
+      const bf16_t* qk = op.qk_norm ? reinterpret_cast<const bf16_t*>(c.slot + op.aux_off + op.qk_off) : qkv;
+      attention_bwd_bf16(st, qkv, qk, op.qk_norm ? 2 * D : 3 * D, o, d_o, lse, dqkv, dsum, I.n, I.h, D, op.heads);
+      char* const after_q = lw_q + align256(op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)R, D, 3 * D)
+                                                     : linear_bf16_ws_bytes(R, D, 3 * D, op.wg_splits[1]));
+      if (op.qk_norm) {  // in place: from the rotated, normalised heads to the projection's
+        const ast_heads dq = qk_heads(dqkv, 3 * D, op), dk = qk_heads(dqkv + D, 3 * D, op);
+        const float* gains = s.W + op.w_off + (size_t)4 * D * D + 4 * D;
+        qk_norm_rope_bwd(st, qk_cfg(op, I), dq, dk, qk_heads(qkv, 3 * D, op), qk_heads(qkv + D, 3 * D, op), gains, gains + 64, dq, dk,
+                         Gbo + D, Gbo + D + 64, true, after_q);
+      }
+      if (!op.wg_grouped && !op.keep8) sw = fork_side(c);
       if (gin)
         linear_bf16_dgrad(st, dqkv, s.shadow + op.sh2_off, (bf16_t*)gin, nullptr,
                           op.dgrad_add >= 0 ? (cb)grad_ptr(c, op.dgrad_add) : nullptr, R, D, 3 * D);
-      if (!op.wg_grouped) linear_bf16_wgrad(sw, dqkv, (cb)act_ptr(c, op.in), Gq, Gbq, true, defer, lw_q, R, D, 3 * D);
+      if (op.keep8) linear_wgrad_stash8(st, dqkv, act8_ptr(c, op.in), (int64_t)R, D, 3 * D, Gq, Gbq, true, lw_q);
+      else if (!op.wg_grouped) linear_bf16_wgrad(sw, dqkv, (cb)act_ptr(c, op.in), Gq, Gbq, true, defer, lw_q, R, D, 3 * D);
       break;
     }
+    case OP_EMBEDDING:
+      embedding_bwd(st, static_cast<const int32_t*>(act_ptr(c, op.in)), (int64_t)I.n * I.h, grad_ptr(c, op.out), true, op.cin, op.cout,
+                    op.scale, true, s.G + op.w_off, scratch(c, op));
+      break;
   }
 }
 
@@ -511,6 +556,7 @@ ast_status run_forward(Stage& s, int slot, const void* x, const int32_t* labels,
                        std::string& err) {
   const bool two = s.fwd_stream != nullptr;
   Ctx c{s, s.slots[slot], final_act_of(s), s.ws, two ? s.fwd_stream : s.stream};
+  s.cur_x = x;
   s.cur_y = y;
   s.cur_dy = nullptr;
   s.cur_dx = nullptr;
@@ -525,8 +571,13 @@ ast_status run_forward(Stage& s, int slot, const void* x, const int32_t* labels,
     }
     if (s.bwd_done_set[slot]) (void)hipStreamWaitEvent(c.st, s.bwd_done[slot], 0);  // the slot's previous reader
   }
-  copy_bytes(c.st, x, c.slot + s.acts[0].slot_off, s.acts[0].bytes);
-  for (const Op& op : s.ops) fwd_op(c, op, labels, loss);
+  if (!s.acts[0].passing) copy_bytes(c.st, x, c.slot + s.acts[0].slot_off, s.acts[0].bytes);
+  keep8_act(c, 0);
+  for (const Op& op : s.ops) {
+    fwd_op(c, op, labels, loss);
+    if (op.out != op.in && op.kind != OP_RES_SWAP) keep8_act(c, op.out);
+    if (op.kind == OP_LINEAR) keep8_act(c, op.skip);  // the pre-activation of a fused GELU
+  }
   if (s.final_in_slot && !s.loss_tail)
     copy_bytes(c.st, c.slot + s.acts[s.final_act].slot_off, y, s.acts[s.final_act].bytes);
   if (two) (void)hipEventRecord(s.fwd_done[slot], c.st);
@@ -537,6 +588,7 @@ ast_status run_backward(Stage& s, int slot, const void* dy, void* dx, char* stat
   Ctx c{s, s.slots[slot], final_act_of(s), static_ws ? static_ws : s.ws, s.stream};
   if (s.fwd_stream) (void)hipStreamWaitEvent(s.stream, s.fwd_done[slot], 0);  // the stash of this micro-batch
   if (static_ws) static_scratch_zero(s.stream, static_ws, s.ws_bytes);  // what the stage's own workspace was at create
+  s.cur_x = nullptr;
   s.cur_y = nullptr;
   s.cur_dy = dy;
   s.cur_dx = dx;
@@ -668,6 +720,7 @@ static ast_status build_wgrad_groups(Stage& s, char* static_ws, std::string& err
     const Act& I = s.acts[op.in];
     char* sc = ws + s.scratch_off + op.sc_off;
     if (op.kind == OP_LINEAR) {
+      if (op.keep8) return false;
       const size_t R = (size_t)I.n * I.h * I.w;
       char* g = (op.act == 3 && !op.gelu_bwd_fused) ? sc : grad_at(ws, op.out);  // the GELU-masked gradient lies in the scratch
       char* x = act_at(slot, op.in);
@@ -687,10 +740,11 @@ static ast_status build_wgrad_groups(Stage& s, char* static_ws, std::string& err
       float* Go = Gbq + 3 * D;
       float* Gbo = Go + (size_t)D * D;
       char* g = grad_at(ws, op.out);
-      char* x = act_at(slot, op.in);
-      if (!g || !x || !wgrad_group_supported(R, D, 3 * D)) return false;
+      char* x = op.keep8 ? nullptr : act_at(slot, op.in);
+      if (!g || (!x && !op.keep8) || !wgrad_group_supported(R, D, 3 * D)) return false;
       char* const lw_o = sc + mha_lw_offset(I.n, I.h, D, op.heads);
       out.push_back({(const bf16_t*)g, o, Go, Gbo, R, D, D, op.wg_splits[0], lw_o});
+      if (op.keep8) return true;  // (that of the qkv projection comes from the kept input)
       out.push_back({dqkv, (const bf16_t*)x, Gq, Gbq, R, D, 3 * D, op.wg_splits[1],
                      lw_o + align256(linear_bf16_ws_bytes(R, D, D, op.wg_splits[0]))});
       return true;
@@ -832,7 +886,7 @@ ast_status build_reduce_tasks(Stage& s, std::string& err) {
                   op.has_bias ? s.G + op.b_off : nullptr, op.cout, op.cin, op.k * op.k);
         break;
       case OP_LINEAR:
-        if (s.bf16) add_linear(sc + align256(s.acts[op.out].bytes), op, 0, s.G + op.w_off, op.has_bias ? s.G + op.b_off : nullptr, op.cin, op.cout);
+        if (s.bf16 && !op.keep8) add_linear(sc + align256(s.acts[op.out].bytes), op, 0, s.G + op.w_off, op.has_bias ? s.G + op.b_off : nullptr, op.cin, op.cout);
         break;
       case OP_MHA: {
         const int D = op.cin;
@@ -844,7 +898,7 @@ ast_status build_reduce_tasks(Stage& s, std::string& err) {
         char* lw_o = sc + mha_lw_offset(I.n, I.h, D, op.heads);
         char* lw_q = lw_o + align256(linear_bf16_ws_bytes(R, D, D, op.wg_splits[0]));
         add_linear(lw_o, op, 0, Go, Gbo, D, D);
-        add_linear(lw_q, op, 1, Gq, Gbq, D, 3 * D);
+        if (!op.keep8) add_linear(lw_q, op, 1, Gq, Gbq, D, 3 * D);
         break;
       }
       case OP_LAYERNORM: {

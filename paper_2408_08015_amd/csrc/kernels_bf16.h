@@ -145,12 +145,13 @@ void layernorm_bwd_params_bf16(hipStream_t st, const void* ws, float* Ggamma, fl
 int layernorm_bwd_parts(size_t R);  // number of [2][D] partial rows the backward kernel writes
 
 // ---- self-attention core on packed qkv [B][S][3D] (head size 64, S % 32 == 0, S <= 256):
-// o [B][S][D], lse [B][H][S]
+// o [B][S][D], lse [B][H][S]; queries and keys come from qk (rows of ldqk, keys D behind the queries): qkv and 3D, or a tensor of
+// their own
 size_t mha_bf16_ws_bytes(int B, int S, int D, int heads);
-void attention_fwd_bf16(hipStream_t st, const bf16_t* qkv, bf16_t* o, float* lse, int B, int S, int D,
+void attention_fwd_bf16(hipStream_t st, const bf16_t* qkv, const bf16_t* qk, int ldqk, bf16_t* o, float* lse, int B, int S, int D,
                         int heads);
 // `dsum` is scratch of mha_bf16_ws_bytes() bytes
-void attention_bwd_bf16(hipStream_t st, const bf16_t* qkv, const bf16_t* o, const bf16_t* d_o,
+void attention_bwd_bf16(hipStream_t st, const bf16_t* qkv, const bf16_t* qk, int ldqk, const bf16_t* o, const bf16_t* d_o,
                         const float* lse, bf16_t* dqkv, float* dsum, int B, int S, int D, int heads);
 
 // bf16 <-> fp32 conversion of flat buffers

@@ -1,11 +1,13 @@
 // Plan construction: shape inference over the layer list, operator fusion, and the
 // layout of the flat arenas, the stash slot and the workspace.  Host code only.
 #include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 
 #include "kernels.h"
 #include "kernels_bf16.h"
+#include "ops.h"
 #include "stage.h"
 
 namespace ast {
@@ -33,6 +35,59 @@ static size_t conv_shadow_elems(int k, int Cin, int Cout) {
   return k == 3 ? std::max(plain, conv_res_pack_elems(Cin, Cout)) : plain;
 }
 
+static bool flag_ok(int v) { return v == 0 || v == 1; }
+
+// Does the backward pass read activation `a` in its bf16 form?
+static bool backward_reads(const Stage& s, int a) {
+  for (const Op& op : s.ops) {
+    switch (op.kind) {
+      case OP_LINEAR: case OP_MHA: if (op.in == a && !op.keep8) return true; break;
+      case OP_RES_BEGIN: case OP_RES_ADD: break;
+      case OP_ACT: if (op.act == 3 ? op.in == a && !op.keep8 : op.in == a || op.out == a) return true; break;
+      default: if (op.in == a || (op.kind == OP_CONV_IGEMM && op.out == a)) return true; break;
+    }
+    if (op.gelu_from == a || op.relu_from == a || (op.kind == OP_LINEAR && op.skip == a && !s.acts[a].kept8)) return true;
+  }
+  for (const Act& t : s.acts)
+    if (t.data_alias == a) return true;  // (a shortcut branch's input: its readers name the alias)
+  return false;
+}
+
+// Activations that the backward pass knows in 8 bits only live in the forward pass's scratch from the op that writes them to the
+// last one that reads them; those that live at different times share their place.  Bytes of that scratch.
+static size_t lay_out_passing(Stage& s) {
+  struct Span { size_t off, bytes; int last; };
+  std::vector<Span> live;
+  size_t end = 0;
+  for (size_t a = 0; a < s.acts.size(); ++a) {  // (in the order in which they are made)
+    Act& t = s.acts[a];
+    t.passing = t.kept8 && (int)a != s.final_act && t.data_alias < 0 && !backward_reads(s, (int)a);
+    if (!t.passing || a == 0) continue;
+    int first = -1, last = -1;
+    for (int j = 0; j < (int)s.ops.size(); ++j) {
+      const Op& op = s.ops[j];
+      const bool makes = (op.out == (int)a && op.in != (int)a) || (op.kind == OP_LINEAR && op.skip == (int)a);
+      if (makes && first < 0) first = j;
+      if (makes || op.in == (int)a || op.res_in == (int)a || op.skip == (int)a) last = j;
+    }
+    std::vector<Span> now;
+    for (const Span& v : live)
+      if (v.last >= first) now.push_back(v);
+    std::sort(now.begin(), now.end(), [](const Span& x, const Span& y) { return x.off < y.off; });
+    size_t off = 0;
+    const size_t bytes = align_up(t.bytes, 256);
+    for (const Span& v : now) {
+      if (off + bytes <= v.off) break;
+      off = std::max(off, v.off + v.bytes);
+    }
+    t.fwd_off = off;
+    now.push_back({off, bytes, last});
+    live = now;
+    end = std::max(end, off + bytes);
+  }
+  return end;
+}
+
 ast_status build_plan(Stage& s, std::string& err) {
   const ast_stage_cfg& cfg = s.cfg;
   const int B = cfg.B;
@@ -45,7 +100,12 @@ ast_status build_plan(Stage& s, std::string& err) {
   if (s.bf16 && cfg.layout == AST_NCHW) { err = "bf16 stages use NHWC or BSD"; return AST_EUNSUPPORTED; }
 
   int cur;
-  if (cfg.layout == AST_BSD) {
+  if (nl > 0 && s.layers[0].kind == AST_EMBEDDING) {  // token ids
+    if (!s.bf16 || cfg.layout != AST_BSD) { err = "layer 0: an embedding needs a bf16 stage of tokens"; return AST_EUNSUPPORTED; }
+    if (cfg.in_shape[0] <= 0 || cfg.in_shape[1] != 1) { err = "an embedding's in_shape is {S, 1}"; return AST_EINVAL; }
+    if (cfg.needs_input_grad) { err = "token ids have no gradient: needs_input_grad must be 0"; return AST_EINVAL; }
+    cur = new_act(s, B, 1, cfg.in_shape[0], 1, 3, -1, 4);
+  } else if (cfg.layout == AST_BSD) {
     if (cfg.in_shape[0] <= 0 || cfg.in_shape[1] <= 0) { err = "bad in_shape"; return AST_EINVAL; }
     cur = new_act(s, B, cfg.in_shape[1], cfg.in_shape[0], 1, 3, -1, es);
   } else if (cfg.layout == AST_NCHW || cfg.layout == AST_NHWC) {
@@ -141,6 +201,11 @@ ast_status build_plan(Stage& s, std::string& err) {
         op.kind = OP_ACT;
         op.act = L.kind == AST_RELU ? 1 : L.kind == AST_RELU6 ? 2 : L.kind == AST_GELU ? 3 : L.kind == AST_SWISH ? 4 : 5;
         if (!s.bf16 && op.act == 3) { err = fmt("layer %d: GELU is bf16-only", i); return AST_EUNSUPPORTED; }
+        if (op.act == 3) {
+          if (!flag_ok(L.p[0])) { err = fmt("layer %d: GELU: p[0] must be 0 or 1", i); return AST_EINVAL; }
+          op.keep8 = L.p[0] != 0;
+          if (op.keep8) s.acts[cur].kept8 = true;
+        }
         if (s.bf16 && op.act > 3) { err = fmt("layer %d: swish / sigmoid are fp32-only", i); return AST_EUNSUPPORTED; }
         op.out = cur = new_act(s, A.n, A.c, A.h, A.w, A.rank, i, es);
         break;
@@ -236,7 +301,11 @@ ast_status build_plan(Stage& s, std::string& err) {
         if (s.bf16 && A.elems / A.c * std::max(Cin, Cout) >= ((size_t)1 << 30)) {  // 32-bit byte offsets
           err = fmt("layer %d: bf16 linear tensors must stay below 2^30 elements", i); return AST_EUNSUPPORTED;
         }
+        if (!flag_ok(L.p[3])) { err = fmt("layer %d: linear: p[3] must be 0 or 1", i); return AST_EINVAL; }
+        if (L.p[3] && !s.bf16) { err = fmt("layer %d: inputs are kept in 8 bits in bf16 stages only", i); return AST_EUNSUPPORTED; }
         op.kind = OP_LINEAR; op.cin = Cin; op.cout = Cout; op.has_bias = hb ? 1 : 0;
+        op.keep8 = L.p[3] != 0;
+        if (op.keep8) s.acts[cur].kept8 = true;
         op.w_off = poff; poff += (size_t)Cout * Cin;
         if (hb) { op.b_off = poff; poff += Cout; }
         if (s.bf16) {
@@ -246,6 +315,8 @@ ast_status build_plan(Stage& s, std::string& err) {
             // pre-activation is stashed for the backward; output = GELU(pre)
             op.act = 3;
             op.skip = new_act(s, A.n, Cout, A.h, A.w, A.rank, i, es);  // pre-activation
+            if (!flag_ok(s.layers[i + 1].p[0])) { err = fmt("layer %d: GELU: p[0] must be 0 or 1", i + 1); return AST_EINVAL; }
+            s.acts[op.skip].kept8 = s.layers[i + 1].p[0] != 0;
             s.layer_act[i] = op.skip;
             ++i;
           }
@@ -293,12 +364,24 @@ ast_status build_plan(Stage& s, std::string& err) {
         if (D != A.c || H <= 0 || D % H) { err = fmt("layer %d: MHA D=%d heads=%d do not match input", i, D, H); return AST_EINVAL; }
         if (D / H != 64 || A.h % 32 || A.h > 256) { err = fmt("layer %d: MHA kernels cover head size 64 and S %% 32 == 0, S <= 256", i); return AST_EUNSUPPORTED; }
         if ((size_t)A.n * A.h * 3 * D >= ((size_t)1 << 30)) { err = fmt("layer %d: MHA tensors must stay below 2^30 elements", i); return AST_EUNSUPPORTED; }
+        if (!flag_ok(L.p[2]) || !flag_ok(L.p[5]) || !flag_ok(L.p[6])) { err = fmt("layer %d: MHA: p[2], p[5], p[6] must be 0 or 1", i); return AST_EINVAL; }
         op.kind = OP_MHA; op.cin = op.cout = D; op.heads = H; op.has_bias = 1;
-        op.w_off = poff; poff += (size_t)3 * D * D + 3 * D + (size_t)D * D + D;
+        op.keep8 = L.p[6] != 0;
+        if (op.keep8) s.acts[cur].kept8 = true;
+        op.qk_norm = L.p[2] != 0;
+        if (op.qk_norm) {
+          op.rotary = L.p[3]; op.theta = L.p[4]; op.interleaved = L.p[5]; op.eps = L.eps;
+          if (op.rotary < 0 || op.rotary > 64 || op.rotary % 2 || (op.rotary && L.p[4] < 1) || !(L.eps > 0.f) || !std::isfinite(L.eps)) {
+            err = fmt("layer %d: MHA: rotary must be even and lie in [0, 64], theta be at least 1 and eps positive", i); return AST_EINVAL; }
+          if (!op.rotary) op.theta = 1.0;
+        }
+        op.w_off = poff; poff += (size_t)3 * D * D + 3 * D + (size_t)D * D + D + (op.qk_norm ? 2 * 64 : 0);
         op.sh_off = shadow; shadow += (size_t)4 * D * D;   // W_qkv [3D][D], W_o [D][D]
         op.sh2_off = shadow; shadow += (size_t)4 * D * D;  // W_qkv^T [D][3D], W_o^T [D][D]
         // per-slot: qkv [rows][3D] bf16, o [rows][D] bf16, lse [B][H][S] fp32
-        take_aux(op, (size_t)A.n * A.h * 4 * D * 2 + (size_t)A.n * H * A.h * 4);
+        // with norm and rotation: the normalised, rotated queries and keys [rows][2D] bf16
+        op.qk_off = align_up((size_t)A.n * A.h * 4 * D * 2 + (size_t)A.n * H * A.h * 4, 256);
+        take_aux(op, op.qk_norm ? op.qk_off + (size_t)A.n * A.h * 2 * D * 2 : (size_t)A.n * A.h * 4 * D * 2 + (size_t)A.n * H * A.h * 4);
         bool mha_res = false;
         if (i + 1 < nl && s.layers[i + 1].kind == AST_RES_ADD && !res_stack.empty() && !res_swapped.back()) {
           const Act& K = s.acts[res_stack.back()];  // residual add folded into the output projection
@@ -313,6 +396,16 @@ ast_status build_plan(Stage& s, std::string& err) {
           s.ops[res_op_stack.back()].skip = cur;
           res_stack.pop_back(); res_op_stack.pop_back(); res_swapped.pop_back();
         }
+        break;
+      }
+      case AST_EMBEDDING: {
+        const int V = L.p[0], D = L.p[1];
+        if (i != 0) { err = fmt("layer %d: an embedding must be the first layer", i); return AST_EINVAL; }
+        if (V < 1 || V > 0x7ffffffe || D < 8 || D % 8 || !std::isfinite(L.eps)) { err = "layer 0: embedding: rows in [1, 2^31 - 2], a width divisible by 8, a finite scale"; return AST_EINVAL; }
+        if ((size_t)B * A.h * D >= ((size_t)1 << 30)) { err = "layer 0: the embedding's output must stay below 2^30 elements"; return AST_EUNSUPPORTED; }
+        op.kind = OP_EMBEDDING; op.cin = V; op.cout = D; op.scale = L.eps;
+        op.w_off = poff; poff += (size_t)V * D;
+        op.out = cur = new_act(s, B, D, A.h, 1, 3, i, es);
         break;
       }
       default:
@@ -374,7 +467,7 @@ ast_status build_plan(Stage& s, std::string& err) {
   for (size_t j = 1; j < s.ops.size(); ++j) {
     Op& pr = s.ops[j - 1];
     Op& nx = s.ops[j];
-    if (s.bf16 && pr.kind == OP_LINEAR && pr.act == 3 && nx.kind == OP_LINEAR && nx.in == pr.out) {
+    if (s.bf16 && pr.kind == OP_LINEAR && pr.act == 3 && !s.acts[pr.skip].kept8 && nx.kind == OP_LINEAR && nx.in == pr.out) {
       nx.gelu_from = pr.skip;
       pr.gelu_bwd_fused = true;
     }
@@ -526,10 +619,20 @@ ast_status build_plan(Stage& s, std::string& err) {
     a.in_unwritten = !read;
     s.acts[a.in].unwritten |= !read;
   }
+  const size_t passing_bytes = lay_out_passing(s);
   for (size_t a = 0; a < s.acts.size(); ++a) {
     s.acts[a].unwritten |= virtual_act[a] != 0;
     if ((int)a == final_act && !s.loss_tail && a != 0 && !s.final_in_slot) continue;
     if (virtual_act[a] || s.acts[a].data_alias >= 0) continue;
+    if (s.acts[a].kept8) {
+      s.acts[a].slot8_off = off;
+      off = align_up(off + stash8_bytes((int64_t)(s.acts[a].elems / s.acts[a].c), s.acts[a].c), 256);
+    }
+    if (s.acts[a].passing) {
+      for (int& la : s.layer_act)
+        if (la == (int)a) la = -1;  // (nothing holds it when the forward pass is over)
+      continue;
+    }
     s.acts[a].slot_off = off;
     off = align_up(off + s.acts[a].bytes, 256);
   }
@@ -581,14 +684,18 @@ ast_status build_plan(Stage& s, std::string& err) {
         case OP_LINEAR:
           if (s.bf16)
             need = align_up(s.acts[op.out].bytes, 256) +
-                   linear_bf16_ws_bytes((size_t)I.n * I.h * I.w, op.cin, op.cout, op.wg_splits[0]);
+                   (op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)I.n * I.h * I.w, op.cin, op.cout)
+                             : linear_bf16_ws_bytes((size_t)I.n * I.h * I.w, op.cin, op.cout, op.wg_splits[0]));
           break;
+        case OP_EMBEDDING: need = embedding_bwd_ws_bytes((int64_t)I.n * I.h, op.cin, op.cout); break;
         case OP_LAYERNORM: need = layernorm_bf16_ws_bytes((size_t)I.n * I.h, I.c); break;
         case OP_MHA:  // d_o and dqkv, the row sums, then the split-K partials of each projection
           need = align_up((size_t)I.n * I.h * 4 * op.cin * 2, 256) +
                  align_up(mha_bf16_ws_bytes(I.n, I.h, op.cin, op.heads), 256) +
                  align_up(linear_bf16_ws_bytes((size_t)I.n * I.h, op.cin, op.cin, op.wg_splits[0]), 256) +
-                 linear_bf16_ws_bytes((size_t)I.n * I.h, op.cin, 3 * op.cin, op.wg_splits[1]);
+                 align_up(op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)I.n * I.h, op.cin, 3 * op.cin)
+                                   : linear_bf16_ws_bytes((size_t)I.n * I.h, op.cin, 3 * op.cin, op.wg_splits[1]), 256) +
+                 (op.qk_norm ? qk_norm_rope_bwd_ws_bytes((int64_t)I.n * I.h, 64) : 0);
           break;
         default: break;
       }
@@ -597,7 +704,7 @@ ast_status build_plan(Stage& s, std::string& err) {
     }
     // The forward pass has scratch of its own (BatchNorm statistics partials), so that the forward of one
     // micro-batch may run beside the backward of another.
-    size_t fsc = 0;
+    size_t fsc = align_up(passing_bytes, 256);
     for (Op& op : s.ops) {
       if (op.kind != OP_BN || op.dws) continue;
       const Act& I = s.acts[op.in];
@@ -619,10 +726,10 @@ ast_status build_plan(Stage& s, std::string& err) {
       if (op.kind != OP_LINEAR && op.kind != OP_MHA) continue;
       const Act& I = s.acts[op.in];
       const size_t rows = (size_t)I.n * I.h * I.w;
-      if (rows < 48) continue;
+      if (rows < 48 || (op.kind == OP_LINEAR && op.keep8)) continue;
       products.push_back({rows, op.cin, op.cout, 1});
       splits.push_back(&op.wg_splits[0]);
-      if (op.kind != OP_MHA) continue;
+      if (op.kind != OP_MHA || op.keep8) continue;
       products.push_back({rows, op.cin, 3 * op.cin, 1});
       splits.push_back(&op.wg_splits[1]);
     }

@@ -36,7 +36,8 @@ enum OpKind {
   OP_LINEAR,       // fp32 rows (vectors) or bf16 token GEMM (+GELU)
   OP_SOFTMAX_CE,
   OP_LAYERNORM,    // (+ residual add fused in front)
-  OP_MHA
+  OP_MHA,
+  OP_EMBEDDING     // rows of a token table; the stage input is int32 ids
 };
 
 struct Act {
@@ -49,6 +50,11 @@ struct Act {
   int grad_alias = -1;             // gradient buffer shared with this activation's
   int data_alias = -1;             // same tensor as this activation (own gradient buffer): the input of a shortcut branch
   int layer = -1;                  // layer index whose output this is (-1: stage input)
+  bool kept8 = false;              // kept in 8 bits for the backward pass ...
+  size_t slot8_off = 0;            // ... at this byte offset of a stash slot
+  bool passing = false;            // ... and in no other form: its bf16 values last from the op that makes them to the forward
+                                   // pass's last reader (the stage input: in the caller's buffer)
+  size_t fwd_off = 0;              // ... at this byte offset of the forward pass's scratch
   bool unwritten = false;          // no kernel writes it: the kernels that need it form it from what they read
 };
 
@@ -64,6 +70,13 @@ struct Op {
   int has_bias = 0;
   int cin = 0, cout = 0, k = 1, stride = 1, pad = 0, groups = 1;
   int heads = 0;
+  bool keep8 = false;     // bf16 linear / MHA / GELU: the input is kept in 8 bits and the weight gradient (of MHA: of the qkv
+                          // projection), or GELU's gradient, is formed from it
+  bool qk_norm = false;   // MHA: norm with gains and rotation of queries and keys
+  int rotary = 0, interleaved = 0;
+  double theta = 1.0;
+  float scale = 1.f;      // embedding
+  size_t qk_off = 0;      // MHA: their result, bytes past aux_off
   float eps = 1e-5f;
   size_t aux_off = 0, aux_bytes = 0;  // per-slot extras (statistics, probabilities, ...)
   size_t run_off = 0;                 // BatchNorm running statistics (floats, persistent)
@@ -184,6 +197,7 @@ struct Stage {
   std::vector<int> free_slots;
 
   // per-call boundary pointers
+  const void* cur_x = nullptr;
   const void* cur_dy = nullptr;
   void* cur_dx = nullptr;
   void* cur_y = nullptr;

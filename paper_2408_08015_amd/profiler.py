@@ -69,6 +69,8 @@ def _out_shape(layers, s):
             s = (s[0],)
         elif k == "linear":
             s = s[:-1] + (L["cout"],)
+        elif k == "embedding":
+            s = s[:-1] + (L["d"],)
     return s
 
 
@@ -93,7 +95,10 @@ def time_unit(layers, in_shape, beta, dtype, layout, needs_input_grad, reps=20, 
     n = st.num_params
     if n:
         st.set_params((0.05 * torch.randn(n, generator=g)).numpy() + 0.5)
-    x = torch.randn(_boundary(layout, in_shape, beta), generator=g).to(dev).to(tdt).contiguous()
+    if layers[0]["kind"] == "embedding":
+        x = torch.randint(0, layers[0]["rows"], (beta, in_shape[0]), generator=g, dtype=torch.int32).to(dev)
+    else:
+        x = torch.randn(_boundary(layout, in_shape, beta), generator=g).to(dev).to(tdt).contiguous()
     dx = torch.zeros_like(x) if needs_input_grad else None
     if loss_tail:
         labels = torch.randint(0, out[0], (beta,), generator=g, dtype=torch.int32).to(dev)

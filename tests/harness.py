@@ -57,7 +57,8 @@ def run_hip(cfg, inp, K=1, rounds=2, debug_layers=None, static_backward=False, f
     if forward_stream:
         fs = A.stream_create()
         st.set_forward_stream(fs)
-    x = torch.from_numpy(inp["x"]).to(dev).to(tdt).contiguous()
+    x = torch.from_numpy(inp["x"]).to(dev)
+    x = x.contiguous() if inp["x"].dtype == np.int32 else x.to(tdt).contiguous()   # token ids stay int32
     B, M = cfg.B, cfg.M
     if cfg.loss_tail:
         labels = torch.from_numpy(inp["labels"]).to(dev)
