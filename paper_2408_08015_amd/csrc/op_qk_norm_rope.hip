@@ -60,6 +60,19 @@ template <> struct Vec<float, 4> {
     *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
   }
 };
+template <> struct Vec<bf16_t, 2> {
+  typedef uint32_t Raw;
+  static __device__ __forceinline__ void expand(const Raw& a, float (&v)[2]) {
+    v[0] = __uint_as_float(a << 16);
+    v[1] = __uint_as_float(a & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void store(bf16_t* p, const float (&v)[2]) { *reinterpret_cast<uint32_t*>(p) = f2bf_pk(v[0], v[1]); }
+};
+template <> struct Vec<float, 2> {
+  typedef float2 Raw;
+  static __device__ __forceinline__ void expand(const Raw& a, float (&v)[2]) { v[0] = a.x; v[1] = a.y; }
+  static __device__ __forceinline__ void store(float* p, const float (&v)[2]) { *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]); }
+};
 template <typename T> struct Vec<T, 1> {
   typedef T Raw;
   static __device__ __forceinline__ void expand(const Raw& a, float (&v)[1]) { v[0] = load1(&a); }
@@ -74,6 +87,17 @@ __device__ __forceinline__ float head_sum(float v, int ls) {
   if (ls > 3) v += dpp_move<DPP_ROW_MIRROR>(v);
   if (ls > 4) v += __shfl_xor(v, 16, 64);
   if (ls > 5) v += __shfl_xor(v, 32, 64);
+  return v;
+}
+
+// ... and over the lanes that hold the same place of the wavefront's heads (rotations inside the rows of 16, then across them)
+__device__ __forceinline__ float places_sum(float v, int ls) {
+  if (ls < 4) v += dpp_move<0x128>(v);
+  if (ls < 3) v += dpp_move<0x124>(v);
+  if (ls < 2) v += dpp_move<0x122>(v);
+  if (ls < 1) v += dpp_move<0x121>(v);
+  if (ls < 5) v += __shfl_xor(v, 16, 64);
+  if (ls < 6) v += __shfl_xor(v, 32, 64);
   return v;
 }
 
@@ -245,8 +269,7 @@ __global__ __launch_bounds__(256, 4) void qk_norm_rope_kernel(const QkArgs g) {
       for (int z = 0; z < 2; ++z)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          float v = acc[i][z][e];
-          for (int o = 1 << g.ls; o < 64; o <<= 1) v += __shfl_xor(v, o, 64);
+          const float v = places_sum(acc[i][z][e], g.ls);
           if ((tid & 63) >> g.ls == 0 && (z ? on_b[i] : on_a[i])) red[wave * 256 + (z ? pb[i] : pa[i]) + e] = v;
         }
     __syncthreads();
@@ -280,21 +303,22 @@ __global__ __launch_bounds__(1024) void qk_gain_sum_kernel(const float* __restri
   }
 }
 
-bool wide(const ast_heads& h, int esize) {
-  return (reinterpret_cast<uintptr_t>(h.dev) % 16) == 0 && (h.token_stride * esize) % 16 == 0 && (h.head_stride * esize) % 16 == 0;
+bool steps_of(const ast_heads& h, int bytes, int esize) {  // every head starts at a multiple of `bytes`
+  return reinterpret_cast<uintptr_t>(h.dev) % bytes == 0 && h.token_stride * esize % bytes == 0 && h.head_stride * esize % bytes == 0;
 }
 
 constexpr int QK_MOST_BLOCKS = 1024;  // of a backward pass and of queries or keys: partial sums of the gains' gradients
 
-struct Shape { int vec, ls, units, rot_units, tb[2]; unsigned blocks[2]; };
+struct Shape { int vec, it, ls, units, rot_units, tb[2]; unsigned blocks[2]; };
 
 // Lanes and blocks of a call.  About 2048 blocks of queries and as many of keys forward, 1024 backward (whose blocks each leave
 // partial sums): a block forms its angles and waits for its first loads once.  us, forward of 32768 tokens, 32 + 8 heads of
 // 128, and backward of 10007 tokens, 12 + 3 fp32 heads of 80: 1024 blocks 145 and 38.4, 2048 blocks 140 and 42.2, blocks that
 // take a token of every lane group 199 and 46.7.
-Shape shape_of(const ast_qk_cfg& c, const int heads[2], bool vec, bool bwd) {
+Shape shape_of(const ast_qk_cfg& c, const int heads[2], int vec, bool bwd) {
   Shape s = {};
-  s.vec = !vec ? 1 : c.dtype == AST_BF16_F32ACC ? 8 : 4;
+  s.vec = vec;
+  s.it = vec == 1 ? 4 : vec == 2 ? 2 : 1;
   if (c.interleaved) {
     s.units = (c.head_dim + 2 * s.vec - 1) / (2 * s.vec);
     s.rot_units = (c.rotary + 2 * s.vec - 1) / (2 * s.vec);
@@ -302,11 +326,14 @@ Shape shape_of(const ast_qk_cfg& c, const int heads[2], bool vec, bool bwd) {
     s.rot_units = c.rotary / 2 / s.vec;
     s.units = s.rot_units + ((c.head_dim - c.rotary) / s.vec + 1) / 2;
   }
-  while (s.ls < 6 && (1 << s.ls) < s.units) ++s.ls;
+  while ((s.it << s.ls) < s.units) ++s.ls;  // (at most 128 units: no more than 32 lanes)
   const int groups = 256 >> s.ls;  // heads at a time
   for (int w = 0; w < 2; ++w) {
     const int most = bwd ? QK_MOST_BLOCKS : 2048;
-    int64_t tb = std::max<int64_t>((c.tokens + most - 1) / most, std::min<int64_t>((groups + heads[w] - 1) / heads[w], c.tokens / 256));
+    // (two heads a lane backward, one forward, where that leaves 128 and 256 blocks)
+    const int64_t fill = bwd ? std::min<int64_t>((2 * groups + heads[w] - 1) / heads[w], c.tokens / 128)
+                             : std::min<int64_t>((groups + heads[w] - 1) / heads[w], c.tokens / 256);
+    int64_t tb = std::max<int64_t>((c.tokens + most - 1) / most, fill);
     if (c.rotary) tb = std::min<int64_t>(tb, QK_TRIG / (c.rotary / 2));
     tb = std::max<int64_t>(1, std::min<int64_t>({tb, 64, (1 << 20) / heads[w]}));
     s.tb[w] = (int)tb;
@@ -320,15 +347,21 @@ void launch(hipStream_t st, const ast_qk_cfg& c, const ast_heads* dy, const ast_
             const ast_heads* y, float* part, unsigned* blocks) {
   const bool bwd = dy != nullptr, bf = c.dtype == AST_BF16_F32ACC;
   QkArgs g = {};
-  const int full = bf ? 8 : 4, esize = bf ? 2 : 4;
-  bool vec = c.head_dim % full == 0 && (c.interleaved ? c.rotary % (2 * full) == 0 || c.rotary == c.head_dim : c.rotary / 2 % full == 0);
+  const int esize = bf ? 2 : 4;
+  // values that are read and written at a time: 16 bytes, two, or one, as the head's parts and its addresses allow
+  auto fits = [&](int v) {
+    if (c.head_dim % v || !(c.interleaved ? c.rotary % (2 * v) == 0 || c.rotary == c.head_dim : c.rotary / 2 % v == 0)) return false;
+    for (int w = 0; w < 2; ++w)
+      if (!steps_of(x[w], v * esize, esize) || !steps_of(y[w], v * esize, esize) || (bwd && !steps_of(dy[w], v * esize, esize))) return false;
+    return true;
+  };
+  const int vec = fits(16 / esize) ? 16 / esize : fits(2) ? 2 : 1;
   for (int w = 0; w < 2; ++w) {
     g.x[w] = {x[w].dev, x[w].token_stride, x[w].head_stride};
     g.y[w] = {y[w].dev, y[w].token_stride, y[w].head_stride};
     if (bwd) g.dy[w] = {dy[w].dev, dy[w].token_stride, dy[w].head_stride};
     g.heads[w] = x[w].heads;
     g.inv_heads[w] = 1.f / (float)x[w].heads;
-    vec = vec && wide(x[w], esize) && wide(y[w], esize) && (!bwd || wide(dy[w], esize));
   }
   const Shape s = shape_of(c, g.heads, vec, bwd);
   g.gain[0] = gq;
@@ -362,9 +395,13 @@ void launch(hipStream_t st, const ast_qk_cfg& c, const ast_heads* dy, const ast_
     }                                                                                                                         \
   } while (0)
   if (bf) {
-    if (vec) GO(bf16_t, 8, 1); else GO(bf16_t, 1, 2);
+    if (vec == 8) GO(bf16_t, 8, 1);
+    else if (vec == 2) GO(bf16_t, 2, 2);
+    else GO(bf16_t, 1, 4);
   } else {
-    if (vec) GO(float, 4, 1); else GO(float, 1, 2);
+    if (vec == 4) GO(float, 4, 1);
+    else if (vec == 2) GO(float, 2, 2);
+    else GO(float, 1, 4);
   }
 #undef GO
 }

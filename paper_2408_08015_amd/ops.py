@@ -52,6 +52,10 @@ def _lib():
     return _LIB
 
 
+# the handle of a device's current stream (without a Stream object around it, where torch offers that)
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+
+
 def _device(t, *others):
     """The GPU that holds the tensors."""
     d = t.get_device()
@@ -66,10 +70,10 @@ def _device(t, *others):
 def _call(d, fn, *args):
     """fn(*args, stream) with device d current (the calls launch on the current one) and its current stream."""
     if torch.cuda.current_device() == d:
-        st = fn(*args, torch.cuda.current_stream(d).cuda_stream)
+        st = fn(*args, _stream(d))
     else:
         with torch.cuda.device(d):
-            st = fn(*args, torch.cuda.current_stream(d).cuda_stream)
+            st = fn(*args, _stream(d))
     if st:
         _check(_LIB, st)
 
@@ -197,13 +201,16 @@ def qk_norm_rope_forward(q, k, q_gain, k_gain, positions=None, period=0, rotary=
     return yq, yk
 
 
-def qk_norm_rope_backward_workspace(tokens, head_dim):
-    """Bytes of workspace that qk_norm_rope_backward takes."""
+def _qk_workspace(cfg):
     n = C.c_size_t()
     lib = _lib()
-    _check(lib, lib.asteroid_qk_norm_rope_backward_workspace(
-        ast_qk_cfg(tokens, 0, head_dim, 0, 0, 1.0, 1.0, None, 1), 1, 1, C.byref(n)))
+    _check(lib, lib.asteroid_qk_norm_rope_backward_workspace(cfg, 1, 1, n))
     return n.value
+
+
+def qk_norm_rope_backward_workspace(tokens, head_dim):
+    """Bytes of workspace that qk_norm_rope_backward takes."""
+    return _qk_workspace(ast_qk_cfg(tokens, 0, head_dim, 0, 0, 1.0, 1.0, None, 1))
 
 
 def qk_norm_rope_backward(dyq, dyk, q, k, q_gain, k_gain, positions=None, period=0, rotary=None, theta=10000.0,
@@ -224,7 +231,7 @@ def qk_norm_rope_backward(dyq, dyk, q, k, q_gain, k_gain, positions=None, period
     a = [_heads(t, n, T, d, q.dtype) for t, n in ((dyq, "dyq"), (dyk, "dyk"), (q, "q"), (k, "k"), (dq, "dq"), (dk, "dk"))]
     lib = _lib()
     on = _device(q, k, dyq, dyk, dq, dk, q_gain, k_gain, gq, gk, positions)
-    ws = _workspace(workspace, qk_norm_rope_backward_workspace(T, d), q.device)
+    ws = _workspace(workspace, _qk_workspace(cfg), q.device)
     _call(on, lib.asteroid_qk_norm_rope_backward, cfg, a[0], a[1], a[2], a[3], q_gain.data_ptr(), k_gain.data_ptr(), a[4], a[5],
           gq.data_ptr(), gk.data_ptr(), bool(accumulate), ws.data_ptr(), ws.numel())
     return dq, dk, gq, gk
