@@ -287,7 +287,9 @@ struct SumArgs {
 constexpr int SUM_COLS = 512;
 
 // How the columns are read and written: eight at 16-byte addresses; eight at any address, where the last lane of a row takes its
-// last eight and so some of its neighbour's (both write the same values); or what there is of rows of fewer than eight.
+// last eight and so some of its neighbour's (both write the same values; the neighbour is a lane of the same wavefront, whose
+// reads of what is added to come before its writes); or what there is, of rows of fewer than eight and of those whose last
+// SUM_COLS columns are fewer than eight.
 enum : int { COLS_EVEN = 0, COLS_ANY = 1, COLS_NARROW = 2 };
 template <int COLS>
 __device__ __forceinline__ int first_col(int width, int lane) {
@@ -592,7 +594,7 @@ void embedding_bwd(hipStream_t st, const int32_t* ids, int64_t tokens, const voi
     if (chunks > 1) KLAUNCH_NAMED("embedding_join_kernel", (embedding_join_kernel<C>), dim3((unsigned)(chunks - 1), cols_blocks), dim3(512), 0, st, g);
   };
   if (even) go(std::integral_constant<int, COLS_EVEN>());
-  else if (width >= 8) go(std::integral_constant<int, COLS_ANY>());
+  else if (width >= 8 && (width % SUM_COLS == 0 || width % SUM_COLS >= 8)) go(std::integral_constant<int, COLS_ANY>());
   else go(std::integral_constant<int, COLS_NARROW>());
 }
 

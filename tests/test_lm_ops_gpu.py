@@ -94,6 +94,22 @@ def test_embedding_backward(ops, T, V, D, kind, dt):
     assert np.array_equal(host(acc)[still], old[still].astype(np.float64))   # rows without a token stay
 
 
+@pytest.mark.parametrize("D", [513, 516, 519, 520, 1025, 1031])
+def test_embedding_rows_that_end_just_behind_a_share_of_the_columns(ops, D):
+    """A block's last columns may be a few only: every column has one writer all the same, which adding needs."""
+    r = rng(11, D)
+    T, V = 700, 90
+    ids = IDS["text"](r, T, V).astype(np.int32)
+    dy, g = dev(r.normal(size=(T, D)), "bf16")
+    want, terms, n = O.embedding_backward(ids, g, V, 1.0)
+    bound = (n[:, None] + 2) * u * terms * 1.001
+    inside(ops.embedding_backward(dev(ids)[0], dy, V), want, bound)
+    old = r.normal(size=(V, D)).astype(np.float32)
+    for _ in range(3):
+        acc = ops.embedding_backward(dev(ids)[0], dy, V, out=dev(old)[0], accumulate=True)
+        inside(acc, old + want, bound + u * 1.001 * (abs(old) + terms))
+
+
 def test_embedding_of_no_tokens(ops):
     ids = torch.zeros(0, dtype=torch.int32, device="cuda")
     assert ops.embedding_forward(ids, torch.ones(3, 4, device="cuda")).shape == (0, 4)
