@@ -32,7 +32,7 @@ __device__ __forceinline__ void restore8(uint2 q, float s, float (&v)[8]) {
   }
 }
 
-template <typename T>
+template <typename T, bool EVEN>
 __global__ __launch_bounds__(256) void stash8_pack_kernel(const T* __restrict__ x, int64_t rows, int cols, int pitch,
                                                           uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
   const int per_row = pitch / 8;
@@ -40,11 +40,9 @@ __global__ __launch_bounds__(256) void stash8_pack_kernel(const T* __restrict__ 
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / per_row;
     const int c = (int)(i - r * per_row) * 8;
-    const T* src = x + r * cols + c;
-    const int live = cols - c;
     float v[8];
-    if (live >= 8) load8(src, v);
-    else load8_part(src, live, v);
+    if (c < cols) load8_row<T, EVEN>(x + r * cols, c, cols, v);
+    else load8_part(x, 0, v);
     uint32_t top = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
@@ -91,7 +89,7 @@ __device__ __forceinline__ float gelu_slope(float z) {
   return 0.5f * erfcf(z * -0.70710678118f) + z * 0.3989422804f * expf(-0.5f * z * z);
 }
 
-template <typename T>
+template <typename T, bool EVEN>
 __global__ __launch_bounds__(256) void gelu_bwd_stash8_kernel(const T* dy, const uint8_t* __restrict__ q,
                                                               const uint8_t* __restrict__ scales, int64_t rows, int cols,
                                                               int pitch, T* dz) {  // (dz may be dy)
@@ -104,8 +102,7 @@ __global__ __launch_bounds__(256) void gelu_bwd_stash8_kernel(const T* dy, const
     float z[8], g[8];
     restore8(*reinterpret_cast<const uint2*>(q + r * pitch + c),
              scale_of(scales[r * (pitch / kStash8Block) + c / kStash8Block]), z);
-    if (live >= 8) load8(dy + r * cols + c, g);
-    else load8_part(dy + r * cols + c, live, g);
+    load8_row<T, EVEN>(dy + r * cols, c, cols, g);  // (in place: what it reads of others' places is not used)
 #pragma unroll
     for (int k = 0; k < 8; ++k) g[k] *= gelu_slope<sizeof(T) == 4>(z[k]);
     if (live >= 8) store8(dz + r * cols + c, g);
@@ -113,6 +110,9 @@ __global__ __launch_bounds__(256) void gelu_bwd_stash8_kernel(const T* dy, const
   }
 }
 
+bool rows_even(const void* p, int64_t cols, bool bf16) {  // every row starts at a 16-byte address
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && cols * (bf16 ? 2 : 4) % 16 == 0;
+}
 unsigned blocks_for(int64_t chunks) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>((chunks + 255) / 256, 1 << 20)); }
 
 }  // namespace
@@ -123,8 +123,10 @@ void stash8_pack(hipStream_t st, const void* x, bool bf16, int64_t rows, int64_t
   uint8_t* q = static_cast<uint8_t*>(stash);
   uint8_t* sc = q + rows * pitch;
   const dim3 grid(blocks_for(rows * (pitch / 8)));
-  if (bf16) KLAUNCH(stash8_pack_kernel<bf16_t>, grid, dim3(256), 0, st, static_cast<const bf16_t*>(x), rows, (int)cols, pitch, q, sc);
-  else KLAUNCH(stash8_pack_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(x), rows, (int)cols, pitch, q, sc);
+  auto go = [&](auto kernel, auto* p) { KLAUNCH_NAMED("stash8_pack_kernel", kernel, grid, dim3(256), 0, st, p, rows, (int)cols, pitch, q, sc); };
+  const bool even = rows_even(x, cols, bf16);
+  if (bf16) go(even ? stash8_pack_kernel<bf16_t, true> : stash8_pack_kernel<bf16_t, false>, static_cast<const bf16_t*>(x));
+  else go(even ? stash8_pack_kernel<float, true> : stash8_pack_kernel<float, false>, static_cast<const float*>(x));
 }
 
 void stash8_unpack(hipStream_t st, const void* stash, int64_t rows, int64_t cols, void* x, bool bf16) {
@@ -143,12 +145,14 @@ void gelu_bwd_stash8(hipStream_t st, const void* dy, bool bf16, const void* stas
   const uint8_t* q = static_cast<const uint8_t*>(stash);
   const uint8_t* sc = q + rows * pitch;
   const dim3 grid(blocks_for(rows * ((cols + 7) / 8)));
+  auto go = [&](auto kernel, auto* p, auto* out) {
+    KLAUNCH_NAMED("gelu_bwd_stash8_kernel", kernel, grid, dim3(256), 0, st, p, q, sc, rows, (int)cols, pitch, out);
+  };
+  const bool even = rows_even(dy, cols, bf16);
   if (bf16)
-    KLAUNCH(gelu_bwd_stash8_kernel<bf16_t>, grid, dim3(256), 0, st, static_cast<const bf16_t*>(dy), q, sc, rows, (int)cols, pitch,
-            static_cast<bf16_t*>(dz));
+    go(even ? gelu_bwd_stash8_kernel<bf16_t, true> : gelu_bwd_stash8_kernel<bf16_t, false>, static_cast<const bf16_t*>(dy), static_cast<bf16_t*>(dz));
   else
-    KLAUNCH(gelu_bwd_stash8_kernel<float>, grid, dim3(256), 0, st, static_cast<const float*>(dy), q, sc, rows, (int)cols, pitch,
-            static_cast<float*>(dz));
+    go(even ? gelu_bwd_stash8_kernel<float, true> : gelu_bwd_stash8_kernel<float, false>, static_cast<const float*>(dy), static_cast<float*>(dz));
 }
 
 }  // namespace ast

@@ -100,6 +100,26 @@ __device__ __forceinline__ void load8_part(const T* p, int n, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = i < n ? load1(p + i) : 0.f;
 }
+// values c .. c + 7 of a row of `cols`, 0 behind its end; EVEN: rows start at 16-byte addresses
+template <typename T, bool EVEN>
+__device__ __forceinline__ void load8_row(const T* row, int c, int cols, float (&v)[8]) {
+  const int over = c + 8 - cols;
+  if (EVEN && over <= 0) {
+    load8(row + c, v);
+  } else if (cols >= 8) {  // (the last eight, moved down)
+    Eight<T, false> e;
+    e.load(row + c - max(over, 0));
+    uint32_t w[Eight<T, false>::W];
+    e.words(w);
+    if (over > 0) {
+      const uint32_t zero[Eight<T, false>::W] = {};
+      funnel(w, zero, (uint32_t)over * (uint32_t)sizeof(T));
+    }
+    eight_values<T>(w, v);
+  } else {
+    load8_part(row + c, cols - c, v);
+  }
+}
 __device__ __forceinline__ void store1(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store1(bf16_t* p, float v) { *p = (bf16_t)(f2bf_pk(v, 0.f) & 0xffffu); }
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {

@@ -243,9 +243,10 @@ class Stash8:
     """A matrix [rows, cols] kept in 8 bits (`data`, a uint8 tensor in the layout of asteroid_ops.h)."""
     __slots__ = ("data", "rows", "cols")
 
-    def __init__(self, rows, cols, device, data=None):
-        need = stash8_bytes(rows, cols)
-        self.data = _workspace(data, need, torch.device(device))
+    def __init__(self, rows, cols, device=None, data=None):
+        if data is None and device is None:
+            raise ValueError("a device, or the tensor to keep the values in, must be given")
+        self.data = _workspace(data, stash8_bytes(rows, cols), device if data is None else data.device)
         self.rows, self.cols = rows, cols
 
 
