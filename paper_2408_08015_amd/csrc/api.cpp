@@ -78,6 +78,7 @@ void free_stage(ast::Stage& s) {
   s.red_block_task = nullptr;
   s.red_nblocks = 0;
   ast::drop_wgrad_groups(s);
+  ast::drop_kept_groups(s);
   if (s.wpack) (void)hipFree(s.wpack);
   s.wpack = nullptr;
   if (s.ws) (void)hipFree(s.ws);

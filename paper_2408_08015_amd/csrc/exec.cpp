@@ -465,6 +465,7 @@ void bwd_op(Ctx& c, const Op& op) {
           linear_bf16_dgrad(st, g, s.shadow + op.sh2_off, (bf16_t*)gin,
                             op.gelu_from >= 0 ? (cb)act_ptr(c, op.gelu_from) : nullptr,
                             op.dgrad_add >= 0 ? (cb)grad_ptr(c, op.dgrad_add) : nullptr, R, op.cin, op.cout);
+        if (op.kept_grouped) break;  // part of the launch at the end of the pass
         if (op.keep8)
           linear_wgrad_stash8(st, g, act8_ptr(c, op.in), (int64_t)R, op.cin, op.cout, s.G + op.w_off,
                               op.has_bias ? s.G + op.b_off : nullptr, true, sc);
@@ -518,8 +519,7 @@ void bwd_op(Ctx& c, const Op& op) {
       if (!op.wg_grouped) linear_bf16_wgrad(sw, g, o, Go, Gbo, true, defer, lw_o, R, D, D);
       const bf16_t* qk = op.qk_norm ? reinterpret_cast<const bf16_t*>(c.slot + op.aux_off + op.qk_off) : qkv;
       attention_bwd_bf16(st, qkv, qk, op.qk_norm ? 2 * D : 3 * D, o, d_o, lse, dqkv, dsum, I.n, I.h, D, op.heads);
-      char* const after_q = lw_q + align256(op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)R, D, 3 * D)
-                                                     : linear_bf16_ws_bytes(R, D, 3 * D, op.wg_splits[1]));
+      char* const after_q = lw_q + align256(mha_qkv_wgrad_ws(op, R));
       if (op.qk_norm) {  // in place: from the rotated, normalised heads to the projection's
         const ast_heads dq = qk_heads(dqkv, 3 * D, op), dk = qk_heads(dqkv + D, 3 * D, op);
         const float* gains = s.W + op.w_off + (size_t)4 * D * D + 4 * D;
@@ -530,6 +530,7 @@ void bwd_op(Ctx& c, const Op& op) {
       if (gin)
         linear_bf16_dgrad(st, dqkv, s.shadow + op.sh2_off, (bf16_t*)gin, nullptr,
                           op.dgrad_add >= 0 ? (cb)grad_ptr(c, op.dgrad_add) : nullptr, R, D, 3 * D);
+      if (op.kept_grouped) break;
       if (op.keep8) linear_wgrad_stash8(st, dqkv, act8_ptr(c, op.in), (int64_t)R, D, 3 * D, Gq, Gbq, true, lw_q);
       else if (!op.wg_grouped) linear_bf16_wgrad(sw, dqkv, (cb)act_ptr(c, op.in), Gq, Gbq, true, defer, lw_q, R, D, 3 * D);
       break;
@@ -599,6 +600,10 @@ ast_status run_backward(Stage& s, int slot, const void* dy, void* dx, char* stat
   if (s.wg_nblocks) {
     const Stage::WgGroup& wg = s.wg_groups[2 * slot + (static_ws ? 1 : 0)];
     wgrad_group_launch(s.stream, wg.tasks, wg.blocks, s.wg_nblocks);
+  }
+  if (s.kept_nblocks) {  // and those that are formed from inputs kept in 8 bits
+    const Stage::WgGroup& kg = s.kept_groups[2 * slot + (static_ws ? 1 : 0)];
+    linear_wgrad_stash8_group(s.stream, kg.tasks, kg.blocks, s.kept_nblocks);
   }
   if (s.red_nblocks)  // every layer's partials -> G, one launch (behind all of this pass's kernels)
     reduce_tasks_f32(c.forked ? fork_side(c) : s.stream, static_cast<const RedTask*>(static_ws ? s.red_tasks_static : s.red_tasks),
@@ -802,6 +807,66 @@ static ast_status build_wgrad_groups(Stage& s, char* static_ws, std::string& err
   return AST_OK;
 }
 
+void drop_kept_groups(Stage& s) {
+  for (Stage::WgGroup& kg : s.kept_groups) {
+    if (kg.tasks) (void)hipFree(kg.tasks);
+    if (kg.blocks) (void)hipFree(kg.blocks);
+  }
+  s.kept_groups.clear();
+  s.kept_nblocks = 0;
+}
+
+// The tables of the weight gradients from inputs kept in 8 bits, for every slot and workspace.
+static ast_status build_kept_groups(Stage& s, char* static_ws, std::string& err) {
+  bool any = false;
+  for (const Op& op : s.ops) any |= op.kept_grouped;
+  if (!any) return AST_OK;
+  s.kept_groups.assign(2 * s.slots.size(), Stage::WgGroup());
+  const size_t tb = stash8_group_task_bytes();
+  for (size_t k = 0; k < s.slots.size(); ++k)
+    for (int v = 0; v < (static_ws ? 2 : 1); ++v) {
+      char* const ws = v ? static_ws : s.ws;
+      std::vector<char> tasks;
+      std::vector<unsigned> blocks;
+      for (size_t j = s.ops.size(); j-- > 0;) {  // the order of the backward pass
+        const Op& op = s.ops[j];
+        if (!op.kept_grouped) continue;
+        const Act& I = s.acts[op.in];
+        char* const sc = ws + s.scratch_off + op.sc_off;
+        const bool mha = op.kind == OP_MHA;
+        const int out = mha ? 3 * op.cin : op.cout;
+        const char* dy = sc;  // the GELU-masked gradient lies in the scratch
+        if (mha) {
+          dy = sc + act_rows(I) * op.cin * sizeof(bf16_t);
+        } else if (op.act != 3 || op.gelu_bwd_fused) {
+          int id = op.out;
+          while (s.acts[id].grad_alias >= 0) id = s.acts[id].grad_alias;
+          dy = ws + s.acts[id].grad_off;
+        }
+        float* const GW = s.G + op.w_off;
+        float* const Gb = mha ? GW + (size_t)3 * op.cin * op.cin : op.has_bias ? s.G + op.b_off : nullptr;
+        const unsigned t = (unsigned)(tasks.size() / tb);
+        tasks.resize(tasks.size() + tb);
+        stash8_group_task(tasks.data() + t * tb, dy, s.slots[k] + I.slot8_off, act_rows(I), op.cin, out, GW, Gb);
+        for (int b = 0; b < stash8_group_blocks(op.cin, out); ++b) {
+          blocks.push_back(t);
+          blocks.push_back((unsigned)b);
+        }
+      }
+      Stage::WgGroup& kg = s.kept_groups[2 * k + v];
+      hipError_t e;
+      if ((e = hipMalloc(&kg.tasks, tasks.size())) != hipSuccess ||
+          (e = hipMalloc((void**)&kg.blocks, blocks.size() * sizeof(unsigned))) != hipSuccess ||
+          (e = hipMemcpy(kg.tasks, tasks.data(), tasks.size(), hipMemcpyHostToDevice)) != hipSuccess ||
+          (e = hipMemcpy(kg.blocks, blocks.data(), blocks.size() * sizeof(unsigned), hipMemcpyHostToDevice)) != hipSuccess) {
+        err = std::string("table of weight gradients from kept inputs: ") + hipGetErrorString(e);
+        return e == hipErrorOutOfMemory ? AST_ENOMEM : AST_EHIP;
+      }
+      s.kept_nblocks = (int)(blocks.size() / 2);
+    }
+  return AST_OK;
+}
+
 void drop_wgrad_groups(Stage& s) {
   for (Stage::WgGroup& wg : s.wg_groups) {
     if (wg.tasks) (void)hipFree(wg.tasks);
@@ -820,6 +885,7 @@ ast_status build_reduce_tasks(Stage& s, std::string& err) {
     (void)static_scratch_ptr(&static_ws, ignore);  // no static variant for this stage if this fails
   }
   s.static_ws = static_ws;
+  if (ast_status r = build_kept_groups(s, static_ws, err)) return r;
   if (const char* e = getenv("ASTEROID_BATCHED_REDUCE"))
     if (e[0] == '0') return AST_OK;  // per-layer reduction launches instead
   if (ast_status r = build_wgrad_groups(s, static_ws, err)) return r;

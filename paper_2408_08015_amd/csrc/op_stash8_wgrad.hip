@@ -65,15 +65,13 @@ __device__ __forceinline__ void sw_restore4(uint32_t w, float s, uint32_t& lo, u
 
 // EVEN: rows of dy start at 16-byte addresses
 template <int WM, int WN, int TM, int TN, bool EVEN>
-__global__ __launch_bounds__(64 * WM * WN, 2) void stash8_wgrad_kernel(const SwArgs g) {
+__device__ __forceinline__ void stash8_wgrad_body(const SwArgs& g, int bid) {  // bid: block of this product
   constexpr int BN = 32 * TM * WM, BC = 32 * TN * WN, NT = 64 * WM * WN;
   static_assert(16 * BN / 8 == NT && 16 * BC / 8 == NT, "a thread fills one chunk of each operand per quarter");
   constexpr int A_BYTES = SW_BK * BN * 2, STAGE = A_BYTES + SW_BK * BC * 2;
   extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave / WN, wn = wave % WN;
-  // neighbouring tiles on one XCD: they share their rows of dy, or the kept values, in its L2
-  int bid = (int)xcd_grouped(blockIdx.x, gridDim.x);
   const int tc = bid % g.tiles_c; bid /= g.tiles_c;
   const int tn = bid % g.tiles_n;
   const int split = bid / g.tiles_n;
@@ -259,6 +257,19 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void stash8_wgrad_kernel(const SwA
     }
 }
 
+template <int WM, int WN, int TM, int TN, bool EVEN>
+__global__ __launch_bounds__(64 * WM * WN, 2) void stash8_wgrad_kernel(const SwArgs g) {
+  // neighbouring tiles on one XCD: they share their rows of dy, or the kept values, in its L2
+  stash8_wgrad_body<WM, WN, TM, TN, EVEN>(g, (int)xcd_grouped(blockIdx.x, gridDim.x));
+}
+
+// Several products in one launch, none in shares: blocks holds (product, block of it).
+__global__ __launch_bounds__(256, 2) void stash8_wgrad_group_kernel(const SwArgs* __restrict__ tasks, const uint2* __restrict__ blocks) {
+  const uint2 b = blocks[xcd_grouped(blockIdx.x, gridDim.x)];
+  const SwArgs g = tasks[__builtin_amdgcn_readfirstlane(b.x)];
+  stash8_wgrad_body<2, 2, 2, 2, true>(g, (int)__builtin_amdgcn_readfirstlane(b.y));
+}
+
 // out (+)= sum over the splits, in their order, in 64 bits; the same for the bias
 __global__ __launch_bounds__(256) void stash8_wgrad_sum_kernel(const float* __restrict__ part, int64_t n, float* out,
                                                                const float* __restrict__ bias_part, int nb, float* bias_out,
@@ -312,6 +323,35 @@ void launch(hipStream_t st, const SwArgs& g, unsigned blocks, bool even) {
 }
 
 }  // namespace
+
+size_t stash8_group_task_bytes() { return sizeof(SwArgs); }
+
+int stash8_group_blocks(int64_t in, int64_t out) { return (int)(((out + 127) / 128) * ((in + 127) / 128)); }
+
+void stash8_group_task(void* task, const void* dy, const void* stash, int64_t rows, int64_t in, int64_t out, float* dw, float* db) {
+  SwArgs g = {};
+  g.dy = static_cast<const bf16_t*>(dy);
+  g.q = static_cast<const uint8_t*>(stash);
+  g.sc = stash8_scales(stash, rows, in);
+  g.out = dw;
+  g.bias_out = db;
+  g.rows = rows;
+  g.rows_per_split = (rows + SW_BK - 1) / SW_BK * SW_BK;
+  g.N = (int)out;
+  g.C = (int)in;
+  g.pitch = (int)stash8_pitch(in);
+  g.tiles_n = (int)((out + 127) / 128);
+  g.tiles_c = (int)((in + 127) / 128);
+  g.add = 1;
+  *static_cast<SwArgs*>(task) = g;
+}
+
+void linear_wgrad_stash8_group(hipStream_t st, const void* tasks_dev, const void* blocks_dev, int blocks) {
+  constexpr int lds = 2 * SW_BK * 2 * (128 + 128);
+  (void)hipFuncSetAttribute(reinterpret_cast<const void*>(stash8_wgrad_group_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  KLAUNCH(stash8_wgrad_group_kernel, dim3((unsigned)blocks), dim3(256), lds, st, static_cast<const SwArgs*>(tasks_dev),
+          static_cast<const uint2*>(blocks_dev));
+}
 
 size_t linear_wgrad_stash8_ws_bytes(int64_t rows, int64_t in, int64_t out) {
   const int s = wgrad_shape(rows, in, out).splits;

@@ -88,6 +88,12 @@ static size_t lay_out_passing(Stage& s) {
   return end;
 }
 
+size_t mha_qkv_wgrad_ws(const Op& op, size_t rows) {
+  if (op.kept_grouped) return 0;
+  return op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)rows, op.cin, 3 * op.cin)
+                  : linear_bf16_ws_bytes(rows, op.cin, 3 * op.cin, op.wg_splits[1]);
+}
+
 ast_status build_plan(Stage& s, std::string& err) {
   const ast_stage_cfg& cfg = s.cfg;
   const int B = cfg.B;
@@ -655,6 +661,24 @@ ast_status build_plan(Stage& s, std::string& err) {
     if (op.kind == OP_RES_ADD) s.acts[op.in].grad_alias = op.out;
   s.grad_bytes = goff;
 
+  // Weight gradients from inputs kept in 8 bits go into one launch at the end of a backward pass where their tiles of 128 x 128
+  // fill the chip and the upstream gradient does not lie in a buffer of the caller's; else each is a product of its own, in
+  // shares of its rows.  (Six encoder layers of 512, 4096 rows, 1056 tiles: a round of four passes 8.10 ms one by one, 7.08 so.)
+  {
+    int tiles = 0;
+    auto can = [&](const Op& op) {
+      if (op.kind == OP_MHA) return op.keep8;  // (its gradient lies in the scratch)
+      if (op.kind != OP_LINEAR || !op.keep8) return false;
+      if (op.act == 3 && !op.gelu_bwd_fused) return true;
+      int id = op.out;
+      while (s.acts[id].grad_alias >= 0) id = s.acts[id].grad_alias;
+      return id != 0 && (id != final_act || s.loss_tail);
+    };
+    for (const Op& op : s.ops)
+      if (can(op)) tiles += stash8_group_blocks(op.cin, op.kind == OP_MHA ? 3 * op.cin : op.cout);
+    for (Op& op : s.ops) op.kept_grouped = tiles >= 192 && can(op);
+  }
+
   auto lay_out_scratch = [&] {
     // Scratch: one private region per op (masked upstream gradients, reduction partials), so
     // that kernels of different ops may overlap on two streams without sharing a buffer.
@@ -684,7 +708,7 @@ ast_status build_plan(Stage& s, std::string& err) {
         case OP_LINEAR:
           if (s.bf16)
             need = align_up(s.acts[op.out].bytes, 256) +
-                   (op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)I.n * I.h * I.w, op.cin, op.cout)
+                   (op.kept_grouped ? 0 : op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)I.n * I.h * I.w, op.cin, op.cout)
                              : linear_bf16_ws_bytes((size_t)I.n * I.h * I.w, op.cin, op.cout, op.wg_splits[0]));
           break;
         case OP_EMBEDDING: need = embedding_bwd_ws_bytes((int64_t)I.n * I.h, op.cin, op.cout); break;
@@ -693,8 +717,7 @@ ast_status build_plan(Stage& s, std::string& err) {
           need = align_up((size_t)I.n * I.h * 4 * op.cin * 2, 256) +
                  align_up(mha_bf16_ws_bytes(I.n, I.h, op.cin, op.heads), 256) +
                  align_up(linear_bf16_ws_bytes((size_t)I.n * I.h, op.cin, op.cin, op.wg_splits[0]), 256) +
-                 align_up(op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)I.n * I.h, op.cin, 3 * op.cin)
-                                   : linear_bf16_ws_bytes((size_t)I.n * I.h, op.cin, 3 * op.cin, op.wg_splits[1]), 256) +
+                 align_up(mha_qkv_wgrad_ws(op, (size_t)I.n * I.h), 256) +
                  (op.qk_norm ? qk_norm_rope_bwd_ws_bytes((int64_t)I.n * I.h, 64) : 0);
           break;
         default: break;

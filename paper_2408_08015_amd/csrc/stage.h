@@ -72,6 +72,7 @@ struct Op {
   int heads = 0;
   bool keep8 = false;     // bf16 linear / MHA / GELU: the input is kept in 8 bits and the weight gradient (of MHA: of the qkv
                           // projection), or GELU's gradient, is formed from it
+  bool kept_grouped = false;  // ... as part of the one launch of such gradients at the end of the backward pass
   bool qk_norm = false;   // MHA: norm with gains and rotation of queries and keys
   int rotary = 0, interleaved = 0;
   double theta = 1.0;
@@ -173,6 +174,8 @@ struct Stage {
   struct WgGroup { void* tasks = nullptr; unsigned* blocks = nullptr; };  // blocks: product << 16 | block of it
   std::vector<WgGroup> wg_groups;
   int wg_nblocks = 0;
+  std::vector<WgGroup> kept_groups;  // the same for the gradients from inputs kept in 8 bits (blocks: pairs product, block of it)
+  int kept_nblocks = 0;
 
   // Second stream for the weight-gradient kernels, which no later kernel of the same
   // backward pass depends on (NULL: everything runs on `stream`).
@@ -206,6 +209,7 @@ struct Stage {
 
 // plan.cpp
 ast_status build_plan(Stage& s, std::string& err);
+size_t mha_qkv_wgrad_ws(const Op& op, size_t rows);  // bytes of an attention's scratch for the partials of that gradient
 // exec.cpp
 ast_status run_forward(Stage& s, int slot, const void* x, const int32_t* labels, void* y, float* loss,
                        std::string& err);
@@ -214,5 +218,6 @@ ast_status run_step(Stage& s, float lr, float mu, std::string& err);
 ast_status refresh_shadow(Stage& s, std::string& err);
 ast_status build_reduce_tasks(Stage& s, std::string& err);  // after the workspace is allocated
 void drop_wgrad_groups(Stage& s);
+void drop_kept_groups(Stage& s);
 
 }  // namespace ast

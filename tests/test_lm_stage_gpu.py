@@ -51,7 +51,8 @@ def check(cfg, inp=None):
 
 
 @pytest.mark.parametrize("keep8", [False, True])
-@pytest.mark.parametrize("kw", [dict(), dict(B=1, M=2, S=32, d=512, heads=8, ffn=2048, nlayers=1, rows=5000)])
+@pytest.mark.parametrize("kw", [dict(), dict(B=1, M=2, S=32, d=512, heads=8, ffn=2048, nlayers=1, rows=5000),
+                                dict(B=3, M=2, S=32, d=512, heads=8, ffn=2048, nlayers=2, rows=500)])   # one launch for all kept inputs
 def test_language_model_stage(A, kw, keep8):
     check(small(keep8=keep8, **kw))
 
@@ -81,9 +82,10 @@ def test_layers_with_kept_inputs(A, layers):
     check(encoder(layers(), B=3, M=1, S=17))
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(B=1, S=32, d=512, heads=8, ffn=2048, rows=100)])
 @pytest.mark.parametrize("K", [1, 2, 3])
-def test_bit_identical_however_it_runs(A, K):
-    cfg = small()
+def test_bit_identical_however_it_runs(A, K, kw):
+    cfg = small(**kw)
     inp = gen.make_inputs(cfg, randomize_affine=True)
     ref, _, mem = harness.run_hip(cfg, inp, K=1, rounds=2)
     assert mem[3] <= 32 << 20
