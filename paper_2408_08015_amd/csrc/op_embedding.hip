@@ -1,8 +1,12 @@
 // Token embedding: y[t] = scale * W[ids[t]] and its gradient dW[v] = scale * sum of dy[t] over the tokens t of id v.
 //
 // Both move bytes and compute next to nothing.  The gradient orders the tokens by id first (stably, ids outside the table
-// last), so that the tokens of a row lie next to each other and one wavefront adds them in their order: no atomics, equal
-// calls give equal bits.
+// last), so that the tokens of a row lie next to each other and are added in their order: no atomics on values, equal calls
+// give equal bits.  A wavefront takes a fixed number of sorted tokens, so an id that fills half of the micro-batch costs no
+// more than many different ones; what crosses the shares is joined by a second launch.
+// Measured: lookup of 65521 rows of 1024 bf16 values 46 us (3.6 TB/s of what has to move), of 1021 56 to 61; gradient of 4096
+// tokens of 512 into 32768 rows 21 us (67 MB of zeros alone take 10), of 65536 of 1024 into 131072 rows 187 us (537 MB of zeros 78
+// to 95, the sums 78).
 #include <algorithm>
 #include <type_traits>
 
@@ -470,9 +474,13 @@ void embedding_fwd(hipStream_t st, const int32_t* ids, int64_t tokens, const voi
 
 namespace {
 
-constexpr int64_t RANK_MOST = 16384;  // tokens that are placed by counting
+// Tokens that are placed by counting (it grows with their square, the passes hardly; the whole gradient of rows of 64, us, counting /
+// passes: 4096 tokens 19 / 33, 8192 28 / 37, 16384 44 / 42, 32768 122 / 42).
+constexpr int64_t RANK_MOST = 16384;
 
-int chunk_of(int64_t tokens) {  // tokens of a wavefront: the chip filled, and no more than 8192 partials
+// Tokens of a wavefront: the chip filled, and no more than 8192 partials.  (65536 tokens of 1024: chunks of 32 187 us, of 16 192, of
+// 8 207; 4096 tokens of 512: of 8 21.4, of 4 21.9.)
+int chunk_of(int64_t tokens) {
   int c = 8;
   while (c < 32 && tokens / c >= 2048) c *= 2;
   while ((tokens + c - 1) / c > 8192) c *= 2;
