@@ -37,6 +37,12 @@ static size_t conv_shadow_elems(int k, int Cin, int Cout) {
 
 static bool flag_ok(int v) { return v == 0 || v == 1; }
 
+// Activation `a` is kept in 8 bits: the tensor itself, where it goes by the name that a shortcut branch has for its input.
+static void keep8(Stage& s, int a) {
+  while (s.acts[a].data_alias >= 0) a = s.acts[a].data_alias;
+  s.acts[a].kept8 = true;
+}
+
 // Does the backward pass read activation `a` in its bf16 form?
 static bool backward_reads(const Stage& s, int a) {
   for (const Op& op : s.ops) {
@@ -210,7 +216,7 @@ ast_status build_plan(Stage& s, std::string& err) {
         if (op.act == 3) {
           if (!flag_ok(L.p[0])) { err = fmt("layer %d: GELU: p[0] must be 0 or 1", i); return AST_EINVAL; }
           op.keep8 = L.p[0] != 0;
-          if (op.keep8) s.acts[cur].kept8 = true;
+          if (op.keep8) keep8(s, cur);
         }
         if (s.bf16 && op.act > 3) { err = fmt("layer %d: swish / sigmoid are fp32-only", i); return AST_EUNSUPPORTED; }
         op.out = cur = new_act(s, A.n, A.c, A.h, A.w, A.rank, i, es);
@@ -311,7 +317,7 @@ ast_status build_plan(Stage& s, std::string& err) {
         if (L.p[3] && !s.bf16) { err = fmt("layer %d: inputs are kept in 8 bits in bf16 stages only", i); return AST_EUNSUPPORTED; }
         op.kind = OP_LINEAR; op.cin = Cin; op.cout = Cout; op.has_bias = hb ? 1 : 0;
         op.keep8 = L.p[3] != 0;
-        if (op.keep8) s.acts[cur].kept8 = true;
+        if (op.keep8) keep8(s, cur);
         op.w_off = poff; poff += (size_t)Cout * Cin;
         if (hb) { op.b_off = poff; poff += Cout; }
         if (s.bf16) {
@@ -373,7 +379,7 @@ ast_status build_plan(Stage& s, std::string& err) {
         if (!flag_ok(L.p[2]) || !flag_ok(L.p[5]) || !flag_ok(L.p[6])) { err = fmt("layer %d: MHA: p[2], p[5], p[6] must be 0 or 1", i); return AST_EINVAL; }
         op.kind = OP_MHA; op.cin = op.cout = D; op.heads = H; op.has_bias = 1;
         op.keep8 = L.p[6] != 0;
-        if (op.keep8) s.acts[cur].kept8 = true;
+        if (op.keep8) keep8(s, cur);
         op.qk_norm = L.p[2] != 0;
         if (op.qk_norm) {
           op.rotary = L.p[3]; op.theta = L.p[4]; op.interleaved = L.p[5]; op.eps = L.eps;
@@ -643,7 +649,10 @@ ast_status build_plan(Stage& s, std::string& err) {
     off = align_up(off + s.acts[a].bytes, 256);
   }
   for (Act& a : s.acts)  // a shortcut branch's input is the tensor RES_BEGIN remembered
-    if (a.data_alias >= 0) a.slot_off = s.acts[a.data_alias].slot_off;
+    if (a.data_alias >= 0) {
+      a.slot_off = s.acts[a.data_alias].slot_off;
+      a.slot8_off = s.acts[a.data_alias].slot8_off;
+    }
   for (Op& op : s.ops) op.aux_off += off;
   s.slot_bytes = align_up(off + aux, 256);
 

@@ -61,6 +61,16 @@ def test_kept_activations_leave_the_stash():
     assert deep[2] - m1[2] == 4 * (m1[2] - one[2])
 
 
+def test_a_shortcut_branch_keeps_the_blocks_input():
+    """The input of a shortcut branch is the block's: its 8-bit form has room of its own, once."""
+    L = lambda a, b: [dict(C.linear(64, 64), keep8=0), C.simple("res_begin"), dict(C.linear(64, 64), keep8=a), C.simple("res_swap"),
+                      dict(C.linear(64, 64), keep8=b), C.simple("res_add")]
+    cfg = small()
+    act = [plan(cfg, layers=L(a, b), in_shape=(32, 64), grad=True)[2] for a, b in ((0, 0), (0, 1), (1, 0), (1, 1))]
+    room = 2 * 32 * 64 * 33 // 32
+    assert act[1] == act[2] == act[3] and room <= act[1] - act[0] <= room + 256
+
+
 def test_the_profiler_cuts_behind_the_embedding():
     from paper_2408_08015_amd import profiler
     cfg = small(nlayers=1)

@@ -74,6 +74,9 @@ def test_attention_variants(A, mha):
     lambda: [dict(kind="layernorm", d=128, eps=1e-5), dict(C.simple("gelu"), keep8=1), C.linear(128, 64)],   # GELU of its own
     lambda: [C.linear(128, 64), C.simple("relu"), dict(C.linear(64, 64), keep8=1)],       # ReLU's backward needs the input too
     lambda: [C.simple("res_begin"), dict(C.linear(128, 128), keep8=1), C.simple("res_swap"), C.linear(128, 128), C.simple("res_add")],
+    lambda: [C.simple("res_begin"), C.linear(128, 128), C.simple("res_swap"), dict(C.linear(128, 128), keep8=1), C.simple("res_add")],
+    lambda: [C.linear(128, 96), C.simple("res_begin"), dict(C.linear(96, 96), keep8=1), C.simple("res_swap"),
+             dict(C.linear(96, 96), keep8=1), C.simple("res_add")],      # both branches keep the block's input
     lambda: [C.simple("res_begin"), dict(C.linear(128, 128), keep8=1), C.simple("gelu"), dict(C.linear(128, 128), keep8=1), C.simple("res_add")],
 ])
 def test_layers_with_kept_inputs(A, layers):
