@@ -122,7 +122,9 @@ def embedding_forward(ids, table, scale=1.0, dtype=None, out=None):
     T, (V, D) = ids.shape[0], table.shape
     if out is None:
         out = torch.empty((T, D), dtype=dtype or table.dtype, device=table.device)
-    _is(out, "out", (dtype,) if dtype else tuple(_DT), (T, D))
+    _is(out, "out", tuple(_DT), (T, D))
+    if dtype not in (None, out.dtype):
+        raise ValueError("out is %s, not %s" % (out.dtype, dtype))
     lib = _lib()
     _call(_device(table, ids, out), lib.asteroid_embedding_forward, ids.data_ptr(), T, table.data_ptr(), _DT[table.dtype],
           V, D, scale, out.data_ptr(), _DT[out.dtype])

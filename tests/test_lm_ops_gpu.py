@@ -242,6 +242,21 @@ def test_qk_norm_rope_tokens_inside_heads(ops):
     assert torch.equal(y[0], base[0]) and torch.equal(y[1], base[1])
 
 
+def test_qk_norm_rope_broadcast_gradients_and_one_head_for_all(ops):
+    """Inputs whose tokens or heads lie on top of each other (strides of zero)."""
+    r = rng(12)
+    T, H, d = 70, 4, 64
+    x = dev(r.normal(size=(T, 1, d)), "bf16")[0]
+    one = dev(r.normal(size=(1, 1, d)), "bf16")[0]
+    g = [dev(1 + 0.1 * r.normal(size=d))[0] for _ in range(2)]
+    for q, dy in ((x.expand(T, H, d), one.expand(T, H, d)), (x.expand(T, H, d), torch.ones_like(one).expand(T, H, d))):
+        a = ops.qk_norm_rope_backward(dy, dy, q, q, g[0], g[1], period=T)
+        b = ops.qk_norm_rope_backward(dy.contiguous(), dy.contiguous(), q.contiguous(), q.contiguous(), g[0], g[1], period=T)
+        assert all(torch.equal(m, n) for m, n in zip(a, b))
+        assert torch.equal(ops.qk_norm_rope_forward(q, q, g[0], g[1], period=T)[0],
+                           ops.qk_norm_rope_forward(q.contiguous(), q, g[0], g[1], period=T)[0])
+
+
 # ------------------------------------------------------------------------------------------------ 8-bit activations
 
 SHAPES = [(1, 1), (1, 32), (3, 31), (5, 33), (2, 64), (7, 1500), (130, 40), (257, 129), (1000, 512), (63, 2048), (4096, 24), (1, 4099)]
@@ -335,6 +350,20 @@ def test_linear_wgrad_stash8(ops, rows, cin, cout):
     inside(acc[1], ob + wb, bb + 1.01 * u * (abs(ob) + abs(g).sum(0)))
     only, none = ops.linear_wgrad_stash8(dy, s, bias=False)
     assert none is None and torch.equal(only, dw)
+
+
+def test_linear_wgrad_stash8_at_the_ends_of_the_range(ops):
+    """Inputs of the largest and smallest sizes that are kept, dy small enough that the products are finite."""
+    r = rng(13)
+    rows, cin, cout = 90, 96, 40
+    x = r.normal(size=(rows, cin))
+    x[:, :32] = np.sign(x[:, :32]) * 3.38e38
+    x[:, 32:64] *= 2.0 ** -120
+    xt, f = dev(x.astype(np.float32), "bf16")
+    dy, g = dev(r.normal(size=(rows, cout)) * 2.0 ** -10, "bf16")
+    xx = O.stash8(f)[0]
+    dw, db = ops.linear_wgrad_stash8(dy, ops.stash8_pack(xt))
+    inside(dw, g.T @ xx, (abs(g).T @ abs(xx)) * (2 * rows + 4) * u + 2.0 ** -149 * rows)
 
 
 def test_linear_wgrad_stash8_keeps_what_is_not_finite_in_its_column(ops):

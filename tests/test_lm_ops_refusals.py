@@ -130,6 +130,10 @@ def test_tensors_are_checked():
     with pytest.raises(ValueError, match="shape"):
         ops.embedding_forward(f(3, dtype=i), f(4, 8), out=f(3, 7))
     with pytest.raises(ValueError, match="float32 or torch.bfloat16"):
+        ops.embedding_forward(f(3, dtype=i), f(4, 8), dtype=torch.float16)
+    with pytest.raises(ValueError, match="not torch.bfloat16"):
+        ops.embedding_forward(f(3, dtype=i), f(4, 8), dtype=torch.bfloat16, out=f(3, 8))
+    with pytest.raises(ValueError, match="float32 or torch.bfloat16"):
         ops.embedding_backward(f(3, dtype=i), f(3, 8, dtype=torch.float16), 4)
     with pytest.raises(ValueError, match="shape"):
         ops.embedding_backward(f(3, dtype=i), f(2, 8), 4)
