@@ -5,8 +5,8 @@
 // give equal bits.  A wavefront takes a fixed number of sorted tokens, so an id that fills half of the micro-batch costs no
 // more than many different ones; what crosses the shares is joined by a second launch.
 // Measured: lookup of 65521 rows of 1024 bf16 values 46 us (3.6 TB/s of what has to move), of 1021 56 to 61; gradient of 4096
-// tokens of 512 into 32768 rows 21 us (67 MB of zeros alone take 10), of 65536 of 1024 into 131072 rows 187 us (537 MB of zeros 78
-// to 95, the sums 78).
+// tokens of 512 into 32768 rows 21 us (67 MB of zeros alone take 10), of 65536 of 1024 into 131072 rows 183 us (537 MB of zeros 78
+// to 95, the sums 76).
 #include <algorithm>
 #include <type_traits>
 
@@ -297,7 +297,7 @@ constexpr int SUM_COLS = 512;
 enum : int { COLS_EVEN = 0, COLS_ANY = 1, COLS_NARROW = 2 };
 template <int COLS>
 __device__ __forceinline__ int first_col(int width, int lane) {
-  const int c = blockIdx.y * SUM_COLS + lane * 8;
+  const int c = blockIdx.x * SUM_COLS + lane * 8;
   return COLS == COLS_ANY && c < width ? min(c, width - 8) : c;
 }
 template <int COLS>
@@ -325,7 +325,7 @@ template <typename T, int COLS>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const SumArgs g, const T* __restrict__ dy) {
   constexpr int B = COLS == COLS_EVEN ? 8 : 4;  // tokens whose rows are requested at a time
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t chunk_id = (int64_t)blockIdx.x * 4 + wave;
+  const int64_t chunk_id = (int64_t)blockIdx.y * 4 + wave;
   const int64_t lo = chunk_id * g.chunk, hi = min(lo + g.chunk, g.tokens);
   if (lo >= hi) return;
   const int c = first_col<COLS>(g.width, lane);
@@ -384,7 +384,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const SumArgs g, con
 template <int COLS>
 __global__ __launch_bounds__(512, 6) void embedding_join_kernel(const SumArgs g) {
   __shared__ double sh[8][SUM_COLS];
-  const int64_t c0 = blockIdx.x;
+  const int64_t c0 = blockIdx.y;
   const int64_t lo = c0 * g.chunk, hi = lo + g.chunk;  // (the last chunk has no block)
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t chunks = (g.tokens + g.chunk - 1) / g.chunk;
@@ -479,7 +479,7 @@ namespace {
 constexpr int64_t RANK_MOST = 16384;
 
 // Tokens of a wavefront: the chip filled, and no more than 8192 partials.  (65536 tokens of 1024: chunks of 32 187 us, of 16 192, of
-// 8 207; 4096 tokens of 512: of 8 21.4, of 4 21.9.)
+// 8 207, each before the shares of a row were put side by side; 4096 tokens of 512: of 8 21.4, of 4 21.9.)
 int chunk_of(int64_t tokens) {
   int c = 8;
   while (c < 32 && tokens / c >= 2048) c *= 2;
@@ -593,13 +593,15 @@ void embedding_bwd(hipStream_t st, const int32_t* ids, int64_t tokens, const voi
   const int64_t chunks = chunks_of(tokens);
   g.part = reinterpret_cast<float*>(take((size_t)chunks * 2 * width * 4));
   const unsigned cols_blocks = (unsigned)((width + SUM_COLS - 1) / SUM_COLS);
-  const dim3 grid((unsigned)((chunks + 3) / 4), cols_blocks);
+  // (The shares of a row's columns in neighbouring blocks, so that its memory is read at one time: 65536 tokens of 1024 183 us; a share
+  // of all rows after another 187.  chunks_of() stays far below the 65535 blocks of this direction.)
+  const dim3 grid(cols_blocks, (unsigned)((chunks + 3) / 4));
   const bool even = width % 8 == 0 && reinterpret_cast<uintptr_t>(dy) % 16 == 0 && reinterpret_cast<uintptr_t>(dtable) % 16 == 0;
   auto go = [&](auto cols) {
     constexpr int C = decltype(cols)::value;
     if (dy_bf16) KLAUNCH_NAMED("embedding_sum_kernel", (embedding_sum_kernel<bf16_t, C>), grid, dim3(256), 0, st, g, static_cast<const bf16_t*>(dy));
     else KLAUNCH_NAMED("embedding_sum_kernel", (embedding_sum_kernel<float, C>), grid, dim3(256), 0, st, g, static_cast<const float*>(dy));
-    if (chunks > 1) KLAUNCH_NAMED("embedding_join_kernel", (embedding_join_kernel<C>), dim3((unsigned)(chunks - 1), cols_blocks), dim3(512), 0, st, g);
+    if (chunks > 1) KLAUNCH_NAMED("embedding_join_kernel", (embedding_join_kernel<C>), dim3(cols_blocks, (unsigned)(chunks - 1)), dim3(512), 0, st, g);
   };
   if (even) go(std::integral_constant<int, COLS_EVEN>());
   else if (width >= 8 && (width % SUM_COLS == 0 || width % SUM_COLS >= 8)) go(std::integral_constant<int, COLS_ANY>());
