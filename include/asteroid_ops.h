@@ -40,7 +40,7 @@ extern "C" {
 /* ------------------------------------------------------------------ token embedding
  *   y[t][:] = scale * table[ids[t]][:]          0 where ids[t] lies outside [0, rows) (padding)
  * ids_dev int32[tokens], table_dev [rows][width], y_dev [tokens][width].
- * tokens >= 0 (0: nothing is done), rows in [1, 2^31 - 2], tokens < 2^31, width in [1, 2^20]. */
+ * tokens >= 0 (0: nothing is done), rows in [1, 2^31 - 2], tokens < 2^31, width in [1, 2^20], scale finite. */
 ast_status asteroid_embedding_forward(const int32_t* ids_dev, int64_t tokens, const void* table_dev,
                                       int32_t table_dtype, int64_t rows, int64_t width, float scale,
                                       void* y_dev, int32_t y_dtype, void* hip_stream);

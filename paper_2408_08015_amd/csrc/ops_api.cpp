@@ -87,6 +87,7 @@ ast_status asteroid_embedding_forward(const int32_t* ids_dev, int64_t tokens, co
   const char* const fn = "embedding_forward";
   if (!dtype_ok(table_dtype) || !dtype_ok(y_dtype)) return fail(fn, "unknown dtype");
   if (const char* e = embedding_sizes(tokens, rows, width)) return fail(fn, e);
+  if (!std::isfinite(scale)) return fail(fn, "scale must be finite");
   if (tokens == 0) return AST_OK;
   if (!ids_dev || !table_dev || !y_dev) return fail(fn, "NULL argument");
   if (!aligned(ids_dev, 4) || !aligned(table_dev, esize(table_dtype)) || !aligned(y_dev, esize(y_dtype)))
@@ -110,6 +111,7 @@ ast_status asteroid_embedding_backward(const int32_t* ids_dev, int64_t tokens, c
   const char* const fn = "embedding_backward";
   if (!dtype_ok(dy_dtype)) return fail(fn, "unknown dtype");
   if (const char* e = embedding_sizes(tokens, rows, width)) return fail(fn, e);
+  if (!std::isfinite(scale)) return fail(fn, "scale must be finite");
   if (!dtable_dev || !aligned(dtable_dev, 4)) return fail(fn, "dtable_dev must be non-NULL and 4-byte aligned");
   if (tokens > 0) {
     if (!ids_dev || !dy_dev) return fail(fn, "NULL argument");

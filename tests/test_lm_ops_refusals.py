@@ -32,6 +32,9 @@ def test_embedding_refusals(lib):
     n = C.c_size_t()
     refused(lib, "embedding_backward_workspace", 8, 100, 16, None)
     refused(lib, "embedding_backward_workspace", 8, 0, 16, C.byref(n))
+    for scale in (float("inf"), float("-inf"), float("nan")):   # (0 times it would not be 0 for ids outside the table)
+        refused(lib, "embedding_forward", P, 8, P, 0, 100, 16, scale, P, 0, None)
+        refused(lib, "embedding_backward", P, 8, P, 0, 100, 16, scale, 0, P, P, 1 << 30, None)
     assert lib.asteroid_embedding_backward_workspace(8, 100, 16, C.byref(n)) == 0
     ok = [P, 8, P, 0, 100, 16, 1.0, 0, P, P, n.value, None]
     for at, bad in ((0, None), (1, -1), (2, None), (2, P + 2), (3, 7), (4, 0), (5, 0), (8, None), (8, P + 2), (9, None), (9, P + 4), (10, n.value - 1)):
