@@ -425,3 +425,87 @@ def test_operators_on_another_stream_and_in_a_replayed_graph(ops):
         torch.cuda.synchronize()
         for _, res in graphs:
             assert all(torch.equal(a, b) for a, b in zip(want, res)), step
+
+
+# ------------------------------------------------------------------------------------------------ more than 2^31 values
+
+def at_the_ends(rows, shape, seed, n=500):
+    """bf16 zeros [rows, *shape] with n random rows at each end."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    t = torch.zeros(rows, *shape, device="cuda", dtype=torch.bfloat16)
+    for part in (t[:n], t[-n:]):
+        part.copy_(torch.randn(part.shape, generator=g, device="cuda"))
+    return t
+
+
+def test_embedding_of_more_than_2_31_values(ops):
+    V, D = (1 << 21) + 5, 1032
+    table = at_the_ends(V, (D,), 1)
+    ids = torch.tensor([V - 1, 0, V, 1 << 20, V - 2, -1, V - 1], device="cuda", dtype=torch.int32)
+    want = table[ids.long().clamp(0, V - 1)]
+    want[[2, 5]] = 0
+    assert torch.equal(ops.embedding_forward(ids, table), want)
+    dy = table[-len(ids):].contiguous()
+    del table
+    out = ops.embedding_backward(ids, dy, V, out=torch.full((V, D), float("nan"), device="cuda"))
+    f = dy.float()
+    assert torch.equal(out[V - 1], f[0] + f[6]) and torch.equal(out[0], f[1]) and torch.equal(out[1 << 20], f[3])
+    assert torch.equal(out[V - 2], f[4])
+    out[[0, 1 << 20, V - 2, V - 1]] = 0
+    assert not out.any()
+    del out
+    # as many tokens, nearly all of one id (a run through thousands of chunks): small whole numbers, so the sums are exact
+    dy = torch.ones(V, D, device="cuda", dtype=torch.bfloat16)
+    dy[-1], dy[-2] = 5, 7
+    ids = torch.full((V,), 3, device="cuda", dtype=torch.int32)
+    ids[-1], ids[0] = 7, -1
+    got = ops.embedding_backward(ids, dy, 9)
+    assert got[7].eq(5).all() and got[3].eq(V - 3 + 7).all() and got[[0, 1, 2, 4, 5, 6, 8]].eq(0).all()
+    y = ops.embedding_forward(ids, got.bfloat16())
+    assert y[-1].eq(5).all() and y[0].eq(0).all() and torch.equal(y[-2], got[3].bfloat16())
+
+
+def test_qk_norm_rope_of_more_than_2_31_values(ops):
+    T, H, d, n = (1 << 20) + 3, 16, 128, 500
+    q, k = at_the_ends(T, (H, d), 2), at_the_ends(T, (1, d), 3)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    gq, gk = 1 + 0.1 * torch.randn(2, d, generator=g, device="cuda")
+    pos = torch.arange(T, device="cuda", dtype=torch.int32) * 3
+    yq, yk = ops.qk_norm_rope_forward(q, k, gq, gk, positions=pos)
+    ends = (slice(0, n), slice(T - n, T))
+    for e in ends:
+        a, b = ops.qk_norm_rope_forward(q[e], k[e], gq, gk, positions=pos[e])
+        assert torch.equal(a, yq[e]) and torch.equal(b, yk[e])
+    assert not yq[n:-n].any() and not yk[n:-n].any()
+    dq, dk, dgq, dgk = ops.qk_norm_rope_backward(yq, yk, q, k, gq, gk, positions=pos, out=(yq.clone(), yk.clone()))
+    sums = [0, 0]
+    for e in ends:
+        a, b, ga, gb = ops.qk_norm_rope_backward(yq[e], yk[e], q[e], k[e], gq, gk, positions=pos[e])
+        assert torch.equal(a, dq[e]) and torch.equal(b, dk[e])
+        sums = [sums[0] + ga.double(), sums[1] + gb.double()]
+    # Both runs add the same terms du n in different orders, 2 n H of a place, u each.  dy is the result, so |du| is at most
+    # the largest gain times the norm of n's pair (1 + 2^-8 for its rounding): the terms' magnitudes add up to at most that
+    # gain times the pair's sum of n^2, which the gradients of the pair, sums of gain n^2 up to 2^-7 of it, give.
+    for got, want, gain, heads in ((dgq, sums[0], gq, H), (dgk, sums[1], gk, 1)):
+        terms = 1.05 * (want + want.roll(d // 2)) * gain.max() / gain.min()
+        assert (want > 0).all() and ((got - want).abs() <= 2 * (2 * n * heads + 4) * u * terms).all()
+
+
+def test_kept_activations_of_more_than_2_31_values(ops):
+    rows, cin, cout, n = (1 << 21) + 67, 1032, 1040, 500
+    x, dy = at_the_ends(rows, (cin,), 5), at_the_ends(rows, (cin,), 6)
+    s = ops.stash8_pack(x)
+    back = ops.stash8_unpack(s)
+    dz = ops.gelu_backward_stash8(dy, s)
+    assert not back[n:-n].any() and not dz[n:-n].any()
+    for e in (slice(0, n), slice(rows - n, rows)):
+        part = ops.stash8_pack(x[e])
+        assert torch.equal(ops.stash8_unpack(part), back[e])
+        assert torch.equal(ops.gelu_backward_stash8(dy[e], part), dz[e])
+    del x, dy, dz
+    dy = at_the_ends(rows, (cout,), 7)
+    dw, db = ops.linear_wgrad_stash8(dy, s)
+    a, b = (torch.cat([t[:n], t[-n:]]).double().cpu() for t in (dy, back))
+    # 2 n terms that are not zero, each sum of them as in test_linear_wgrad_stash8
+    inside(dw, (a.t() @ b).numpy(), (a.abs().t() @ b.abs()).numpy() * (4 * n + 4) * u)
+    inside(db, a.sum(0).numpy(), a.abs().sum(0).numpy() * (2 * n + 4) * u)
