@@ -291,9 +291,8 @@ struct SumArgs {
 constexpr int SUM_COLS = 512;
 
 // How the columns are read and written: eight at 16-byte addresses; eight at any address, where the last lane of a row takes its
-// last eight and so some of its neighbour's (both write the same values; the neighbour is a lane of the same wavefront, whose
-// reads of what is added to come before its writes); or what there is, of rows of fewer than eight and of those whose last
-// SUM_COLS columns are fewer than eight.
+// last eight and so some of its neighbour's (what is written comes out the same from both; what is added to is written by its
+// own lane alone); or what there is, of rows of fewer than eight and of those whose last SUM_COLS columns are fewer than eight.
 enum : int { COLS_EVEN = 0, COLS_ANY = 1, COLS_NARROW = 2 };
 template <int COLS>
 __device__ __forceinline__ int first_col(int width, int lane) {
@@ -314,6 +313,13 @@ __device__ __forceinline__ void put_row(const SumArgs& g, uint32_t k, int c, con
     else load8(p, f);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = fmaf(v[i], g.scale, f[i]);
+    const int over = blockIdx.x * SUM_COLS + (threadIdx.x & 63) * 8 - c;  // leading ones that are the neighbour's
+    if (COLS == COLS_ANY && over > 0) {
+#pragma unroll
+      for (int i = 1; i < 8; ++i)
+        if (i >= over) p[i] = f[i];
+      return;
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = v[i] * g.scale;

@@ -110,6 +110,24 @@ def test_embedding_rows_that_end_just_behind_a_share_of_the_columns(ops, D):
         inside(acc, old + want, bound + u * 1.001 * (abs(old) + terms))
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("D", [9, 15, 63, 127, 519, 526, 1021, 1535])
+def test_embedding_adds_a_tokens_gradient_to_every_column_once(ops, D, dt):
+    """Rows that do not end with a lane's eight columns, every row of the table inside a chunk, at a chunk's end and across
+    chunks; small whole numbers, so the sums are exact."""
+    r = rng(14, D)
+    for T, V in ((700, 311), (3000, 40), (20000, 3001)):
+        ids = r.integers(0, V, T)
+        dy = r.integers(-4, 5, (T, D))
+        old = r.integers(-100, 101, (V, D))
+        want = old.copy()
+        np.add.at(want, ids, 2 * dy)
+        got = dev(old.astype(np.float32))[0]
+        for n in range(2):
+            ops.embedding_backward(dev(ids.astype(np.int32))[0], dev(dy.astype(np.float32), dt)[0], V, scale=2.0, out=got, accumulate=True)
+            assert np.array_equal(host(got), old + (n + 1) * (want - old)), (T, V, n)
+
+
 def test_embedding_of_no_tokens(ops):
     ids = torch.zeros(0, dtype=torch.int32, device="cuda")
     assert ops.embedding_forward(ids, torch.ones(3, 4, device="cuda")).shape == (0, 4)
