@@ -195,6 +195,13 @@ __global__ __launch_bounds__(256) void embedding_count_kernel(const RadixArgs a,
   for (int b = threadIdx.x; b < bins; b += 256) a.count[(size_t)blockIdx.x * bins + b] = bin[b];
 }
 
+// LDS accesses of the wavefront's lanes in front of it are made before those behind it (no instruction: the hardware keeps a
+// wavefront's LDS accesses in order, the compiler only what one lane can see)
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 __global__ __launch_bounds__(256) void embedding_place_kernel(const RadixArgs a, ZeroShare z) {
   if (blockIdx.x >= a.tiles) {
     zero_share(z, blockIdx.x - a.tiles, gridDim.x - a.tiles);
@@ -254,11 +261,10 @@ __global__ __launch_bounds__(256) void embedding_place_kernel(const RadixArgs a,
         same &= (d >> b) & 1 ? bit : ~bit;
       }
       const uint64_t below = same & ((1ull << lane) - 1);
-      at[r] = 0;
-      if (on) {
-        at[r] = seen[wave][d] + (uint32_t)__popcll(below);
-        if (below == 0) seen[wave][d] += (uint32_t)__popcll(same);  // (behind every lane's read: a wavefront's LDS accesses are in order)
-      }
+      at[r] = on ? seen[wave][d] + (uint32_t)__popcll(below) : 0;
+      wave_order();
+      if (on && below == 0) seen[wave][d] = at[r] + (uint32_t)__popcll(same);  // one lane a digit, behind every lane's read
+      wave_order();
     }
     __syncthreads();
 #pragma unroll

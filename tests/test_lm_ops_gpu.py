@@ -128,6 +128,22 @@ def test_embedding_adds_a_tokens_gradient_to_every_column_once(ops, D, dt):
             assert np.array_equal(host(got), old + (n + 1) * (want - old)), (T, V, n)
 
 
+@pytest.mark.parametrize("T,step", [(64, 1), (4096, 1), (16384, 3), (20480, 1), (32768, 40), (65536, 100), (262144, 1)])
+@pytest.mark.parametrize("D", [3, 8, 13])
+def test_embedding_adds_the_tokens_of_an_id_in_their_order(ops, T, step, D):
+    """Every id four times, so that no run of sorted tokens crosses a chunk: the fp32 sums from the first token to the last, bit
+    for bit, which needs an order that is stable among equal ids."""
+    r = rng(15, T, D)
+    ids = r.permutation(np.repeat(np.arange(T // 4) * step, 4))
+    dy = (r.normal(size=(T, D)) * np.exp(4 * r.normal(size=(T, 1)))).astype(np.float32)
+    V = T // 4 * step
+    got = ops.embedding_backward(dev(ids.astype(np.int32))[0], dev(dy)[0], V).cpu().numpy()
+    a = dy[np.argsort(ids, kind="stable")].reshape(T // 4, 4, D)
+    want = np.zeros((V, D), np.float32)
+    want[::step] = ((a[:, 0] + a[:, 1]) + a[:, 2]) + a[:, 3]
+    assert np.array_equal(got, want)
+
+
 def test_embedding_of_no_tokens(ops):
     ids = torch.zeros(0, dtype=torch.int32, device="cuda")
     assert ops.embedding_forward(ids, torch.ones(3, 4, device="cuda")).shape == (0, 4)
