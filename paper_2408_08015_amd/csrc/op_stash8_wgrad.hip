@@ -192,7 +192,9 @@ __device__ __forceinline__ void stash8_wgrad_body(const SwArgs& g, int bid) {  /
     for (int j = 0; j < TN; ++j) fb[ks & 1][j] = sw_frag<BC>(smem, stage + bo[j] + ks * 16 * BC * 2);
   };
   // every LDS access of the wavefront has been made; loads from memory stay in flight (__syncthreads() would wait for them)
+  // (the empty statements keep the compiler from moving accesses across the wait or the barrier, which it knows of neither)
   auto barrier = [&]() __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0xc07f);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
