@@ -298,8 +298,11 @@ __global__ __launch_bounds__(256) void stash8_wgrad_sum_kernel(const float* __re
 // Tile and shares of the rows: the cheapest by a model in us of what was measured - 64 rows of a 256 x 256 tile take 1.85, of a
 // 128 x 128 tile 0.85 (one block a compute unit), a launch's ends 8 and 6, and shares write and read partials of 4 bytes
 // (6 TB/s) and cost a second launch, 5.  2048 -> 512 of 4096 rows in small tiles and 4 shares 28 us, in big ones 42 by the model;
-// 4096 -> 4096 of 16384 rows in big tiles 472 us, in small ones 870.
-struct WgradShape { bool big; int64_t tiles_n, tiles_c; int splits; };
+// 4096 -> 4096 of 16384 rows in big tiles 472 us, in small ones 870.  A round pays its rows by the part of a stage, and nearly a
+// stage more for its first loads: by whole stages alone the model takes 22 shares instead of 15 for 5465 rows of 1408 -> 128, 22.0
+// us instead of 19.4, and the small tiles for 64 rows of 4096 -> 4096, 15.8 instead of 15.5.  Then shares that have no rows are left
+// out (4097 rows of 40 -> 300: 32 shares of 192 rows 18.1 us, the 22 that have any 15.7).
+struct WgradShape { bool big; int64_t tiles_n, tiles_c; int splits; int64_t rows_per_split; };
 WgradShape wgrad_shape(int64_t rows, int64_t in, int64_t out) {
   WgradShape best = {};
   double least = 0;
@@ -313,10 +316,13 @@ WgradShape wgrad_shape(int64_t rows, int64_t in, int64_t out) {
       if (s > 1) us += 5 + (double)s * (double)in * (double)out * 8 / 6e6;
       if (!best.splits || us < least) {
         least = us;
-        best = {big, tn, tc, s};
+        best = {big, tn, tc, s, 0};
       }
     }
   }
+  // whole stages of 64 rows a share, and as many shares as then have any
+  best.rows_per_split = std::max<int64_t>(((rows + best.splits - 1) / best.splits + SW_BK - 1) / SW_BK, 1) * SW_BK;
+  best.splits = (int)std::max<int64_t>((rows + best.rows_per_split - 1) / best.rows_per_split, 1);
   return best;
 }
 
@@ -376,7 +382,7 @@ void linear_wgrad_stash8(hipStream_t st, const void* dy, const void* stash, int6
   g.q = static_cast<const uint8_t*>(stash);
   g.sc = stash8_scales(stash, rows, in);
   g.rows = rows;
-  g.rows_per_split = ((rows + splits - 1) / splits + SW_BK - 1) / SW_BK * SW_BK;
+  g.rows_per_split = s.rows_per_split;
   g.N = (int)out;
   g.C = (int)in;
   g.pitch = (int)stash8_pitch(in);

@@ -122,6 +122,19 @@ def test_stash8_refusals(lib):
         refused(lib, "linear_wgrad_stash8", *[bad if i == at else a for i, a in enumerate(ok)])
 
 
+def test_every_share_of_a_weight_gradient_has_rows(lib):
+    """Shares are whole steps of 64 rows; as many as have any."""
+    n = C.c_size_t()
+    for cin, cout in ((40, 300), (128, 128), (512, 192), (2816, 31), (2048, 512)):
+        for rows in list(range(250, 1200, 13)) + [2049, 4097, 5732, 8645, 8787, 10099, 16384, 100003]:
+            assert lib.asteroid_linear_wgrad_stash8_workspace(rows, cin, cout, C.byref(n)) == 0
+            shares, rest = divmod(n.value, 4 * (cin + 1) * cout)
+            assert rest == 0 and shares != 1
+            if shares:
+                per = -(-rows // shares)
+                assert (shares - 1) * (-(-per // 64) * 64) < rows, (rows, cin, cout, shares)
+
+
 def test_tensors_are_checked():
     f, i = torch.zeros, torch.int32
     with pytest.raises(ValueError, match="GPU"):
