@@ -450,6 +450,9 @@ __global__ __launch_bounds__(512, 6) void embedding_join_kernel(const SumArgs g)
   }
 }
 
+// Groups of eight values of a thread: four where that leaves the chip full; 0: rows of fewer than eight, a value a thread.
+int fwd_groups(int64_t tokens, int64_t width) { return width < 8 ? 0 : tokens * width >= 8 * 256 * 4 * 1024 ? 4 : 1; }
+
 }  // namespace
 
 void embedding_fwd(hipStream_t st, const int32_t* ids, int64_t tokens, const void* table, bool table_bf16, int64_t rows,
@@ -464,14 +467,13 @@ void embedding_fwd(hipStream_t st, const int32_t* ids, int64_t tokens, const voi
   KLAUNCH((embedding_fwd_kernel<TW, TY, U, EVEN>), dim3((unsigned)std::min<int64_t>((total + 2048 * U - 1) / (2048 * U), most)), \
           dim3(256), 0, st, ids, tokens, static_cast<const TW*>(table), (uint32_t)rows, (int)width, 1.f / (float)width, scale,  \
           static_cast<TY*>(y))
-  // (four groups a thread where that leaves the chip full)
-  const bool wide = total >= 8 * 256 * 4 * 1024;
+  const int groups = fwd_groups(tokens, width);
   const bool even = width * (table_bf16 ? 2 : 4) % 16 == 0 && reinterpret_cast<uintptr_t>(table) % 16 == 0;
 #define PICK(TW, TY)                            \
   do {                                          \
-    if (width < 8) NARROW(TW, TY);              \
-    else if (wide && even) LAUNCH(TW, TY, 4, true);  \
-    else if (wide) LAUNCH(TW, TY, 4, false);    \
+    if (!groups) NARROW(TW, TY);                \
+    else if (groups == 4 && even) LAUNCH(TW, TY, 4, true);  \
+    else if (groups == 4) LAUNCH(TW, TY, 4, false);         \
     else LAUNCH(TW, TY, 1, false);              \
   } while (0)
   if (table_bf16) {
@@ -621,3 +623,6 @@ void embedding_bwd(hipStream_t st, const int32_t* ids, int64_t tokens, const voi
 }
 
 }  // namespace ast
+
+// The choice of the lookup's kernel, for tests: groups of eight values of a thread (0: a value a thread).
+extern "C" int ast_embedding_fwd_choice(int64_t tokens, int64_t width) { return ast::fwd_groups(tokens, width); }

@@ -405,3 +405,10 @@ void linear_wgrad_stash8(hipStream_t st, const void* dy, const void* stash, int6
 }
 
 }  // namespace ast
+
+// The choice of wgrad_shape, for tests: the tile's edge, shares of the rows.
+extern "C" void ast_stash8_wgrad_choice(int64_t rows, int64_t in, int64_t out, int choice[2]) {
+  const ast::WgradShape s = ast::wgrad_shape(rows, in, out);
+  choice[0] = s.big ? 256 : 128;
+  choice[1] = s.splits;
+}

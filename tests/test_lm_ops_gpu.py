@@ -2,6 +2,8 @@
 
 Bounds: u = 2^-24 is half a step of fp32.  A sum of n terms in any order is off by at most n u times the sum of the terms'
 magnitudes, a rounding to bf16 by 2^-8 of the value; what an entry is added up from comes from the oracle."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -71,6 +73,22 @@ def test_embedding_forward(ops, T, V, D, kind, table_t, out_t):
     y = ops.embedding_forward(dev(ids)[0], table, scale=1.7, dtype=DT[out_t])
     want = O.embedding_forward(ids, W, float(np.float32(1.7)))
     inside(y, want, abs(want) * (u + HALF[out_t]) * 1.001)
+
+
+@pytest.mark.parametrize("table_t,out_t", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("T,V,D", [(9000, 5003, 1024), (9001, 5003, 1021), (9000, 700, 1026), (1000003, 300, 9), (1100001, 50, 8), (300007, 64, 28)])
+def test_embedding_forward_of_many_values(ops, T, V, D, table_t, out_t):
+    """Four groups of eight a thread, rows at 16-byte addresses and not."""
+    from paper_2408_08015_amd import lib_path
+    assert C.CDLL(lib_path()).ast_embedding_fwd_choice(C.c_int64(T), C.c_int64(D)) == 4
+    g = torch.Generator(device="cuda").manual_seed(T + D)
+    table = torch.randn(V, D, generator=g, device="cuda").to(DT[table_t])
+    ids = torch.randint(-V // 8, V + V // 8, (T,), generator=g, device="cuda", dtype=torch.int32)
+    ids[-1], ids[0] = V - 1, 0
+    y = ops.embedding_forward(ids, table, scale=1.7, dtype=DT[out_t])
+    live = (ids >= 0) & (ids < V)
+    want = table.double()[ids.long().clamp(0, V - 1)] * float(np.float32(1.7)) * live.unsqueeze(1)
+    assert ((y.double() - want).abs() <= want.abs() * (u + HALF[out_t]) * 1.001).all()
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
@@ -382,6 +400,35 @@ def test_linear_wgrad_stash8(ops, rows, cin, cout):
     acc = ops.linear_wgrad_stash8(dy, s, out=old, bias_out=oldb, accumulate=True)
     inside(acc[0], ow + want, bound + 1.01 * u * (abs(ow) + abs(g).T @ abs(xx)))
     inside(acc[1], ob + wb, bb + 1.01 * u * (abs(ob) + abs(g).sum(0)))
+    only, none = ops.linear_wgrad_stash8(dy, s, bias=False)
+    assert none is None and torch.equal(only, dw)
+
+
+@pytest.mark.parametrize("rows,cin,cout,shares", [
+    (64, 4096, 4096, 1), (257, 4096, 4096, 1), (1000, 4096, 4096, 1), (257, 4096, 4093, 1), (1000, 4096, 4093, 1), (2111, 4000, 3999, 1),
+    (1000, 4095, 4096, 1), (4862, 1430, 1024, 8), (4862, 1430, 1019, 8)])
+def test_linear_wgrad_stash8_in_the_large_tile(ops, rows, cin, cout, shares):
+    """Rows of dy at 16-byte addresses and not, dW written by the product itself and from shares, with and without adding."""
+    from paper_2408_08015_amd import lib_path
+    pick = (C.c_int * 2)()
+    C.CDLL(lib_path()).ast_stash8_wgrad_choice(C.c_int64(rows), C.c_int64(cin), C.c_int64(cout), pick)
+    assert tuple(pick) == (256, shares)
+    gen = torch.Generator(device="cuda").manual_seed(rows + cin + cout)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    s = ops.stash8_pack((rnd(rows, cin) * torch.exp(rnd(cin))).bfloat16())
+    xx = ops.stash8_unpack(s, torch.float32).double()
+    dy = rnd(rows, cout).bfloat16()
+    g = dy.double()
+    want, terms = torch.mm(g.t(), xx), torch.mm(g.abs().t(), xx.abs())
+    wb, tb = g.sum(0), g.abs().sum(0)
+    # as in test_linear_wgrad_stash8
+    near = lambda got, want, bound: bool(((got.double() - want).abs() <= bound).all())
+    dw, db = ops.linear_wgrad_stash8(dy, s)
+    assert near(dw, want, terms * ((2 * rows + 4) * u)) and near(db, wb, tb * ((rows + 4) * u))
+    old, oldb = rnd(cout, cin), rnd(cout)
+    acc, accb = ops.linear_wgrad_stash8(dy, s, out=old.clone(), bias_out=oldb.clone(), accumulate=True)
+    assert near(acc, old.double() + want, terms * ((2 * rows + 4) * u) + 1.01 * u * (old.double().abs() + terms))
+    assert near(accb, oldb.double() + wb, tb * ((rows + 4) * u) + 1.01 * u * (oldb.double().abs() + tb))
     only, none = ops.linear_wgrad_stash8(dy, s, bias=False)
     assert none is None and torch.equal(only, dw)
 
