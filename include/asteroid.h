@@ -189,7 +189,8 @@ ast_status asteroid_stream_destroy(void* hip_stream);
  * a file-scope device array of AST_STATIC_SCRATCH_BYTES instead of the memory the stage allocated
  * at create.  Same arguments, same results (bit-identical), same AST_ESTATE rules; the call itself
  * allocates nothing and records no memset (the array's used part is cleared by a kernel).
- * AST_EINVAL if the stage's workspace (asteroid_stage_memory) is larger than the array.  Every GPU
+ * AST_EINVAL if the stage's workspace (asteroid_stage_memory; without the activations that live there for
+ * a forward pass, see "8-bit stash") is larger than the array.  Every GPU
  * the library runs on holds one such array until the process ends, and all stages on that GPU
  * share it: calls that overlap in time on one GPU race; calls on one stream do not. */
 #define AST_STATIC_SCRATCH_BYTES (32u << 20)

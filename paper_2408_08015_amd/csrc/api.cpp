@@ -196,7 +196,7 @@ ast_status asteroid_stage_create(const ast_layer* layers, int32_t n_layers, cons
     return bail(e, "create: hipMalloc(packed weights)");
   if (s.running_floats && (e = hipMalloc((void**)&s.running, s.running_floats * sizeof(float))) != hipSuccess)
     return bail(e, "create: hipMalloc(running stats)");
-  if ((e = hipMalloc((void**)&s.ws, s.ws_bytes)) != hipSuccess) return bail(e, "create: hipMalloc(workspace)");
+  if ((e = hipMalloc((void**)&s.ws, s.ws_bytes + s.passing_bytes)) != hipSuccess) return bail(e, "create: hipMalloc(workspace)");
   s.slots.assign(cfg->K, nullptr);
   for (int k = 0; k < cfg->K; ++k)
     if ((e = hipMalloc((void**)&s.slots[k], s.slot_bytes)) != hipSuccess) return bail(e, "create: hipMalloc(stash)");
@@ -311,7 +311,7 @@ static ast_status backward_impl(asteroid_stage* h, int32_t mb, const void* dy_de
   if (!aligned16(dy_dev) || !aligned16(dx_dev)) return fail(AST_EINVAL, "backward: buffers must be 16-byte aligned");
   if (use_static) {
     if (s.ws_bytes > (size_t)AST_STATIC_SCRATCH_BYTES)
-      return fail(AST_EINVAL, "backward_static: the stage's workspace (" + std::to_string(s.ws_bytes) +
+      return fail(AST_EINVAL, "backward_static: the workspace of the stage's backward pass (" + std::to_string(s.ws_bytes) +
                                   " bytes) exceeds AST_STATIC_SCRATCH_BYTES (" + std::to_string((size_t)AST_STATIC_SCRATCH_BYTES) + ")");
     if (!s.static_ws) return fail(AST_EHIP, "backward_static: the static workspace of this device could not be located at create");
   }
@@ -394,7 +394,7 @@ ast_status asteroid_stage_memory(const asteroid_stage* h, size_t* mod, size_t* o
   if (mod) *mod = 2 * s.nparams * sizeof(float) + s.shadow_elems * 2 + s.wpack_floats * sizeof(float);
   if (opt) *opt = s.nparams * sizeof(float);
   if (act_per_mb) *act_per_mb = s.slot_bytes;
-  if (workspace) *workspace = s.ws_bytes;
+  if (workspace) *workspace = s.ws_bytes + s.passing_bytes;
   return AST_OK;
 }
 

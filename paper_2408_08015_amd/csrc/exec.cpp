@@ -28,7 +28,7 @@ inline int final_act_of(const Stage& s) { return s.final_act; }
 
 inline void* act_ptr(Ctx& c, int id) {
   if (id == c.final_act && !c.s.loss_tail && id != 0 && !c.s.final_in_slot) return c.s.cur_y;
-  if (c.s.acts[id].passing) return id == 0 ? const_cast<void*>(c.s.cur_x) : c.s.ws + c.s.fscratch_off + c.s.acts[id].fwd_off;
+  if (c.s.acts[id].passing) return id == 0 ? const_cast<void*>(c.s.cur_x) : c.s.ws + c.s.ws_bytes + c.s.acts[id].fwd_off;
   return c.slot + c.s.acts[id].slot_off;
 }
 inline char* act8_ptr(Ctx& c, int id) { return c.slot + c.s.acts[id].slot8_off; }  // an activation kept in 8 bits
@@ -468,7 +468,7 @@ void bwd_op(Ctx& c, const Op& op) {
         if (op.kept_grouped) break;  // part of the launch at the end of the pass
         if (op.keep8)
           linear_wgrad_stash8(st, g, act8_ptr(c, op.in), (int64_t)R, op.cin, op.cout, s.G + op.w_off,
-                              op.has_bias ? s.G + op.b_off : nullptr, true, sc);
+                              op.has_bias ? s.G + op.b_off : nullptr, true, sc, op.kept_most);
         else if (!op.wg_grouped)  // else: part of the grouped launch at the end of the pass
           linear_bf16_wgrad(sw, g, (cb)act_ptr(c, op.in), s.G + op.w_off, s.G + op.b_off, op.has_bias != 0,
                             s.red_nblocks != 0, sc, R, op.cin, op.cout);
@@ -531,7 +531,7 @@ void bwd_op(Ctx& c, const Op& op) {
         linear_bf16_dgrad(st, dqkv, s.shadow + op.sh2_off, (bf16_t*)gin, nullptr,
                           op.dgrad_add >= 0 ? (cb)grad_ptr(c, op.dgrad_add) : nullptr, R, D, 3 * D);
       if (op.kept_grouped) break;
-      if (op.keep8) linear_wgrad_stash8(st, dqkv, act8_ptr(c, op.in), (int64_t)R, D, 3 * D, Gq, Gbq, true, lw_q);
+      if (op.keep8) linear_wgrad_stash8(st, dqkv, act8_ptr(c, op.in), (int64_t)R, D, 3 * D, Gq, Gbq, true, lw_q, op.kept_most);
       else if (!op.wg_grouped) linear_bf16_wgrad(sw, dqkv, (cb)act_ptr(c, op.in), Gq, Gbq, true, defer, lw_q, R, D, 3 * D);
       break;
     }

@@ -303,14 +303,14 @@ __global__ __launch_bounds__(256) void stash8_wgrad_sum_kernel(const float* __re
 // us instead of 19.4, and the small tiles for 64 rows of 4096 -> 4096, 15.8 instead of 15.5.  Then shares that have no rows are left
 // out (4097 rows of 40 -> 300: 32 shares of 192 rows 18.1 us, the 22 that have any 15.7).
 struct WgradShape { bool big; int64_t tiles_n, tiles_c; int splits; int64_t rows_per_split; };
-WgradShape wgrad_shape(int64_t rows, int64_t in, int64_t out) {
+WgradShape wgrad_shape(int64_t rows, int64_t in, int64_t out, int most) {
   WgradShape best = {};
   double least = 0;
   for (const bool big : {false, true}) {
     const int b = big ? 256 : 128;
     const int64_t tn = (out + b - 1) / b, tc = (in + b - 1) / b;
     for (const int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-      if (s > 1 && rows < (int64_t)s * 128) break;
+      if (s > most || (s > 1 && rows < (int64_t)s * 128)) break;
       const double steps = (double)((rows + s - 1) / s + SW_BK - 1) / SW_BK, rounds = (double)((tn * tc * s + 255) / 256);
       double us = rounds * steps * (big ? 1.85 : 0.85) + (big ? 8 : 6);
       if (s > 1) us += 5 + (double)s * (double)in * (double)out * 8 / 6e6;
@@ -368,14 +368,14 @@ void linear_wgrad_stash8_group(hipStream_t st, const void* tasks_dev, const void
           static_cast<const uint2*>(blocks_dev));
 }
 
-size_t linear_wgrad_stash8_ws_bytes(int64_t rows, int64_t in, int64_t out) {
-  const int s = wgrad_shape(rows, in, out).splits;
+size_t linear_wgrad_stash8_ws_bytes(int64_t rows, int64_t in, int64_t out, int most) {
+  const int s = wgrad_shape(rows, in, out, most).splits;
   return s > 1 ? (size_t)s * (size_t)(out * in + out) * sizeof(float) : 0;
 }
 
 void linear_wgrad_stash8(hipStream_t st, const void* dy, const void* stash, int64_t rows, int64_t in, int64_t out, float* dw,
-                         float* db, bool accumulate, void* ws) {
-  const WgradShape s = wgrad_shape(rows, in, out);
+                         float* db, bool accumulate, void* ws, int most) {
+  const WgradShape s = wgrad_shape(rows, in, out, most);
   const int splits = s.splits;
   SwArgs g = {};
   g.dy = static_cast<const bf16_t*>(dy);
@@ -408,7 +408,7 @@ void linear_wgrad_stash8(hipStream_t st, const void* dy, const void* stash, int6
 
 // The choice of wgrad_shape, for tests: the tile's edge, shares of the rows.
 extern "C" void ast_stash8_wgrad_choice(int64_t rows, int64_t in, int64_t out, int choice[2]) {
-  const ast::WgradShape s = ast::wgrad_shape(rows, in, out);
+  const ast::WgradShape s = ast::wgrad_shape(rows, in, out, INT_MAX);
   choice[0] = s.big ? 256 : 128;
   choice[1] = s.splits;
 }

@@ -2,6 +2,7 @@
 // Arguments have been checked; everything is enqueued on `st`.
 #pragma once
 #include <hip/hip_runtime.h>
+#include <limits.h>
 #include <stddef.h>
 #include <stdint.h>
 
@@ -36,7 +37,8 @@ inline const uint8_t* stash8_scales(const void* stash, int64_t rows, int64_t col
 void stash8_pack(hipStream_t st, const void* x, bool bf16, int64_t rows, int64_t cols, void* stash);
 void stash8_unpack(hipStream_t st, const void* stash, int64_t rows, int64_t cols, void* x, bool bf16);
 void gelu_bwd_stash8(hipStream_t st, const void* dy, bool bf16, const void* stash, int64_t rows, int64_t cols, void* dz);
-size_t linear_wgrad_stash8_ws_bytes(int64_t rows, int64_t in, int64_t out);
+// most: an upper bound on the shares of the rows, for callers whose workspace is limited (one share takes none)
+size_t linear_wgrad_stash8_ws_bytes(int64_t rows, int64_t in, int64_t out, int most = INT_MAX);
 // Several such gradients, each added to dw and db, in one launch: dy 16-byte aligned with out a multiple of 8, nothing in shares (no
 // workspace).  A stage builds the tables once: `task` is host memory of stash8_group_task_bytes(), blocks_dev holds pairs
 // (product, block of it) of uint32_t.
@@ -45,6 +47,6 @@ int stash8_group_blocks(int64_t in, int64_t out);
 void stash8_group_task(void* task, const void* dy, const void* stash, int64_t rows, int64_t in, int64_t out, float* dw, float* db);
 void linear_wgrad_stash8_group(hipStream_t st, const void* tasks_dev, const void* blocks_dev, int blocks);
 void linear_wgrad_stash8(hipStream_t st, const void* dy, const void* stash, int64_t rows, int64_t in, int64_t out, float* dw,
-                         float* db, bool accumulate, void* ws);
+                         float* db, bool accumulate, void* ws, int most = INT_MAX);
 
 }  // namespace ast

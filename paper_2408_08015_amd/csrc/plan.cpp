@@ -59,8 +59,8 @@ static bool backward_reads(const Stage& s, int a) {
   return false;
 }
 
-// Activations that the backward pass knows in 8 bits only live in the forward pass's scratch from the op that writes them to the
-// last one that reads them; those that live at different times share their place.  Bytes of that scratch.
+// Activations that the backward pass knows in 8 bits only live behind the workspace from the op that writes them to the last one
+// that reads them; those that live at different times share their place.  Bytes that they take.
 static size_t lay_out_passing(Stage& s) {
   struct Span { size_t off, bytes; int last; };
   std::vector<Span> live;
@@ -96,7 +96,7 @@ static size_t lay_out_passing(Stage& s) {
 
 size_t mha_qkv_wgrad_ws(const Op& op, size_t rows) {
   if (op.kept_grouped) return 0;
-  return op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)rows, op.cin, 3 * op.cin)
+  return op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)rows, op.cin, 3 * op.cin, op.kept_most)
                   : linear_bf16_ws_bytes(rows, op.cin, 3 * op.cin, op.wg_splits[1]);
 }
 
@@ -631,7 +631,7 @@ ast_status build_plan(Stage& s, std::string& err) {
     a.in_unwritten = !read;
     s.acts[a.in].unwritten |= !read;
   }
-  const size_t passing_bytes = lay_out_passing(s);
+  s.passing_bytes = lay_out_passing(s);
   for (size_t a = 0; a < s.acts.size(); ++a) {
     s.acts[a].unwritten |= virtual_act[a] != 0;
     if ((int)a == final_act && !s.loss_tail && a != 0 && !s.final_in_slot) continue;
@@ -717,7 +717,7 @@ ast_status build_plan(Stage& s, std::string& err) {
         case OP_LINEAR:
           if (s.bf16)
             need = align_up(s.acts[op.out].bytes, 256) +
-                   (op.kept_grouped ? 0 : op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)I.n * I.h * I.w, op.cin, op.cout)
+                   (op.kept_grouped ? 0 : op.keep8 ? linear_wgrad_stash8_ws_bytes((int64_t)I.n * I.h * I.w, op.cin, op.cout, op.kept_most)
                              : linear_bf16_ws_bytes((size_t)I.n * I.h * I.w, op.cin, op.cout, op.wg_splits[0]));
           break;
         case OP_EMBEDDING: need = embedding_bwd_ws_bytes((int64_t)I.n * I.h, op.cin, op.cout); break;
@@ -736,7 +736,7 @@ ast_status build_plan(Stage& s, std::string& err) {
     }
     // The forward pass has scratch of its own (BatchNorm statistics partials), so that the forward of one
     // micro-batch may run beside the backward of another.
-    size_t fsc = align_up(passing_bytes, 256);
+    size_t fsc = 0;
     for (Op& op : s.ops) {
       if (op.kind != OP_BN || op.dws) continue;
       const Act& I = s.acts[op.in];
@@ -771,6 +771,7 @@ ast_status build_plan(Stage& s, std::string& err) {
       wgrad_group_split(products.data(), products.size(), most);
       for (size_t i = 0; i < products.size(); ++i) *splits[i] = products[i].splits;
       for (Op& op : s.ops) {
+        op.kept_most = most < kWgradMostShares ? most : INT_MAX;
         if (op.kind != OP_CONV_IGEMM) continue;
         const Act& I = s.acts[op.in];
         const int other = conv_wgrad_tr_splits((long)I.n * I.h * I.w, op.cin, op.cout, op.k * op.k);

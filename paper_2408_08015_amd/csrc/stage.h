@@ -54,7 +54,7 @@ struct Act {
   size_t slot8_off = 0;            // ... at this byte offset of a stash slot
   bool passing = false;            // ... and in no other form: its bf16 values last from the op that makes them to the forward
                                    // pass's last reader (the stage input: in the caller's buffer)
-  size_t fwd_off = 0;              // ... at this byte offset of the forward pass's scratch
+  size_t fwd_off = 0;              // ... at this byte offset behind the workspace
   bool unwritten = false;          // no kernel writes it: the kernels that need it form it from what they read
 };
 
@@ -72,6 +72,7 @@ struct Op {
   int heads = 0;
   bool keep8 = false;     // bf16 linear / MHA / GELU: the input is kept in 8 bits and the weight gradient (of MHA: of the qkv
                           // projection), or GELU's gradient, is formed from it
+  int kept_most = INT_MAX;  // ... in at most so many shares of its rows
   bool kept_grouped = false;  // ... as part of the one launch of such gradients at the end of the backward pass
   bool qk_norm = false;   // MHA: norm with gains and rotation of queries and keys
   int rotary = 0, interleaved = 0;
@@ -152,6 +153,7 @@ struct Stage {
   std::vector<char*> slots;  // K stash slots
   char* ws = nullptr;        // workspace: activation gradients + scratch
   size_t ws_bytes = 0, grad_bytes = 0;
+  size_t passing_bytes = 0;  // behind the workspace: activations that last for a forward pass (a backward pass has no use for them)
   size_t scratch_off = 0, scratch_bytes = 0;  // per-op scratch regions (masked gradients, partials)
   size_t fscratch_off = 0;                    // per-op scratch of the forward pass (behind the backward's)
 

@@ -71,6 +71,16 @@ def test_a_shortcut_branch_keeps_the_blocks_input():
     assert act[1] == act[2] == act[3] and room <= act[1] - act[0] <= room + 256
 
 
+@pytest.mark.parametrize("d,n,B,act", [(512, 2, 32, 0), (512, 3, 24, 0), (256, 4, 32, 0), (1024, 2, 8, 0), (512, 2, 32, 1), (768, 3, 8, 1), (448, 2, 36, 0)])
+def test_a_stage_that_fits_the_static_array_fits_it_with_kept_inputs(d, n, B, act):
+    """What only a forward pass uses does not count, and the weight gradients take fewer shares where theirs would not fit."""
+    L = lambda k: sum([[dict(C.linear(d, d), keep8=k)] + ([dict(C.simple("gelu"), keep8=k)] if act else []) for _ in range(n)], [])
+    ws = [A.plan_memory(L(k), B, 1, 1, (128, d), "bf16", "bsd", True)[3] for k in (0, 1)]
+    # tensors of a forward pass that are alive together: a layer's input and output, and the value in front of a GELU
+    passing = B * 128 * d * 2 * ((2 if act or n > 2 else 1) + act * (n > 2))
+    assert ws[0] <= 32 << 20 and ws[1] - passing <= 32 << 20
+
+
 def test_the_profiler_cuts_behind_the_embedding():
     from paper_2408_08015_amd import profiler
     cfg = small(nlayers=1)

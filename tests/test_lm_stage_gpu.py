@@ -99,6 +99,22 @@ def test_bit_identical_however_it_runs(A, K, kw):
                 assert np.array_equal(ref[r][k], got[r][k]), (K, kw, r, k)
 
 
+@pytest.mark.parametrize("layers", [
+    lambda: [dict(C.linear(512, 512), keep8=1), dict(C.linear(512, 512), keep8=1)],
+    lambda: [dict(C.linear(512, 512), keep8=1), dict(C.simple("gelu"), keep8=1), dict(C.linear(512, 512), keep8=1)],
+])
+def test_static_backward_of_a_stage_whose_shares_were_brought_down(A, layers):
+    cfg = encoder(layers(), B=32, M=2, S=128, d=512)
+    inp = gen.make_inputs(cfg, randomize_affine=True)
+    ref, _, _ = harness.run_hip(cfg, inp, K=1, rounds=2)
+    for kw in (dict(), dict(forward_stream=True)):
+        got, _, _ = harness.run_hip(cfg, inp, K=2, rounds=2, static_backward=True, **kw)
+        for r in range(2):
+            for k in ("y", "dx", "G", "W"):
+                assert np.array_equal(ref[r][k], got[r][k]), (kw, r, k)
+    check(cfg, inp)
+
+
 def test_keeping_changes_nothing_but_the_gradients_it_forms(A):
     """Forward pass and input gradient of dense layers are those of the stage without it, bit for bit; the flagged weight
     gradients are the operator's on the same tensors."""
