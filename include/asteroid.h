@@ -142,7 +142,8 @@ ast_status asteroid_stage_create(const ast_layer* layers, int32_t n_layers,
 
 /* FP of micro-batch `mb` (Sec. 3.2).  x_dev: B samples in `layout`/`dtype`, read before
  * the call's work completes on the stream and copied into the stash (the caller may reuse
- * it after the stream passes this call).  labels_dev: int32[B], required iff the stage
+ * it after the stream passes this call); an x that is kept in 8 bits only is not copied, so
+ * where the layer that writes y_dev reads x, y_dev may not overlap it (AST_EINVAL).  labels_dev: int32[B], required iff the stage
  * ends in SOFTMAX_CE.  y_dev: receives the stage output (B samples) or, for a loss tail,
  * the fp32 logits [B][classes]; may be NULL for a loss tail.  loss_dev: one fp32 that
  * receives this micro-batch's share of the mini-batch mean loss; may be NULL.

@@ -287,6 +287,11 @@ ast_status asteroid_stage_forward(asteroid_stage* h, int32_t mb, const void* x_d
   if (!aligned16(x_dev) || !aligned16(y_dev) || !aligned16(labels_dev)) return fail(AST_EINVAL, "forward: buffers must be 16-byte aligned");
   if (s.loss_tail && !labels_dev) return fail(AST_EINVAL, "forward: labels_dev required for a SOFTMAX_CE tail");
   if (!s.loss_tail && !y_dev) return fail(AST_EINVAL, "forward: y_dev is NULL");
+  if (s.x_meets_y) {
+    const char *x = static_cast<const char*>(x_dev), *y = static_cast<const char*>(y_dev);
+    if (x < y + s.acts[s.final_act].bytes && y < x + s.acts[0].bytes)
+      return fail(AST_EINVAL, "forward: x_dev, which is kept in 8 bits only, is still read when y_dev is written: they may not overlap");
+  }
   int slot = s.free_slots.back();
   std::string err;
   ProfGuard pg(h);

@@ -632,6 +632,13 @@ ast_status build_plan(Stage& s, std::string& err) {
     s.acts[a.in].unwritten |= !read;
   }
   s.passing_bytes = lay_out_passing(s);
+  if (s.acts[0].passing && !s.final_in_slot) {
+    bool written = false;
+    for (const Op& op : s.ops) {
+      written |= op.out == final_act && op.in != final_act;
+      s.x_meets_y |= written && (op.in == 0 || op.res_in == 0 || op.skip == 0);
+    }
+  }
   for (size_t a = 0; a < s.acts.size(); ++a) {
     s.acts[a].unwritten |= virtual_act[a] != 0;
     if ((int)a == final_act && !s.loss_tail && a != 0 && !s.final_in_slot) continue;

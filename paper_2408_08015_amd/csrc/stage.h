@@ -153,6 +153,7 @@ struct Stage {
   std::vector<char*> slots;  // K stash slots
   char* ws = nullptr;        // workspace: activation gradients + scratch
   size_t ws_bytes = 0, grad_bytes = 0;
+  bool x_meets_y = false;    // the forward pass reads the caller's x while, or after, it writes the caller's y
   size_t passing_bytes = 0;  // behind the workspace: activations that last for a forward pass (a backward pass has no use for them)
   size_t scratch_off = 0, scratch_bytes = 0;  // per-op scratch regions (masked gradients, partials)
   size_t fscratch_off = 0;                    // per-op scratch of the forward pass (behind the backward's)

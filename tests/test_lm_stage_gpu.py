@@ -115,6 +115,41 @@ def test_static_backward_of_a_stage_whose_shares_were_brought_down(A, layers):
     check(cfg, inp)
 
 
+def test_results_over_an_input_that_is_kept_in_8_bits_only(A):
+    """The caller's x is read as it lies: y may take its place where x has been read by then, and is refused where not."""
+    import torch
+    k = dict(C.linear(128, 128), keep8=1)
+    for layers, ok in (([k], False), ([C.simple("res_begin"), k, C.simple("res_add")], False),
+                       ([C.simple("res_begin"), k, C.simple("gelu"), k, C.simple("res_add")], False),
+                       ([k, C.simple("gelu")], False), ([k, dict(kind="layernorm", d=128, eps=1e-5)], True), ([k, k], True),
+                       ([k, C.simple("relu")], True), ([C.linear(128, 128)], True)):
+        cfg = encoder(layers, M=1)
+        inp = gen.make_inputs(cfg, randomize_affine=True)
+        ref, _, _ = harness.run_hip(cfg, inp, rounds=1)
+        st = A.Stage(cfg.layers, cfg.B, 1, 1, cfg.in_shape, cfg.dtype, cfg.layout, True, stream=torch.cuda.current_stream().cuda_stream)
+        st.set_params(inp["params"])
+        room = torch.zeros(3 * inp["x"].size, device="cuda", dtype=torch.bfloat16)
+        n = inp["x"].size
+        x = room[n:2 * n].view(inp["x"].shape)
+        x.copy_(torch.from_numpy(inp["x"]))
+        dy, dx = torch.from_numpy(inp["dy"]).cuda().bfloat16(), torch.zeros_like(x)
+        if ok:
+            st.forward(0, x, None, x)
+            y = x
+        else:
+            for at in (n, 1024, 2 * n - 1024):
+                with pytest.raises(A.AsteroidError, match="overlap") as e:
+                    st.forward(0, x, None, room[at:at + n])
+                assert e.value.status == -1
+            y = room[2 * n:].view(x.shape)
+            st.forward(0, x, None, y)
+        st.backward(0, dy, dx)
+        torch.cuda.synchronize()
+        assert np.array_equal(y.float().cpu().numpy(), ref[0]["y"]) and np.array_equal(dx.float().cpu().numpy(), ref[0]["dx"])
+        assert np.array_equal(st.get_grads(), ref[0]["G"])
+        st.close()
+
+
 def test_keeping_changes_nothing_but_the_gradients_it_forms(A):
     """Forward pass and input gradient of dense layers are those of the stage without it, bit for bit; the flagged weight
     gradients are the operator's on the same tensors."""
