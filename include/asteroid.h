@@ -70,16 +70,16 @@ typedef enum {
   AST_RES_BEGIN = 4,   /* remembers the current activation as the skip input                  */
   AST_RES_ADD = 5,     /* adds the remembered skip input                                      */
   AST_GLOBAL_AVGPOOL = 6,
-  AST_LINEAR = 7,      /* p = {in, out, has_bias, keep8}; y = x W^T + b on the last dimension; keep8: see
-                          "8-bit stash" below                                                   */
+  AST_LINEAR = 7,      /* p = {in, out, has_bias | keep8}; y = x W^T + b on the last dimension; what stands
+                          behind a | : see AST_LAYER_MORE below                                 */
   AST_SOFTMAX_CE = 8,  /* loss tail: mean over the whole mini-batch (divides by M*B)          */
   AST_MAXPOOL2X2 = 9,  /* 2x2 window, stride 2; gradient to the first maximum in row-major order */
   AST_LAYERNORM = 10,  /* p = {D}; eps; over the last dimension                               */
-  AST_MHA = 11,        /* p = {D, heads, qk_norm, rotary, theta, interleaved, keep8}; self-attention, no mask, no
+  AST_MHA = 11,        /* p = {D, heads | qk_norm, rotary, theta, interleaved, keep8}; | eps; self-attention, no mask, no
                           dropout.  qk_norm: every query and key head is normalised (RMS, eps) and
                           scaled by a gain, and its first `rotary` values are rotated by the
                           position in the sequence (asteroid_qk_norm_rope_forward), before the scores */
-  AST_GELU = 12,       /* p = {keep8}; x * Phi(x) with the exact erf form                     */
+  AST_GELU = 12,       /* p = { | keep8}; x * Phi(x) with the exact erf form                     */
   AST_SWISH = 13,      /* x * sigmoid(x)  (fp32 stages; the EfficientNet workload of Table 4)  */
   AST_SIGMOID = 14,    /* 1 / (1 + exp(-x))  (fp32 stages)                                     */
   AST_SE_BEGIN = 15,   /* squeeze-and-excitation: remembers the current image tensor x; must be
@@ -101,15 +101,21 @@ typedef enum {
                           stays fp32, the result is rounded once                                */
 } ast_layer_kind;
 
+/* Added to AST_LINEAR, AST_MHA or AST_GELU in ast_layer.kind (AST_MHA + AST_LAYER_MORE): the entries of p behind the
+ * | of that kind count too (0 where a layer has no use for one; AST_EINVAL for what they cannot be), and for
+ * AST_MHA eps.  A description without it is read as far as the | only, whatever stands behind. */
+#define AST_LAYER_MORE 0x100
+
 /* 8-bit stash (bf16 stages).  keep8 = 1 keeps a layer's input (AST_MHA: the input of its query, key and
  * value projection) between the forward and the backward pass in the 8-bit form of asteroid_ops.h, and
- * the weight gradient (AST_GELU: the input gradient) is formed from the restored values; the forward
- * pass and the input gradients of dense layers are those of keep8 = 0.  An activation that no other
+ * the weight gradient (AST_GELU: the input gradient) is formed from the restored values.  The forward
+ * pass is that of keep8 = 0, bit for bit, and so are input gradients, as far down as the first AST_GELU
+ * that is kept: everything in front of it receives a gradient formed from the 8-bit slope.  An activation that no other
  * layer's backward pass needs leaves the stash - act_per_mb falls by what it held - and lives in the
- * workspace during a forward pass.  Entries of p that a kind does not list are 0. */
+ * workspace during a forward pass. */
 
 typedef struct {
-  int32_t kind;  /* ast_layer_kind */
+  int32_t kind;  /* ast_layer_kind (+ AST_LAYER_MORE) */
   int32_t p[8];
   float eps;
 } ast_layer;

@@ -13,6 +13,8 @@ KINDS = {"conv2d": 0, "batchnorm2d": 1, "relu": 2, "relu6": 3, "res_begin": 4, "
          "global_avgpool": 6, "linear": 7, "softmax_ce": 8, "maxpool2x2": 9, "layernorm": 10,
          "mha": 11, "gelu": 12, "swish": 13, "sigmoid": 14, "se_begin": 15, "se_scale": 16, "res_swap": 17, "maxpool3x3s2": 18,
          "embedding": 19}
+LAYER_MORE = 0x100
+MORE_KEYS = {"linear": {"keep8"}, "gelu": {"keep8"}, "mha": {"qk_norm", "rotary", "theta", "interleaved", "keep8"}}
 DTYPES = {"f32": 0, "bf16": 1}
 LAYOUTS = {"nchw": 0, "nhwc": 1, "bsd": 2}
 
@@ -89,7 +91,7 @@ def _marshal_layers(layers):
     arr = (ast_layer * len(layers))()
     for a, L in zip(arr, layers):
         k = L["kind"]
-        a.kind = KINDS[k]
+        a.kind = KINDS[k] + (LAYER_MORE if MORE_KEYS.get(k, set()) & L.keys() else 0)
         a.eps = float(L.get("eps", 0.0))
         if k == "conv2d":
             vals = [L["cin"], L["cout"], L["k"], L["stride"], L["pad"], L["groups"], int(L["bias"])]

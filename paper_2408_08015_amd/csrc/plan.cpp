@@ -125,6 +125,13 @@ ast_status build_plan(Stage& s, std::string& err) {
     cur = new_act(s, B, cfg.in_shape[0], cfg.in_shape[1], cfg.in_shape[2], 4, -1, es);
   } else { err = "unknown layout"; return AST_EINVAL; }
 
+  for (ast_layer& L : s.layers) {  // entries of p that a description without AST_LAYER_MORE need not have set
+    const int kind = L.kind & ~AST_LAYER_MORE, own = kind == AST_LINEAR ? 3 : kind == AST_MHA ? 2 : kind == AST_GELU ? 0 : -1;
+    if (own < 0) continue;
+    if (L.kind == kind) std::fill(L.p + own, L.p + 8, 0);
+    L.kind = kind;
+  }
+
   s.layer_act.assign(nl, -1);
   std::vector<int> res_stack;      // activation ids of open RES_BEGINs
   std::vector<int> res_op_stack;   // op indices of those RES_BEGINs

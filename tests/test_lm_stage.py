@@ -120,6 +120,47 @@ def test_refusals():
     no(L, status=-5, dtype="f32", layout="nchw", in_shape=(8, 4, 4), grad=True)
 
 
+def plan_described(arr, cfg, in_shape, needs_input_grad=1):
+    """asteroid_stage_plan_memory of C descriptions: its status, and the four byte counts."""
+    import ctypes
+    from paper_2408_08015_amd import binding as Bd
+    lib = A.load_library()
+    out = [ctypes.c_size_t() for _ in range(4)]
+    c = Bd._marshal_cfg(cfg.B, cfg.M, 1, in_shape, cfg.dtype, cfg.layout, needs_input_grad)
+    return lib.asteroid_stage_plan_memory(arr, len(arr), ctypes.byref(c), *[ctypes.byref(o) for o in out]), [o.value for o in out]
+
+
+@pytest.mark.parametrize("junk", [1, 2, -1, 1 << 30])
+def test_descriptions_that_leave_the_entries_behind_their_own_unset(junk):
+    """p beyond what a kind had, and eps of an attention, were never looked at: a description that leaves them as they come means
+    the plain layer still.  With AST_LAYER_MORE they count."""
+    from paper_2408_08015_amd import binding as Bd
+    cfg = C.cfg5(B=2, M=2, S=32, d=128, heads=2, ffn=256, nlayers=1)
+    layers = cfg.layers + [dict(kind="gelu")]
+    own = {"linear": 3, "mha": 2, "gelu": 0}
+    zeroed = plan_described(Bd._marshal_layers(layers), cfg, cfg.in_shape)
+    arr = Bd._marshal_layers(layers)
+    for a, L in zip(arr, layers):
+        for i in range(own.get(L["kind"], 8), 8):
+            a.p[i] = junk
+        if L["kind"] in own:
+            a.eps = float("nan")
+    assert zeroed[0] == 0 and plan_described(arr, cfg, cfg.in_shape) == zeroed
+    for a, L in zip(arr, layers):   # counted: no layer takes these
+        b = Bd._marshal_layers(layers)
+        if L["kind"] in own and junk != 1 or L["kind"] == "mha":
+            i = [x is L for x in layers].index(True)
+            b[i] = a
+            b[i].kind += Bd.LAYER_MORE
+            assert plan_described(b, cfg, cfg.in_shape)[0] == -1, L
+    b = Bd._marshal_layers(layers)
+    b[[L["kind"] for L in layers].index("layernorm")].kind += Bd.LAYER_MORE
+    assert plan_described(b, cfg, cfg.in_shape)[0] == -1
+    kept = Bd._marshal_layers([dict(L, keep8=1) for L in layers])
+    st, mem = plan_described(kept, cfg, cfg.in_shape)
+    assert st == 0 and mem[2] < zeroed[1][2]
+
+
 def test_what_was_planned_before_is_planned_the_same():
     """Layers without the new entries keep their byte counts."""
     cfg = C.cfg5(B=2, M=2, S=32, d=128, heads=2, ffn=256, nlayers=1)
