@@ -160,14 +160,16 @@ def _ptr(t):
 
 class Stage:
     """One pipeline stage on one GPU.  Tensors passed to forward/backward are torch CUDA
-    tensors (contiguous, in the stage's layout and dtype); only their data pointers cross."""
+    tensors (contiguous, in the stage's layout and dtype); only their data pointers cross.  Token ids, the
+    input of a stage that begins with an embedding, are int32: other integers are refused, since their
+    bytes would be taken for ids."""
 
     def __init__(self, layers, B, M, K, in_shape, dtype="f32", layout="nchw", needs_input_grad=True,
                  stream=None):
         self.lib = load_library()
         self.layers = list(layers)
         self.B, self.M, self.K = B, M, K
-        self.dtype, self.layout = dtype, layout
+        self.dtype, self.layout, self.in_shape = dtype, layout, tuple(in_shape)
         arr = _marshal_layers(layers)
         cfg = _marshal_cfg(B, M, K, in_shape, dtype, layout, needs_input_grad)
         h = C.c_void_p()
@@ -183,6 +185,10 @@ class Stage:
     __del__ = close
 
     def forward(self, mb, x, labels=None, y=None, loss=None):
+        if x is not None and self.layers[0]["kind"] == "embedding":
+            n = self.B * self.in_shape[0]
+            if str(x.dtype) != "torch.int32" or not x.is_contiguous() or x.numel() != n:
+                raise ValueError("token ids must be a contiguous int32 tensor of %d values, got %s %s" % (n, x.dtype, tuple(x.shape)))
         _check(self.lib, self.lib.asteroid_stage_forward(self.h, mb, _ptr(x), _ptr(labels), _ptr(y), _ptr(loss)))
 
     def set_forward_stream(self, stream):

@@ -89,6 +89,18 @@ def test_the_profiler_cuts_behind_the_embedding():
     assert profiler._out_shape(cfg.layers[:1], cfg.in_shape) == (32, 128)
 
 
+def test_token_ids_are_int32():
+    """An int64 tensor, torch's own integer type, would be read as pairs of ids."""
+    import torch
+    cfg = small()
+    st = A.Stage.__new__(A.Stage)     # (checked before anything is asked of the library)
+    st.layers, st.B, st.in_shape, st.lib = cfg.layers, cfg.B, cfg.in_shape, None
+    for ids in (torch.zeros(2, 32, dtype=torch.int64), torch.zeros(2, 32), torch.zeros(2, 31, dtype=torch.int32),
+                torch.zeros(2, 64, dtype=torch.int32)[:, ::2], torch.zeros(4, 32, dtype=torch.int32)):
+        with pytest.raises(ValueError, match="int32"):
+            st.forward(0, ids)
+
+
 def test_refusals():
     cfg = small(nlayers=1)
 
