@@ -112,6 +112,8 @@ def _marshal_layers(layers):
         else:
             vals = []
         for i, v in enumerate(vals):
+            if k in ("mha", "embedding") and (int(v) != v or not -2**31 <= v < 2**31):   # (ctypes would cut it off)
+                raise ValueError("%s: entry %d must be a whole number of 32 bits, got %r" % (k, i, v))
             a.p[i] = int(v)
     return arr
 

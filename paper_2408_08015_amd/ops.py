@@ -177,8 +177,10 @@ def _qk_cfg(q, positions, period, rotary, theta, interleaved, eps):
     T, _, d = q.shape
     if positions is not None:
         _vector_i32(positions, "positions", T)
-    elif period < 1:
-        raise ValueError("positions, or the period of the sequences, must be given")
+    elif not 1 <= period < 1 << 31:   # (ctypes would cut it off)
+        raise ValueError("positions, or the period of the sequences (below 2^31), must be given")
+    if rotary is not None and not -1 << 31 <= rotary < 1 << 31:
+        raise ValueError("rotary must lie in [0, head_dim]")
     return ast_qk_cfg(T, _DT[q.dtype], d, d // 2 * 2 if rotary is None else rotary, int(bool(interleaved)), eps, theta,
                       None if positions is None else positions.data_ptr(), period)
 

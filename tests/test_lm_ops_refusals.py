@@ -180,3 +180,11 @@ def test_tensors_are_checked():
         ops.linear_wgrad_stash8(f(4, 8), s)
     with pytest.raises(ValueError, match="workspace"):
         ops.Stash8(4, 40, "cpu", data=f(10, dtype=torch.uint8))
+
+
+def test_numbers_that_the_c_interface_has_no_room_for():
+    q, g = torch.zeros(3, 2, 8), torch.zeros(8)
+    with pytest.raises(ValueError, match="period"):
+        ops.qk_norm_rope_forward(q, q, g, g, period=(1 << 32) + 3)
+    with pytest.raises(ValueError, match="rotary"):
+        ops.qk_norm_rope_forward(q, q, g, g, period=3, rotary=(1 << 32) + 8)

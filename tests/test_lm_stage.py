@@ -132,6 +132,20 @@ def test_refusals():
     no(L, status=-5, dtype="f32", layout="nchw", in_shape=(8, 4, 4), grad=True)
 
 
+def test_numbers_that_a_description_has_no_room_for():
+    cfg = small(nlayers=1)
+
+    def with_layer(i, **kw):
+        return plan(cfg, layers=[dict(l, **kw) if j == i else l for j, l in enumerate(cfg.layers)])
+
+    mha = 2
+    for i, bad in ((0, dict(rows=2**32 + 300)), (0, dict(d=2**32 + 128)), (mha, dict(theta=2**32 + 10000)), (mha, dict(theta=0.5)),
+                   (mha, dict(theta=10000.5)), (mha, dict(rotary=2**32))):
+        with pytest.raises(ValueError, match="32 bits"):
+            with_layer(i, **bad)
+    assert with_layer(mha, theta=10000.0) == plan(cfg)
+
+
 def plan_described(arr, cfg, in_shape, needs_input_grad=1):
     """asteroid_stage_plan_memory of C descriptions: its status, and the four byte counts."""
     import ctypes
