@@ -16,8 +16,8 @@
  * and nothing else: no allocation, no memset, no host synchronisation, nothing kept between calls, so a
  * call may be recorded into a HIP graph.  `workspace_dev` is the call's alone until the stream has
  * passed it: calls that may overlap in time (two streams, two graphs replayed side by side) take one
- * each.  Its contents before the call do not matter.  Outputs may not overlap inputs or the workspace
- * except where a call allows it.
+ * each.  Its contents before the call do not matter.  Outputs may not overlap each other, nor inputs or
+ * the workspace except where a call allows it.
  * Element types are AST_F32 and AST_BF16_F32ACC (bf16) of ast_dtype; sums, norms and angles are formed
  * in 32 bits or more and every result is rounded once.  Results do not depend on the order in which
  * blocks run: equal calls give equal bits.

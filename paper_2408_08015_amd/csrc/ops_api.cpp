@@ -137,6 +137,7 @@ ast_status asteroid_qk_norm_rope_forward(const ast_qk_cfg* cfg, const ast_heads*
   if (cfg->tokens == 0) return AST_OK;
   if (!q_gain_dev || !k_gain_dev || !aligned(q_gain_dev, 4) || !aligned(k_gain_dev, 4))
     return fail(fn, "gains must be non-NULL and 4-byte aligned");
+  if (yq->dev == yk->dev) return fail(fn, "yq and yk are one tensor");
   ast::qk_norm_rope_fwd(stream_of(hip_stream), *cfg, *q, *k, q_gain_dev, k_gain_dev, *yq, *yk);
   return launched(fn);
 }
@@ -166,6 +167,9 @@ ast_status asteroid_qk_norm_rope_backward(const ast_qk_cfg* cfg, const ast_heads
   const size_t need = ast::qk_norm_rope_bwd_ws_bytes(cfg->tokens, cfg->head_dim);
   if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
     return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  if (dq_gain_dev < dk_gain_dev + cfg->head_dim && dk_gain_dev < dq_gain_dev + cfg->head_dim)
+    return fail(fn, "the gains' gradients overlap");
+  if (cfg->tokens > 0 && dq->dev == dk->dev) return fail(fn, "dq and dk are one tensor");
   ast::qk_norm_rope_bwd(stream_of(hip_stream), *cfg, *dyq, *dyk, *q, *k, q_gain_dev, k_gain_dev, *dq, *dk, dq_gain_dev, dk_gain_dev,
                         accumulate != 0, workspace_dev);
   return launched(fn);
@@ -222,6 +226,7 @@ ast_status asteroid_linear_wgrad_stash8(const void* dy_dev, const void* stash_de
   const size_t need = ast::linear_wgrad_stash8_ws_bytes(rows, in, out);
   if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
     return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  if (db_dev && db_dev < dw_dev + in * out && dw_dev < db_dev + out) return fail(fn, "dw_dev and db_dev overlap");
   ast::linear_wgrad_stash8(stream_of(hip_stream), dy_dev, stash_dev, rows, in, out, dw_dev, db_dev, accumulate != 0, workspace_dev);
   return launched(fn);
 }

@@ -188,3 +188,22 @@ def test_numbers_that_the_c_interface_has_no_room_for():
         ops.qk_norm_rope_forward(q, q, g, g, period=(1 << 32) + 3)
     with pytest.raises(ValueError, match="rotary"):
         ops.qk_norm_rope_forward(q, q, g, g, period=3, rotary=(1 << 32) + 8)
+
+
+def test_outputs_that_lie_on_each_other(lib):
+    """Two writers of one place: gradients of a gain that queries and keys share, one tensor for both results, dW over db."""
+    n = C.c_size_t()
+    assert lib.asteroid_qk_norm_rope_backward_workspace(cfg(), 8, 8, C.byref(n)) == 0
+    h, far = heads(), heads(dev=P + (1 << 20))
+    bwd = lambda dq, dk, g, w: refused(lib, "qk_norm_rope_backward", cfg(), h, h, h, h, P, P, dq, dk, g, w, 1, P, n.value, None)
+    for by in (0, 4, 252, -252):
+        bwd(h, far, P + 1024, P + 1024 + by)
+        assert "gains" in lib.asteroid_last_error().decode()
+    bwd(h, h, P, P + 256)
+    assert "one tensor" in lib.asteroid_last_error().decode()
+    refused(lib, "qk_norm_rope_forward", cfg(), h, h, P, P, far, far, None)
+    assert "one tensor" in lib.asteroid_last_error().decode()
+    assert lib.asteroid_linear_wgrad_stash8_workspace(64, 40, 24, C.byref(n)) == 0
+    for by in (0, 4 * 40 * 24 - 4, -4 * 23):
+        refused(lib, "linear_wgrad_stash8", P, P, 64, 40, 24, P + 4096, P + 4096 + by, 0, P, 1 << 30, None)
+        assert "overlap" in lib.asteroid_last_error().decode()
