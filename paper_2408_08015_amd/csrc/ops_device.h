@@ -6,7 +6,6 @@ namespace ast {
 
 // (The hardware takes global accesses of 16 bytes at any address that is a multiple of the element size.)
 struct __attribute__((packed, aligned(1))) Raw16 { uint32_t w[4]; };
-struct __attribute__((packed, aligned(1))) Raw8 { uint32_t w[2]; };
 
 // eight consecutive values as fp32
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {

@@ -115,6 +115,37 @@ def test_static_backward_of_a_stage_whose_shares_were_brought_down(A, layers):
     check(cfg, inp)
 
 
+@pytest.mark.parametrize("layers", [
+    # both branches of a block, products without a bias, and a GELU in front of a kept product and behind one
+    lambda: [dict(C.linear(512, 768), keep8=1), C.simple("res_begin"), dict(C.linear(768, 768), keep8=1), C.simple("gelu"),
+             dict(C.linear(768, 768, bias=False), keep8=1), C.simple("res_swap"), dict(C.linear(768, 768), keep8=1), C.simple("res_add"),
+             dict(kind="layernorm", d=768, eps=1e-5), dict(C.linear(768, 1024), keep8=1), dict(C.simple("gelu"), keep8=1),
+             dict(C.linear(1024, 520), keep8=1), dict(kind="layernorm", d=520, eps=1e-5)],
+    # the last product's upstream gradient is the caller's: a product of its own beside the launch
+    lambda: [dict(C.linear(512, 1536), keep8=1), C.simple("relu"), dict(C.linear(1536, 1000), keep8=1), C.simple("res_begin"),
+             dict(C.linear(1000, 1000), keep8=1), C.simple("res_add"), dict(C.linear(1000, 512), keep8=1)],
+])
+def test_one_launch_for_kept_inputs(A, layers):
+    """More than 192 tiles of 128 x 128, so that the weight gradients are one launch; rows that end inside a step."""
+    cfg = encoder(layers(), B=3, M=2, S=37, d=512)
+    inp = gen.make_inputs(cfg, randomize_affine=True)
+    check(cfg, inp)
+    ref, _, _ = harness.run_hip(cfg, inp, K=1, rounds=2)
+    for kw in (dict(), dict(static_backward=True), dict(forward_stream=True)):
+        got, _, _ = harness.run_hip(cfg, inp, K=2, rounds=2, **kw)
+        for r in range(2):
+            for k in ("y", "dx", "G", "W"):
+                assert np.array_equal(ref[r][k], got[r][k]), (kw, r, k)
+    import torch
+    st = A.Stage(cfg.layers, cfg.B, 1, 1, cfg.in_shape, cfg.dtype, cfg.layout, True, stream=torch.cuda.current_stream().cuda_stream)
+    x, dy = torch.from_numpy(inp["x"][:3]).cuda().bfloat16(), torch.from_numpy(inp["dy"][:3]).cuda().bfloat16()
+    st.forward(0, x, None, torch.zeros_like(dy))
+    st.profile_begin()
+    st.backward(0, dy, torch.zeros_like(x))
+    assert st.profile_end()["stash8_wgrad_group_kernel"][0] == 1
+    st.close()
+
+
 def test_results_over_an_input_that_is_kept_in_8_bits_only(A):
     """The caller's x is read as it lies: y may take its place where x has been read by then, and is refused where not."""
     import torch
