@@ -125,8 +125,12 @@ class OracleStage:
 
     @staticmethod
     def _kept(l, a):
-        """What the backward pass sees of a layer's input: with keep8 its 8-bit form."""
-        return lm_ops.stash8(a.reshape(-1, a.shape[-1]))[0].reshape(a.shape) if l.get("keep8") else a
+        """What the backward pass sees of a layer's input: with keep8 its 8-bit form (of images: blocks of a pixel's channels)."""
+        if not l.get("keep8"):
+            return a
+        to, back = ((0, 2, 3, 1), (0, 3, 1, 2)) if a.ndim == 4 else (range(a.ndim), range(a.ndim))
+        t = a.transpose(to)
+        return lm_ops.stash8(t.reshape(-1, t.shape[-1]))[0].reshape(t.shape).transpose(back)
 
     def _qk(self, l, P, S):
         """Norm and rotation of queries and keys: () or (gains, arguments of lm_ops.norm_rope_forward)."""

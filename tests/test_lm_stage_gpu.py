@@ -85,6 +85,14 @@ def test_layers_with_kept_inputs(A, layers):
     check(encoder(layers(), B=3, M=1, S=17))
 
 
+@pytest.mark.parametrize("cin,c,hw", [(16, 24, 9), (8, 40, 12), (32, 64, 7)])
+def test_a_kept_gelu_between_convolutions(A, cin, c, hw):
+    """Images: a row is a pixel's channels."""
+    kept = dict(C.simple("gelu"), keep8=1)
+    for layers in ([C.conv(cin, c, 3, 1, 1, bias=True), kept, C.conv(c, cin, 3, 1, 1, bias=True)], [kept, C.conv(cin, c, 3, 1, 1, bias=True)]):
+        check(C.StageConfig("images", layers, 3, 2, (cin, hw, hw), "bf16", "nhwc", True, 78, init="normal0.02"))
+
+
 @pytest.mark.parametrize("kw", [dict(), dict(B=1, S=32, d=512, heads=8, ffn=2048, rows=100)])
 @pytest.mark.parametrize("K", [1, 2, 3])
 def test_bit_identical_however_it_runs(A, K, kw):
