@@ -488,8 +488,9 @@ void embedding_fwd(hipStream_t st, const int32_t* ids, int64_t tokens, const voi
 
 namespace {
 
-// Tokens that are placed by counting (it grows with their square, the passes hardly; the whole gradient of rows of 64, us, counting /
-// passes: 4096 tokens 19 / 33, 8192 28 / 37, 16384 44 / 42, 32768 122 / 42).
+// Tokens that are placed by counting (it grows with their square, the passes hardly; the whole gradient, added to, us, counting /
+// passes: 32768 rows of 512, 8192 tokens 28.7 / 38.5, 12288 38.8 / 45.2, 16384 48.7 / 50.3; 2000 rows of 64, 8192 23.8 / 31.4,
+// 12288 32.0 / 35.3, 16384 37.2 / 35.1; written, rows of 64, 16384 44 / 42, 32768 122 / 42).
 constexpr int64_t RANK_MOST = 16384;
 
 // Tokens of a wavefront: the chip filled, and no more than 8192 partials.  (65536 tokens of 1024: chunks of 32 187 us, of 16 192, of
