@@ -9,8 +9,8 @@
 // and 8 kept values a thread, requested one stage earlier and restored on the way into LDS, each once per block (a conversion, a
 // multiplication, half a byte permutation).  The operands of a step are read while the step in front of it is multiplied.
 //
-// 16384 rows, 4096 -> 4096: 475 us, 1160 TFLOP/s; the matrix cores are busy 63 % of the cycles, at a clock that they pull down
-// (a library's product of the same shape in bf16 takes 460 to 540).  4096 rows, 2048 -> 512: 22 us in four shares and 5.6 for
+// 16384 rows, 4096 -> 4096: 470 to 490 us, 1120 to 1170 TFLOP/s; the matrix cores are busy 63 % of the cycles, at a clock that they
+// pull down (a library's product of the same shape in bf16 takes 460 to 540).  4096 rows, 2048 -> 512: 22 us in four shares and 5.6 for
 // their sum; a step of 64 rows takes 0.75 us where its matrix instructions are 0.25: one wavefront to a vector unit waits for its
 // own LDS reads, conversions and products in turn (two groups of wavefronts in a block, each with half of the rows, were
 // no faster, nor were loads two or three stages ahead).  What a short launch runs once counts too: with the epilogue as branches
