@@ -81,28 +81,6 @@ template <typename T> struct Vec<T, 1> {
   static __device__ __forceinline__ void store(T* p, const float (&v)[1]) { store1(p, v[0]); }
 };
 
-// sum over the 2^ls lanes of a head, valid in each of them
-__device__ __forceinline__ float head_sum(float v, int ls) {
-  if (ls > 0) v += dpp_move<DPP_QUAD_SWAP1>(v);
-  if (ls > 1) v += dpp_move<DPP_QUAD_SWAP2>(v);
-  if (ls > 2) v += dpp_move<DPP_HALF_MIRROR>(v);
-  if (ls > 3) v += dpp_move<DPP_ROW_MIRROR>(v);
-  if (ls > 4) v += __shfl_xor(v, 16, 64);
-  if (ls > 5) v += __shfl_xor(v, 32, 64);
-  return v;
-}
-
-// ... and over the lanes that hold the same place of the wavefront's heads (rotations inside the rows of 16, then across them)
-__device__ __forceinline__ float places_sum(float v, int ls) {
-  if (ls < 4) v += dpp_move<0x128>(v);
-  if (ls < 3) v += dpp_move<0x124>(v);
-  if (ls < 2) v += dpp_move<0x122>(v);
-  if (ls < 1) v += dpp_move<0x121>(v);
-  if (ls < 5) v += __shfl_xor(v, 16, 64);
-  if (ls < 6) v += __shfl_xor(v, 32, 64);
-  return v;
-}
-
 // One lane's share of a head: IT units of 2 x VEC values.
 template <typename T, int VEC, int IT, bool INTER, bool BWD>
 __global__ __launch_bounds__(256, 4) void qk_norm_rope_kernel(const QkArgs g) {
@@ -228,9 +206,9 @@ __global__ __launch_bounds__(256, 4) void qk_norm_rope_kernel(const QkArgs g) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) dot += d[i][z][e] * gain[i][z][e] * x[i][z][e];
         }
-        dot = head_sum(dot, g.ls);
+        dot = row_sum(dot, g.ls);
       }
-      ss = head_sum(ss, g.ls);
+      ss = row_sum(ss, g.ls);
       const float r = rsqrtf(ss * g.inv_dim + g.eps);
       if (BWD) {
         const float m = r * r * dot * g.inv_dim;  // r mean(h n) = r^2 mean(h x)

@@ -1,0 +1,619 @@
+// Gated linear recurrence, forward and backward, one pass over the tokens each.
+//
+//   a = sigmoid(f),  h_t = a_t h_{t-1} + (1 - a_t) z_t,  y_t = h_t swish(o_t)
+//   G_t = dy_t swish(o_t) + K_{t+1},  K_t = a_t G_t      (G: the gradient that reaches h_t; K: what it passes on to h_{t-1})
+//   dz = (1 - a) G,  df = a (1 - a) (h_{t-1} - z) G,  do = dy h swish'(o)
+//
+// Both are scans of affine maps, x -> A x + U for a run of tokens, and bound by the bytes of the tokens' rows.  So the rows are read
+// once: a wavefront holds TOK tokens of 64 (fp32) or 128 (bf16) channels in registers, forms their map, learns what comes in
+// and finishes.  WAVES wavefronts of a block join their maps through LDS, blocks through the workspace:
+//
+//   a block leaves the map of its tokens in one 64-bit word a channel (A, U) as soon as it has it; 16 blocks in a row make a
+//   group, and the last of them leaves the value behind the group.  What comes in to a block is the value in front of its group and the
+//   maps of the group's earlier blocks, joined in their order: the result does not depend on which block ran when.
+//
+// A word is its own flag: the preparing launch fills them with a pattern that no map has, and a word is written once, by
+// one atomic store.  Blocks take their place in the chain from a counter when they start, so a block only waits for ones that
+// have started before it and wait for none behind them: every wait ends.
+// A run in which a sequence starts passes nothing through: its A is -0 (products with it stay -0, and none of a sequence's
+// infinities or NaN reach the next one).
+#include <algorithm>
+
+#include "ops.h"
+#include "ops_device.h"
+#include "prof.h"
+
+namespace ast {
+
+namespace {
+
+constexpr int WAVES = 8;
+constexpr int GROUP = 16;               // blocks of a chain whose maps are joined one by one
+constexpr int FWD_TOK = 16, BWD_TOK = 8;  // tokens of a wavefront: 48 and 32 registers of loads (16 bits: two channels a register)
+static_assert(BWD_TOK * WAVES == AST_RECURRENCE_CHUNK, "a block of the backward pass starts where a state was kept");
+static_assert(FWD_TOK * WAVES % AST_RECURRENCE_CHUNK == 0 && AST_RECURRENCE_CHUNK % FWD_TOK == 0, "kept states are a wavefront's first");
+
+constexpr uint32_t NOT_YET = 0xffffffffu;  // a NaN with a sign: maps are made without it
+
+struct Rows { const void* p; int64_t stride; };
+
+struct RecArgs {
+  Rows f, z, o, dy;             // o.p may be nullptr
+  void *y;                      // forward
+  void *df, *dz, *dgo;          // backward
+  int64_t df_stride, dz_stride, do_stride;
+  const float *state, *dfinal;  // [sequences][channels] or nullptr
+  float *final, *dstate;
+  float* saved;                 // state in front of every AST_RECURRENCE_CHUNK-th token
+  const int32_t* seq;           // a token's sequence, -1: none; nullptr: t / period
+  int64_t tokens, period;
+  unsigned long long *maps, *heads;  // the chain: [chunk][channels], [group][channels]; nullptr: chunks on their own
+  unsigned* counter;
+  int channels, columns, chunks;
+};
+
+template <typename T> struct Lane;  // consecutive channels of a lane, as they are loaded
+template <> struct Lane<float> {
+  static constexpr int V = 1;
+  static __device__ __forceinline__ uint32_t load(const float* p, bool) { return __float_as_uint(*p); }
+  static __device__ __forceinline__ void values(uint32_t w, float (&v)[1]) { v[0] = __uint_as_float(w); }
+  static __device__ __forceinline__ void store(float* p, bool, const float (&v)[1]) { *p = v[0]; }
+};
+struct __attribute__((packed, aligned(2))) Raw4 { uint32_t w; };
+template <> struct Lane<bf16_t> {
+  static constexpr int V = 2;
+  static __device__ __forceinline__ uint32_t load(const bf16_t* p, bool both) {
+    return both ? reinterpret_cast<const Raw4*>(p)->w : *p;
+  }
+  static __device__ __forceinline__ void values(uint32_t w, float (&v)[2]) {
+    v[0] = __uint_as_float(w << 16);
+    v[1] = __uint_as_float(w & 0xffff0000u);
+  }
+  static __device__ __forceinline__ void store(bf16_t* p, bool both, const float (&v)[2]) {
+    const uint32_t w = f2bf_pk(v[0], v[1]);
+    if (both) reinterpret_cast<Raw4*>(p)->w = w;
+    else *p = (bf16_t)w;
+  }
+};
+
+// exp(-|x|), within about 2^-22 of it for fp32 results (the rest of the product with log2 e is added behind the exponential:
+// 2^-24 of an argument of 20 would be 1e-6 of the result), with a product alone for bf16 results
+template <bool EXACT>
+__device__ __forceinline__ float exp_neg(float x) {
+  const float n = -fabsf(x), t = n * 1.44269504f;
+  const float e = __builtin_amdgcn_exp2f(t);
+  if (!EXACT) return e;
+  const float rest = fmaf(n, 1.44269504f, -t) + n * 1.925963033e-8f;  // (log2 e in two parts)
+  return n < -100.f ? 0.f : fmaf(e, rest * 0.69314718f, e);
+}
+// sigmoid(x) and 1 - sigmoid(x), each to its own relative precision; 0 and 1 at the infinities
+template <bool EXACT>
+__device__ __forceinline__ void gates(float x, float& a, float& b) {
+  const float e = exp_neg<EXACT>(x);
+  float r = __builtin_amdgcn_rcpf(1.f + e);
+  if (EXACT) r = fmaf(r, fmaf(-(1.f + e), r, 1.f), r);  // (a step of Newton's method: the reciprocal is good to an ulp)
+  const float s = e * r;
+  a = x >= 0.f ? r : s;
+  b = x >= 0.f ? s : r;
+}
+
+__device__ __forceinline__ bool cut(float A) { return (int)__float_as_uint(A) < 0; }  // nothing passes through
+// (A, U) behind (a, u): x -> A (a x + u) + U
+__device__ __forceinline__ void join(float& a, float& u, float A, float U) {
+  u = cut(A) ? U : fmaf(A, u, U);
+  a = cut(A) ? A : a * A;
+}
+
+__device__ __forceinline__ unsigned long long map_word(float A, float U) {
+  const uint32_t a = A != A ? 0x7fc00000u : __float_as_uint(A);
+  return (unsigned long long)__float_as_uint(U) << 32 | a;
+}
+__device__ __forceinline__ void leave(unsigned long long* p, unsigned long long w) {
+  __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ unsigned long long take(unsigned long long* p) {
+  unsigned long long w;
+  while ((uint32_t)(w = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == NOT_YET) __builtin_amdgcn_s_sleep(1);
+  return w;
+}
+
+// What a wavefront's tokens are (the same in all its lanes): bit i stands for token i.
+template <int TOK>
+struct Tokens {
+  unsigned live, start, last;  // belongs to a sequence; is its first; its last
+  int64_t t0;
+  int64_t seq0, left;          // by period: the sequence of token 0, and how far the sequence goes from there
+  __device__ __forceinline__ Tokens(const RecArgs& g, int64_t t) : live(0), start(0), last(0), t0(t), seq0(0), left(0) {
+    if (t0 >= g.tokens) return;
+    const int n = (int)min((int64_t)TOK, g.tokens - t0);
+    if (g.seq) {
+      int before = t0 > 0 ? g.seq[t0 - 1] : -1, at = g.seq[t0];
+#pragma unroll
+      for (int i = 0; i < TOK; ++i) {
+        if (i >= n) break;
+        const int next = t0 + i + 1 < g.tokens ? g.seq[t0 + i + 1] : -1;
+        if (at >= 0) {
+          live |= 1u << i;
+          if (at != before) start |= 1u << i;
+          if (at != next) last |= 1u << i;
+        }
+        before = at;
+        at = next;
+      }
+    } else {
+      live = n == 32 ? ~0u : (1u << n) - 1;
+      seq0 = t0 / g.period;
+      const int64_t into = t0 - seq0 * g.period;
+      left = g.period - into;
+      if (into == 0) start |= 1;
+      for (int64_t i = left; i < n; i += g.period) start |= 1u << i;
+      for (int64_t i = left - 1; i < n; i += g.period) last |= 1u << i;
+      if (t0 + n == g.tokens) last |= 1u << (n - 1);
+    }
+  }
+  __device__ __forceinline__ int64_t sequence(const RecArgs& g, int i) const {
+    if (g.seq) return g.seq[t0 + i];
+    return i < left ? seq0 : (t0 + i) / g.period;
+  }
+};
+
+// The value that comes in to a block whose place in the chain is `at` (in the order of the scan), for this lane's channels; all
+// threads of the block call it.  got: LDS [GROUP][64 V], head: LDS [64 V].
+template <int V>
+__device__ __forceinline__ void come_in(const RecArgs& g, int at, int c, int wave, int lane, float2 (*got)[64 * V], float* head,
+                                        float (&x)[V]) {
+  const int group = at / GROUP, r = at % GROUP;
+  const unsigned long long* const maps = g.maps + (int64_t)group * GROUP * g.channels;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    if (c + v >= g.channels) continue;
+    for (int j = wave; j < r; j += WAVES) {
+      const unsigned long long w = take(const_cast<unsigned long long*>(maps) + (int64_t)j * g.channels + c + v);
+      got[j][lane * V + v] = make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+    }
+    if (wave == WAVES - 1)
+      head[lane * V + v] = group == 0 ? 0.f : __uint_as_float((uint32_t)(take(g.heads + (int64_t)group * g.channels + c + v) >> 32));
+  }
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < V; ++v) x[v] = head[lane * V + v];
+  for (int j = 0; j < r; ++j)
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float2 m = got[j][lane * V + v];
+      x[v] = cut(m.x) ? m.y : fmaf(m.x, x[v], m.y);
+    }
+}
+// ... and what it leaves: its map (A, U), and behind the last block of a group, once x has come in, the value there
+template <int V>
+__device__ __forceinline__ void leave_map(const RecArgs& g, int at, int c, const float (&A)[V], const float (&U)[V]) {
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if (c + v < g.channels) leave(g.maps + (int64_t)at * g.channels + c + v, map_word(A[v], U[v]));
+}
+template <int V>
+__device__ __forceinline__ void leave_head(const RecArgs& g, int at, int c, const float (&A)[V], const float (&U)[V], const float (&x)[V]) {
+  if (at % GROUP != GROUP - 1 || at + 1 >= g.chunks) return;
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+    if (c + v < g.channels)
+      leave(g.heads + (int64_t)(at / GROUP + 1) * g.channels + c + v, map_word(0.f, cut(A[v]) ? U[v] : fmaf(A[v], x[v], U[v])));
+}
+
+// A block's place: in the order in which blocks start where they wait for each other.
+__device__ __forceinline__ unsigned place(const RecArgs& g) {
+  if (!g.maps) return blockIdx.x;
+  __shared__ unsigned p;
+  if (threadIdx.x == 0) p = atomicAdd(g.counter, 1u);
+  __syncthreads();
+  return p;
+}
+
+template <typename T, bool GATE>
+__global__ __launch_bounds__(64 * WAVES, 4) void recurrence_kernel(const RecArgs g) {
+  typedef Lane<T> L;
+  constexpr int V = L::V, TOK = FWD_TOK;
+  constexpr bool EXACT = sizeof(T) == 4;
+  __shared__ float2 mine[WAVES][64 * V];
+  __shared__ float2 got[GROUP][64 * V];
+  __shared__ float head[64 * V];
+  const unsigned p = place(g);
+  const int chunk = (int)(p / (unsigned)g.columns), column = (int)(p - (unsigned)chunk * (unsigned)g.columns);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = (column * 64 + lane) * V;
+  const bool on = c < g.channels, both = c + V <= g.channels;
+  const int64_t t0 = ((int64_t)chunk * WAVES + wave) * TOK;
+
+  uint32_t rf[TOK], rz[TOK], ro[GATE ? TOK : 1];
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    rf[i] = rz[i] = 0;
+    if (GATE) ro[GATE ? i : 0] = 0;
+    if (on && t0 + i < g.tokens) {
+      rf[i] = L::load(static_cast<const T*>(g.f.p) + (t0 + i) * g.f.stride + c, both);
+      rz[i] = L::load(static_cast<const T*>(g.z.p) + (t0 + i) * g.z.stride + c, both);
+      if (GATE) ro[GATE ? i : 0] = L::load(static_cast<const T*>(g.o.p) + (t0 + i) * g.o.stride + c, both);
+    }
+  }
+  const Tokens<TOK> tk(g, t0);
+  // the wavefront's map, token by token: value behind token i = P[i] x + H[i]
+  float P[TOK][V], H[TOK][V], A[V], U[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) A[v] = 1.f, U[v] = 0.f;
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    float f[V], z[V];
+    L::values(rf[i], f);
+    L::values(rz[i], z);
+    if (tk.start >> i & 1) {
+      const float* const s = g.state ? g.state + tk.sequence(g, i) * g.channels + c : nullptr;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        A[v] = -0.f;
+        U[v] = s && c + v < g.channels ? s[v] : 0.f;
+      }
+    }
+    if (tk.live >> i & 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float a, b;
+        gates<EXACT>(f[v], a, b);
+        U[v] = fmaf(a, U[v], b * z[v]);
+        A[v] *= a;
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) P[i][v] = A[v], H[i][v] = U[v];
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) mine[wave][lane * V + v] = make_float2(tk.start ? -0.f : A[v], U[v]);  // (a NaN gate is no way through)
+  __syncthreads();
+  // the block's map, and that of the wavefronts in front of this one
+  float pa[V], pu[V], x[V] = {};
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    A[v] = 1.f, U[v] = 0.f, pa[v] = 1.f, pu[v] = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float2 m = mine[w][lane * V + v];
+      if (w == wave) pa[v] = A[v], pu[v] = U[v];
+      join(A[v], U[v], m.x, m.y);
+    }
+  }
+  if (g.maps) {
+    if (wave == 0) leave_map<V>(g, chunk, c, A, U);
+    come_in<V>(g, chunk, c, wave, lane, got, head, x);
+    if (wave == 0) leave_head<V>(g, chunk, c, A, U, x);
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) x[v] = cut(pa[v]) ? pu[v] : fmaf(pa[v], x[v], pu[v]);
+  if (g.saved && on && t0 < g.tokens && t0 % AST_RECURRENCE_CHUNK == 0) {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (c + v < g.channels) g.saved[t0 / AST_RECURRENCE_CHUNK * g.channels + c + v] = x[v];
+  }
+  bool through = true;  // what came in reaches the token
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    if (tk.start >> i & 1) through = false;
+    if (!(tk.live >> i & 1) || !on) continue;
+    float h[V], y[V], o[V];
+    if (GATE) L::values(ro[GATE ? i : 0], o);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      h[v] = through ? fmaf(P[i][v], x[v], H[i][v]) : H[i][v];
+      y[v] = h[v];
+      if (GATE) {
+        float a, b;
+        gates<EXACT>(o[v], a, b);
+        y[v] *= o[v] * a;
+      }
+    }
+    L::store(static_cast<T*>(g.y) + (t0 + i) * g.channels + c, both, y);
+    if (g.final && (tk.last >> i & 1)) {
+      float* const s = g.final + tk.sequence(g, i) * g.channels + c;
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (c + v < g.channels) s[v] = h[v];
+    }
+  }
+}
+
+template <typename T, bool GATE>
+__global__ __launch_bounds__(64 * WAVES, 4) void recurrence_bwd_kernel(const RecArgs g) {
+  typedef Lane<T> L;
+  constexpr int V = L::V, TOK = BWD_TOK;
+  constexpr bool EXACT = sizeof(T) == 4;
+  __shared__ float2 mine[WAVES][64 * V];
+  __shared__ float mine_k[WAVES][64 * V];
+  __shared__ float2 got[GROUP][64 * V];
+  __shared__ float head[64 * V];
+  const unsigned p = place(g);
+  const int at = (int)(p / (unsigned)g.columns), column = (int)(p - (unsigned)at * (unsigned)g.columns);
+  const int chunk = g.chunks - 1 - at;  // (the scan runs from the last token to the first)
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c = (column * 64 + lane) * V;
+  const bool on = c < g.channels, both = c + V <= g.channels;
+  const int64_t t0 = ((int64_t)chunk * WAVES + wave) * TOK;
+
+  uint32_t rf[TOK], rz[TOK], rd[TOK], ro[GATE ? TOK : 1];
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    rf[i] = rz[i] = rd[i] = 0;
+    if (GATE) ro[GATE ? i : 0] = 0;
+    if (on && t0 + i < g.tokens) {
+      rf[i] = L::load(static_cast<const T*>(g.f.p) + (t0 + i) * g.f.stride + c, both);
+      rd[i] = L::load(static_cast<const T*>(g.dy.p) + (t0 + i) * g.dy.stride + c, both);
+      if (GATE) ro[GATE ? i : 0] = L::load(static_cast<const T*>(g.o.p) + (t0 + i) * g.o.stride + c, both);
+      rz[i] = L::load(static_cast<const T*>(g.z.p) + (t0 + i) * g.z.stride + c, both);
+    }
+  }
+  float h[V];  // the state in front of the block
+#pragma unroll
+  for (int v = 0; v < V; ++v) h[v] = c + v < g.channels ? g.saved[(int64_t)chunk * g.channels + c + v] : 0.f;
+  const Tokens<TOK> tk(g, t0);
+
+  // forwards: the gates, the map of the states, the gradients at the tokens
+  float a[TOK][V], b[TOK][V], d[TOK][V], q[GATE ? TOK : 1][V], A[V], U[V], K[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) A[v] = 1.f, U[v] = 0.f;
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    float f[V], z[V], o[V];
+    L::values(rf[i], f);
+    L::values(rz[i], z);
+    L::values(rd[i], d[i]);
+    if (GATE) L::values(ro[GATE ? i : 0], o);
+    if (tk.start >> i & 1) {
+      const float* const s = g.state ? g.state + tk.sequence(g, i) * g.channels + c : nullptr;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        A[v] = -0.f;
+        U[v] = s && c + v < g.channels ? s[v] : 0.f;
+      }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      gates<EXACT>(f[v], a[i][v], b[i][v]);
+      if (GATE) {
+        float s, n;
+        gates<EXACT>(o[v], s, n);
+        q[GATE ? i : 0][v] = d[i][v] * fmaf(o[v] * s, n, s);  // dy swish'(o)
+        d[i][v] *= o[v] * s;
+      }
+    }
+    if (tk.live >> i & 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        U[v] = fmaf(a[i][v], U[v], b[i][v] * z[v]);
+        A[v] *= a[i][v];
+      }
+    }
+  }
+  // backwards: what the tokens pass on to the ones in front of them, without what comes in from behind
+#pragma unroll
+  for (int v = 0; v < V; ++v) K[v] = 0.f;
+#pragma unroll
+  for (int i = TOK - 1; i >= 0; --i) {
+    if (!(tk.live >> i & 1)) continue;
+    if (tk.last >> i & 1) {
+      const float* const s = g.dfinal ? g.dfinal + tk.sequence(g, i) * g.channels + c : nullptr;
+#pragma unroll
+      for (int v = 0; v < V; ++v) K[v] = s && c + v < g.channels ? s[v] : 0.f;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) K[v] = tk.start >> i & 1 ? 0.f : a[i][v] * (d[i][v] + K[v]);
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    mine[wave][lane * V + v] = make_float2(tk.start ? -0.f : A[v], U[v]);  // (a NaN gate is no way through)
+    mine_k[wave][lane * V + v] = K[v];
+  }
+  __syncthreads();
+  // the block's map of K, and that of the wavefronts behind this one; the state in front of this wavefront
+  float pa[V], pu[V], x[V] = {};
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    A[v] = 1.f, K[v] = 0.f, pa[v] = 1.f, pu[v] = 0.f;
+#pragma unroll
+    for (int w = WAVES - 1; w >= 0; --w) {
+      const float m = mine[w][lane * V + v].x;
+      if (w == wave) pa[v] = A[v], pu[v] = K[v];
+      join(A[v], K[v], m, mine_k[w][lane * V + v]);
+    }
+  }
+  if (g.maps && wave == 0) leave_map<V>(g, at, c, A, K);
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w) {
+      const float2 m = mine[w][lane * V + v];
+      if (w < wave) h[v] = cut(m.x) ? m.y : fmaf(m.x, h[v], m.y);
+    }
+  // forwards again, with the states: the output gate's gradient; hz: h_{t-1} - z
+  float hz[TOK][V];
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    float z[V], e[V];
+    L::values(rz[i], z);
+    if (tk.start >> i & 1) {
+      const float* const s = g.state ? g.state + tk.sequence(g, i) * g.channels + c : nullptr;
+#pragma unroll
+      for (int v = 0; v < V; ++v) h[v] = s && c + v < g.channels ? s[v] : 0.f;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      hz[i][v] = h[v] - z[v];
+      if (tk.live >> i & 1) h[v] = fmaf(a[i][v], h[v], b[i][v] * z[v]);
+      if (GATE) e[v] = q[GATE ? i : 0][v] * h[v];
+    }
+    if (GATE && on && (tk.live >> i & 1)) L::store(static_cast<T*>(g.dgo) + (t0 + i) * g.do_stride + c, both, e);
+  }
+  if (g.maps) {
+    come_in<V>(g, at, c, wave, lane, got, head, x);
+    if (wave == 0) leave_head<V>(g, at, c, A, K, x);
+  }
+#pragma unroll
+  for (int v = 0; v < V; ++v) x[v] = cut(pa[v]) ? pu[v] : fmaf(pa[v], x[v], pu[v]);
+  // and backwards with what comes in
+#pragma unroll
+  for (int i = TOK - 1; i >= 0; --i) {
+    if (!(tk.live >> i & 1)) continue;
+    const bool first = tk.start >> i & 1;
+    if (tk.last >> i & 1) {
+      const float* const s = g.dfinal ? g.dfinal + tk.sequence(g, i) * g.channels + c : nullptr;
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[v] = s && c + v < g.channels ? s[v] : 0.f;
+    }
+    float df[V], dz[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const float G = d[i][v] + x[v];
+      dz[v] = b[i][v] * G;
+      df[v] = a[i][v] * hz[i][v] * dz[v];
+      x[v] = a[i][v] * G;
+    }
+    if (on) {
+      L::store(static_cast<T*>(g.df) + (t0 + i) * g.df_stride + c, both, df);
+      L::store(static_cast<T*>(g.dz) + (t0 + i) * g.dz_stride + c, both, dz);
+    }
+    if (first) {
+      if (g.dstate) {
+        float* const s = g.dstate + tk.sequence(g, i) * g.channels + c;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+          if (c + v < g.channels) s[v] = x[v];
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[v] = 0.f;
+    }
+  }
+}
+
+// In front of a scan: the words of its chain and its counter, the tokens' sequences, and what comes out of sequences without
+// tokens (copied, or 0 where nothing is passed in).
+__global__ __launch_bounds__(256) void recurrence_prepare_kernel(unsigned long long* words, int64_t n_words, unsigned* counter,
+                                                                 const int32_t* offsets, int64_t sequences, int64_t tokens,
+                                                                 int32_t* seq, const float* in, float* out, int channels) {
+  const int64_t me = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)gridDim.x * 256;
+  if (me == 0 && counter) *counter = 0;
+  for (int64_t i = me; i < n_words; i += all) words[i] = ~0ull;
+  if (!offsets) return;
+  const int32_t first = offsets[0], end = offsets[sequences];
+  for (int64_t t = me; t < tokens; t += all) {  // the last sequence that begins at the token or in front of it
+    int64_t lo = 0, hi = sequences;             // offsets[lo] <= t < offsets[hi]
+    if (t < first || t >= end) {
+      seq[t] = -1;
+      continue;
+    }
+    while (hi - lo > 1) {
+      const int64_t mid = (lo + hi) / 2;
+      if (offsets[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    seq[t] = (int32_t)lo;
+  }
+  if (!out) return;
+  const int64_t wave = me >> 6, waves = all >> 6;
+  for (int64_t s = wave; s < sequences; s += waves) {
+    if (offsets[s] != offsets[s + 1]) continue;
+    for (int64_t c = threadIdx.x & 63; c < channels; c += 64) out[s * channels + c] = in ? in[s * channels + c] : 0.f;
+  }
+}
+
+// The workspace: words of the chain, the counter, the tokens' sequences.
+struct Layout { size_t maps, heads, counter, seq, end; int64_t words; int chunks, columns; bool chained; };
+Layout layout_of(const ast_recurrence_cfg& c, int tok) {
+  Layout l = {};
+  const int per = tok * WAVES, width = 64 * (c.dtype == AST_F32 ? 1 : 2);
+  l.chunks = (int)((c.tokens + per - 1) / per);
+  l.columns = (int)((c.channels + width - 1) / width);
+  // (chunks that each begin with a sequence's first token need nothing from each other)
+  l.chained = l.chunks > 1 && (c.offsets_dev || per % c.period != 0);
+  size_t at = 0;
+  if (l.chained) {
+    l.words = ((int64_t)l.chunks + (l.chunks + GROUP - 1) / GROUP) * c.channels;
+    l.heads = (size_t)l.chunks * c.channels * 8;
+    at = l.counter = (size_t)l.words * 8;
+    at += 16;
+  }
+  l.seq = at;
+  if (c.offsets_dev) at += ((size_t)c.tokens * 4 + 15) / 16 * 16;
+  l.end = at;
+  return l;
+}
+
+void prepare(hipStream_t st, const ast_recurrence_cfg& c, const Layout& l, void* ws, const float* in, float* out, RecArgs& g) {
+  char* const w = static_cast<char*>(ws);
+  g.tokens = c.tokens;
+  g.period = c.period;
+  g.channels = (int)c.channels;
+  g.columns = l.columns;
+  g.chunks = l.chunks;
+  if (l.chained) {
+    g.maps = reinterpret_cast<unsigned long long*>(w + l.maps);
+    g.heads = reinterpret_cast<unsigned long long*>(w + l.heads);
+    g.counter = reinterpret_cast<unsigned*>(w + l.counter);
+  }
+  if (c.offsets_dev) g.seq = reinterpret_cast<int32_t*>(w + l.seq);
+  if (!l.chained && !c.offsets_dev) return;
+  const int64_t most = std::max<int64_t>({l.words / 4, c.offsets_dev ? c.tokens : 0, c.offsets_dev && out ? 64 * c.sequences : 0, 1});
+  KLAUNCH(recurrence_prepare_kernel, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 2048)), dim3(256), 0, st, g.maps, l.words,
+          g.counter, c.offsets_dev, c.sequences, c.tokens, reinterpret_cast<int32_t*>(w + l.seq), in, out, (int)c.channels);
+}
+
+}  // namespace
+
+size_t recurrence_ws_bytes(const ast_recurrence_cfg& c) {
+  return std::max(layout_of(c, FWD_TOK).end, layout_of(c, BWD_TOK).end);
+}
+
+void recurrence_fwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows& f, const ast_rows& z, const ast_rows* o,
+                    const float* state, void* y, float* final, float* saved, void* ws) {
+  const Layout l = layout_of(c, FWD_TOK);
+  RecArgs g = {};
+  g.f = {f.dev, f.stride};
+  g.z = {z.dev, z.stride};
+  if (o) g.o = {o->dev, o->stride};
+  g.state = state;
+  g.y = y;
+  g.final = final;
+  g.saved = saved;
+  prepare(st, c, l, ws, state, final, g);
+  if (l.chunks == 0) return;
+  const dim3 grid((unsigned)l.chunks * (unsigned)l.columns), block(64 * WAVES);
+  auto go = [&](auto kernel) { KLAUNCH_NAMED("recurrence_kernel", kernel, grid, block, 0, st, g); };
+  if (c.dtype == AST_F32) go(o ? recurrence_kernel<float, true> : recurrence_kernel<float, false>);
+  else go(o ? recurrence_kernel<bf16_t, true> : recurrence_kernel<bf16_t, false>);
+}
+
+void recurrence_bwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows& dy, const ast_rows& f, const ast_rows& z,
+                    const ast_rows* o, const float* state, const float* saved, const float* dfinal, const ast_rows& df,
+                    const ast_rows& dz, const ast_rows* dgo, float* dstate, void* ws) {
+  const Layout l = layout_of(c, BWD_TOK);
+  RecArgs g = {};
+  g.f = {f.dev, f.stride};
+  g.z = {z.dev, z.stride};
+  if (o) g.o = {o->dev, o->stride};
+  g.dy = {dy.dev, dy.stride};
+  g.df = const_cast<void*>(df.dev);
+  g.dz = const_cast<void*>(dz.dev);
+  g.df_stride = df.stride;
+  g.dz_stride = dz.stride;
+  if (dgo) {
+    g.dgo = const_cast<void*>(dgo->dev);
+    g.do_stride = dgo->stride;
+  }
+  g.state = state;
+  g.saved = const_cast<float*>(saved);
+  g.dfinal = dfinal;
+  g.dstate = dstate;
+  prepare(st, c, l, ws, dfinal, dstate, g);
+  if (l.chunks == 0) return;
+  const dim3 grid((unsigned)l.chunks * (unsigned)l.columns), block(64 * WAVES);
+  auto go = [&](auto kernel) { KLAUNCH_NAMED("recurrence_bwd_kernel", kernel, grid, block, 0, st, g); };
+  if (c.dtype == AST_F32) go(o ? recurrence_bwd_kernel<float, true> : recurrence_bwd_kernel<float, false>);
+  else go(o ? recurrence_bwd_kernel<bf16_t, true> : recurrence_bwd_kernel<bf16_t, false>);
+}
+
+}  // namespace ast

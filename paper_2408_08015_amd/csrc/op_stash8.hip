@@ -22,10 +22,6 @@ namespace {
 
 __device__ __forceinline__ float scale_of(uint8_t b) { return __uint_as_float((uint32_t)b << 23); }
 
-__device__ __forceinline__ uint32_t code(float steps) {
-  return (uint32_t)(int)rintf(fminf(fmaxf(steps, -127.f), 127.f)) & 0xffu;
-}
-
 __device__ __forceinline__ void restore8(uint2 q, float s, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -45,25 +41,10 @@ __global__ __launch_bounds__(256) void stash8_pack_kernel(const T* __restrict__ 
     float v[8];
     if (c < cols) load8_row<T, EVEN>(x + r * cols, c, cols, v);
     else load8_part(x, 0, v);
-    uint32_t top = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
-    // maximum over the block's four lanes, as bits (those of a NaN are above all others)
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, DPP_QUAD_SWAP1, 0xF, 0xF, true));
-    top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, DPP_QUAD_SWAP2, 0xF, 0xF, true));
-    const bool finite = top < 0x7f800000u;
-    const int e = min(max((int)((top + 0x01ffffu) >> 23) - 127 - 6, -126), 121);
-    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-    uint2 w = make_uint2(0, 0);
-    if (finite) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        w.x |= code(v[k] * inv) << (8 * k);
-        w.y |= code(v[4 + k] * inv) << (8 * k);
-      }
-    }
+    uint2 w;
+    const uint8_t scale = stash8_block(v, w);
     *reinterpret_cast<uint2*>(q + r * pitch + c) = w;
-    if ((threadIdx.x & 3) == 0) scales[r * (pitch / kStash8Block) + c / kStash8Block] = (uint8_t)(finite ? e + 127 : 255);
+    if ((threadIdx.x & 3) == 0) scales[r * (pitch / kStash8Block) + c / kStash8Block] = scale;
   }
 }
 

@@ -25,6 +25,28 @@ void qk_norm_rope_bwd(hipStream_t st, const ast_qk_cfg& c, const ast_heads& dyq,
                       const ast_heads& k, const float* gq, const float* gk, const ast_heads& dq, const ast_heads& dk,
                       float* dgq, float* dgk, bool accumulate, void* ws);
 
+// ---- RMS norm with the residual's addition (op_rms_norm.hip)
+void rms_norm_fwd(hipStream_t st, const ast_norm_cfg& c, const void* x, const void* residual, const float* gain, void* y,
+                  void* sum, void* stash);
+size_t rms_norm_bwd_ws_bytes(int64_t rows, int64_t width);
+void rms_norm_bwd(hipStream_t st, const ast_norm_cfg& c, const void* dy, const void* sum, const float* gain, const void* dsum,
+                  void* dx, void* ds, float* dgain, bool accumulate, void* ws);
+
+// ---- gated linear recurrence (op_recurrence.hip)
+size_t recurrence_ws_bytes(const ast_recurrence_cfg& c);
+void recurrence_fwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows& f, const ast_rows& z, const ast_rows* o,
+                    const float* state, void* y, float* final, float* saved, void* ws);
+void recurrence_bwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows& dy, const ast_rows& f, const ast_rows& z,
+                    const ast_rows* o, const float* state, const float* saved, const float* dfinal, const ast_rows& df,
+                    const ast_rows& dz, const ast_rows* dgo, float* dstate, void* ws);
+
+// ---- distillation from a teacher's top logits (op_distill.hip)
+void distill_fwd(hipStream_t st, const ast_distill_cfg& c, const void* z, const int32_t* ids, const void* t, float* loss, float* stats);
+void distill_bwd(hipStream_t st, const ast_distill_cfg& c, const float* dloss, const void* z, const int32_t* ids, const void* t,
+                 const float* stats, void* dz, int64_t dz_stride);
+void distill_step(hipStream_t st, const ast_distill_cfg& c, const float* dloss, const void* z, const int32_t* ids, const void* t,
+                  float* loss, void* dz, int64_t dz_stride);
+
 // ---- activations kept in 8 bits (op_stash8.hip, op_stash8_wgrad.hip)
 constexpr int kStash8Block = 32;  // values that share a scale
 inline int64_t stash8_pitch(int64_t cols) { return (cols + kStash8Block - 1) / kStash8Block * kStash8Block; }

@@ -78,6 +78,84 @@ const char* heads_apart(const ast_qk_cfg& c, const ast_heads& h) {
   return head_inner || token_inner ? nullptr : "the heads of an output overlap";
 }
 
+
+// ranges of bytes that lie on each other (NULL lies on nothing)
+bool overlap(const void* p, size_t n, const void* q, size_t m) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a && b && a < b + m && b < a + n;
+}
+
+const char* norm_cfg(const ast_norm_cfg* c) {
+  if (!c) return "cfg is NULL";
+  if (!dtype_ok(c->dtype) || !dtype_ok(c->sum_dtype)) return "unknown dtype";
+  if (c->sum_dtype != c->dtype && c->sum_dtype != AST_F32) return "sum_dtype must be dtype or AST_F32";
+  if (c->rows < 0 || c->rows > kMostRows) return "rows must lie in [0, 2^31)";
+  if (c->width < 1 || c->width > 16384) return "width must lie in [1, 16384]";
+  if (!(c->eps > 0.f) || !std::isfinite(c->eps)) return "eps must be positive";
+  return nullptr;
+}
+
+const char* recurrence_cfg(const ast_recurrence_cfg* c) {
+  if (!c) return "cfg is NULL";
+  if (!dtype_ok(c->dtype)) return "unknown dtype";
+  if (c->tokens < 0 || c->tokens > kMostRows) return "tokens must lie in [0, 2^31)";
+  if (c->channels < 1 || c->channels > kMostWidth) return "channels must lie in [1, 2^20]";
+  if (c->tokens * c->channels >= (int64_t)1 << 40) return "tokens * channels must stay below 2^40";
+  if (c->offsets_dev) {
+    if (!aligned(c->offsets_dev, 4)) return "offsets_dev must be 4-byte aligned";
+    if (c->sequences < 0 || c->sequences > kMostRows - 1) return "sequences must lie in [0, 2^31 - 2]";
+  } else if (c->period < 1 || c->period > kMostRows) {
+    return "offsets_dev, or a period in [1, 2^31), must be given";
+  }
+  return nullptr;
+}
+
+const char* rows_ok(const ast_recurrence_cfg& c, const ast_rows* r, bool out) {
+  if (!r) return "a tensor is NULL";
+  if (r->stride < 0 || r->stride > (int64_t)1 << 40) return "strides must lie in [0, 2^40]";
+  if (c.tokens > 0 && (!r->dev || !aligned(r->dev, esize(c.dtype)))) return "tensors must be non-NULL and aligned to their element size";
+  if (out && c.tokens > 1 && r->stride < c.channels) return "the rows of an output overlap";
+  return nullptr;
+}
+// two outputs of which rows lie on each other (with different strides: of which the ranges do)
+bool rows_meet(const ast_recurrence_cfg& c, const ast_rows& p, const ast_rows& q) {
+  if (c.tokens == 0) return false;
+  const int64_t e = (int64_t)esize(c.dtype);
+  auto span = [&](const ast_rows& r) { return (size_t)(((c.tokens - 1) * r.stride + c.channels) * e); };
+  if (!overlap(p.dev, span(p), q.dev, span(q))) return false;
+  if (p.stride != q.stride || c.tokens == 1) return true;
+  const int64_t step = p.stride * e, wide = c.channels * e;
+  int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(q.dev) - reinterpret_cast<uintptr_t>(p.dev)) % step;
+  if (apart < 0) apart += step;
+  return apart < wide || step - apart < wide;
+}
+
+const char* distill_cfg(const ast_distill_cfg* c) {
+  if (!c) return "cfg is NULL";
+  if (!dtype_ok(c->dtype) || !dtype_ok(c->teacher_dtype)) return "unknown dtype";
+  if (c->rows < 0 || c->rows > kMostRows) return "rows must lie in [0, 2^31)";
+  if (c->vocab < 1 || c->vocab > (int64_t)1 << 30) return "vocab must lie in [1, 2^30]";
+  if (c->logits_stride < c->vocab || c->logits_stride > (int64_t)1 << 31) return "logits_stride must lie in [vocab, 2^31]";
+  if (c->entries < 1 || c->entries > 1024) return "entries must lie in [1, 1024]";
+  if (!(c->temperature > 0.f) || !std::isfinite(c->temperature)) return "temperature must be positive";
+  if (!(c->label_weight >= 0.f && c->label_weight <= 1.f)) return "label_weight must lie in [0, 1]";
+  if (!c->labels_dev && c->label_weight != 0.f) return "a label_weight needs labels";
+  if (!aligned(c->labels_dev, 4)) return "labels_dev must be 4-byte aligned";
+  return nullptr;
+}
+const char* distill_inputs(const ast_distill_cfg& c, const void* z, const int32_t* ids, const void* t) {
+  if (!z || !ids || !t) return "NULL argument";
+  if (!aligned(z, esize(c.dtype)) || !aligned(ids, 4) || !aligned(t, esize(c.teacher_dtype))) return "buffers must be aligned to their element size";
+  return nullptr;
+}
+const char* distill_gradient(const ast_distill_cfg& c, const float* dloss, const void* z, const void* dz, int64_t stride) {
+  if (!dloss || !dz) return "NULL argument";
+  if (!aligned(dloss, 4) || !aligned(dz, esize(c.dtype))) return "buffers must be aligned to their element size";
+  if (stride < c.vocab || stride > (int64_t)1 << 31) return "dlogits_stride must lie in [vocab, 2^31]";
+  if (z == dz && stride != c.logits_stride) return "a gradient in place of the logits needs their stride";
+  return nullptr;
+}
+
 }  // namespace
 
 extern "C" {
@@ -172,6 +250,151 @@ ast_status asteroid_qk_norm_rope_backward(const ast_qk_cfg* cfg, const ast_heads
   if (cfg->tokens > 0 && dq->dev == dk->dev) return fail(fn, "dq and dk are one tensor");
   ast::qk_norm_rope_bwd(stream_of(hip_stream), *cfg, *dyq, *dyk, *q, *k, q_gain_dev, k_gain_dev, *dq, *dk, dq_gain_dev, dk_gain_dev,
                         accumulate != 0, workspace_dev);
+  return launched(fn);
+}
+
+ast_status asteroid_rms_norm_forward(const ast_norm_cfg* cfg, const void* x_dev, const void* residual_dev, const float* gain_dev,
+                                     void* y_dev, void* sum_dev, void* stash_dev, void* hip_stream) {
+  const char* const fn = "rms_norm_forward";
+  if (const char* e = norm_cfg(cfg)) return fail(fn, e);
+  if (!residual_dev != !sum_dev) return fail(fn, "the residual and the sum go together");
+  if (!residual_dev && cfg->sum_dtype != cfg->dtype && cfg->rows > 0) return fail(fn, "without a residual the sum is x: sum_dtype must be dtype");
+  if (cfg->rows == 0) return AST_OK;
+  if (!x_dev || !gain_dev || !y_dev) return fail(fn, "NULL argument");
+  if (!aligned(x_dev, esize(cfg->dtype)) || !aligned(y_dev, esize(cfg->dtype)) || !aligned(residual_dev, esize(cfg->sum_dtype)) ||
+      !aligned(sum_dev, esize(cfg->sum_dtype)) || !aligned(gain_dev, 4) || !aligned(stash_dev, 16))
+    return fail(fn, "buffers must be aligned to their element size, the stash to 16 bytes");
+  const size_t n = (size_t)cfg->rows * (size_t)cfg->width, ny = n * esize(cfg->dtype), ns = n * esize(cfg->sum_dtype);
+  const size_t nk = ast::stash8_bytes(cfg->rows, cfg->width);
+  if (overlap(y_dev, ny, sum_dev, ns) || overlap(y_dev, ny, stash_dev, nk) || overlap(sum_dev, ns, stash_dev, nk)) return fail(fn, "outputs overlap");
+  ast::rms_norm_fwd(stream_of(hip_stream), *cfg, x_dev, residual_dev, gain_dev, y_dev, sum_dev, stash_dev);
+  return launched(fn);
+}
+
+ast_status asteroid_rms_norm_backward_workspace(const ast_norm_cfg* cfg, size_t* bytes) {
+  const char* const fn = "rms_norm_backward_workspace";
+  if (!bytes) return fail(fn, "NULL argument");
+  if (const char* e = norm_cfg(cfg)) return fail(fn, e);
+  *bytes = ast::rms_norm_bwd_ws_bytes(cfg->rows, cfg->width);
+  return AST_OK;
+}
+
+ast_status asteroid_rms_norm_backward(const ast_norm_cfg* cfg, const void* dy_dev, const void* sum_dev, const float* gain_dev,
+                                      const void* dsum_dev, void* dx_dev, void* ds_dev, float* dgain_dev, int32_t accumulate,
+                                      void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  const char* const fn = "rms_norm_backward";
+  if (const char* e = norm_cfg(cfg)) return fail(fn, e);
+  if (!gain_dev || !dgain_dev || !aligned(gain_dev, 4) || !aligned(dgain_dev, 4))
+    return fail(fn, "the gain and its gradient must be non-NULL and 4-byte aligned");
+  if (cfg->rows > 0) {
+    if (!dy_dev || !sum_dev) return fail(fn, "NULL argument");
+    if (!dx_dev && !ds_dev) return fail(fn, "dx_dev or ds_dev must be given");
+    if (!aligned(dy_dev, esize(cfg->dtype)) || !aligned(dx_dev, esize(cfg->dtype)) || !aligned(sum_dev, esize(cfg->sum_dtype)) ||
+        !aligned(dsum_dev, esize(cfg->sum_dtype)) || !aligned(ds_dev, esize(cfg->sum_dtype)))
+      return fail(fn, "buffers must be aligned to their element size");
+    const size_t n = (size_t)cfg->rows * (size_t)cfg->width;
+    if (overlap(dx_dev, n * esize(cfg->dtype), ds_dev, n * esize(cfg->sum_dtype)) ||
+        overlap(dgain_dev, 4 * (size_t)cfg->width, dx_dev, n * esize(cfg->dtype)) ||
+        overlap(dgain_dev, 4 * (size_t)cfg->width, ds_dev, n * esize(cfg->sum_dtype)))
+      return fail(fn, "outputs overlap");
+  }
+  const size_t need = ast::rms_norm_bwd_ws_bytes(cfg->rows, cfg->width);
+  if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
+    return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  ast::rms_norm_bwd(stream_of(hip_stream), *cfg, dy_dev, sum_dev, gain_dev, dsum_dev, dx_dev, ds_dev, dgain_dev, accumulate != 0,
+                    workspace_dev);
+  return launched(fn);
+}
+
+ast_status asteroid_recurrence_workspace(const ast_recurrence_cfg* cfg, size_t* bytes) {
+  const char* const fn = "recurrence_workspace";
+  if (!bytes) return fail(fn, "NULL argument");
+  if (const char* e = recurrence_cfg(cfg)) return fail(fn, e);
+  *bytes = ast::recurrence_ws_bytes(*cfg);
+  return AST_OK;
+}
+
+ast_status asteroid_recurrence_forward(const ast_recurrence_cfg* cfg, const ast_rows* f, const ast_rows* z, const ast_rows* o,
+                                       const float* state_dev, void* y_dev, float* final_dev, float* saved_dev,
+                                       void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  const char* const fn = "recurrence_forward";
+  if (const char* e = recurrence_cfg(cfg)) return fail(fn, e);
+  for (const ast_rows* r : {f, z, o ? o : z})
+    if (const char* e = rows_ok(*cfg, r, false)) return fail(fn, e);
+  if (!aligned(state_dev, 4) || !aligned(final_dev, 4) || !aligned(saved_dev, 4)) return fail(fn, "states must be 4-byte aligned");
+  if (cfg->tokens > 0) {
+    if (!y_dev || !aligned(y_dev, esize(cfg->dtype))) return fail(fn, "y_dev must be non-NULL and aligned to its element size");
+    const int64_t sequences = cfg->offsets_dev ? cfg->sequences : (cfg->tokens + cfg->period - 1) / cfg->period;
+    const size_t ny = (size_t)(cfg->tokens * cfg->channels) * esize(cfg->dtype), nf = 4 * (size_t)sequences * (size_t)cfg->channels;
+    const size_t ns = 4 * (size_t)((cfg->tokens + AST_RECURRENCE_CHUNK - 1) / AST_RECURRENCE_CHUNK) * (size_t)cfg->channels;
+    if (overlap(y_dev, ny, final_dev, nf) || overlap(y_dev, ny, saved_dev, ns) || overlap(final_dev, nf, saved_dev, ns)) return fail(fn, "outputs overlap");
+  }
+  const size_t need = ast::recurrence_ws_bytes(*cfg);
+  if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
+    return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  ast::recurrence_fwd(stream_of(hip_stream), *cfg, *f, *z, o, state_dev, y_dev, final_dev, saved_dev, workspace_dev);
+  return launched(fn);
+}
+
+ast_status asteroid_recurrence_backward(const ast_recurrence_cfg* cfg, const ast_rows* dy, const ast_rows* f, const ast_rows* z,
+                                        const ast_rows* o, const float* state_dev, const float* saved_dev,
+                                        const float* dfinal_dev, const ast_rows* df, const ast_rows* dz, const ast_rows* dgo,
+                                        float* dstate_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  const char* const fn = "recurrence_backward";
+  if (const char* e = recurrence_cfg(cfg)) return fail(fn, e);
+  if (!o != !dgo) return fail(fn, "o and its gradient go together");
+  for (const ast_rows* r : {dy, f, z, o ? o : z})
+    if (const char* e = rows_ok(*cfg, r, false)) return fail(fn, e);
+  for (const ast_rows* r : {df, dz, dgo ? dgo : dz})
+    if (const char* e = rows_ok(*cfg, r, true)) return fail(fn, e);
+  if (rows_meet(*cfg, *df, *dz) || (dgo && (rows_meet(*cfg, *df, *dgo) || rows_meet(*cfg, *dz, *dgo)))) return fail(fn, "outputs overlap");
+  if (cfg->tokens > 0 && !saved_dev) return fail(fn, "saved_dev is NULL");
+  if (!aligned(state_dev, 4) || !aligned(saved_dev, 4) || !aligned(dfinal_dev, 4) || !aligned(dstate_dev, 4))
+    return fail(fn, "states must be 4-byte aligned");
+  const size_t need = ast::recurrence_ws_bytes(*cfg);
+  if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
+    return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  ast::recurrence_bwd(stream_of(hip_stream), *cfg, *dy, *f, *z, o, state_dev, saved_dev, dfinal_dev, *df, *dz, dgo, dstate_dev,
+                      workspace_dev);
+  return launched(fn);
+}
+
+ast_status asteroid_distill_forward(const ast_distill_cfg* cfg, const void* logits_dev, const int32_t* ids_dev, const void* teacher_dev,
+                                    float* loss_dev, float* stats_dev, void* hip_stream) {
+  const char* const fn = "distill_forward";
+  if (const char* e = distill_cfg(cfg)) return fail(fn, e);
+  if (cfg->rows == 0) return AST_OK;
+  if (const char* e = distill_inputs(*cfg, logits_dev, ids_dev, teacher_dev)) return fail(fn, e);
+  if (!loss_dev || !stats_dev || !aligned(loss_dev, 4) || !aligned(stats_dev, 4)) return fail(fn, "loss_dev and stats_dev must be non-NULL and 4-byte aligned");
+  if (overlap(loss_dev, 4 * (size_t)cfg->rows, stats_dev, 12 * (size_t)cfg->rows)) return fail(fn, "outputs overlap");
+  ast::distill_fwd(stream_of(hip_stream), *cfg, logits_dev, ids_dev, teacher_dev, loss_dev, stats_dev);
+  return launched(fn);
+}
+
+ast_status asteroid_distill_backward(const ast_distill_cfg* cfg, const float* dloss_dev, const void* logits_dev,
+                                     const int32_t* ids_dev, const void* teacher_dev, const float* stats_dev, void* dlogits_dev,
+                                     int64_t dlogits_stride, void* hip_stream) {
+  const char* const fn = "distill_backward";
+  if (const char* e = distill_cfg(cfg)) return fail(fn, e);
+  if (cfg->rows == 0) return AST_OK;
+  if (const char* e = distill_inputs(*cfg, logits_dev, ids_dev, teacher_dev)) return fail(fn, e);
+  if (const char* e = distill_gradient(*cfg, dloss_dev, logits_dev, dlogits_dev, dlogits_stride)) return fail(fn, e);
+  if (!stats_dev || !aligned(stats_dev, 4)) return fail(fn, "stats_dev must be non-NULL and 4-byte aligned");
+  ast::distill_bwd(stream_of(hip_stream), *cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, stats_dev, dlogits_dev, dlogits_stride);
+  return launched(fn);
+}
+
+ast_status asteroid_distill_step(const ast_distill_cfg* cfg, const float* dloss_dev, const void* logits_dev, const int32_t* ids_dev,
+                                 const void* teacher_dev, float* loss_dev, void* dlogits_dev, int64_t dlogits_stride, void* hip_stream) {
+  const char* const fn = "distill_step";
+  if (const char* e = distill_cfg(cfg)) return fail(fn, e);
+  if (cfg->rows == 0) return AST_OK;
+  if (const char* e = distill_inputs(*cfg, logits_dev, ids_dev, teacher_dev)) return fail(fn, e);
+  if (const char* e = distill_gradient(*cfg, dloss_dev, logits_dev, dlogits_dev, dlogits_stride)) return fail(fn, e);
+  if (!loss_dev || !aligned(loss_dev, 4)) return fail(fn, "loss_dev must be non-NULL and 4-byte aligned");
+  const size_t nd = ((size_t)(cfg->rows - 1) * (size_t)dlogits_stride + (size_t)cfg->vocab) * esize(cfg->dtype);
+  if (overlap(loss_dev, 4 * (size_t)cfg->rows, dlogits_dev, nd)) return fail(fn, "outputs overlap");
+  ast::distill_step(stream_of(hip_stream), *cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, loss_dev, dlogits_dev, dlogits_stride);
   return launched(fn);
 }
 

@@ -144,4 +144,94 @@ __device__ __forceinline__ void store8_part(T* p, int n, const float (&v)[8]) {
     if (i < n) store1(p + i, v[i]);
 }
 
+
+// ---- a block of 32 values in 8 bits (op_stash8.hip): eight of them a lane, four neighbouring lanes a block, all four active.
+// The lane's eight codes, and the block's byte (its exponent + 127, or 255), which all four lanes get.
+__device__ __forceinline__ uint32_t stash8_code(float steps) {
+  return (uint32_t)(int)rintf(fminf(fmaxf(steps, -127.f), 127.f)) & 0xffu;
+}
+__device__ __forceinline__ uint8_t stash8_block(const float (&v)[8], uint2& w) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = max(top, __float_as_uint(v[k]) & 0x7fffffffu);
+  // maximum over the block's four lanes, as bits (those of a NaN are above all others)
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, DPP_QUAD_SWAP1, 0xF, 0xF, true));
+  top = max(top, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)top, DPP_QUAD_SWAP2, 0xF, 0xF, true));
+  const bool finite = top < 0x7f800000u;
+  const int e = min(max((int)((top + 0x01ffffu) >> 23) - 127 - 6, -126), 121);
+  const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+  w = make_uint2(0, 0);
+  if (finite) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      w.x |= stash8_code(v[k] * inv) << (8 * k);
+      w.y |= stash8_code(v[4 + k] * inv) << (8 * k);
+    }
+  }
+  return (uint8_t)(finite ? e + 127 : 255);
+}
+
+// Eight values of a row of `cols`, from place c on, as they are loaded (0 behind the row's end), to be asked for early; EVEN: rows
+// start at 16-byte addresses and hold a multiple of eight values.
+template <typename T, bool EVEN>
+struct RowEight {
+  Eight<T, EVEN> e;
+  int over;  // places behind the row's end: the last eight values were read
+  __device__ __forceinline__ void load(const T* row, int c, int cols) {
+    over = 0;
+    if (EVEN) {
+      e.load(row + c);
+    } else if (cols >= 8) {
+      over = max(c + 8 - cols, 0);
+      e.load(row + c - over);
+    } else {  // (c is 0)
+      e.m = 0;
+#pragma unroll
+      for (int i = 0; i < Eight<T, EVEN>::N; ++i) e.v[i] = 0;
+#pragma unroll
+      for (int i = 0; i < 7; ++i) {
+        if (i >= cols) break;
+        if (sizeof(T) == 4) e.v[i] = reinterpret_cast<const uint32_t*>(row)[i];
+        else e.v[i / 2] |= (uint32_t) reinterpret_cast<const uint16_t*>(row)[i] << (i % 2 * 16);
+      }
+    }
+  }
+  __device__ __forceinline__ void values(float (&f)[8]) const {
+    uint32_t w[Eight<T, EVEN>::W];
+    e.words(w);
+    if (!EVEN && over > 0) {
+      const uint32_t zero[Eight<T, EVEN>::W] = {};
+      funnel(w, zero, (uint32_t)over * (uint32_t)sizeof(T));
+    }
+    eight_values<T>(w, f);
+  }
+};
+template <typename T, bool EVEN>
+__device__ __forceinline__ void store_row8(T* row, int c, int cols, const float (&v)[8]) {
+  if (EVEN || cols - c >= 8) store8(row + c, v);
+  else store8_part(row + c, cols - c, v);
+}
+
+// ---- rows (heads) of 2^ls lanes each, ls <= 6: sum over the lanes of a row, valid in each of them
+__device__ __forceinline__ float row_sum(float v, int ls) {
+  if (ls > 0) v += dpp_move<DPP_QUAD_SWAP1>(v);
+  if (ls > 1) v += dpp_move<DPP_QUAD_SWAP2>(v);
+  if (ls > 2) v += dpp_move<DPP_HALF_MIRROR>(v);
+  if (ls > 3) v += dpp_move<DPP_ROW_MIRROR>(v);
+  if (ls > 4) v += __shfl_xor(v, 16, 64);
+  if (ls > 5) v += __shfl_xor(v, 32, 64);
+  return v;
+}
+
+// ... and over the lanes that hold the same place of the wavefront's rows (rotations inside 16 lanes, then across them)
+__device__ __forceinline__ float places_sum(float v, int ls) {
+  if (ls < 4) v += dpp_move<0x128>(v);
+  if (ls < 3) v += dpp_move<0x124>(v);
+  if (ls < 2) v += dpp_move<0x122>(v);
+  if (ls < 1) v += dpp_move<0x121>(v);
+  if (ls < 5) v += __shfl_xor(v, 16, 64);
+  if (ls < 6) v += __shfl_xor(v, 32, 64);
+  return v;
+}
+
 }  // namespace ast

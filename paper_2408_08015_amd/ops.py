@@ -24,6 +24,27 @@ class ast_qk_cfg(C.Structure):
                 ("positions_dev", C.c_void_p), ("period", C.c_int32)]
 
 
+class ast_norm_cfg(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("width", C.c_int64), ("dtype", C.c_int32), ("sum_dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class ast_rows(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("stride", C.c_int64)]
+
+
+class ast_recurrence_cfg(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("channels", C.c_int64), ("dtype", C.c_int32), ("offsets_dev", C.c_void_p),
+                ("sequences", C.c_int64), ("period", C.c_int64)]
+
+
+class ast_distill_cfg(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("vocab", C.c_int64), ("logits_stride", C.c_int64), ("dtype", C.c_int32),
+                ("entries", C.c_int32), ("teacher_dtype", C.c_int32), ("temperature", C.c_float), ("label_weight", C.c_float),
+                ("labels_dev", C.c_void_p)]
+
+
+RECURRENCE_CHUNK = 64   # AST_RECURRENCE_CHUNK
+
 _LIB = None
 
 
@@ -33,6 +54,7 @@ def _lib():
         lib = load_library()
         vp, i32, i64, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_float, C.c_size_t
         szp, hp, qp = C.POINTER(sz), C.POINTER(ast_heads), C.POINTER(ast_qk_cfg)
+        np_, rp, sp, dp = (C.POINTER(t) for t in (ast_norm_cfg, ast_recurrence_cfg, ast_rows, ast_distill_cfg))
         for name, types in {
             "embedding_forward": [vp, i64, vp, i32, i64, i64, f32, vp, i32, vp],
             "embedding_backward_workspace": [i64, i64, i64, szp],
@@ -46,6 +68,15 @@ def _lib():
             "linear_wgrad_stash8_workspace": [i64, i64, i64, szp],
             "linear_wgrad_stash8": [vp, vp, i64, i64, i64, vp, vp, i32, vp, sz, vp],
             "gelu_backward_stash8": [vp, i32, vp, i64, i64, vp, vp],
+            "rms_norm_forward": [np_, vp, vp, vp, vp, vp, vp, vp],
+            "rms_norm_backward_workspace": [np_, szp],
+            "rms_norm_backward": [np_, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp],
+            "recurrence_workspace": [rp, szp],
+            "recurrence_forward": [rp, sp, sp, sp, vp, vp, vp, vp, vp, sz, vp],
+            "recurrence_backward": [rp, sp, sp, sp, sp, vp, vp, vp, sp, sp, sp, vp, vp, sz, vp],
+            "distill_forward": [dp, vp, vp, vp, vp, vp, vp],
+            "distill_backward": [dp, vp, vp, vp, vp, vp, vp, i64, vp],
+            "distill_step": [dp, vp, vp, vp, vp, vp, vp, i64, vp],
         }.items():
             getattr(lib, "asteroid_" + name).argtypes = types
         _LIB = lib
@@ -334,3 +365,251 @@ def gelu_backward_stash8(dy, stash, out=None):
     _call(_device(dy, s.data, out), lib.asteroid_gelu_backward_stash8, dy.data_ptr(), _DT[dy.dtype], s.data.data_ptr(), s.rows,
           s.cols, out.data_ptr())
     return out
+
+
+# ------------------------------------------------------------------------------------------------ RMS norm and residual
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def rms_norm_forward(x, gain, residual=None, eps=1e-6, keep8=False, out=None, sum_out=None, kept_out=None):
+    """(y, s, kept): s = x + residual in the residual's type (x itself without one), y = s / sqrt(mean s^2 + eps) * gain
+    in x's type, kept = y in 8 bits (a Stash8; None unless keep8).  x float32 or bfloat16 [rows, width], residual of the same
+    shape in x's type or float32, gain float32 [width].  out may be x, sum_out the residual."""
+    _matrix(x, "x")
+    _is(gain, "gain", _F32, (x.shape[1],))
+    if residual is not None:
+        _is(residual, "residual", (x.dtype, torch.float32), x.shape)
+        if sum_out is None:
+            sum_out = torch.empty_like(residual)
+        _is(sum_out, "sum_out", (residual.dtype,), x.shape)
+    elif sum_out is not None:
+        raise ValueError("without a residual there is no sum to write")
+    if out is None:
+        out = torch.empty_like(x)
+    _is(out, "out", (x.dtype,), x.shape)
+    kept = None
+    if keep8 or kept_out is not None:
+        kept = Stash8(x.shape[0], x.shape[1], x.device) if kept_out is None else _stash(kept_out)
+        if (kept.rows, kept.cols) != tuple(x.shape):
+            raise ValueError("the stash keeps [%d, %d], x is %s" % (kept.rows, kept.cols, tuple(x.shape)))
+    sums = x if residual is None else sum_out
+    lib = _lib()
+    cfg = ast_norm_cfg(x.shape[0], x.shape[1], _DT[x.dtype], _DT[sums.dtype], eps)
+    _call(_device(x, gain, residual, out, sum_out, None if kept is None else kept.data), lib.asteroid_rms_norm_forward, cfg,
+          x.data_ptr(), _ptr(residual), gain.data_ptr(), out.data_ptr(), _ptr(sum_out), None if kept is None else kept.data.data_ptr())
+    return out, sums, kept
+
+
+def _norm_workspace(cfg):
+    n = C.c_size_t()
+    lib = _lib()
+    _check(lib, lib.asteroid_rms_norm_backward_workspace(cfg, n))
+    return n.value
+
+
+def rms_norm_backward_workspace(rows, width):
+    """Bytes of workspace that rms_norm_backward takes."""
+    return _norm_workspace(ast_norm_cfg(rows, width, 0, 0, 1.0))
+
+
+def rms_norm_backward(dy, s, gain, dsum=None, eps=1e-6, out=None, sum_out=None, gain_out=None, accumulate=False, workspace=None):
+    """(dx, ds, dgain) of rms_norm_forward: the gradient of x and the residual in dy's type and in that of s (one tensor
+    where these are the same), and the gain's, float32.  s is the sum that the forward pass returned, dsum (of s's
+    type) the gradient that reaches it from further on.  out may be dy, sum_out may be dsum or s.  accumulate: added to gain_out."""
+    _matrix(dy, "dy")
+    _is(s, "s", (dy.dtype, torch.float32), dy.shape)
+    _is(gain, "gain", _F32, (dy.shape[1],))
+    if dsum is not None:
+        _is(dsum, "dsum", (s.dtype,), dy.shape)
+    one = s.dtype == dy.dtype
+    if one and out is not None and sum_out is not None and out is not sum_out:
+        raise ValueError("out and sum_out are one tensor where the types are the same")
+    if out is None:
+        out = sum_out if one and sum_out is not None else torch.empty_like(dy)
+    _is(out, "out", (dy.dtype,), dy.shape)
+    if one:
+        sum_out = out
+    elif sum_out is None:
+        sum_out = torch.empty_like(s)
+    _is(sum_out, "sum_out", (s.dtype,), dy.shape)
+    if gain_out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the tensor to add to")
+        gain_out = torch.empty_like(gain)
+    _is(gain_out, "gain_out", _F32, gain.shape)
+    cfg = ast_norm_cfg(dy.shape[0], dy.shape[1], _DT[dy.dtype], _DT[s.dtype], eps)
+    lib = _lib()
+    d = _device(dy, s, gain, dsum, out, sum_out, gain_out)
+    ws = _workspace(workspace, _norm_workspace(cfg), dy.device)
+    _call(d, lib.asteroid_rms_norm_backward, cfg, dy.data_ptr(), s.data_ptr(), gain.data_ptr(), _ptr(dsum), out.data_ptr(),
+          None if one else sum_out.data_ptr(), gain_out.data_ptr(), bool(accumulate), ws.data_ptr(), ws.numel())
+    return out, sum_out, gain_out
+
+
+# ------------------------------------------------------------------------------------------------ gated recurrence
+
+def _tokens(t, name, like=None):
+    """A matrix [tokens, channels] in rows of any stride, as the C calls take it."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _DT:
+        raise ValueError("%s must be a float32 or bfloat16 tensor [tokens, channels]" % name)
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise ValueError("%s must be a %s tensor %s" % (name, like.dtype, tuple(like.shape)))
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise ValueError("%s must have unit stride inside a row" % name)
+    return ast_rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _recurrence_cfg(f, offsets, period):
+    T, D = f.shape
+    if offsets is not None:
+        _vector_i32(offsets, "offsets")
+        if offsets.shape[0] < 1:
+            raise ValueError("offsets must hold one number more than there are sequences")
+        return ast_recurrence_cfg(T, D, _DT[f.dtype], offsets.data_ptr(), offsets.shape[0] - 1, 0), offsets.shape[0] - 1
+    if not 1 <= period < 1 << 31:
+        raise ValueError("offsets, or the period of the sequences (below 2^31), must be given")
+    return ast_recurrence_cfg(T, D, _DT[f.dtype], None, 0, period), -(-T // period)
+
+
+def _states(t, name, n, f):
+    """None, a tensor [sequences, channels], or (True) one that is made here."""
+    if t is None or t is False:
+        return None
+    if t is True:
+        return torch.empty((n, f.shape[1]), dtype=torch.float32, device=f.device)
+    return _is(t, name, _F32, (n, f.shape[1]))
+
+
+def _recurrence_workspace(cfg):
+    n = C.c_size_t()
+    lib = _lib()
+    _check(lib, lib.asteroid_recurrence_workspace(cfg, n))
+    return n.value
+
+
+def recurrence_workspace(tokens, channels, dtype, offsets=False, period=0):
+    """Bytes of workspace that recurrence_forward and recurrence_backward take (offsets: whether they are given)."""
+    return _recurrence_workspace(ast_recurrence_cfg(tokens, channels, _DT[dtype], 4 if offsets else None, 0, period))
+
+
+def recurrence_forward(f, z, o=None, offsets=None, period=0, state=None, final=None, saved=None, out=None, workspace=None):
+    """(y, final, saved): h_t = a_t h_{t-1} + (1 - a_t) z_t with a = sigmoid(f), y = h * o sigmoid(o) (h without o).
+    f, z, o float32 or bfloat16 [tokens, channels] with unit stride inside a row; sequences one behind the other: offsets int32
+    [sequences + 1], or `period` tokens each.  state float32 [sequences, channels]: in front of every sequence (0 if not given).
+    final: True or a tensor (state itself allowed) to receive the states behind them.  saved: True or a float32 tensor
+    [tokens / 64 rounded up, channels] for recurrence_backward.  y is dense; rows of no sequence are not written."""
+    a = [_tokens(f, "f"), _tokens(z, "z", f), None if o is None else _tokens(o, "o", f)]
+    cfg, n = _recurrence_cfg(f, offsets, period)
+    state = _states(state, "state", n, f)
+    final = _states(final, "final", n, f)
+    saved = _states(saved, "saved", -(-f.shape[0] // RECURRENCE_CHUNK), f)
+    if out is None:
+        out = torch.empty(f.shape, dtype=f.dtype, device=f.device)
+    _is(out, "out", (f.dtype,), f.shape)
+    lib = _lib()
+    d = _device(f, z, o, offsets, state, final, saved, out)
+    ws = _workspace(workspace, _recurrence_workspace(cfg), f.device)
+    _call(d, lib.asteroid_recurrence_forward, cfg, a[0], a[1], a[2], _ptr(state), out.data_ptr(), _ptr(final), _ptr(saved),
+          ws.data_ptr(), ws.numel())
+    return out, final, saved
+
+
+def recurrence_backward(dy, f, z, saved, o=None, offsets=None, period=0, state=None, dfinal=None, dstate=None, out=None,
+                        workspace=None):
+    """(df, dz, do, dstate) of recurrence_forward with the same arguments; saved is what it left.  dfinal float32
+    [sequences, channels]: the gradient of final (0 if not given).  dstate: True or a tensor to receive the gradient of state.
+    out: (df, dz, do), rows with any stride; (f, z, o) themselves allowed.  do is None where o is."""
+    a = [_tokens(f, "f"), _tokens(z, "z", f), None if o is None else _tokens(o, "o", f)]
+    cfg, n = _recurrence_cfg(f, offsets, period)
+    _is(saved, "saved", _F32, (-(-f.shape[0] // RECURRENCE_CHUNK), f.shape[1]))
+    state = _states(state, "state", n, f)
+    dfinal = _states(dfinal, "dfinal", n, f)
+    dstate = _states(dstate, "dstate", n, f)
+    if out is None:
+        out = [torch.empty(f.shape, dtype=f.dtype, device=f.device) for _ in range(2 if o is None else 3)]
+    df, dz, do = (tuple(out) + (None,))[:3]
+    if (do is None) != (o is None):
+        raise ValueError("out holds the gradient of o where o is given, and only there")
+    b = [_tokens(dy, "dy", f), _tokens(df, "df", f), _tokens(dz, "dz", f), None if do is None else _tokens(do, "do", f)]
+    lib = _lib()
+    d = _device(f, z, o, dy, saved, offsets, state, dfinal, dstate, df, dz, do)
+    ws = _workspace(workspace, _recurrence_workspace(cfg), f.device)
+    _call(d, lib.asteroid_recurrence_backward, cfg, b[0], a[0], a[1], a[2], _ptr(state), saved.data_ptr(), _ptr(dfinal), b[1], b[2],
+          b[3], _ptr(dstate), ws.data_ptr(), ws.numel())
+    return df, dz, do, dstate
+
+
+# ------------------------------------------------------------------------------------------------ distillation
+
+def _distill_cfg(logits, ids, teacher, temperature, labels, label_weight):
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2 or logits.dtype not in _DT:
+        raise ValueError("logits must be a float32 or bfloat16 tensor [rows, vocab]")
+    T, V = logits.shape
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 2:
+        raise ValueError("ids must be a matrix")
+    _is(ids, "ids", _I32, (T, ids.shape[1]))
+    _is(teacher, "teacher", tuple(_DT), ids.shape)
+    if labels is not None:
+        _vector_i32(labels, "labels", T)
+    return ast_distill_cfg(T, V, _vocab_rows(logits, "logits"), _DT[logits.dtype], ids.shape[1], _DT[teacher.dtype], temperature,
+                           label_weight, None if labels is None else labels.data_ptr())
+
+
+def _vocab_rows(t, name):
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise ValueError("%s must have unit stride inside a row" % name)
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _gradient_of(logits, out, dloss):
+    _is(dloss, "dloss", _F32, (logits.shape[0],))
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if not isinstance(out, torch.Tensor) or out.shape != logits.shape or out.dtype != logits.dtype:
+        raise ValueError("out must be a %s tensor %s" % (logits.dtype, tuple(logits.shape)))
+    return out, _vocab_rows(out, "out")
+
+
+def distill_forward(logits, ids, teacher, temperature=1.0, labels=None, label_weight=0.0, out=None, stats_out=None):
+    """(loss [rows], stats [rows, 3]), float32: (1 - l) T^2 KL(p || q) + l CE(label) of every row, p the softmax of the
+    teacher's logits [rows, entries] / T over the entries whose ids lie in the vocabulary, q that of the student's / T.
+    logits float32 or bfloat16 [rows, vocab] with unit stride inside a row, ids int32 [rows, entries], labels int32 [rows].
+    stats is for distill_backward."""
+    cfg = _distill_cfg(logits, ids, teacher, temperature, labels, label_weight)
+    T = logits.shape[0]
+    if out is None:
+        out = torch.empty((T,), dtype=torch.float32, device=logits.device)
+    if stats_out is None:
+        stats_out = torch.empty((T, 3), dtype=torch.float32, device=logits.device)
+    _is(out, "out", _F32, (T,))
+    _is(stats_out, "stats_out", _F32, (T, 3))
+    lib = _lib()
+    _call(_device(logits, ids, teacher, labels, out, stats_out), lib.asteroid_distill_forward, cfg, logits.data_ptr(), ids.data_ptr(),
+          teacher.data_ptr(), out.data_ptr(), stats_out.data_ptr())
+    return out, stats_out
+
+
+def distill_backward(dloss, logits, ids, teacher, stats, temperature=1.0, labels=None, label_weight=0.0, out=None):
+    """The logits' gradient for dloss float32 [rows]; stats is what distill_forward left.  out may be logits."""
+    cfg = _distill_cfg(logits, ids, teacher, temperature, labels, label_weight)
+    _is(stats, "stats", _F32, (logits.shape[0], 3))
+    out, stride = _gradient_of(logits, out, dloss)
+    lib = _lib()
+    _call(_device(logits, ids, teacher, labels, stats, dloss, out), lib.asteroid_distill_backward, cfg, dloss.data_ptr(),
+          logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(), stats.data_ptr(), out.data_ptr(), stride)
+    return out
+
+
+def distill_step(dloss, logits, ids, teacher, temperature=1.0, labels=None, label_weight=0.0, out=None, loss_out=None):
+    """(loss, the logits' gradient) at once, where dloss is known beforehand.  out may be logits."""
+    cfg = _distill_cfg(logits, ids, teacher, temperature, labels, label_weight)
+    out, stride = _gradient_of(logits, out, dloss)
+    if loss_out is None:
+        loss_out = torch.empty((logits.shape[0],), dtype=torch.float32, device=logits.device)
+    _is(loss_out, "loss_out", _F32, (logits.shape[0],))
+    lib = _lib()
+    _call(_device(logits, ids, teacher, labels, dloss, loss_out, out), lib.asteroid_distill_step, cfg, dloss.data_ptr(),
+          logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(), loss_out.data_ptr(), out.data_ptr(), stride)
+    return loss_out, out
