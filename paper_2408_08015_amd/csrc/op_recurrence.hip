@@ -8,7 +8,7 @@
 // once: a wavefront holds TOK tokens of 64 (fp32) or 128 (bf16) channels in registers, forms their map, learns what comes in
 // and finishes.  WAVES wavefronts of a block join their maps through LDS, blocks through the workspace:
 //
-//   a block leaves the map of its tokens in one 64-bit word a channel (A, U) as soon as it has it; 16 blocks in a row make a
+//   a block leaves the map of its tokens in one 64-bit word a channel (A, U) as soon as it has it; 32 blocks in a row make a
 //   group, and the last of them leaves the value behind the group.  What comes in to a block is the value in front of its group and the
 //   maps of the group's earlier blocks, joined in their order: the result does not depend on which block ran when.
 //
@@ -18,6 +18,7 @@
 // A run in which a sequence starts passes nothing through: its A is -0 (products with it stay -0, and none of a sequence's
 // infinities or NaN reach the next one).
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 #include "ops_device.h"
@@ -27,11 +28,11 @@ namespace ast {
 
 namespace {
 
-constexpr int WAVES = 8;
-constexpr int GROUP = 16;               // blocks of a chain whose maps are joined one by one
+constexpr int FWD_WAVES = 8, BWD_WAVES = 8;
+constexpr int GROUP = 32;               // blocks of a chain whose maps are joined one by one
 constexpr int FWD_TOK = 16, BWD_TOK = 8;  // tokens of a wavefront: 48 and 32 registers of loads (16 bits: two channels a register)
-static_assert(BWD_TOK * WAVES == AST_RECURRENCE_CHUNK, "a block of the backward pass starts where a state was kept");
-static_assert(FWD_TOK * WAVES % AST_RECURRENCE_CHUNK == 0 && AST_RECURRENCE_CHUNK % FWD_TOK == 0, "kept states are a wavefront's first");
+static_assert(BWD_TOK * BWD_WAVES == AST_RECURRENCE_CHUNK, "a block of the backward pass starts where a state was kept");
+static_assert(FWD_TOK * FWD_WAVES % AST_RECURRENCE_CHUNK == 0 && AST_RECURRENCE_CHUNK % FWD_TOK == 0, "kept states are a wavefront's first");
 
 constexpr uint32_t NOT_YET = 0xffffffffu;  // a NaN with a sign: maps are made without it
 
@@ -52,29 +53,74 @@ struct RecArgs {
   int channels, columns, chunks;
 };
 
-template <typename T> struct Lane;  // consecutive channels of a lane, as they are loaded
-template <> struct Lane<float> {
+// Consecutive channels of a lane, one register of a row.  Lanes behind the last channel read the last ones, and a lane that has
+// one channel where others have two reads a pair and takes its upper half, so that no load waits for a condition.
+struct Lane32 {
+  typedef float T;
   static constexpr int V = 1;
-  static __device__ __forceinline__ uint32_t load(const float* p, bool) { return __float_as_uint(*p); }
-  static __device__ __forceinline__ void values(uint32_t w, float (&v)[1]) { v[0] = __uint_as_float(w); }
-  static __device__ __forceinline__ void store(float* p, bool, const float (&v)[1]) { *p = v[0]; }
+  uint32_t at;  // bytes from a row's first value
+  __device__ __forceinline__ Lane32(int c, int channels) : at(4u * (uint32_t)min(c, channels - 1)) {}
+  __device__ __forceinline__ uint32_t load(const void* row) const { return *reinterpret_cast<const uint32_t*>(static_cast<const char*>(row) + at); }
+  __device__ __forceinline__ void values(uint32_t w, float (&v)[1]) const { v[0] = __uint_as_float(w); }
+  template <bool FULL> __device__ __forceinline__ void store(void* row, const float (&v)[1]) const {
+    *reinterpret_cast<float*>(static_cast<char*>(row) + at) = v[0];
+  }
 };
 struct __attribute__((packed, aligned(2))) Raw4 { uint32_t w; };
-template <> struct Lane<bf16_t> {
+struct Lane16 {  // (two channels or more)
+  typedef bf16_t T;
   static constexpr int V = 2;
-  static __device__ __forceinline__ uint32_t load(const bf16_t* p, bool both) {
-    return both ? reinterpret_cast<const Raw4*>(p)->w : *p;
-  }
-  static __device__ __forceinline__ void values(uint32_t w, float (&v)[2]) {
-    v[0] = __uint_as_float(w << 16);
+  uint32_t at, first;  // first: the bytes that become the first value (v_perm_b32)
+  __device__ __forceinline__ Lane16(int c, int channels)
+      : at(2u * (uint32_t)min(c, channels - 2)), first(c < channels - 1 ? 0x01000c0cu : 0x03020c0cu) {}
+  __device__ __forceinline__ uint32_t load(const void* row) const { return reinterpret_cast<const Raw4*>(static_cast<const char*>(row) + at)->w; }
+  __device__ __forceinline__ void values(uint32_t w, float (&v)[2]) const {
+    v[0] = __uint_as_float(__builtin_amdgcn_perm(w, w, first));
     v[1] = __uint_as_float(w & 0xffff0000u);
   }
-  static __device__ __forceinline__ void store(bf16_t* p, bool both, const float (&v)[2]) {
+  template <bool FULL> __device__ __forceinline__ void store(void* row, const float (&v)[2]) const {
     const uint32_t w = f2bf_pk(v[0], v[1]);
-    if (both) reinterpret_cast<Raw4*>(p)->w = w;
-    else *p = (bf16_t)w;
+    char* const p = static_cast<char*>(row) + at;
+    if (FULL || first == 0x01000c0cu) reinterpret_cast<Raw4*>(p)->w = w;
+    else *reinterpret_cast<bf16_t*>(p + 2) = (bf16_t)w;
   }
 };
+struct Lane16One {  // rows of a single channel
+  typedef bf16_t T;
+  static constexpr int V = 1;
+  __device__ __forceinline__ Lane16One(int, int) {}
+  __device__ __forceinline__ uint32_t load(const void* row) const { return *static_cast<const bf16_t*>(row); }
+  __device__ __forceinline__ void values(uint32_t w, float (&v)[1]) const { v[0] = __uint_as_float(w << 16); }
+  template <bool FULL> __device__ __forceinline__ void store(void* row, const float (&v)[1]) const { store1(static_cast<bf16_t*>(row), v[0]); }
+};
+// the rows of a wavefront's tokens, one after the other; behind the last token: that one again
+template <int TOK>
+struct RowsFrom {
+  const char* p;
+  int64_t step;
+  int left;
+  __device__ __forceinline__ RowsFrom(const Rows& r, int64_t t0, int64_t tokens, int esize)
+      : p(static_cast<const char*>(r.p) + min(t0, tokens - 1) * r.stride * esize), step(r.stride * esize), left((int)min((int64_t)TOK, tokens - t0)) {}
+  __device__ __forceinline__ const void* next() {
+    const void* const at = p;
+    if (--left > 0) p += step;
+    return at;
+  }
+};
+// a lane's channels of a row of fp32 states
+template <int V>
+__device__ __forceinline__ void load_state(const float* rows, int64_t row, int c, int channels, float (&v)[V]) {
+  const float* const p = rows + row * channels;
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = p[(uint32_t)min(c + i, channels - 1)];
+}
+template <int V>
+__device__ __forceinline__ void store_state(float* rows, int64_t row, int c, int channels, const float (&v)[V]) {
+  float* const p = rows + row * channels;
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (c + i < channels) p[(uint32_t)(c + i)] = v[i];
+}
 
 // exp(-|x|), within about 2^-22 of it for fp32 results (the rest of the product with log2 e is added behind the exponential:
 // 2^-24 of an argument of 20 would be 1e-6 of the result), with a product alone for bf16 results
@@ -95,6 +141,7 @@ __device__ __forceinline__ void gates(float x, float& a, float& b) {
   const float s = e * r;
   a = x >= 0.f ? r : s;
   b = x >= 0.f ? s : r;
+  asm volatile("" : "+v"(a), "+v"(b));  // (chosen here: kept for later, each choice would hold two more registers and a mask)
 }
 
 __device__ __forceinline__ bool cut(float A) { return (int)__float_as_uint(A) < 0; }  // nothing passes through
@@ -111,9 +158,12 @@ __device__ __forceinline__ unsigned long long map_word(float A, float U) {
 __device__ __forceinline__ void leave(unsigned long long* p, unsigned long long w) {
   __hip_atomic_store(p, w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+__device__ __forceinline__ unsigned long long look(unsigned long long* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 __device__ __forceinline__ unsigned long long take(unsigned long long* p) {
   unsigned long long w;
-  while ((uint32_t)(w = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) == NOT_YET) __builtin_amdgcn_s_sleep(1);
+  while ((uint32_t)(w = look(p)) == NOT_YET) __builtin_amdgcn_s_sleep(1);
   return w;
 }
 
@@ -121,83 +171,88 @@ __device__ __forceinline__ unsigned long long take(unsigned long long* p) {
 template <int TOK>
 struct Tokens {
   unsigned live, start, last;  // belongs to a sequence; is its first; its last
-  int64_t t0;
-  int64_t seq0, left;          // by period: the sequence of token 0, and how far the sequence goes from there
-  __device__ __forceinline__ Tokens(const RecArgs& g, int64_t t) : live(0), start(0), last(0), t0(t), seq0(0), left(0) {
+  int32_t at;                  // lane i: the sequence of token i (0: with the token in front) or, by period, of token 0
+  bool listed;
+  __device__ __forceinline__ Tokens(const RecArgs& g, int64_t t0, int lane) : live(0), start(0), last(0), at(0), listed(g.seq != nullptr) {
     if (t0 >= g.tokens) return;
     const int n = (int)min((int64_t)TOK, g.tokens - t0);
-    if (g.seq) {
-      int before = t0 > 0 ? g.seq[t0 - 1] : -1, at = g.seq[t0];
-#pragma unroll
-      for (int i = 0; i < TOK; ++i) {
-        if (i >= n) break;
-        const int next = t0 + i + 1 < g.tokens ? g.seq[t0 + i + 1] : -1;
-        if (at >= 0) {
-          live |= 1u << i;
-          if (at != before) start |= 1u << i;
-          if (at != next) last |= 1u << i;
-        }
-        before = at;
-        at = next;
-      }
+    if (listed) {
+      const int64_t t = t0 - 1 + lane;  // (lanes 0 .. TOK + 1 count)
+      at = t >= 0 && t < g.tokens && lane <= TOK + 1 ? g.seq[t] : -1;
+      const int32_t next = __builtin_amdgcn_update_dpp(-1, at, DPP_WAVE_SHL1, 0xF, 0xF, false);
+      const bool differ = at != next;
+      const unsigned long long all = (1ull << n) - 1, change = __ballot(differ);  // bit i: tokens i - 1 and i differ
+      live = (unsigned)(__ballot(at >= 0) >> 1 & all);
+      start = (unsigned)(change & live);
+      last = (unsigned)(change >> 1 & live);
     } else {
-      live = n == 32 ? ~0u : (1u << n) - 1;
-      seq0 = t0 / g.period;
-      const int64_t into = t0 - seq0 * g.period;
-      left = g.period - into;
+      live = (1u << n) - 1;
+      const unsigned period = (unsigned)g.period, s = (unsigned)t0 / period, into = (unsigned)t0 - s * period;  // (tokens < 2^31)
+      at = (int32_t)s;
       if (into == 0) start |= 1;
-      for (int64_t i = left; i < n; i += g.period) start |= 1u << i;
-      for (int64_t i = left - 1; i < n; i += g.period) last |= 1u << i;
+      for (unsigned i = period - into; i < (unsigned)n; i += period) start |= 1u << i;
+      for (unsigned i = period - into - 1; i < (unsigned)n; i += period) last |= 1u << i;
       if (t0 + n == g.tokens) last |= 1u << (n - 1);
     }
   }
-  __device__ __forceinline__ int64_t sequence(const RecArgs& g, int i) const {
-    if (g.seq) return g.seq[t0 + i];
-    return i < left ? seq0 : (t0 + i) / g.period;
+  __device__ __forceinline__ int64_t sequence(int i) const {
+    return (int64_t)__builtin_amdgcn_readlane(at, listed ? i + 1 : 0) + (listed ? 0 : __popc(start & ((2u << i) - 2)));
   }
 };
 
-// The value that comes in to a block whose place in the chain is `at` (in the order of the scan), for this lane's channels; all
-// threads of the block call it.  got: LDS [GROUP][64 V], head: LDS [64 V].
-template <int V>
-__device__ __forceinline__ void come_in(const RecArgs& g, int at, int c, int wave, int lane, float2 (*got)[64 * V], float* head,
-                                        float (&x)[V]) {
+// The value that comes in to a block whose place in the chain is `at` (in the order of the scan), for this lane's channels, and
+// what it leaves: its map (A, U) has been left before.  All threads of the block call it; got: LDS [WAVES][64 V].
+// Every wavefront joins the maps of SHARE blocks in front, then all join the wavefronts' maps, and only then the value in front
+// of the group is asked for: the last block of a group has nothing left to do but one step when it appears.
+template <int V, int WAVES>
+__device__ __forceinline__ void come_in(const RecArgs& g, int at, int c, int wave, int lane, float2 (*got)[64 * V], const float (&A)[V],
+                                        const float (&U)[V], float (&x)[V]) {
+  constexpr int SHARE = GROUP / WAVES;
   const int group = at / GROUP, r = at % GROUP;
-  const unsigned long long* const maps = g.maps + (int64_t)group * GROUP * g.channels;
+  unsigned long long* const maps = g.maps + ((int64_t)group * GROUP + wave * SHARE) * g.channels;
+  float a[V], b[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    if (c + v >= g.channels) continue;
-    for (int j = wave; j < r; j += WAVES) {
-      const unsigned long long w = take(const_cast<unsigned long long*>(maps) + (int64_t)j * g.channels + c + v);
-      got[j][lane * V + v] = make_float2(__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32)));
+    a[v] = 1.f, b[v] = 0.f;
+    unsigned long long w[SHARE];
+#pragma unroll
+    for (int j = 0; j < SHARE; ++j)  // (all asked for at once)
+      w[j] = wave * SHARE + j < r && c + v < g.channels ? look(maps + (int64_t)j * g.channels + c + v) : 0x3f800000u;
+#pragma unroll
+    for (int j = 0; j < SHARE; ++j) {
+      while ((uint32_t)w[j] == NOT_YET) {
+        __builtin_amdgcn_s_sleep(1);
+        w[j] = look(maps + (int64_t)j * g.channels + c + v);
+      }
+      join(a[v], b[v], __uint_as_float((uint32_t)w[j]), __uint_as_float((uint32_t)(w[j] >> 32)));
     }
-    if (wave == WAVES - 1)
-      head[lane * V + v] = group == 0 ? 0.f : __uint_as_float((uint32_t)(take(g.heads + (int64_t)group * g.channels + c + v) >> 32));
+    got[wave][lane * V + v] = make_float2(a[v], b[v]);
   }
   __syncthreads();
 #pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = head[lane * V + v];
-  for (int j = 0; j < r; ++j)
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float2 m = got[j][lane * V + v];
-      x[v] = cut(m.x) ? m.y : fmaf(m.x, x[v], m.y);
+  for (int v = 0; v < V; ++v) {
+    a[v] = 1.f, b[v] = 0.f;
+#pragma unroll 2
+    for (int w = 0; w < WAVES; ++w) {
+      const float2 m = got[w][lane * V + v];
+      join(a[v], b[v], m.x, m.y);
     }
+  }
+  const bool hand_on = r == GROUP - 1 && at + 1 < g.chunks && wave == 0;
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    x[v] = 0.f;
+    if (group > 0 && c + v < g.channels) x[v] = __uint_as_float((uint32_t)(take(g.heads + (int64_t)group * g.channels + c + v) >> 32));
+    x[v] = cut(a[v]) ? b[v] : fmaf(a[v], x[v], b[v]);
+    if (hand_on && c + v < g.channels)
+      leave(g.heads + (int64_t)(group + 1) * g.channels + c + v, map_word(0.f, cut(A[v]) ? U[v] : fmaf(A[v], x[v], U[v])));
+  }
 }
-// ... and what it leaves: its map (A, U), and behind the last block of a group, once x has come in, the value there
 template <int V>
 __device__ __forceinline__ void leave_map(const RecArgs& g, int at, int c, const float (&A)[V], const float (&U)[V]) {
 #pragma unroll
   for (int v = 0; v < V; ++v)
     if (c + v < g.channels) leave(g.maps + (int64_t)at * g.channels + c + v, map_word(A[v], U[v]));
-}
-template <int V>
-__device__ __forceinline__ void leave_head(const RecArgs& g, int at, int c, const float (&A)[V], const float (&U)[V], const float (&x)[V]) {
-  if (at % GROUP != GROUP - 1 || at + 1 >= g.chunks) return;
-#pragma unroll
-  for (int v = 0; v < V; ++v)
-    if (c + v < g.channels)
-      leave(g.heads + (int64_t)(at / GROUP + 1) * g.channels + c + v, map_word(0.f, cut(A[v]) ? U[v] : fmaf(A[v], x[v], U[v])));
 }
 
 // A block's place: in the order in which blocks start where they wait for each other.
@@ -206,36 +261,34 @@ __device__ __forceinline__ unsigned place(const RecArgs& g) {
   __shared__ unsigned p;
   if (threadIdx.x == 0) p = atomicAdd(g.counter, 1u);
   __syncthreads();
-  return p;
+  return __builtin_amdgcn_readfirstlane(p);  // (the same in all lanes: rows have scalar addresses)
 }
 
-template <typename T, bool GATE>
-__global__ __launch_bounds__(64 * WAVES, 4) void recurrence_kernel(const RecArgs g) {
-  typedef Lane<T> L;
-  constexpr int V = L::V, TOK = FWD_TOK;
+template <typename L, bool GATE>
+__global__ __launch_bounds__(64 * FWD_WAVES, 4) void recurrence_kernel(const RecArgs g) {
+  typedef typename L::T T;
+  constexpr int V = L::V, TOK = FWD_TOK, WAVES = FWD_WAVES, ES = sizeof(T);
   constexpr bool EXACT = sizeof(T) == 4;
   __shared__ float2 mine[WAVES][64 * V];
-  __shared__ float2 got[GROUP][64 * V];
-  __shared__ float head[64 * V];
+  __shared__ float2 got[WAVES][64 * V];
   const unsigned p = place(g);
   const int chunk = (int)(p / (unsigned)g.columns), column = (int)(p - (unsigned)chunk * (unsigned)g.columns);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = (column * 64 + lane) * V;
-  const bool on = c < g.channels, both = c + V <= g.channels;
+  const L at(c, g.channels);
   const int64_t t0 = ((int64_t)chunk * WAVES + wave) * TOK;
 
   uint32_t rf[TOK], rz[TOK], ro[GATE ? TOK : 1];
+  {
+    RowsFrom<TOK> f(g.f, t0, g.tokens, ES), z(g.z, t0, g.tokens, ES), o(GATE ? g.o : g.z, t0, g.tokens, ES);
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    rf[i] = rz[i] = 0;
-    if (GATE) ro[GATE ? i : 0] = 0;
-    if (on && t0 + i < g.tokens) {
-      rf[i] = L::load(static_cast<const T*>(g.f.p) + (t0 + i) * g.f.stride + c, both);
-      rz[i] = L::load(static_cast<const T*>(g.z.p) + (t0 + i) * g.z.stride + c, both);
-      if (GATE) ro[GATE ? i : 0] = L::load(static_cast<const T*>(g.o.p) + (t0 + i) * g.o.stride + c, both);
+    for (int i = 0; i < TOK; ++i) {
+      rf[i] = at.load(f.next());
+      rz[i] = at.load(z.next());
+      if (GATE) ro[GATE ? i : 0] = at.load(o.next());
     }
   }
-  const Tokens<TOK> tk(g, t0);
+  const Tokens<TOK> tk(g, t0, lane);
   // the wavefront's map, token by token: value behind token i = P[i] x + H[i]
   float P[TOK][V], H[TOK][V], A[V], U[V];
 #pragma unroll
@@ -243,15 +296,12 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_kernel(const RecArgs
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
     float f[V], z[V];
-    L::values(rf[i], f);
-    L::values(rz[i], z);
+    at.values(rf[i], f);
+    at.values(rz[i], z);
     if (tk.start >> i & 1) {
-      const float* const s = g.state ? g.state + tk.sequence(g, i) * g.channels + c : nullptr;
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        A[v] = -0.f;
-        U[v] = s && c + v < g.channels ? s[v] : 0.f;
-      }
+      for (int v = 0; v < V; ++v) U[v] = 0.f;
+      if (g.state) load_state(g.state, tk.sequence(i), c, g.channels, U);
     }
     if (tk.live >> i & 1) {
 #pragma unroll
@@ -273,7 +323,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_kernel(const RecArgs
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     A[v] = 1.f, U[v] = 0.f, pa[v] = 1.f, pu[v] = 0.f;
-#pragma unroll
+#pragma unroll 2
     for (int w = 0; w < WAVES; ++w) {
       const float2 m = mine[w][lane * V + v];
       if (w == wave) pa[v] = A[v], pu[v] = U[v];
@@ -282,96 +332,79 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_kernel(const RecArgs
   }
   if (g.maps) {
     if (wave == 0) leave_map<V>(g, chunk, c, A, U);
-    come_in<V>(g, chunk, c, wave, lane, got, head, x);
-    if (wave == 0) leave_head<V>(g, chunk, c, A, U, x);
+    come_in<V, WAVES>(g, chunk, c, wave, lane, got, A, U, x);
   }
+  if (c >= g.channels || t0 >= g.tokens) return;
 #pragma unroll
   for (int v = 0; v < V; ++v) x[v] = cut(pa[v]) ? pu[v] : fmaf(pa[v], x[v], pu[v]);
-  if (g.saved && on && t0 < g.tokens && t0 % AST_RECURRENCE_CHUNK == 0) {
+  if (g.saved && t0 % AST_RECURRENCE_CHUNK == 0) store_state(g.saved, t0 / AST_RECURRENCE_CHUNK, c, g.channels, x);
+  const unsigned through = tk.start ? (tk.start & 0u - tk.start) - 1 : ~0u;  // the tokens that x reaches
+  auto finish = [&](auto full) __attribute__((always_inline)) {
+    constexpr bool FULL = decltype(full)::value;
+    char* row = static_cast<char*>(g.y) + t0 * g.channels * ES;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-      if (c + v < g.channels) g.saved[t0 / AST_RECURRENCE_CHUNK * g.channels + c + v] = x[v];
-  }
-  bool through = true;  // what came in reaches the token
+    for (int i = 0; i < TOK; ++i, row += (int64_t)g.channels * ES) {
+      if (!(tk.live >> i & 1)) continue;
+      float h[V], y[V], o[V];
+      if (GATE) at.values(ro[GATE ? i : 0], o);
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    if (tk.start >> i & 1) through = false;
-    if (!(tk.live >> i & 1) || !on) continue;
-    float h[V], y[V], o[V];
-    if (GATE) L::values(ro[GATE ? i : 0], o);
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      h[v] = through ? fmaf(P[i][v], x[v], H[i][v]) : H[i][v];
-      y[v] = h[v];
-      if (GATE) {
-        float a, b;
-        gates<EXACT>(o[v], a, b);
-        y[v] *= o[v] * a;
+      for (int v = 0; v < V; ++v) {
+        h[v] = through >> i & 1 ? fmaf(P[i][v], x[v], H[i][v]) : H[i][v];
+        y[v] = h[v];
+        if (GATE) {
+          float a, b;
+          gates<EXACT>(o[v], a, b);
+          y[v] *= o[v] * a;
+        }
       }
+      at.template store<FULL>(row, y);
+      if (g.final && (tk.last >> i & 1)) store_state(g.final, tk.sequence(i), c, g.channels, h);
     }
-    L::store(static_cast<T*>(g.y) + (t0 + i) * g.channels + c, both, y);
-    if (g.final && (tk.last >> i & 1)) {
-      float* const s = g.final + tk.sequence(g, i) * g.channels + c;
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (c + v < g.channels) s[v] = h[v];
-    }
-  }
+  };
+  if ((column + 1) * 64 * V <= g.channels) finish(std::true_type{});
+  else finish(std::false_type{});
 }
 
-template <typename T, bool GATE>
-__global__ __launch_bounds__(64 * WAVES, 4) void recurrence_bwd_kernel(const RecArgs g) {
-  typedef Lane<T> L;
-  constexpr int V = L::V, TOK = BWD_TOK;
+template <typename L, bool GATE>
+__global__ __launch_bounds__(64 * BWD_WAVES, 4) void recurrence_bwd_kernel(const RecArgs g) {
+  typedef typename L::T T;
+  constexpr int V = L::V, TOK = BWD_TOK, WAVES = BWD_WAVES, ES = sizeof(T);
   constexpr bool EXACT = sizeof(T) == 4;
   __shared__ float2 mine[WAVES][64 * V];
   __shared__ float mine_k[WAVES][64 * V];
-  __shared__ float2 got[GROUP][64 * V];
-  __shared__ float head[64 * V];
+  __shared__ float2 got[WAVES][64 * V];
   const unsigned p = place(g);
-  const int at = (int)(p / (unsigned)g.columns), column = (int)(p - (unsigned)at * (unsigned)g.columns);
-  const int chunk = g.chunks - 1 - at;  // (the scan runs from the last token to the first)
+  const int place_at = (int)(p / (unsigned)g.columns), column = (int)(p - (unsigned)place_at * (unsigned)g.columns);
+  const int chunk = g.chunks - 1 - place_at;  // (the scan runs from the last token to the first)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = (column * 64 + lane) * V;
-  const bool on = c < g.channels, both = c + V <= g.channels;
+  const L at(c, g.channels);
+  const bool full = (column + 1) * 64 * V <= g.channels;
   const int64_t t0 = ((int64_t)chunk * WAVES + wave) * TOK;
 
   uint32_t rf[TOK], rz[TOK], rd[TOK], ro[GATE ? TOK : 1];
+  {
+    RowsFrom<TOK> f(g.f, t0, g.tokens, ES), z(g.z, t0, g.tokens, ES), d(g.dy, t0, g.tokens, ES), o(GATE ? g.o : g.z, t0, g.tokens, ES);
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    rf[i] = rz[i] = rd[i] = 0;
-    if (GATE) ro[GATE ? i : 0] = 0;
-    if (on && t0 + i < g.tokens) {
-      rf[i] = L::load(static_cast<const T*>(g.f.p) + (t0 + i) * g.f.stride + c, both);
-      rd[i] = L::load(static_cast<const T*>(g.dy.p) + (t0 + i) * g.dy.stride + c, both);
-      if (GATE) ro[GATE ? i : 0] = L::load(static_cast<const T*>(g.o.p) + (t0 + i) * g.o.stride + c, both);
-      rz[i] = L::load(static_cast<const T*>(g.z.p) + (t0 + i) * g.z.stride + c, both);
+    for (int i = 0; i < TOK; ++i) {
+      rf[i] = at.load(f.next());
+      rd[i] = at.load(d.next());
+      if (GATE) ro[GATE ? i : 0] = at.load(o.next());
+      rz[i] = at.load(z.next());
     }
   }
   float h[V];  // the state in front of the block
-#pragma unroll
-  for (int v = 0; v < V; ++v) h[v] = c + v < g.channels ? g.saved[(int64_t)chunk * g.channels + c + v] : 0.f;
-  const Tokens<TOK> tk(g, t0);
+  load_state(g.saved, chunk, c, g.channels, h);
+  const Tokens<TOK> tk(g, t0, lane);
 
-  // forwards: the gates, the map of the states, the gradients at the tokens
+  // the gates, and the gradients at the tokens
   float a[TOK][V], b[TOK][V], d[TOK][V], q[GATE ? TOK : 1][V], A[V], U[V], K[V];
 #pragma unroll
-  for (int v = 0; v < V; ++v) A[v] = 1.f, U[v] = 0.f;
-#pragma unroll
   for (int i = 0; i < TOK; ++i) {
-    float f[V], z[V], o[V];
-    L::values(rf[i], f);
-    L::values(rz[i], z);
-    L::values(rd[i], d[i]);
-    if (GATE) L::values(ro[GATE ? i : 0], o);
-    if (tk.start >> i & 1) {
-      const float* const s = g.state ? g.state + tk.sequence(g, i) * g.channels + c : nullptr;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        A[v] = -0.f;
-        U[v] = s && c + v < g.channels ? s[v] : 0.f;
-      }
-    }
+    float f[V], o[V];
+    at.values(rf[i], f);
+    at.values(rd[i], d[i]);
+    if (GATE) at.values(ro[GATE ? i : 0], o);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       gates<EXACT>(f[v], a[i][v], b[i][v]);
@@ -380,7 +413,21 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_bwd_kernel(const Rec
         gates<EXACT>(o[v], s, n);
         q[GATE ? i : 0][v] = d[i][v] * fmaf(o[v] * s, n, s);  // dy swish'(o)
         d[i][v] *= o[v] * s;
+        asm volatile("" : "+v"(d[i][v]), "+v"(q[GATE ? i : 0][v]));
       }
+    }
+  }
+  // forwards: the map of the states
+#pragma unroll
+  for (int v = 0; v < V; ++v) A[v] = 1.f, U[v] = 0.f;
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    float z[V];
+    at.values(rz[i], z);
+    if (tk.start >> i & 1) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) U[v] = 0.f;
+      if (g.state) load_state(g.state, tk.sequence(i), c, g.channels, U);
     }
     if (tk.live >> i & 1) {
 #pragma unroll
@@ -390,6 +437,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_bwd_kernel(const Rec
       }
     }
   }
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) asm volatile("" : "+v"(rz[i]));  // (the products with z are formed again below, not kept)
   // backwards: what the tokens pass on to the ones in front of them, without what comes in from behind
 #pragma unroll
   for (int v = 0; v < V; ++v) K[v] = 0.f;
@@ -397,9 +446,9 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_bwd_kernel(const Rec
   for (int i = TOK - 1; i >= 0; --i) {
     if (!(tk.live >> i & 1)) continue;
     if (tk.last >> i & 1) {
-      const float* const s = g.dfinal ? g.dfinal + tk.sequence(g, i) * g.channels + c : nullptr;
 #pragma unroll
-      for (int v = 0; v < V; ++v) K[v] = s && c + v < g.channels ? s[v] : 0.f;
+      for (int v = 0; v < V; ++v) K[v] = 0.f;
+      if (g.dfinal) load_state(g.dfinal, tk.sequence(i), c, g.channels, K);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) K[v] = tk.start >> i & 1 ? 0.f : a[i][v] * (d[i][v] + K[v]);
@@ -415,79 +464,81 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_bwd_kernel(const Rec
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     A[v] = 1.f, K[v] = 0.f, pa[v] = 1.f, pu[v] = 0.f;
-#pragma unroll
+#pragma unroll 2
     for (int w = WAVES - 1; w >= 0; --w) {
       const float m = mine[w][lane * V + v].x;
       if (w == wave) pa[v] = A[v], pu[v] = K[v];
       join(A[v], K[v], m, mine_k[w][lane * V + v]);
     }
   }
-  if (g.maps && wave == 0) leave_map<V>(g, at, c, A, K);
+  if (g.maps && wave == 0) leave_map<V>(g, place_at, c, A, K);
 #pragma unroll
   for (int v = 0; v < V; ++v)
-#pragma unroll
-    for (int w = 0; w < WAVES - 1; ++w) {
+#pragma unroll 2
+    for (int w = 0; w < wave; ++w) {
       const float2 m = mine[w][lane * V + v];
-      if (w < wave) h[v] = cut(m.x) ? m.y : fmaf(m.x, h[v], m.y);
+      h[v] = cut(m.x) ? m.y : fmaf(m.x, h[v], m.y);
     }
-  // forwards again, with the states: the output gate's gradient; hz: h_{t-1} - z
-  float hz[TOK][V];
+  // forwards again, with the states: the output gate's gradient; w: a (h_{t-1} - z)
+  float w[TOK][V];
+  auto states = [&](auto whole) __attribute__((always_inline)) {
+    char* row = GATE ? static_cast<char*>(g.dgo) + t0 * g.do_stride * ES : nullptr;
 #pragma unroll
-  for (int i = 0; i < TOK; ++i) {
-    float z[V], e[V];
-    L::values(rz[i], z);
-    if (tk.start >> i & 1) {
-      const float* const s = g.state ? g.state + tk.sequence(g, i) * g.channels + c : nullptr;
+    for (int i = 0; i < TOK; ++i, row += g.do_stride * ES) {
+      float z[V], e[V];
+      at.values(rz[i], z);
+      if (tk.start >> i & 1) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) h[v] = s && c + v < g.channels ? s[v] : 0.f;
+        for (int v = 0; v < V; ++v) h[v] = 0.f;
+        if (g.state) load_state(g.state, tk.sequence(i), c, g.channels, h);
+      }
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        w[i][v] = a[i][v] * (h[v] - z[v]);
+        asm volatile("" : "+v"(w[i][v]));
+        h[v] = fmaf(a[i][v], h[v], b[i][v] * z[v]);
+        if (GATE) e[v] = q[GATE ? i : 0][v] * h[v];
+      }
+      if (GATE && (tk.live >> i & 1) && (decltype(whole)::value || c < g.channels)) at.template store<decltype(whole)::value>(row, e);
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      hz[i][v] = h[v] - z[v];
-      if (tk.live >> i & 1) h[v] = fmaf(a[i][v], h[v], b[i][v] * z[v]);
-      if (GATE) e[v] = q[GATE ? i : 0][v] * h[v];
-    }
-    if (GATE && on && (tk.live >> i & 1)) L::store(static_cast<T*>(g.dgo) + (t0 + i) * g.do_stride + c, both, e);
-  }
-  if (g.maps) {
-    come_in<V>(g, at, c, wave, lane, got, head, x);
-    if (wave == 0) leave_head<V>(g, at, c, A, K, x);
-  }
+  };
+  if (full) states(std::true_type{});
+  else states(std::false_type{});
+  if (g.maps) come_in<V, WAVES>(g, place_at, c, wave, lane, got, A, K, x);
+  if (c >= g.channels || t0 >= g.tokens) return;
 #pragma unroll
   for (int v = 0; v < V; ++v) x[v] = cut(pa[v]) ? pu[v] : fmaf(pa[v], x[v], pu[v]);
   // and backwards with what comes in
+  auto finish = [&](auto whole) __attribute__((always_inline)) {
+    char* fr = static_cast<char*>(g.df) + (t0 + TOK - 1) * g.df_stride * ES;
+    char* zr = static_cast<char*>(g.dz) + (t0 + TOK - 1) * g.dz_stride * ES;
 #pragma unroll
-  for (int i = TOK - 1; i >= 0; --i) {
-    if (!(tk.live >> i & 1)) continue;
-    const bool first = tk.start >> i & 1;
-    if (tk.last >> i & 1) {
-      const float* const s = g.dfinal ? g.dfinal + tk.sequence(g, i) * g.channels + c : nullptr;
+    for (int i = TOK - 1; i >= 0; --i, fr -= g.df_stride * ES, zr -= g.dz_stride * ES) {
+      if (!(tk.live >> i & 1)) continue;
+      if (tk.last >> i & 1) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) x[v] = s && c + v < g.channels ? s[v] : 0.f;
-    }
-    float df[V], dz[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const float G = d[i][v] + x[v];
-      dz[v] = b[i][v] * G;
-      df[v] = a[i][v] * hz[i][v] * dz[v];
-      x[v] = a[i][v] * G;
-    }
-    if (on) {
-      L::store(static_cast<T*>(g.df) + (t0 + i) * g.df_stride + c, both, df);
-      L::store(static_cast<T*>(g.dz) + (t0 + i) * g.dz_stride + c, both, dz);
-    }
-    if (first) {
-      if (g.dstate) {
-        float* const s = g.dstate + tk.sequence(g, i) * g.channels + c;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (c + v < g.channels) s[v] = x[v];
+        for (int v = 0; v < V; ++v) x[v] = 0.f;
+        if (g.dfinal) load_state(g.dfinal, tk.sequence(i), c, g.channels, x);
       }
+      float df[V], dz[V];
 #pragma unroll
-      for (int v = 0; v < V; ++v) x[v] = 0.f;
+      for (int v = 0; v < V; ++v) {
+        const float G = d[i][v] + x[v];
+        dz[v] = b[i][v] * G;
+        df[v] = w[i][v] * dz[v];
+        x[v] = a[i][v] * G;
+      }
+      at.template store<decltype(whole)::value>(fr, df);
+      at.template store<decltype(whole)::value>(zr, dz);
+      if (tk.start >> i & 1) {
+        if (g.dstate) store_state(g.dstate, tk.sequence(i), c, g.channels, x);
+#pragma unroll
+        for (int v = 0; v < V; ++v) x[v] = 0.f;
+      }
     }
-  }
+  };
+  if (full) finish(std::true_type{});
+  else finish(std::false_type{});
 }
 
 // In front of a scan: the words of its chain and its counter, the tokens' sequences, and what comes out of sequences without
@@ -523,10 +574,11 @@ __global__ __launch_bounds__(256) void recurrence_prepare_kernel(unsigned long l
 
 // The workspace: words of the chain, the counter, the tokens' sequences.
 struct Layout { size_t maps, heads, counter, seq, end; int64_t words; int chunks, columns; bool chained; };
-Layout layout_of(const ast_recurrence_cfg& c, int tok) {
+Layout layout_of(const ast_recurrence_cfg& c, int per) {
   Layout l = {};
-  const int per = tok * WAVES, width = 64 * (c.dtype == AST_F32 ? 1 : 2);
+  
   l.chunks = (int)((c.tokens + per - 1) / per);
+  const int width = 64 * (c.dtype == AST_F32 ? 1 : 2);  // channels of a block
   l.columns = (int)((c.channels + width - 1) / width);
   // (chunks that each begin with a sequence's first token need nothing from each other)
   l.chained = l.chunks > 1 && (c.offsets_dev || per % c.period != 0);
@@ -565,12 +617,12 @@ void prepare(hipStream_t st, const ast_recurrence_cfg& c, const Layout& l, void*
 }  // namespace
 
 size_t recurrence_ws_bytes(const ast_recurrence_cfg& c) {
-  return std::max(layout_of(c, FWD_TOK).end, layout_of(c, BWD_TOK).end);
+  return std::max(layout_of(c, FWD_TOK * FWD_WAVES).end, layout_of(c, BWD_TOK * BWD_WAVES).end);
 }
 
 void recurrence_fwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows& f, const ast_rows& z, const ast_rows* o,
                     const float* state, void* y, float* final, float* saved, void* ws) {
-  const Layout l = layout_of(c, FWD_TOK);
+  const Layout l = layout_of(c, FWD_TOK * FWD_WAVES);
   RecArgs g = {};
   g.f = {f.dev, f.stride};
   g.z = {z.dev, z.stride};
@@ -581,16 +633,17 @@ void recurrence_fwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows&
   g.saved = saved;
   prepare(st, c, l, ws, state, final, g);
   if (l.chunks == 0) return;
-  const dim3 grid((unsigned)l.chunks * (unsigned)l.columns), block(64 * WAVES);
+  const dim3 grid((unsigned)l.chunks * (unsigned)l.columns), block(64 * FWD_WAVES);
   auto go = [&](auto kernel) { KLAUNCH_NAMED("recurrence_kernel", kernel, grid, block, 0, st, g); };
-  if (c.dtype == AST_F32) go(o ? recurrence_kernel<float, true> : recurrence_kernel<float, false>);
-  else go(o ? recurrence_kernel<bf16_t, true> : recurrence_kernel<bf16_t, false>);
+  if (c.dtype == AST_F32) go(o ? recurrence_kernel<Lane32, true> : recurrence_kernel<Lane32, false>);
+  else if (c.channels > 1) go(o ? recurrence_kernel<Lane16, true> : recurrence_kernel<Lane16, false>);
+  else go(o ? recurrence_kernel<Lane16One, true> : recurrence_kernel<Lane16One, false>);
 }
 
 void recurrence_bwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows& dy, const ast_rows& f, const ast_rows& z,
                     const ast_rows* o, const float* state, const float* saved, const float* dfinal, const ast_rows& df,
                     const ast_rows& dz, const ast_rows* dgo, float* dstate, void* ws) {
-  const Layout l = layout_of(c, BWD_TOK);
+  const Layout l = layout_of(c, BWD_TOK * BWD_WAVES);
   RecArgs g = {};
   g.f = {f.dev, f.stride};
   g.z = {z.dev, z.stride};
@@ -610,10 +663,11 @@ void recurrence_bwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows&
   g.dstate = dstate;
   prepare(st, c, l, ws, dfinal, dstate, g);
   if (l.chunks == 0) return;
-  const dim3 grid((unsigned)l.chunks * (unsigned)l.columns), block(64 * WAVES);
+  const dim3 grid((unsigned)l.chunks * (unsigned)l.columns), block(64 * BWD_WAVES);
   auto go = [&](auto kernel) { KLAUNCH_NAMED("recurrence_bwd_kernel", kernel, grid, block, 0, st, g); };
-  if (c.dtype == AST_F32) go(o ? recurrence_bwd_kernel<float, true> : recurrence_bwd_kernel<float, false>);
-  else go(o ? recurrence_bwd_kernel<bf16_t, true> : recurrence_bwd_kernel<bf16_t, false>);
+  if (c.dtype == AST_F32) go(o ? recurrence_bwd_kernel<Lane32, true> : recurrence_bwd_kernel<Lane32, false>);
+  else if (c.channels > 1) go(o ? recurrence_bwd_kernel<Lane16, true> : recurrence_bwd_kernel<Lane16, false>);
+  else go(o ? recurrence_bwd_kernel<Lane16One, true> : recurrence_bwd_kernel<Lane16One, false>);
 }
 
 }  // namespace ast
