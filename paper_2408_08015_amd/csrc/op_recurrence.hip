@@ -31,6 +31,7 @@ namespace {
 constexpr int FWD_WAVES = 8, BWD_WAVES = 8;
 constexpr int GROUP = 32;               // blocks of a chain whose maps are joined one by one
 constexpr int FWD_TOK = 16, BWD_TOK = 8;  // tokens of a wavefront: 48 and 32 registers of loads (16 bits: two channels a register)
+constexpr int COUNTER = 64;              // a counter's words: no two in one cache line
 static_assert(BWD_TOK * BWD_WAVES == AST_RECURRENCE_CHUNK, "a block of the backward pass starts where a state was kept");
 static_assert(FWD_TOK * FWD_WAVES % AST_RECURRENCE_CHUNK == 0 && AST_RECURRENCE_CHUNK % FWD_TOK == 0, "kept states are a wavefront's first");
 
@@ -49,7 +50,7 @@ struct RecArgs {
   const int32_t* seq;           // a token's sequence, -1: none; nullptr: t / period
   int64_t tokens, period;
   unsigned long long *maps, *heads;  // the chain: [chunk][channels], [group][channels]; nullptr: chunks on their own
-  unsigned* counter;
+  unsigned* counters;           // [columns], COUNTER apart
   int channels, columns, chunks;
 };
 
@@ -161,12 +162,6 @@ __device__ __forceinline__ void leave(unsigned long long* p, unsigned long long 
 __device__ __forceinline__ unsigned long long look(unsigned long long* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ __forceinline__ unsigned long long take(unsigned long long* p) {
-  unsigned long long w;
-  while ((uint32_t)(w = look(p)) == NOT_YET) __builtin_amdgcn_s_sleep(1);
-  return w;
-}
-
 // What a wavefront's tokens are (the same in all its lanes): bit i stands for token i.
 template <int TOK>
 struct Tokens {
@@ -200,68 +195,93 @@ struct Tokens {
   }
 };
 
-// The value that comes in to a block whose place in the chain is `at` (in the order of the scan), for this lane's channels, and
-// what it leaves: its map (A, U) has been left before.  All threads of the block call it; got: LDS [WAVES][64 V].
-// Every wavefront joins the maps of SHARE blocks in front, then all join the wavefronts' maps, and only then the value in front
-// of the group is asked for: the last block of a group has nothing left to do but one step when it appears.
+// The chain.  Lane i takes the block's channels i, i + 64 here (words side by side), whichever it computes with.
+// A block leaves its map: that of its wavefronts' maps in the order of the scan (`back`: from the last).
 template <int V, int WAVES>
-__device__ __forceinline__ void come_in(const RecArgs& g, int at, int c, int wave, int lane, float2 (*got)[64 * V], const float (&A)[V],
-                                        const float (&U)[V], float (&x)[V]) {
+__device__ __forceinline__ void leave_map(const RecArgs& g, int at, int first, int lane, bool back, const float2 (*mine)[64 * V],
+                                          float (&A)[V], float (&U)[V]) {
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    const int c = first + lane + 64 * v;
+    A[v] = 1.f, U[v] = 0.f;
+#pragma unroll 2
+    for (int i = 0; i < WAVES; ++i) {
+      const float2 m = mine[back ? WAVES - 1 - i : i][lane + 64 * v];
+      join(A[v], U[v], m.x, m.y);
+    }
+    if (c < g.channels) leave(g.maps + (int64_t)at * g.channels + c, map_word(A[v], U[v]));
+  }
+}
+// What comes in to a block whose place in the chain is `at`, in x[channel]; all threads of the block call it.  Every wavefront joins
+// the maps of SHARE blocks in front; the first one joins theirs, steps from the value in front of the group, and leaves the
+// next group's value if this block is its group's last ((A, U): what leave_map gave it).
+template <int V, int WAVES>
+__device__ __forceinline__ void come_in(const RecArgs& g, int at, int first, int wave, int lane, float2 (*got)[64 * V], const float (&A)[V],
+                                        const float (&U)[V], float* x) {
   constexpr int SHARE = GROUP / WAVES;
   const int group = at / GROUP, r = at % GROUP;
   unsigned long long* const maps = g.maps + ((int64_t)group * GROUP + wave * SHARE) * g.channels;
-  float a[V], b[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    a[v] = 1.f, b[v] = 0.f;
-    unsigned long long w[SHARE];
-#pragma unroll
-    for (int j = 0; j < SHARE; ++j)  // (all asked for at once)
-      w[j] = wave * SHARE + j < r && c + v < g.channels ? look(maps + (int64_t)j * g.channels + c + v) : 0x3f800000u;
-#pragma unroll
-    for (int j = 0; j < SHARE; ++j) {
-      while ((uint32_t)w[j] == NOT_YET) {
-        __builtin_amdgcn_s_sleep(1);
-        w[j] = look(maps + (int64_t)j * g.channels + c + v);
-      }
-      join(a[v], b[v], __uint_as_float((uint32_t)w[j]), __uint_as_float((uint32_t)(w[j] >> 32)));
-    }
-    got[wave][lane * V + v] = make_float2(a[v], b[v]);
-  }
-  __syncthreads();
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    a[v] = 1.f, b[v] = 0.f;
-#pragma unroll 2
-    for (int w = 0; w < WAVES; ++w) {
-      const float2 m = got[w][lane * V + v];
-      join(a[v], b[v], m.x, m.y);
-    }
-  }
-  const bool hand_on = r == GROUP - 1 && at + 1 < g.chunks && wave == 0;
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    x[v] = 0.f;
-    if (group > 0 && c + v < g.channels) x[v] = __uint_as_float((uint32_t)(take(g.heads + (int64_t)group * g.channels + c + v) >> 32));
-    x[v] = cut(a[v]) ? b[v] : fmaf(a[v], x[v], b[v]);
-    if (hand_on && c + v < g.channels)
-      leave(g.heads + (int64_t)(group + 1) * g.channels + c + v, map_word(0.f, cut(A[v]) ? U[v] : fmaf(A[v], x[v], U[v])));
-  }
-}
-template <int V>
-__device__ __forceinline__ void leave_map(const RecArgs& g, int at, int c, const float (&A)[V], const float (&U)[V]) {
+  unsigned long long w[V][SHARE];
 #pragma unroll
   for (int v = 0; v < V; ++v)
-    if (c + v < g.channels) leave(g.maps + (int64_t)at * g.channels + c + v, map_word(A[v], U[v]));
+#pragma unroll
+    for (int j = 0; j < SHARE; ++j) {  // (all asked for at once)
+      const int c = first + lane + 64 * v;
+      w[v][j] = wave * SHARE + j < r && c < g.channels ? look(maps + (int64_t)j * g.channels + c) : 0x3f800000u;  // (1, 0) from nobody
+    }
+#pragma unroll
+  for (int v = 0; v < V; ++v) {
+    float a = 1.f, b = 0.f;
+#pragma unroll
+    for (int j = 0; j < SHARE; ++j) {
+      while ((uint32_t)w[v][j] == NOT_YET) {
+        __builtin_amdgcn_s_sleep(1);
+        w[v][j] = look(maps + (int64_t)j * g.channels + first + lane + 64 * v);
+      }
+      join(a, b, __uint_as_float((uint32_t)w[v][j]), __uint_as_float((uint32_t)(w[v][j] >> 32)));
+    }
+    got[wave][lane + 64 * v] = make_float2(a, b);
+  }
+  __syncthreads();
+  if (wave == 0) {
+    unsigned long long h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = first + lane + 64 * v;
+      h[v] = group > 0 && c < g.channels ? look(g.heads + (int64_t)group * g.channels + c) : 0;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = first + lane + 64 * v;
+      float a = 1.f, b = 0.f;
+#pragma unroll 2
+      for (int i = 0; i < WAVES; ++i) {
+        const float2 m = got[i][lane + 64 * v];
+        join(a, b, m.x, m.y);
+      }
+      while ((uint32_t)h[v] == NOT_YET && !cut(a)) {
+        __builtin_amdgcn_s_sleep(1);
+        h[v] = look(g.heads + (int64_t)group * g.channels + c);
+      }
+      const float in = cut(a) ? b : fmaf(a, __uint_as_float((uint32_t)(h[v] >> 32)), b);
+      if (r == GROUP - 1 && at + 1 < g.chunks && c < g.channels)
+        leave(g.heads + (int64_t)(group + 1) * g.channels + c, map_word(0.f, cut(A[v]) ? U[v] : fmaf(A[v], in, U[v])));
+      x[lane + 64 * v] = in;
+    }
+  }
+  __syncthreads();
 }
 
-// A block's place: in the order in which blocks start where they wait for each other.
-__device__ __forceinline__ unsigned place(const RecArgs& g) {
-  if (!g.maps) return blockIdx.x;
-  __shared__ unsigned p;
-  if (threadIdx.x == 0) p = atomicAdd(g.counter, 1u);
+// A block's channels and its place in their chain: in the order in which the blocks of these channels start where they wait for each
+// other (one counter for all channels would be the call's bound: 8 to 10 ns a block).
+struct Place { int at, column; };
+__device__ __forceinline__ Place place(const RecArgs& g) {
+  const int n = (int)(blockIdx.x / (unsigned)g.columns), column = (int)(blockIdx.x - (unsigned)n * (unsigned)g.columns);
+  if (!g.maps) return {n, column};
+  __shared__ int p;
+  if (threadIdx.x == 0) p = (int)atomicAdd(g.counters + column * COUNTER, 1u);
   __syncthreads();
-  return __builtin_amdgcn_readfirstlane(p);  // (the same in all lanes: rows have scalar addresses)
+  return {__builtin_amdgcn_readfirstlane(p), column};  // (the same in all lanes: rows have scalar addresses)
 }
 
 template <typename L, bool GATE>
@@ -271,8 +291,9 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 4) void recurrence_kernel(const Rec
   constexpr bool EXACT = sizeof(T) == 4;
   __shared__ float2 mine[WAVES][64 * V];
   __shared__ float2 got[WAVES][64 * V];
-  const unsigned p = place(g);
-  const int chunk = (int)(p / (unsigned)g.columns), column = (int)(p - (unsigned)chunk * (unsigned)g.columns);
+  __shared__ float head[64 * V];
+  const Place p = place(g);
+  const int chunk = p.at, column = p.column;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = (column * 64 + lane) * V;
   const L at(c, g.channels);
@@ -318,25 +339,24 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 4) void recurrence_kernel(const Rec
 #pragma unroll
   for (int v = 0; v < V; ++v) mine[wave][lane * V + v] = make_float2(tk.start ? -0.f : A[v], U[v]);  // (a NaN gate is no way through)
   __syncthreads();
-  // the block's map, and that of the wavefronts in front of this one
-  float pa[V], pu[V], x[V] = {};
+  float in[V] = {}, x[V];
+  if (g.maps) {
+    if (wave == 0) leave_map<V, WAVES>(g, chunk, column * 64 * V, lane, false, mine, A, U);
+    come_in<V, WAVES>(g, chunk, column * 64 * V, wave, lane, got, A, U, head);
+#pragma unroll
+    for (int v = 0; v < V; ++v) in[v] = head[lane * V + v];
+  }
+  // through the wavefronts in front of this one
 #pragma unroll
   for (int v = 0; v < V; ++v) {
-    A[v] = 1.f, U[v] = 0.f, pa[v] = 1.f, pu[v] = 0.f;
+    x[v] = in[v];
 #pragma unroll 2
-    for (int w = 0; w < WAVES; ++w) {
-      const float2 m = mine[w][lane * V + v];
-      if (w == wave) pa[v] = A[v], pu[v] = U[v];
-      join(A[v], U[v], m.x, m.y);
+    for (int i = 0; i < wave; ++i) {
+      const float2 m = mine[i][lane * V + v];
+      x[v] = cut(m.x) ? m.y : fmaf(m.x, x[v], m.y);
     }
   }
-  if (g.maps) {
-    if (wave == 0) leave_map<V>(g, chunk, c, A, U);
-    come_in<V, WAVES>(g, chunk, c, wave, lane, got, A, U, x);
-  }
   if (c >= g.channels || t0 >= g.tokens) return;
-#pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = cut(pa[v]) ? pu[v] : fmaf(pa[v], x[v], pu[v]);
   if (g.saved && t0 % AST_RECURRENCE_CHUNK == 0) store_state(g.saved, t0 / AST_RECURRENCE_CHUNK, c, g.channels, x);
   const unsigned through = tk.start ? (tk.start & 0u - tk.start) - 1 : ~0u;  // the tokens that x reaches
   auto finish = [&](auto full) __attribute__((always_inline)) {
@@ -371,11 +391,11 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 4) void recurrence_bwd_kernel(const
   constexpr int V = L::V, TOK = BWD_TOK, WAVES = BWD_WAVES, ES = sizeof(T);
   constexpr bool EXACT = sizeof(T) == 4;
   __shared__ float2 mine[WAVES][64 * V];
-  __shared__ float mine_k[WAVES][64 * V];
+  __shared__ float2 mine_k[WAVES][64 * V];
   __shared__ float2 got[WAVES][64 * V];
-  const unsigned p = place(g);
-  const int place_at = (int)(p / (unsigned)g.columns), column = (int)(p - (unsigned)place_at * (unsigned)g.columns);
-  const int chunk = g.chunks - 1 - place_at;  // (the scan runs from the last token to the first)
+  __shared__ float head[64 * V];
+  const Place p = place(g);
+  const int chunk = g.chunks - 1 - p.at, column = p.column;  // (the scan runs from the last token to the first)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int c = (column * 64 + lane) * V;
   const L at(c, g.channels);
@@ -456,22 +476,11 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 4) void recurrence_bwd_kernel(const
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     mine[wave][lane * V + v] = make_float2(tk.start ? -0.f : A[v], U[v]);  // (a NaN gate is no way through)
-    mine_k[wave][lane * V + v] = K[v];
+    mine_k[wave][lane * V + v] = make_float2(tk.start ? -0.f : A[v], K[v]);
   }
   __syncthreads();
-  // the block's map of K, and that of the wavefronts behind this one; the state in front of this wavefront
-  float pa[V], pu[V], x[V] = {};
-#pragma unroll
-  for (int v = 0; v < V; ++v) {
-    A[v] = 1.f, K[v] = 0.f, pa[v] = 1.f, pu[v] = 0.f;
-#pragma unroll 2
-    for (int w = WAVES - 1; w >= 0; --w) {
-      const float m = mine[w][lane * V + v].x;
-      if (w == wave) pa[v] = A[v], pu[v] = K[v];
-      join(A[v], K[v], m, mine_k[w][lane * V + v]);
-    }
-  }
-  if (g.maps && wave == 0) leave_map<V>(g, place_at, c, A, K);
+  if (g.maps && wave == 0) leave_map<V, WAVES>(g, p.at, column * 64 * V, lane, true, mine_k, A, K);
+  // the state in front of this wavefront
 #pragma unroll
   for (int v = 0; v < V; ++v)
 #pragma unroll 2
@@ -504,10 +513,20 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 4) void recurrence_bwd_kernel(const
   };
   if (full) states(std::true_type{});
   else states(std::false_type{});
-  if (g.maps) come_in<V, WAVES>(g, place_at, c, wave, lane, got, A, K, x);
+  float x[V] = {};
+  if (g.maps) {
+    come_in<V, WAVES>(g, p.at, column * 64 * V, wave, lane, got, A, K, head);
+#pragma unroll
+    for (int v = 0; v < V; ++v) x[v] = head[lane * V + v];
+  }
   if (c >= g.channels || t0 >= g.tokens) return;
 #pragma unroll
-  for (int v = 0; v < V; ++v) x[v] = cut(pa[v]) ? pu[v] : fmaf(pa[v], x[v], pu[v]);
+  for (int v = 0; v < V; ++v)  // through the wavefronts behind this one
+#pragma unroll 2
+    for (int i = WAVES - 1; i > wave; --i) {
+      const float2 m = mine_k[i][lane * V + v];
+      x[v] = cut(m.x) ? m.y : fmaf(m.x, x[v], m.y);
+    }
   // and backwards with what comes in
   auto finish = [&](auto whole) __attribute__((always_inline)) {
     char* fr = static_cast<char*>(g.df) + (t0 + TOK - 1) * g.df_stride * ES;
@@ -541,13 +560,14 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 4) void recurrence_bwd_kernel(const
   else finish(std::false_type{});
 }
 
-// In front of a scan: the words of its chain and its counter, the tokens' sequences, and what comes out of sequences without
+// In front of a scan: the words of its chain and its counters, the tokens' sequences, and what comes out of sequences without
 // tokens (copied, or 0 where nothing is passed in).
-__global__ __launch_bounds__(256) void recurrence_prepare_kernel(unsigned long long* words, int64_t n_words, unsigned* counter,
+__global__ __launch_bounds__(256) void recurrence_prepare_kernel(unsigned long long* words, int64_t n_words, unsigned* counters, int columns,
                                                                  const int32_t* offsets, int64_t sequences, int64_t tokens,
                                                                  int32_t* seq, const float* in, float* out, int channels) {
   const int64_t me = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)gridDim.x * 256;
-  if (me == 0 && counter) *counter = 0;
+  if (counters)
+    for (int64_t i = me; i < columns; i += all) counters[i * COUNTER] = 0;
   for (int64_t i = me; i < n_words; i += all) words[i] = ~0ull;
   if (!offsets) return;
   const int32_t first = offsets[0], end = offsets[sequences];
@@ -572,8 +592,8 @@ __global__ __launch_bounds__(256) void recurrence_prepare_kernel(unsigned long l
   }
 }
 
-// The workspace: words of the chain, the counter, the tokens' sequences.
-struct Layout { size_t maps, heads, counter, seq, end; int64_t words; int chunks, columns; bool chained; };
+// The workspace: words of the chain, the counters, the tokens' sequences.
+struct Layout { size_t maps, heads, counters, seq, end; int64_t words; int chunks, columns; bool chained; };
 Layout layout_of(const ast_recurrence_cfg& c, int per) {
   Layout l = {};
   
@@ -586,8 +606,8 @@ Layout layout_of(const ast_recurrence_cfg& c, int per) {
   if (l.chained) {
     l.words = ((int64_t)l.chunks + (l.chunks + GROUP - 1) / GROUP) * c.channels;
     l.heads = (size_t)l.chunks * c.channels * 8;
-    at = l.counter = (size_t)l.words * 8;
-    at += 16;
+    at = l.counters = (size_t)l.words * 8;
+    at += (size_t)l.columns * COUNTER * 4;
   }
   l.seq = at;
   if (c.offsets_dev) at += ((size_t)c.tokens * 4 + 15) / 16 * 16;
@@ -605,13 +625,13 @@ void prepare(hipStream_t st, const ast_recurrence_cfg& c, const Layout& l, void*
   if (l.chained) {
     g.maps = reinterpret_cast<unsigned long long*>(w + l.maps);
     g.heads = reinterpret_cast<unsigned long long*>(w + l.heads);
-    g.counter = reinterpret_cast<unsigned*>(w + l.counter);
+    g.counters = reinterpret_cast<unsigned*>(w + l.counters);
   }
   if (c.offsets_dev) g.seq = reinterpret_cast<int32_t*>(w + l.seq);
   if (!l.chained && !c.offsets_dev) return;
   const int64_t most = std::max<int64_t>({l.words / 4, c.offsets_dev ? c.tokens : 0, c.offsets_dev && out ? 64 * c.sequences : 0, 1});
   KLAUNCH(recurrence_prepare_kernel, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 2048)), dim3(256), 0, st, g.maps, l.words,
-          g.counter, c.offsets_dev, c.sequences, c.tokens, reinterpret_cast<int32_t*>(w + l.seq), in, out, (int)c.channels);
+          g.counters, l.columns, c.offsets_dev, c.sequences, c.tokens, reinterpret_cast<int32_t*>(w + l.seq), in, out, (int)c.channels);
 }
 
 }  // namespace
