@@ -86,13 +86,16 @@ struct Lane16 {  // (two channels or more)
     else *reinterpret_cast<bf16_t*>(p + 2) = (bf16_t)w;
   }
 };
-struct Lane16One {  // rows of a single channel
+struct Lane16One {  // one channel a lane: rows of a single one, and calls that would leave compute units without a block
   typedef bf16_t T;
   static constexpr int V = 1;
-  __device__ __forceinline__ Lane16One(int, int) {}
-  __device__ __forceinline__ uint32_t load(const void* row) const { return *static_cast<const bf16_t*>(row); }
+  uint32_t at;
+  __device__ __forceinline__ Lane16One(int c, int channels) : at(2u * (uint32_t)min(c, channels - 1)) {}
+  __device__ __forceinline__ uint32_t load(const void* row) const { return *reinterpret_cast<const bf16_t*>(static_cast<const char*>(row) + at); }
   __device__ __forceinline__ void values(uint32_t w, float (&v)[1]) const { v[0] = __uint_as_float(w << 16); }
-  template <bool FULL> __device__ __forceinline__ void store(void* row, const float (&v)[1]) const { store1(static_cast<bf16_t*>(row), v[0]); }
+  template <bool FULL> __device__ __forceinline__ void store(void* row, const float (&v)[1]) const {
+    store1(reinterpret_cast<bf16_t*>(static_cast<char*>(row) + at), v[0]);
+  }
 };
 // the rows of a wavefront's tokens, one after the other; behind the last token: that one again
 template <int TOK>
@@ -143,6 +146,28 @@ __device__ __forceinline__ void gates(float x, float& a, float& b) {
   a = x >= 0.f ? r : s;
   b = x >= 0.f ? s : r;
   asm volatile("" : "+v"(a), "+v"(b));  // (chosen here: kept for later, each choice would hold two more registers and a mask)
+}
+
+// Both in one register: the smaller one, which a subtraction from 1 gives the larger one of to its full precision, with the sign
+// bit where it is sigmoid(x).
+template <bool EXACT>
+__device__ __forceinline__ float small_gate(float x) {
+  const float e = exp_neg<EXACT>(x);
+  float r = __builtin_amdgcn_rcpf(1.f + e);
+  if (EXACT) r = fmaf(r, fmaf(-(1.f + e), r, 1.f), r);
+  float s = __builtin_copysignf(e * r, x);
+  asm volatile("" : "+v"(s));
+  return s;
+}
+// a h + (1 - a) z, and A a
+__device__ __forceinline__ float step(float s, float h, float z) {
+  const float m = fabsf(s), big = 1.f - m;
+  const bool neg = (int)__float_as_uint(s) < 0;
+  return fmaf(m, neg ? h : z, big * (neg ? z : h));
+}
+__device__ __forceinline__ float keep(float s, float A) {
+  const float m = fabsf(s);
+  return A * ((int)__float_as_uint(s) < 0 ? m : 1.f - m);
 }
 
 __device__ __forceinline__ bool cut(float A) { return (int)__float_as_uint(A) < 0; }  // nothing passes through
@@ -310,14 +335,20 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 4) void recurrence_kernel(const Rec
     }
   }
   const Tokens<TOK> tk(g, t0, lane);
-  // the wavefront's map, token by token: value behind token i = P[i] x + H[i]
-  float P[TOK][V], H[TOK][V], A[V], U[V];
+  // the gates, and the wavefront's map
+  float s[TOK][V], A[V], U[V];
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) {
+    float f[V];
+    at.values(rf[i], f);
+#pragma unroll
+    for (int v = 0; v < V; ++v) s[i][v] = small_gate<EXACT>(f[v]);
+  }
 #pragma unroll
   for (int v = 0; v < V; ++v) A[v] = 1.f, U[v] = 0.f;
 #pragma unroll
   for (int i = 0; i < TOK; ++i) {
-    float f[V], z[V];
-    at.values(rf[i], f);
+    float z[V];
     at.values(rz[i], z);
     if (tk.start >> i & 1) {
 #pragma unroll
@@ -327,21 +358,37 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 4) void recurrence_kernel(const Rec
     if (tk.live >> i & 1) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        float a, b;
-        gates<EXACT>(f[v], a, b);
-        U[v] = fmaf(a, U[v], b * z[v]);
-        A[v] *= a;
+        U[v] = step(s[i][v], U[v], z[v]);
+        A[v] = keep(s[i][v], A[v]);
+        // (a first token's gate gives way to its state: the one in front, which may have been replaced by then, is read once)
+        if (tk.start >> i & 1) s[i][v] = U[v];
       }
     }
-#pragma unroll
-    for (int v = 0; v < V; ++v) P[i][v] = A[v], H[i][v] = U[v];
   }
+#pragma unroll
+  for (int i = 0; i < TOK; ++i) asm volatile("" : "+v"(rz[i]));  // (what is formed of z and the gates is formed again below, not kept)
 #pragma unroll
   for (int v = 0; v < V; ++v) mine[wave][lane * V + v] = make_float2(tk.start ? -0.f : A[v], U[v]);  // (a NaN gate is no way through)
   __syncthreads();
+  if (g.maps && wave == 0) leave_map<V, WAVES>(g, chunk, column * 64 * V, lane, false, mine, A, U);
+  // the output gates, while the map is under way
+  float w[GATE ? TOK : 1][V];
+  if (GATE) {
+#pragma unroll
+    for (int i = 0; i < TOK; ++i) {
+      float o[V];
+      at.values(ro[GATE ? i : 0], o);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        float a, b;
+        gates<EXACT>(o[v], a, b);
+        w[GATE ? i : 0][v] = o[v] * a;
+        asm volatile("" : "+v"(w[GATE ? i : 0][v]));
+      }
+    }
+  }
   float in[V] = {}, x[V];
   if (g.maps) {
-    if (wave == 0) leave_map<V, WAVES>(g, chunk, column * 64 * V, lane, false, mine, A, U);
     come_in<V, WAVES>(g, chunk, column * 64 * V, wave, lane, got, A, U, head);
 #pragma unroll
     for (int v = 0; v < V; ++v) in[v] = head[lane * V + v];
@@ -358,27 +405,21 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 4) void recurrence_kernel(const Rec
   }
   if (c >= g.channels || t0 >= g.tokens) return;
   if (g.saved && t0 % AST_RECURRENCE_CHUNK == 0) store_state(g.saved, t0 / AST_RECURRENCE_CHUNK, c, g.channels, x);
-  const unsigned through = tk.start ? (tk.start & 0u - tk.start) - 1 : ~0u;  // the tokens that x reaches
   auto finish = [&](auto full) __attribute__((always_inline)) {
     constexpr bool FULL = decltype(full)::value;
     char* row = static_cast<char*>(g.y) + t0 * g.channels * ES;
 #pragma unroll
     for (int i = 0; i < TOK; ++i, row += (int64_t)g.channels * ES) {
       if (!(tk.live >> i & 1)) continue;
-      float h[V], y[V], o[V];
-      if (GATE) at.values(ro[GATE ? i : 0], o);
+      float z[V], y[V];
+      at.values(rz[i], z);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        h[v] = through >> i & 1 ? fmaf(P[i][v], x[v], H[i][v]) : H[i][v];
-        y[v] = h[v];
-        if (GATE) {
-          float a, b;
-          gates<EXACT>(o[v], a, b);
-          y[v] *= o[v] * a;
-        }
+        x[v] = tk.start >> i & 1 ? s[i][v] : step(s[i][v], x[v], z[v]);
+        y[v] = GATE ? x[v] * w[GATE ? i : 0][v] : x[v];
       }
       at.template store<FULL>(row, y);
-      if (g.final && (tk.last >> i & 1)) store_state(g.final, tk.sequence(i), c, g.channels, h);
+      if (g.final && (tk.last >> i & 1)) store_state(g.final, tk.sequence(i), c, g.channels, x);
     }
   };
   if ((column + 1) * 64 * V <= g.channels) finish(std::true_type{});
@@ -465,10 +506,17 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 4) void recurrence_bwd_kernel(const
 #pragma unroll
   for (int i = TOK - 1; i >= 0; --i) {
     if (!(tk.live >> i & 1)) continue;
-    if (tk.last >> i & 1) {
+    if (tk.last >> i & 1) {  // (what reaches the state behind a sequence is read once: dstate may be the same tensor)
 #pragma unroll
       for (int v = 0; v < V; ++v) K[v] = 0.f;
-      if (g.dfinal) load_state(g.dfinal, tk.sequence(i), c, g.channels, K);
+      if (g.dfinal) {
+        load_state(g.dfinal, tk.sequence(i), c, g.channels, K);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          d[i][v] += K[v];
+          K[v] = 0.f;
+        }
+      }
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) K[v] = tk.start >> i & 1 ? 0.f : a[i][v] * (d[i][v] + K[v]);
@@ -537,7 +585,6 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 4) void recurrence_bwd_kernel(const
       if (tk.last >> i & 1) {
 #pragma unroll
         for (int v = 0; v < V; ++v) x[v] = 0.f;
-        if (g.dfinal) load_state(g.dfinal, tk.sequence(i), c, g.channels, x);
       }
       float df[V], dz[V];
 #pragma unroll
@@ -558,6 +605,45 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 4) void recurrence_bwd_kernel(const
   };
   if (full) finish(std::true_type{});
   else finish(std::false_type{});
+}
+
+// Sequences of one token each, forward: nothing is scanned.  Four channels a thread.
+template <typename T, bool GATE>
+__global__ __launch_bounds__(256) void recurrence_token_kernel(const RecArgs g) {
+  constexpr bool EXACT = sizeof(T) == 4;
+  const int per_row = (g.channels + 3) / 4;
+  const int64_t n = g.tokens * per_row;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t t = i / per_row;
+    const int c = (int)(i - t * per_row) * 4, some = min(4, g.channels - c);
+    const T* const f = static_cast<const T*>(g.f.p) + t * g.f.stride + c;
+    const T* const z = static_cast<const T*>(g.z.p) + t * g.z.stride + c;
+    const T* const o = GATE ? static_cast<const T*>(g.o.p) + t * g.o.stride + c : nullptr;
+    const int64_t at = t * g.channels + c;
+    float fv[4], zv[4], ov[4], h[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int e = min(k, some - 1);
+      fv[k] = load1(f + e);
+      zv[k] = load1(z + e);
+      if (GATE) ov[k] = load1(o + e);
+      h[k] = g.state ? g.state[at + e] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (k >= some) break;
+      const float x = step(small_gate<EXACT>(fv[k]), h[k], zv[k]);
+      float y = x;
+      if (GATE) {
+        float a, b;
+        gates<EXACT>(ov[k], a, b);
+        y *= ov[k] * a;
+      }
+      store1(static_cast<T*>(g.y) + at + k, y);
+      if (g.final) g.final[at + k] = x;
+      if (g.saved && t % AST_RECURRENCE_CHUNK == 0) g.saved[t / AST_RECURRENCE_CHUNK * g.channels + c + k] = 0.f;  // (the token begins a sequence)
+    }
+  }
 }
 
 // In front of a scan: the words of its chain and its counters, the tokens' sequences, and what comes out of sequences without
@@ -593,12 +679,12 @@ __global__ __launch_bounds__(256) void recurrence_prepare_kernel(unsigned long l
 }
 
 // The workspace: words of the chain, the counters, the tokens' sequences.
-struct Layout { size_t maps, heads, counters, seq, end; int64_t words; int chunks, columns; bool chained; };
+struct Layout { size_t maps, heads, counters, seq, end; int64_t words; int chunks, columns; bool chained, pairs; };
 Layout layout_of(const ast_recurrence_cfg& c, int per) {
   Layout l = {};
-  
   l.chunks = (int)((c.tokens + per - 1) / per);
-  const int width = 64 * (c.dtype == AST_F32 ? 1 : 2);  // channels of a block
+  l.pairs = c.dtype != AST_F32 && c.channels > 1 && (int64_t)l.chunks * ((c.channels + 127) / 128) >= 256;
+  const int width = l.pairs ? 128 : 64;  // channels of a block
   l.columns = (int)((c.channels + width - 1) / width);
   // (chunks that each begin with a sequence's first token need nothing from each other)
   l.chained = l.chunks > 1 && (c.offsets_dev || per % c.period != 0);
@@ -653,10 +739,18 @@ void recurrence_fwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows&
   g.saved = saved;
   prepare(st, c, l, ws, state, final, g);
   if (l.chunks == 0) return;
+  if (!c.offsets_dev && c.period == 1) {
+    const int64_t n = c.tokens * ((c.channels + 3) / 4);
+    const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 16));
+    auto go = [&](auto kernel) { KLAUNCH_NAMED("recurrence_token_kernel", kernel, grid, dim3(256), 0, st, g); };
+    if (c.dtype == AST_F32) go(o ? recurrence_token_kernel<float, true> : recurrence_token_kernel<float, false>);
+    else go(o ? recurrence_token_kernel<bf16_t, true> : recurrence_token_kernel<bf16_t, false>);
+    return;
+  }
   const dim3 grid((unsigned)l.chunks * (unsigned)l.columns), block(64 * FWD_WAVES);
   auto go = [&](auto kernel) { KLAUNCH_NAMED("recurrence_kernel", kernel, grid, block, 0, st, g); };
   if (c.dtype == AST_F32) go(o ? recurrence_kernel<Lane32, true> : recurrence_kernel<Lane32, false>);
-  else if (c.channels > 1) go(o ? recurrence_kernel<Lane16, true> : recurrence_kernel<Lane16, false>);
+  else if (l.pairs) go(o ? recurrence_kernel<Lane16, true> : recurrence_kernel<Lane16, false>);
   else go(o ? recurrence_kernel<Lane16One, true> : recurrence_kernel<Lane16One, false>);
 }
 
@@ -686,7 +780,7 @@ void recurrence_bwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows&
   const dim3 grid((unsigned)l.chunks * (unsigned)l.columns), block(64 * BWD_WAVES);
   auto go = [&](auto kernel) { KLAUNCH_NAMED("recurrence_bwd_kernel", kernel, grid, block, 0, st, g); };
   if (c.dtype == AST_F32) go(o ? recurrence_bwd_kernel<Lane32, true> : recurrence_bwd_kernel<Lane32, false>);
-  else if (c.channels > 1) go(o ? recurrence_bwd_kernel<Lane16, true> : recurrence_bwd_kernel<Lane16, false>);
+  else if (l.pairs) go(o ? recurrence_bwd_kernel<Lane16, true> : recurrence_bwd_kernel<Lane16, false>);
   else go(o ? recurrence_bwd_kernel<Lane16One, true> : recurrence_bwd_kernel<Lane16One, false>);
 }
 

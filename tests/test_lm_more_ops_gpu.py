@@ -255,6 +255,9 @@ def test_recurrence(ops, T, C, how, dt, gate, state, layout):
     two = ops.recurrence_backward(dy, f, z, saved, o=o, state=h0, dfinal=dfin, dstate=True, **kw)
     rows = torch.from_numpy(live[:, 0]).cuda()
     assert all(p is None or torch.equal(p[rows], q[rows]) for p, q in zip(two[:3], (df, dz, do))) and torch.equal(two[3], dstate)
+    if state:   # the states' gradients in place
+        moved = dfin.clone()
+        assert ops.recurrence_backward(dy, f, z, saved, o=o, state=h0, dfinal=moved, dstate=moved, **kw)[3] is moved and torch.equal(moved, dstate)
     three = ops.recurrence_backward(dy, f, z, saved, o=o, state=h0, dfinal=dfin, out=[t for t in (f, z, o) if t is not None], **kw)
     assert three[0] is f and all(p is None or torch.equal(p[rows], q[rows]) for p, q in zip(three[:3], (df, dz, do)))
 
