@@ -33,61 +33,92 @@ struct DistillArgs {
 constexpr float kLog2e = 1.44269504f;
 constexpr float kLowest = -3.402823466e38f;  // where a running maximum starts (an infinity would give NaN for -inf - -inf)
 constexpr int kMostEntries = 1024;
+constexpr int kSeen = 32768;  // places that an id's lowest bits tell apart
 
 __device__ __forceinline__ float exp_scaled(float x, float s) { return __builtin_amdgcn_exp2f(x * s); }
 
+// How the two exponentials of a value are formed.  ONE: there is one only (no label counts, or the temperature is 1); SQUARE,
+// FOURTH: the temperature is 2 or 4, and exp(x) is a power of exp(x / T); BOTH: any other temperature.
+enum Exps : int { ONE = 0, SQUARE = 1, FOURTH = 2, BOTH = 3 };
+template <Exps E>
+__device__ __forceinline__ void exps(float d, float scale, float& a, float& b) {
+  a = exp_scaled(d, scale);
+  b = E == BOTH ? exp_scaled(d, kLog2e) : a;
+  if (E == SQUARE || E == FOURTH) b *= b;
+  if (E == FOURTH) b *= b;
+}
+
 struct Sums { float m, a, b; };  // maximum, sum at the temperature, sum without it
-template <bool TWO>
+template <Exps E>
 __device__ __forceinline__ void merge(Sums& s, float m, float a, float b, float scale) {
-  const float top = fmaxf(s.m, m), x = exp_scaled(s.m - top, scale), y = exp_scaled(m - top, scale);
-  s.a = s.a * x + a * y;
-  if (TWO) s.b = s.b * exp_scaled(s.m - top, kLog2e) + b * exp_scaled(m - top, kLog2e);
+  const float top = fmaxf(s.m, m);
+  float xa, xb, ya, yb;
+  exps<E>(s.m - top, scale, xa, xb);
+  exps<E>(m - top, scale, ya, yb);
+  s.a = s.a * xa + a * ya;
+  if (E != ONE) s.b = s.b * xb + b * yb;
   s.m = top;
 }
 
-template <int THREADS, bool TWO>
+template <int THREADS, Exps E>
 __device__ __forceinline__ Sums block_sums(Sums s, float scale, float (*sh)[16]) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2)
-    merge<TWO>(s, __shfl_xor(s.m, d, 64), __shfl_xor(s.a, d, 64), TWO ? __shfl_xor(s.b, d, 64) : 0.f, scale);
+    merge<E>(s, __shfl_xor(s.m, d, 64), __shfl_xor(s.a, d, 64), E != ONE ? __shfl_xor(s.b, d, 64) : 0.f, scale);
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) {
     sh[0][wave] = s.m;
     sh[1][wave] = s.a;
-    if (TWO) sh[2][wave] = s.b;
+    if (E != ONE) sh[2][wave] = s.b;
   }
   __syncthreads();
-  s.m = sh[0][0], s.a = sh[1][0], s.b = TWO ? sh[2][0] : 0.f;
+  s.m = sh[0][0], s.a = sh[1][0], s.b = E != ONE ? sh[2][0] : 0.f;
 #pragma unroll
-  for (int w = 1; w < THREADS / 64; ++w) merge<TWO>(s, sh[0][w], sh[1][w], TWO ? sh[2][w] : 0.f, scale);
+  for (int w = 1; w < THREADS / 64; ++w) merge<E>(s, sh[0][w], sh[1][w], E != ONE ? sh[2][w] : 0.f, scale);
+  if (E == ONE) s.b = s.a;
   return s;
 }
 
-// The teacher's side of a row, by one wavefront: p and log p of every entry, the student's logits at their places.
+// The teacher's side of a row, and the student's logits at its places.
 struct Entries {
-  int id[kMostEntries];
+  __attribute__((aligned(16))) int id[kMostEntries];  // -1: does not count
   float p[kMostEntries], logp[kMostEntries], z[kMostEntries];
-  bool any;  // one of them counts
+  float z_label;
 };
-template <typename T>
-__device__ __forceinline__ void teacher(const DistillArgs& g, int64_t row, const T* z, Entries& e, int lane) {
-  float top = -INFINITY;
-  for (int k = lane; k < g.entries; k += 64) {
+struct Places { uint32_t seen[kSeen / 32], twice[kSeen / 32]; };  // of the ids' lowest bits: stand in the row, stand more than once
+// every one of THREADS threads its entries; returns whether it has one that counts
+template <typename T, int THREADS>
+__device__ __forceinline__ bool gather(const DistillArgs& g, int64_t row, const T* z, int label, Entries& e) {
+  bool any = false;
+  for (int k = threadIdx.x; k < g.entries; k += THREADS) {
     const int64_t at = row * g.entries + k;
     int id = g.ids[at];
     const float t = g.teacher_bf16 ? bf2f(static_cast<const bf16_t*>(g.t)[at]) : static_cast<const float*>(g.t)[at];
     if (id < 0 || id >= g.vocab || t == -INFINITY) id = -1;
     e.id[k] = id;
     e.logp[k] = t;
-    e.z[k] = id >= 0 ? load1(z + id) : 0.f;
-    if (id >= 0) top = t > top || t != t ? t : top;
+    if (id >= 0) {
+      e.z[k] = load1(z + id);
+      any = true;
+    }
+  }
+  if (threadIdx.x < 3)  // (what a group of four reads behind the last entry)
+    if (g.entries + (int)threadIdx.x < kMostEntries) e.id[g.entries + threadIdx.x] = -1;
+  if (threadIdx.x == THREADS - 1 && label >= 0) e.z_label = load1(z + label);
+  return any;
+}
+// p and log p, by one wavefront, once all entries are there; and which ids may stand several times
+__device__ __forceinline__ void teacher(const DistillArgs& g, Entries& e, int lane, Places* places) {
+  float top = -INFINITY;
+  for (int k = lane; k < g.entries; k += 64) {
+    const float t = e.logp[k];
+    if (e.id[k] >= 0) top = t > top || t != t ? t : top;
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
     const float o = __shfl_xor(top, d, 64);
     top = o > top || o != o ? o : top;
   }
-  if (lane == 0) e.any = top != -INFINITY;
   float sum = 0.f;
   for (int k = lane; k < g.entries; k += 64) {
     const float l = (e.logp[k] - top) * g.inv_tau, p = e.id[k] >= 0 ? expf(l) : 0.f;
@@ -99,54 +130,63 @@ __device__ __forceinline__ void teacher(const DistillArgs& g, int64_t row, const
   for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
   const float inv = 1.f / sum, ls = logf(sum);
   for (int k = lane; k < g.entries; k += 64) {
-    if (e.id[k] < 0) continue;
+    const int id = e.id[k];
+    if (id < 0) continue;
     e.p[k] *= inv;
     e.logp[k] -= ls;
+    if (!places) continue;
+    const uint32_t at = (uint32_t)id % kSeen, bit = 1u << (at & 31);
+    if (atomicOr(&places->seen[at / 32], bit) & bit) atomicOr(&places->twice[at / 32], bit);
   }
 }
 
-template <typename T, bool EVEN, int THREADS, bool TWO>
-__device__ __forceinline__ Sums row_stats(const DistillArgs& g, const T* z, float (*sh)[16]) {
-  constexpr int U = 4;  // groups of eight that are asked for together
-  Sums s = {kLowest, 0.f, 0.f};
-  const int groups = g.vocab / 8;
-  for (int at = threadIdx.x; at < groups; at += U * THREADS) {
-    Eight<T, EVEN> e[U];
+// A row in groups of eight from its first 16-byte address on; `head` values in front of them and `tail` behind, fewer than eight.
+struct Split { int head, groups, tail; };
+template <typename T>
+__device__ __forceinline__ Split split_row(const T* z, int vocab) {
+  Split s;
+  s.head = min((int)((0u - (uint32_t)reinterpret_cast<uintptr_t>(z)) & 15) / (int)sizeof(T), vocab);
+  s.groups = (vocab - s.head) / 8;
+  s.tail = vocab - s.head - s.groups * 8;
+  return s;
+}
+
+// the sums of N groups at a time, each thread's own
+template <typename T, Exps E, int N>
+__device__ __forceinline__ void add_groups(Sums& s, const Eight<T, true> (&e)[N], float scale) {
+  float v[N][8], top = s.m;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (at + u * THREADS < groups) e[u].load(z + (at + u * THREADS) * 8);
-    float v[U][8], top = s.m;
+  for (int u = 0; u < N; ++u) {
+    e[u].values(v[u]);
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, v[u][i]);
+  }
+  float a, b;
+  exps<E>(s.m - top, scale, a, b);
+  s.a *= a;
+  if (E != ONE) s.b *= b;
+  s.m = top;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[u][i] = -INFINITY;
-      if (at + u * THREADS < groups) e[u].values(v[u]);
+  for (int u = 0; u < N; ++u)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, v[u][i]);
+    for (int i = 0; i < 8; ++i) {
+      exps<E>(v[u][i] - top, scale, a, b);
+      s.a += a;
+      if (E != ONE) s.b += b;
     }
-    s.a *= exp_scaled(s.m - top, g.scale);
-    if (TWO) s.b *= exp_scaled(s.m - top, kLog2e);
-    s.m = top;
+}
+// group `at` of a row, or -inf behind its last one
+template <typename T>
+__device__ __forceinline__ void load_group(Eight<T, true>& e, const T* z, int at, int groups, bool all) {
+  e.load(z + (all ? at : min(at, groups - 1)) * 8);
+  if (!all) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float d = v[u][i] - top;
-        s.a += exp_scaled(d, g.scale);
-        if (TWO) s.b += exp_scaled(d, kLog2e);
-      }
+    for (int i = 0; i < Eight<T, true>::N; ++i) e.v[i] = at < groups ? e.v[i] : sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
   }
-  if (groups * 8 + (int)threadIdx.x < g.vocab) {  // (the last values, fewer than eight)
-    const float v = load1(z + groups * 8 + threadIdx.x), top = fmaxf(s.m, v);
-    s.a = s.a * exp_scaled(s.m - top, g.scale) + exp_scaled(v - top, g.scale);
-    if (TWO) s.b = s.b * exp_scaled(s.m - top, kLog2e) + exp_scaled(v - top, kLog2e);
-    s.m = top;
-  }
-  return block_sums<THREADS, TWO>(s, g.scale, sh);
 }
 
 // the loss of a row, by one wavefront
-__device__ __forceinline__ float row_loss(const DistillArgs& g, const Entries& e, const Sums& s, float zl, bool label, int lane) {
+__device__ __forceinline__ float row_loss(const DistillArgs& g, const Entries& e, const Sums& s, bool label, int lane) {
   float loss = 0.f;
   if (g.kl != 0.f) {
     const float ls = logf(s.a);
@@ -156,35 +196,76 @@ __device__ __forceinline__ float row_loss(const DistillArgs& g, const Entries& e
     for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d, 64);
     loss *= g.kl;
   }
-  if (label) loss -= g.mix * ((zl - s.m) - logf(s.b));
+  if (label) loss -= g.mix * ((e.z_label - s.m) - logf(s.b));
   return loss;
 }
 
-// MODE 0: loss and statistics; 1: the gradient from them; 2: loss and gradient.
-template <typename T, bool EVEN, int THREADS, bool TWO, int MODE>
-__global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs g) {
+// MODE 0: loss and statistics; 1: the gradient from them; 2: loss and gradient.  With MODE 2 a thread keeps the first KEEP groups that
+// it reads in registers; what a row has more is read again (from the caches, where it stayed there).
+template <typename T, int THREADS, int KEEP, Exps E, int MODE>
+__global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g) {
+  constexpr int U = 4, K = KEEP ? KEEP : 1;  // U: groups that are asked for together
   __shared__ Entries e;
   __shared__ float sh[3][16];
-  __shared__ float zl_sh;
   const int64_t row = blockIdx.x;
   const T* const z = static_cast<const T*>(g.z) + row * g.z_stride;
-  const int lane = threadIdx.x & 63;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const Split sp = split_row(z, g.vocab);
+  const T* const zg = z + sp.head;
+  // the value in front of or behind the groups that falls to this thread
+  const int odd = tid < sp.head ? tid : tid - sp.head < sp.tail ? sp.groups * 8 + tid : -1;
+
   int label = g.labels && g.mix != 0.f ? g.labels[row] : -1;
   if (label < 0 || label >= g.vocab) label = -1;
   const float w = MODE ? g.dloss[row] : 1.f;
-  if (threadIdx.x < 64) {
-    teacher(g, row, z, e, lane);
-    if (lane == 0) zl_sh = label >= 0 ? load1(z + label) : 0.f;
+  Eight<T, true> kept[K];
+#pragma unroll
+  for (int u = 0; u < KEEP; ++u)
+    if (u * THREADS < sp.groups) load_group(kept[u], zg, tid + u * THREADS, sp.groups, (u + 1) * THREADS <= sp.groups);
+  const float zodd = odd >= 0 ? load1(z + odd) : -INFINITY;
+  bool any = false;  // an entry of the teacher's counts
+  Places* places = nullptr;
+  if constexpr (MODE != 0) {
+    __shared__ Places store;
+    places = &store;
   }
-  Sums s;
+  if (MODE == 0) {  // (the others go on to the row)
+    if (tid < 64) {
+      gather<T, 64>(g, row, z, label, e);
+      teacher(g, e, lane, nullptr);
+    }
+  } else {  // (what may be written in place of the logits waits for their values at the entries' places)
+    for (int i = tid; i < kSeen / 32; i += THREADS) places->seen[i] = places->twice[i] = 0;
+    any = __syncthreads_or(gather<T, THREADS>(g, row, z, label, e));
+    if (tid < 64) teacher(g, e, lane, places);
+  }
+
+  Sums s = {kLowest, 0.f, 0.f};
   if (MODE == 1) {
     s = {g.stats_in[row * 3], g.stats_in[row * 3 + 1], g.stats_in[row * 3 + 2]};
-    __syncthreads();
   } else {
-    s = row_stats<T, EVEN, THREADS, TWO>(g, z, sh);
-    if (!TWO) s.b = s.a;  // (no label, or a temperature of 1)
-    if (threadIdx.x < 64) {
-      const float loss = row_loss(g, e, s, zl_sh, label >= 0, lane);
+    for (int at = tid + KEEP * THREADS; at - tid < sp.groups; at += U * THREADS) {
+      Eight<T, true> r[U];
+      const bool all = at - tid + U * THREADS <= sp.groups;
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_group(r[u], zg, at + u * THREADS, sp.groups, all);
+      add_groups<T, E>(s, r, g.scale);
+    }
+#pragma unroll
+    for (int u = 0; u < KEEP; u += 2)  // (the last slots may be empty)
+      if ((u + 1) * THREADS < sp.groups) {
+        const Eight<T, true> two[2] = {kept[u], kept[u + 1 < K ? u + 1 : u]};
+        add_groups<T, E>(s, two, g.scale);
+      } else if (u * THREADS < sp.groups) {
+        const Eight<T, true> one[1] = {kept[u]};
+        add_groups<T, E>(s, one, g.scale);
+      }
+    float oa, ob;
+    exps<E>(zodd - fmaxf(zodd, kLowest), g.scale, oa, ob);
+    merge<E>(s, fmaxf(zodd, kLowest), oa, ob, g.scale);
+    s = block_sums<THREADS, E>(s, g.scale, sh);
+    if (tid < 64) {
+      const float loss = row_loss(g, e, s, label >= 0, lane);
       if (lane == 0) {
         g.loss[row] = loss;
         if (MODE == 0) {
@@ -198,64 +279,96 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(const DistillArgs g) {
   if (MODE == 0) return;
 
   T* const dz = static_cast<T*>(g.dz) + row * g.dz_stride;
-  const float rate = e.any && g.rate != 0.f ? w * g.rate : 0.f, mix = label >= 0 ? w * g.mix : 0.f;
+  T* const dg = dz + sp.head;
+  const float rate = any && g.rate != 0.f ? w * g.rate : 0.f, mix = label >= 0 ? w * g.mix : 0.f;
   const float ca = rate != 0.f ? rate / s.a : 0.f, cb = mix != 0.f ? mix / s.b : 0.f;
   auto slope = [&](float v) __attribute__((always_inline)) {  // dloss (rate q + mix q1)
-    const float d = v - s.m;
-    float x = 0.f;
-    if (ca != 0.f) x = ca * exp_scaled(d, g.scale);
-    if (cb != 0.f) x += cb * exp_scaled(d, kLog2e);
-    return x;
+    float a, b;
+    exps<E>(v - s.m, g.scale, a, b);
+    return E == ONE ? (ca + cb) * a : ca * a + cb * b;
   };
-  const int groups = g.vocab / 8;
-  for (int at = threadIdx.x; at < groups; at += THREADS) {
-    Eight<T, EVEN> r;
-    r.load(z + at * 8);
+  auto write = [&](const Eight<T, true>& r, int at) __attribute__((always_inline)) {
     float v[8];
     r.values(v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = slope(v[i]);
-    store8(dz + at * 8, v);
+    store8(dg + at * 8, v);
+  };
+  if (ca == 0.f && cb == 0.f) {  // (a token that does not count: zeros, whatever its logits are)
+    const float zero[8] = {};
+    for (int at = tid; at < sp.groups; at += THREADS) store8(dg + at * 8, zero);
+    if (odd >= 0) store1(dz + odd, 0.f);
+    return;
   }
-  if (groups * 8 + (int)threadIdx.x < g.vocab) {
-    const int at = groups * 8 + threadIdx.x;
-    store1(dz + at, slope(load1(z + at)));
+#pragma unroll
+  for (int u = 0; u < KEEP; ++u)
+    if (tid + u * THREADS < sp.groups) write(kept[u], tid + u * THREADS);
+  for (int at = tid + KEEP * THREADS; at < sp.groups; at += U * THREADS) {
+    Eight<T, true> r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at + u * THREADS < sp.groups) r[u].load(zg + (at + u * THREADS) * 8);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at + u * THREADS < sp.groups) write(r[u], at + u * THREADS);
   }
+  if (odd >= 0) store1(dz + odd, slope(zodd));
   __syncthreads();
-  // the places of the teacher's entries and of the label: the first of equal ones writes the whole
-  for (int k = threadIdx.x; k <= g.entries; k += THREADS) {
+  // The places of the teacher's entries and of the label: the first of equal ids writes the whole.  Few ids share their lowest bits
+  // with another: only those look through the row for equal ones.
+  for (int k = tid; k <= g.entries; k += THREADS) {
     const int id = k < g.entries ? e.id[k] : label;
     if (id < 0) continue;
-    float p = 0.f;
+    float p = k < g.entries ? e.p[k] : 0.f;
     bool first = true;
-    for (int j = 0; j < g.entries; ++j)
-      if (e.id[j] == id) {
-        p += e.p[j];
-        first = first && j >= k;
+    const uint32_t at = (uint32_t)id % kSeen;
+    if ((k < g.entries ? places->twice : places->seen)[at / 32] >> (at & 31) & 1) {
+      p = 0.f;
+      for (int j = 0; j < g.entries; j += 4) {
+        const int4 q = *reinterpret_cast<const int4*>(e.id + j);
+        if (q.x == id) p += e.p[j], first = first && j >= k;
+        if (q.y == id) p += e.p[j + 1], first = first && j + 1 >= k;
+        if (q.z == id) p += e.p[j + 2], first = first && j + 2 >= k;
+        if (q.w == id) p += e.p[j + 3], first = first && j + 3 >= k;
       }
+    }
     if (!first) continue;
-    const float d = (k < g.entries ? e.z[k] : zl_sh) - s.m;
+    float a, b;
+    exps<E>((k < g.entries ? e.z[k] : e.z_label) - s.m, g.scale, a, b);
     float x = 0.f;
-    if (rate != 0.f) x = rate * (exp_scaled(d, g.scale) / s.a - p);
-    if (mix != 0.f) x += mix * (exp_scaled(d, kLog2e) / s.b - (id == label ? 1.f : 0.f));
+    if (rate != 0.f) x = rate * (a / s.a - p);
+    if (mix != 0.f) x += mix * (b / s.b - (id == label ? 1.f : 0.f));
     store1(dz + id, x);
   }
 }
 
-template <int MODE, typename T, bool EVEN>
-void go(hipStream_t st, int64_t rows, const DistillArgs& g, bool two) {
-  auto run = [&](auto kernel, int threads) { KLAUNCH_NAMED(MODE == 0 ? "distill_kernel" : MODE == 1 ? "distill_bwd_kernel" : "distill_step_kernel", kernel, dim3((unsigned)rows), dim3(threads), 0, st, g); };
-  if (MODE == 1 || !two) run(distill_kernel<T, EVEN, 512, false, MODE>, 512);
-  else run(distill_kernel<T, EVEN, 512, true, MODE>, 512);
+template <int MODE, typename T, int THREADS, int KEEP>
+void go(hipStream_t st, int64_t rows, const DistillArgs& g, Exps e) {
+  const char* const name = MODE == 0 ? "distill_kernel" : MODE == 1 ? "distill_bwd_kernel" : "distill_step_kernel";
+  auto run = [&](auto kernel) { KLAUNCH_NAMED(name, kernel, dim3((unsigned)rows), dim3(THREADS), 0, st, g); };
+  if (e == ONE) run(distill_kernel<T, THREADS, KEEP, ONE, MODE>);
+  else if (e == SQUARE) run(distill_kernel<T, THREADS, KEEP, SQUARE, MODE>);
+  else if (e == FOURTH) run(distill_kernel<T, THREADS, KEEP, FOURTH, MODE>);
+  else run(distill_kernel<T, THREADS, KEEP, BOTH, MODE>);
+}
+template <int MODE, typename T>
+void pick(hipStream_t st, const ast_distill_cfg& c, const DistillArgs& g, Exps e) {
+  const int64_t r = c.rows, v = c.vocab;
+  if constexpr (MODE == 2) {
+    if (v <= 8192) go<MODE, T, 256, 4>(st, r, g, e);
+    else if (v <= 16384) go<MODE, T, 256, 8>(st, r, g, e);
+    else go<MODE, T, 512, sizeof(T) == 2 ? 16 : 8>(st, r, g, e);
+  } else {
+    if (v <= 8192) go<MODE, T, 256, 0>(st, r, g, e);
+    else go<MODE, T, 512, 0>(st, r, g, e);
+  }
 }
 template <int MODE>
 void launch(hipStream_t st, const ast_distill_cfg& c, DistillArgs g) {
-  const int es = c.dtype == AST_F32 ? 4 : 2;
-  bool even = reinterpret_cast<uintptr_t>(g.z) % 16 == 0 && g.z_stride * es % 16 == 0;
-  if (MODE) even = even && reinterpret_cast<uintptr_t>(g.dz) % 16 == 0 && g.dz_stride * es % 16 == 0;
-  const bool two = g.labels && g.mix != 0.f && c.temperature != 1.f;
-  if (c.dtype == AST_F32) even ? go<MODE, float, true>(st, c.rows, g, two) : go<MODE, float, false>(st, c.rows, g, two);
-  else even ? go<MODE, bf16_t, true>(st, c.rows, g, two) : go<MODE, bf16_t, false>(st, c.rows, g, two);
+  const float tau = c.temperature;
+  const Exps e = !g.labels || g.mix == 0.f || tau == 1.f ? ONE : tau == 2.f ? SQUARE : tau == 4.f ? FOURTH : BOTH;
+  if (c.dtype == AST_F32) pick<MODE, float>(st, c, g, e);
+  else pick<MODE, bf16_t>(st, c, g, e);
 }
 
 DistillArgs args_of(const ast_distill_cfg& c, const void* z, const int32_t* ids, const void* t) {

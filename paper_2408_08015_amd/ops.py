@@ -566,7 +566,11 @@ def _vocab_rows(t, name):
 def _gradient_of(logits, out, dloss):
     _is(dloss, "dloss", _F32, (logits.shape[0],))
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+        T, V = logits.shape
+        step = logits.stride(0) if T > 1 and 0 < logits.stride(0) - V < 64 else V   # rows padded a little stay so
+        out = torch.empty((T, step), dtype=logits.dtype, device=logits.device)
+        if step != V:
+            out = out[:, :V]
     if not isinstance(out, torch.Tensor) or out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must be a %s tensor %s" % (logits.dtype, tuple(logits.shape)))
     return out, _vocab_rows(out, "out")
@@ -592,7 +596,8 @@ def distill_forward(logits, ids, teacher, temperature=1.0, labels=None, label_we
 
 
 def distill_backward(dloss, logits, ids, teacher, stats, temperature=1.0, labels=None, label_weight=0.0, out=None):
-    """The logits' gradient for dloss float32 [rows]; stats is what distill_forward left.  out may be logits."""
+    """The logits' gradient for dloss float32 [rows]; stats is what distill_forward left.  out may be logits (made here,
+    its rows are padded as those of logits are, where that is by fewer than 64 values)."""
     cfg = _distill_cfg(logits, ids, teacher, temperature, labels, label_weight)
     _is(stats, "stats", _F32, (logits.shape[0], 3))
     out, stride = _gradient_of(logits, out, dloss)
