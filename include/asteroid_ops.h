@@ -143,7 +143,8 @@ ast_status asteroid_gelu_backward_stash8(const void* dy_dev, int32_t dtype, cons
  * x_dev, y_dev [rows][width] of dtype; residual_dev, sum_dev [rows][width] of sum_dtype, which is dtype or AST_F32 (an fp32
  * residual stream between bf16 layers); gain_dev fp32[width].  The norm is that of s as it is written.
  * residual_dev == NULL: s is x, sum_dtype == dtype, nothing is written to sum_dev (NULL).
- * stash_dev (NULL: none) receives y, as it is written, in 8 bits: the bytes of asteroid_stash8_pack(y_dev).
+ * stash_dev (NULL: none) receives y, as it is written, in 8 bits: the bytes of asteroid_stash8_pack(y_dev).  (s is the same with and
+ * without it; y too, bit for bit, where width is a multiple of 8, otherwise the squares may be added up in another order.)
  * rows < 2^31, width in [1, 16384], eps > 0.  sum_dev may be residual_dev, y_dev may be x_dev, and where the types
  * are the same sum_dev may be x_dev and y_dev residual_dev. */
 typedef struct {

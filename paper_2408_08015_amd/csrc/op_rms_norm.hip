@@ -9,6 +9,9 @@
 // lanes of a wavefront for up to 1024 values, a block for more, so it is read once and both sums of the backward pass are of
 // values at hand.  A lane keeps its columns from row to row: gains are loaded once, and the gains' gradients are summed in
 // registers, then over the wavefronts, then over the blocks in 64 bits, in a fixed order.
+// Rows whose length is no multiple of eight begin anywhere in a group of eight of the tensor, at the same place of it in every eighth
+// row.  So a wavefront takes every eighth row (or a multiple of that), in the tensor's groups: loads and stores stay aligned, and its
+// lanes keep their columns; only the groups at a row's ends, which it shares with its neighbours, are written value by value.
 #include <algorithm>
 
 #include "ops.h"
@@ -42,9 +45,53 @@ __device__ __forceinline__ void round_to(float (&v)[8], const bf16_t*) {
   }
 }
 
+// How a row is read and written.  EVEN: its length is a multiple of eight and every tensor begins at a 16-byte address; GROUPS: the
+// tensors do, in the tensor's groups of eight; ANY: from any address, shifted into place.
+enum Way : int { ANY = 0, EVEN = 1, GROUPS = 2 };
+template <typename T, Way W>
+struct Part {  // eight values of a row from place c on (GROUPS: c may lie in front of the row)
+  RowEight<T, W == EVEN> e;
+  __device__ __forceinline__ void load(const void* base, int64_t row, int c, int cols, int64_t all) {
+    const T* const p = static_cast<const T*>(base) + row * cols;
+    e.load(p, c, cols);
+  }
+  __device__ __forceinline__ void values(float (&f)[8], int, int) const { e.values(f); }
+};
+template <typename T>
+struct Part<T, GROUPS> {
+  uint32_t v[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const void* base, int64_t row, int c, int cols, int64_t all) {
+    const int64_t at = row * cols + c;  // (a multiple of eight; the tensor's last 16 bytes are read again where nothing follows them)
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+      const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const T*>(base) + at + (i == 0 || at + 4 < all ? 4 * i : 0));
+      v[4 * i] = a.x; v[4 * i + 1] = a.y; v[4 * i + 2] = a.z; v[4 * i + 3] = a.w;
+    }
+  }
+  __device__ __forceinline__ void values(float (&f)[8], int c, int cols) const {
+    eight_values<T>(v, f);
+    if (c < 0 || c + 8 > cols) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = (unsigned)(c + i) < (unsigned)cols ? f[i] : 0.f;
+    }
+  }
+};
+template <typename T, Way W>
+__device__ __forceinline__ void store_part(void* base, int64_t row, int c, int cols, const float (&v)[8]) {
+  T* const p = static_cast<T*>(base) + row * cols;
+  if (W != GROUPS) {
+    store_row8<T, W == EVEN>(p, c, cols, v);
+  } else if (c >= 0 && c + 8 <= cols) {
+    store8(p + c, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((unsigned)(c + i) < (unsigned)cols) store1(p + c + i, v[i]);
+  }
+}
 __device__ __forceinline__ void gains(const NormArgs& g, int c, float (&v)[8]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = c + e < g.cols ? g.gain[c + e] : 0.f;
+  for (int e = 0; e < 8; ++e) v[e] = (unsigned)(c + e) < (unsigned)g.cols ? g.gain[c + e] : 0.f;
 }
 __device__ __forceinline__ void copy8(const float (&a)[8], float (&b)[8]) {
 #pragma unroll
@@ -76,51 +123,74 @@ __device__ __forceinline__ void row_sums(float& a, float& b, bool two, int ls, f
   }
 }
 
-// BLOCK: threads that take one row together, 0: 2^ls lanes do (blocks of 256 threads).
-template <typename T, typename S, bool EVEN, int IT, int BLOCK>
-__global__ __launch_bounds__(BLOCK ? BLOCK : 256) void rms_norm_kernel(const NormArgs g) {
+// The rows of a group of lanes: the first one, how far it is to the next, and where it begins in a group of eight.
+// BLOCK: threads that take one row together; 0: 2^ls lanes do, of 256 threads (GROUPS: 512, a wavefront for every row modulo eight).
+template <Way W, int BLOCK>
+struct Rows {
+  static constexpr int THREADS = BLOCK ? BLOCK : W == GROUPS ? 512 : 256;
+  int lanes, lane, shift;
+  int64_t row, step;
+  __device__ __forceinline__ Rows(const NormArgs& g) {
+    lanes = BLOCK ? BLOCK : 1 << g.ls;
+    lane = threadIdx.x & (lanes - 1);
+    const int some = BLOCK ? 1 : THREADS >> g.ls;  // (by the block)
+    if (BLOCK) {
+      row = blockIdx.x;  // (the same for the block: rows have scalar addresses)
+    } else if (W != GROUPS) {
+      row = (int64_t)blockIdx.x * some + (threadIdx.x >> g.ls);
+    } else {
+      const int wave = threadIdx.x >> 6, of = (threadIdx.x & 63) >> g.ls;
+      row = ((int64_t)blockIdx.x * (some / 8) + of) * 8 + wave;
+    }
+    step = (int64_t)gridDim.x * some;  // (GROUPS: a multiple of eight)
+    shift = W == GROUPS ? (int)(row * g.cols & 7) : 0;
+  }
+  __device__ __forceinline__ int place(int i) const { return (lane + i * lanes) * 8 - shift; }
+};
+
+template <typename T, typename S, Way W, int IT, int BLOCK>
+__global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_kernel(const NormArgs g) {
   __shared__ float sh[2][32];
-  const int lanes = BLOCK ? BLOCK : 1 << g.ls;
-  const int lane = threadIdx.x & (lanes - 1);
-  const int64_t step = (int64_t)gridDim.x * (BLOCK ? 1 : 256 >> g.ls);
-  int64_t row = BLOCK ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (256 >> g.ls) + (threadIdx.x >> g.ls);
+  Rows<W, BLOCK> at(g);
+  const int64_t all = g.rows * g.cols;
   constexpr bool AHEAD = BLOCK < 1024;  // the next row is asked for before this one is worked on, and gains stay in registers
   float kept[AHEAD ? IT : 1][8];
 #pragma unroll
-  for (int i = 0; i < (AHEAD ? IT : 0); ++i) gains(g, (lane + i * lanes) * 8, kept[i]);
+  for (int i = 0; i < (AHEAD ? IT : 0); ++i) gains(g, at.place(i), kept[i]);
   struct Row {
-    RowEight<T, EVEN> x[IT];
-    RowEight<S, EVEN> r[IT];
+    Part<T, W> x[IT];
+    Part<S, W> r[IT];
   };
-  auto fetch = [&](int64_t at, Row& w) __attribute__((always_inline)) {
-    if (at >= g.rows) return;
+  auto fetch = [&](int64_t row, Row& w) __attribute__((always_inline)) {
+    if (row >= g.rows) return;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = (lane + i * lanes) * 8;
+      const int c = at.place(i);
       if (c >= g.cols) continue;
-      w.x[i].load(static_cast<const T*>(g.x) + at * g.cols, c, g.cols);
-      if (g.r) w.r[i].load(static_cast<const S*>(g.r) + at * g.cols, c, g.cols);
+      w.x[i].load(g.x, row, c, g.cols, all);
+      if (g.r) w.r[i].load(g.r, row, c, g.cols, all);
     }
   };
   Row cur;
-  if (AHEAD) fetch(row, cur);
-  for (int turn = 0; row < g.rows; row += step, turn ^= 1) {
+  if (AHEAD) fetch(at.row, cur);
+  int turn = 0;
+  for (int64_t row = at.row; row < g.rows; row += at.step, turn ^= 1) {
     Row next;
-    if (AHEAD) fetch(row + step, next);
+    if (AHEAD) fetch(row + at.step, next);
     else fetch(row, cur);
     float v[IT][8], ss = 0.f, none = 0.f;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = (lane + i * lanes) * 8;
+      const int c = at.place(i);
       if (c < g.cols) {
-        cur.x[i].values(v[i]);
+        cur.x[i].values(v[i], c, g.cols);
         if (g.r) {
           float r[8];
-          cur.r[i].values(r);
+          cur.r[i].values(r, c, g.cols);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[i][e] += r[e];
           round_to(v[i], static_cast<const S*>(nullptr));
-          store_row8<S, EVEN>(static_cast<S*>(g.sum) + row * g.cols, c, g.cols, v[i]);
+          store_part<S, W>(g.sum, row, c, g.cols, v[i]);
         }
       } else {
 #pragma unroll
@@ -133,15 +203,15 @@ __global__ __launch_bounds__(BLOCK ? BLOCK : 256) void rms_norm_kernel(const Nor
     const float rho = rsqrtf(ss * g.inv + g.eps);
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = (lane + i * lanes) * 8;
+      const int c = at.place(i);
       float gain[8];
       if (AHEAD) copy8(kept[AHEAD ? i : 0], gain);
       else gains(g, c, gain);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * rho * gain[e];
-      if (c < g.cols) store_row8<T, EVEN>(static_cast<T*>(g.y) + row * g.cols, c, g.cols, v[i]);
-      if (g.q && c < g.pitch) {  // (a block of 32 values is four lanes' groups, all inside the pitch or none)
-        if (!EVEN) {
+      if (c < g.cols) store_part<T, W>(g.y, row, c, g.cols, v[i]);
+      if (W != GROUPS && g.q && c < g.pitch) {  // (a block of 32 values is four lanes' groups, all inside the pitch or none)
+        if (W != EVEN) {
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[i][e] = c + e < g.cols ? v[i][e] : 0.f;  // (0 times an infinite rho is no zero)
         }
@@ -149,56 +219,55 @@ __global__ __launch_bounds__(BLOCK ? BLOCK : 256) void rms_norm_kernel(const Nor
         uint2 w;
         const uint8_t scale = stash8_block(v[i], w);
         *reinterpret_cast<uint2*>(g.q + row * g.pitch + c) = w;
-        if ((lane & 3) == 0) g.scales[row * (g.pitch / kStash8Block) + c / kStash8Block] = scale;
+        if ((at.lane & 3) == 0) g.scales[row * (g.pitch / kStash8Block) + c / kStash8Block] = scale;
       }
     }
     if (AHEAD) cur = next;
   }
 }
 
-template <typename T, typename S, bool EVEN, int IT, int BLOCK>
-__global__ __launch_bounds__(BLOCK ? BLOCK : 256) void rms_norm_bwd_kernel(const NormArgs g) {
+template <typename T, typename S, Way W, int IT, int BLOCK>
+__global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_bwd_kernel(const NormArgs g) {
   __shared__ float sh[2][32];
-  const int lanes = BLOCK ? BLOCK : 1 << g.ls;
-  const int lane = threadIdx.x & (lanes - 1);
-  const int64_t step = (int64_t)gridDim.x * (BLOCK ? 1 : 256 >> g.ls);
-  int64_t row = BLOCK ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (256 >> g.ls) + (threadIdx.x >> g.ls);
+  Rows<W, BLOCK> at(g);
+  const int64_t all = g.rows * g.cols;
   constexpr bool AHEAD = BLOCK < 1024;
   float kept[AHEAD ? IT : 1][8], acc[IT][8];
 #pragma unroll
   for (int i = 0; i < IT; ++i) {
-    if (AHEAD) gains(g, (lane + i * lanes) * 8, kept[AHEAD ? i : 0]);
+    if (AHEAD) gains(g, at.place(i), kept[AHEAD ? i : 0]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[i][e] = 0.f;
   }
   struct Row {
-    RowEight<T, EVEN> d[IT];
-    RowEight<S, EVEN> s[IT], r[IT];
+    Part<T, W> d[IT];
+    Part<S, W> s[IT], r[IT];
   };
-  auto fetch = [&](int64_t at, Row& w) __attribute__((always_inline)) {
-    if (at >= g.rows) return;
+  auto fetch = [&](int64_t row, Row& w) __attribute__((always_inline)) {
+    if (row >= g.rows) return;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = (lane + i * lanes) * 8;
+      const int c = at.place(i);
       if (c >= g.cols) continue;
-      w.d[i].load(static_cast<const T*>(g.x) + at * g.cols, c, g.cols);
-      w.s[i].load(static_cast<const S*>(g.s) + at * g.cols, c, g.cols);
-      if (g.r) w.r[i].load(static_cast<const S*>(g.r) + at * g.cols, c, g.cols);
+      w.d[i].load(g.x, row, c, g.cols, all);
+      w.s[i].load(g.s, row, c, g.cols, all);
+      if (g.r) w.r[i].load(g.r, row, c, g.cols, all);
     }
   };
   Row cur;
-  if (AHEAD) fetch(row, cur);
-  for (int turn = 0; row < g.rows; row += step, turn ^= 1) {
+  if (AHEAD) fetch(at.row, cur);
+  int turn = 0;
+  for (int64_t row = at.row; row < g.rows; row += at.step, turn ^= 1) {
     Row next;
-    if (AHEAD) fetch(row + step, next);
+    if (AHEAD) fetch(row + at.step, next);
     else fetch(row, cur);
     float s[IT][8], d[IT][8], ss = 0.f, dot = 0.f;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = (lane + i * lanes) * 8;
+      const int c = at.place(i);
       if (c < g.cols) {
-        cur.s[i].values(s[i]);
-        cur.d[i].values(d[i]);
+        cur.s[i].values(s[i], c, g.cols);
+        cur.d[i].values(d[i], c, g.cols);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[i][e] = d[i][e] = 0.f;
@@ -217,19 +286,19 @@ __global__ __launch_bounds__(BLOCK ? BLOCK : 256) void rms_norm_bwd_kernel(const
     const float m = rho * rho * dot * g.inv;  // mean(h n) rho = rho^2 mean(h s)
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = (lane + i * lanes) * 8;
+      const int c = at.place(i);
       if (c >= g.cols) continue;
       float r[8] = {}, gain[8];
       if (AHEAD) copy8(kept[AHEAD ? i : 0], gain);
       else gains(g, c, gain);
-      if (g.r) cur.r[i].values(r);
+      if (g.r) cur.r[i].values(r, c, g.cols);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         acc[i][e] += d[i][e] * (s[i][e] * rho);
         s[i][e] = rho * (d[i][e] * gain[e] - s[i][e] * m) + r[e];
       }
-      if (g.y) store_row8<T, EVEN>(static_cast<T*>(g.y) + row * g.cols, c, g.cols, s[i]);
-      if (g.sum) store_row8<S, EVEN>(static_cast<S*>(g.sum) + row * g.cols, c, g.cols, s[i]);
+      if (g.y) store_part<T, W>(g.y, row, c, g.cols, s[i]);
+      if (g.sum) store_part<S, W>(g.sum, row, c, g.cols, s[i]);
     }
     if (AHEAD) cur = next;
   }
@@ -238,27 +307,31 @@ __global__ __launch_bounds__(BLOCK ? BLOCK : 256) void rms_norm_bwd_kernel(const
   if (BLOCK) {
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
-      const int c = (lane + i * lanes) * 8;
+      const int c = at.place(i);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (c + e < g.cols) part[c + e] = acc[i][e];
+        if ((unsigned)(c + e) < (unsigned)g.cols) part[c + e] = acc[i][e];
     }
     return;
   }
-  constexpr int WIDE = IT * 64 * 8;
-  __shared__ float red[BLOCK ? 1 : 4 * WIDE];
+  constexpr int WIDE = IT * 64 * 8, WAVES = Rows<W, BLOCK>::THREADS / 64;
+  __shared__ float red[BLOCK ? 1 : WAVES * WIDE];
   const int wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < IT; ++i)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int c = (lane + i * lanes) * 8 + e;
+      const int c = at.place(i) + e;
       const float v = places_sum(acc[i][e], g.ls);
-      if ((threadIdx.x & 63) >> g.ls == 0 && c < g.cols) red[wave * WIDE + c] = v;
+      if ((threadIdx.x & 63) >> g.ls == 0 && (unsigned)c < (unsigned)g.cols) red[wave * WIDE + c] = v;
     }
   __syncthreads();
-  for (int c = threadIdx.x; c < g.cols; c += 256)
-    part[c] = red[c] + red[WIDE + c] + red[2 * WIDE + c] + red[3 * WIDE + c];
+  for (int c = threadIdx.x; c < g.cols; c += WAVES * 64) {
+    float v = red[c];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) v += red[i * WIDE + c];
+    part[c] = v;
+  }
 }
 
 // dgain[c] (+)= sum over the blocks, in 64 bits: 32 columns a block, 32 rows of it at a time
@@ -284,8 +357,8 @@ struct Shape { int it, block, ls; };
 
 // Lanes of a row: one group of eight values a lane up to 512 values, two up to 1024; then a block's of 256, 512, 1024 threads, two
 // groups a lane.
-Shape shape_of(int cols, bool keep) {
-  const int groups = (cols + 7) / 8;
+Shape shape_of(int cols, bool keep, Way way) {
+  const int groups = (cols + (way == GROUPS ? 14 : 7)) / 8;
   Shape s = {1, 0, keep ? 2 : 0};  // (8 bits: four lanes a block of 32 values)
   if (groups <= 128) {
     if (groups > 64) s.it = 2;
@@ -293,42 +366,58 @@ Shape shape_of(int cols, bool keep) {
     return s;
   }
   s.block = groups <= 512 ? 256 : groups <= 1024 ? 512 : 1024;
-  s.it = groups <= s.block ? 1 : 2;  // (16384 values at most)
+  s.it = groups <= s.block ? 1 : 2;
   return s;
 }
 
-constexpr int kMostPartials = 1024;
-int64_t bwd_blocks(int64_t rows, const Shape& s) {
-  const int64_t at_once = s.block ? 1 : 256 >> s.ls;
-  return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, s.block == 1024 ? kMostPartials / 2 : kMostPartials));
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+Way way_of(int cols, bool aligned, bool keep) {
+  if (!aligned) return ANY;
+  if (cols % 8 == 0) return EVEN;
+  // (8 bits lie in groups of a row's own; and where the one group more, that of a row which begins inside one, would take twice the
+  // threads, nothing is gained: 4096 bf16 rows of 8191 backward 184 us in 1024 threads, 104 shifted into place in 512)
+  const bool over = (cols + 14) / 8 > 1024 && cols <= 8192;
+  return keep || over || cols > 16376 ? ANY : GROUPS;
 }
 
-template <bool BWD, typename T, typename S, bool EVEN, int IT, int BLOCK>
-void go(hipStream_t st, int64_t blocks, const NormArgs& g) {
-  const dim3 grid((unsigned)blocks), block(BLOCK ? BLOCK : 256);
-  if (BWD) KLAUNCH_NAMED("rms_norm_bwd_kernel", (rms_norm_bwd_kernel<T, S, EVEN, IT, BLOCK>), grid, block, 0, st, g);
-  else KLAUNCH_NAMED("rms_norm_kernel", (rms_norm_kernel<T, S, EVEN, IT, BLOCK>), grid, block, 0, st, g);
+// Blocks of a call: as many as rows need, at most 2048 forward.  Backward every block leaves partial sums; us of 12288 rows of 1504,
+// bf16 on an fp32 stream, of 32768 of 1024, and of 4096 of 8192 in bf16: 1024 blocks 63.6, 61.0, 84.5; 512 57.9, 56.2, 68.2;
+// 256 74.1, 65.7, 60.7.  Rows that are shifted into place keep more of them busy (12289 of 1501 so: 68.7, 74.4, 127).
+constexpr int kMostPartials = 1024;
+int64_t blocks_of(int64_t rows, const Shape& s, Way way, bool bwd) {
+  const int64_t at_once = s.block ? 1 : (way == GROUPS ? 512 : 256) >> s.ls;
+  const int64_t most = !bwd ? 2048 : way == ANY && s.block < 512 ? kMostPartials : s.block < 512 ? 512 : 256;
+  int64_t n = std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, most));
+  if (bwd && s.block) n = std::min(n, std::max<int64_t>(256, rows / 4));  // (1024 bf16 rows of 4096: 512 blocks 20.1 us, 256 16.7)
+  return s.block && way == GROUPS ? (n + 7) / 8 * 8 : n;  // (a block's rows begin at one place of a group)
 }
-template <bool BWD, typename T, typename S, bool EVEN>
+
+template <bool BWD, typename T, typename S, Way W, int IT, int BLOCK>
+void go(hipStream_t st, int64_t blocks, const NormArgs& g) {
+  const dim3 grid((unsigned)blocks), block(Rows<W, BLOCK>::THREADS);
+  if (BWD) KLAUNCH_NAMED("rms_norm_bwd_kernel", (rms_norm_bwd_kernel<T, S, W, IT, BLOCK>), grid, block, 0, st, g);
+  else KLAUNCH_NAMED("rms_norm_kernel", (rms_norm_kernel<T, S, W, IT, BLOCK>), grid, block, 0, st, g);
+}
+template <bool BWD, typename T, typename S, Way W>
 void pick(hipStream_t st, int64_t blocks, const Shape& s, const NormArgs& g) {
   if (s.block == 0) {
-    if (s.it == 1) go<BWD, T, S, EVEN, 1, 0>(st, blocks, g);
-    else go<BWD, T, S, EVEN, 2, 0>(st, blocks, g);
+    if (s.it == 1) go<BWD, T, S, W, 1, 0>(st, blocks, g);
+    else go<BWD, T, S, W, 2, 0>(st, blocks, g);
   } else if (s.block == 256) {
-    if (s.it == 1) go<BWD, T, S, EVEN, 1, 256>(st, blocks, g);
-    else go<BWD, T, S, EVEN, 2, 256>(st, blocks, g);
+    if (s.it == 1) go<BWD, T, S, W, 1, 256>(st, blocks, g);
+    else go<BWD, T, S, W, 2, 256>(st, blocks, g);
   } else if (s.block == 512) {
-    go<BWD, T, S, EVEN, 2, 512>(st, blocks, g);
+    go<BWD, T, S, W, 2, 512>(st, blocks, g);
   } else {
-    go<BWD, T, S, EVEN, 2, 1024>(st, blocks, g);
+    go<BWD, T, S, W, 2, 1024>(st, blocks, g);
   }
 }
 template <bool BWD>
-void launch(hipStream_t st, const ast_norm_cfg& c, const Shape& s, int64_t blocks, const NormArgs& g) {
-  bool even = c.width % 8 == 0;
-  for (const void* p : {g.x, g.r, g.s, (const void*)g.y, (const void*)g.sum}) even = even && reinterpret_cast<uintptr_t>(p) % 16 == 0;
+void launch(hipStream_t st, const ast_norm_cfg& c, Way way, const Shape& s, int64_t blocks, const NormArgs& g) {
   const bool tb = c.dtype != AST_F32, sb = c.sum_dtype != AST_F32;
-#define PICK(T, S) (even ? pick<BWD, T, S, true>(st, blocks, s, g) : pick<BWD, T, S, false>(st, blocks, s, g))
+#define PICK(T, S)                                                  \
+  (way == EVEN ? pick<BWD, T, S, EVEN>(st, blocks, s, g)            \
+               : way == GROUPS ? pick<BWD, T, S, GROUPS>(st, blocks, s, g) : pick<BWD, T, S, ANY>(st, blocks, s, g))
   if (tb && sb) PICK(bf16_t, bf16_t);
   else if (tb) PICK(bf16_t, float);
   else PICK(float, float);
@@ -351,7 +440,9 @@ NormArgs args_of(const ast_norm_cfg& c, const Shape& s, const float* gain) {
 void rms_norm_fwd(hipStream_t st, const ast_norm_cfg& c, const void* x, const void* residual, const float* gain, void* y,
                   void* sum, void* stash) {
   if (c.rows <= 0) return;
-  const Shape s = shape_of((int)c.width, stash != nullptr);
+  const int cols = (int)c.width;
+  const Way way = way_of(cols, aligned16(x) && aligned16(residual) && aligned16(y) && aligned16(sum), stash != nullptr);
+  const Shape s = shape_of(cols, stash != nullptr, way);
   NormArgs g = args_of(c, s, gain);
   g.x = x;
   g.r = residual;
@@ -362,18 +453,21 @@ void rms_norm_fwd(hipStream_t st, const ast_norm_cfg& c, const void* x, const vo
     g.q = static_cast<uint8_t*>(stash);
     g.scales = g.q + c.rows * g.pitch;
   }
-  const int64_t at_once = s.block ? 1 : 256 >> s.ls;
-  launch<false>(st, c, s, std::min<int64_t>((c.rows + at_once - 1) / at_once, 2048), g);
+  launch<false>(st, c, way, s, blocks_of(c.rows, s, way, false), g);
 }
 
-size_t rms_norm_bwd_ws_bytes(int64_t rows, int64_t width) {
-  return (size_t)bwd_blocks(rows, shape_of((int)width, false)) * (size_t)width * sizeof(float);
+size_t rms_norm_bwd_ws_bytes(int64_t rows, int64_t width) {  // (whatever the tensors' addresses)
+  int64_t most = 0;
+  for (const Way way : {ANY, EVEN, GROUPS}) most = std::max(most, blocks_of(rows, shape_of((int)width, false, way), way, true));
+  return (size_t)most * (size_t)width * sizeof(float);
 }
 
 void rms_norm_bwd(hipStream_t st, const ast_norm_cfg& c, const void* dy, const void* sum, const float* gain, const void* dsum,
                   void* dx, void* ds, float* dgain, bool accumulate, void* ws) {
-  const Shape s = shape_of((int)c.width, false);
-  const int64_t blocks = c.rows > 0 ? bwd_blocks(c.rows, s) : 0;
+  const int cols = (int)c.width;
+  const Way way = way_of(cols, aligned16(dy) && aligned16(sum) && aligned16(dsum) && aligned16(dx) && aligned16(ds), false);
+  const Shape s = shape_of(cols, false, way);
+  const int64_t blocks = c.rows > 0 ? blocks_of(c.rows, s, way, true) : 0;
   NormArgs g = args_of(c, s, gain);
   g.x = dy;
   g.s = sum;
@@ -381,7 +475,7 @@ void rms_norm_bwd(hipStream_t st, const ast_norm_cfg& c, const void* dy, const v
   g.y = dx;
   g.sum = ds;
   g.part = static_cast<float*>(ws);
-  if (blocks) launch<true>(st, c, s, blocks, g);
+  if (blocks) launch<true>(st, c, way, s, blocks, g);
   KLAUNCH(rms_norm_gain_sum_kernel, dim3((unsigned)((c.width + 31) / 32)), dim3(1024), 0, st, g.part, (int)blocks, (int)c.width,
           dgain, (int)accumulate);
 }

@@ -450,48 +450,61 @@ def rms_norm_backward(dy, s, gain, dsum=None, eps=1e-6, out=None, sum_out=None, 
 
 # ------------------------------------------------------------------------------------------------ gated recurrence
 
-def _tokens(t, name, like=None):
+def _tokens(t, name, shape, dtype):
     """A matrix [tokens, channels] in rows of any stride, as the C calls take it."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in _DT:
-        raise ValueError("%s must be a float32 or bfloat16 tensor [tokens, channels]" % name)
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
-        raise ValueError("%s must be a %s tensor %s" % (name, like.dtype, tuple(like.shape)))
-    if t.stride(1) != 1 and t.shape[1] > 1:
+    if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype:
+        raise ValueError("%s must be a %s tensor %s" % (name, dtype, tuple(shape)))
+    step, unit = t.stride()
+    if unit != 1 and shape[1] > 1:
         raise ValueError("%s must have unit stride inside a row" % name)
-    return ast_rows(t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    return ast_rows(t.data_ptr(), step if shape[0] > 1 else shape[1])
 
 
-def _recurrence_cfg(f, offsets, period):
-    T, D = f.shape
+def _recurrence_inputs(f, z, o, offsets, period):
+    """The call's cfg, its sequences, and f, z, o as the C calls take them."""
+    if not isinstance(f, torch.Tensor) or f.dim() != 2 or f.dtype not in _DT:
+        raise ValueError("f must be a float32 or bfloat16 tensor [tokens, channels]")
+    shape, dtype = f.shape, f.dtype
+    rows = _tokens(f, "f", shape, dtype), _tokens(z, "z", shape, dtype), None if o is None else _tokens(o, "o", shape, dtype)
+    T, D = shape
     if offsets is not None:
         _vector_i32(offsets, "offsets")
-        if offsets.shape[0] < 1:
+        n = offsets.shape[0] - 1
+        if n < 0:
             raise ValueError("offsets must hold one number more than there are sequences")
-        return ast_recurrence_cfg(T, D, _DT[f.dtype], offsets.data_ptr(), offsets.shape[0] - 1, 0), offsets.shape[0] - 1
+        return ast_recurrence_cfg(T, D, _DT[dtype], offsets.data_ptr(), n, 0), n, rows
     if not 1 <= period < 1 << 31:
         raise ValueError("offsets, or the period of the sequences (below 2^31), must be given")
-    return ast_recurrence_cfg(T, D, _DT[f.dtype], None, 0, period), -(-T // period)
+    return ast_recurrence_cfg(T, D, _DT[dtype], None, 0, period), -(-T // period), rows
 
 
 def _states(t, name, n, f):
     """None, a tensor [sequences, channels], or (True) one that is made here."""
     if t is None or t is False:
         return None
-    if t is True:
-        return torch.empty((n, f.shape[1]), dtype=torch.float32, device=f.device)
-    return _is(t, name, _F32, (n, f.shape[1]))
+    shape = (n, f.shape[1])
+    return torch.empty(shape, dtype=torch.float32, device=f.device) if t is True else _is(t, name, _F32, shape)
 
 
-def _recurrence_workspace(cfg):
+def _recurrence_workspace(cfg, given, device):
+    """The workspace and its size; none where the call takes none."""
     n = C.c_size_t()
     lib = _lib()
-    _check(lib, lib.asteroid_recurrence_workspace(cfg, n))
-    return n.value
+    st = lib.asteroid_recurrence_workspace(cfg, n)
+    if st:
+        _check(lib, st)
+    if not n.value:
+        return None, 0
+    ws = _workspace(given, n.value, device)
+    return ws.data_ptr(), ws.numel()
 
 
 def recurrence_workspace(tokens, channels, dtype, offsets=False, period=0):
     """Bytes of workspace that recurrence_forward and recurrence_backward take (offsets: whether they are given)."""
-    return _recurrence_workspace(ast_recurrence_cfg(tokens, channels, _DT[dtype], 4 if offsets else None, 0, period))
+    n = C.c_size_t()
+    lib = _lib()
+    _check(lib, lib.asteroid_recurrence_workspace(ast_recurrence_cfg(tokens, channels, _DT[dtype], 4 if offsets else None, 0, period), n))
+    return n.value
 
 
 def recurrence_forward(f, z, o=None, offsets=None, period=0, state=None, final=None, saved=None, out=None, workspace=None):
@@ -500,19 +513,18 @@ def recurrence_forward(f, z, o=None, offsets=None, period=0, state=None, final=N
     [sequences + 1], or `period` tokens each.  state float32 [sequences, channels]: in front of every sequence (0 if not given).
     final: True or a tensor (state itself allowed) to receive the states behind them.  saved: True or a float32 tensor
     [tokens / 64 rounded up, channels] for recurrence_backward.  y is dense; rows of no sequence are not written."""
-    a = [_tokens(f, "f"), _tokens(z, "z", f), None if o is None else _tokens(o, "o", f)]
-    cfg, n = _recurrence_cfg(f, offsets, period)
+    cfg, n, a = _recurrence_inputs(f, z, o, offsets, period)
     state = _states(state, "state", n, f)
     final = _states(final, "final", n, f)
     saved = _states(saved, "saved", -(-f.shape[0] // RECURRENCE_CHUNK), f)
     if out is None:
         out = torch.empty(f.shape, dtype=f.dtype, device=f.device)
-    _is(out, "out", (f.dtype,), f.shape)
+    else:
+        _is(out, "out", (f.dtype,), f.shape)
     lib = _lib()
     d = _device(f, z, o, offsets, state, final, saved, out)
-    ws = _workspace(workspace, _recurrence_workspace(cfg), f.device)
-    _call(d, lib.asteroid_recurrence_forward, cfg, a[0], a[1], a[2], _ptr(state), out.data_ptr(), _ptr(final), _ptr(saved),
-          ws.data_ptr(), ws.numel())
+    ws, size = _recurrence_workspace(cfg, workspace, f.device)
+    _call(d, lib.asteroid_recurrence_forward, cfg, a[0], a[1], a[2], _ptr(state), out.data_ptr(), _ptr(final), _ptr(saved), ws, size)
     return out, final, saved
 
 
@@ -521,23 +533,24 @@ def recurrence_backward(dy, f, z, saved, o=None, offsets=None, period=0, state=N
     """(df, dz, do, dstate) of recurrence_forward with the same arguments; saved is what it left.  dfinal float32
     [sequences, channels]: the gradient of final (0 if not given).  dstate: True or a tensor to receive the gradient of state.
     out: (df, dz, do), rows with any stride; (f, z, o) themselves allowed.  do is None where o is."""
-    a = [_tokens(f, "f"), _tokens(z, "z", f), None if o is None else _tokens(o, "o", f)]
-    cfg, n = _recurrence_cfg(f, offsets, period)
+    cfg, n, a = _recurrence_inputs(f, z, o, offsets, period)
     _is(saved, "saved", _F32, (-(-f.shape[0] // RECURRENCE_CHUNK), f.shape[1]))
     state = _states(state, "state", n, f)
     dfinal = _states(dfinal, "dfinal", n, f)
     dstate = _states(dstate, "dstate", n, f)
+    shape, dtype = f.shape, f.dtype
     if out is None:
-        out = [torch.empty(f.shape, dtype=f.dtype, device=f.device) for _ in range(2 if o is None else 3)]
+        out = torch.empty((2 if o is None else 3,) + tuple(shape), dtype=dtype, device=f.device).unbind(0)
     df, dz, do = (tuple(out) + (None,))[:3]
     if (do is None) != (o is None):
         raise ValueError("out holds the gradient of o where o is given, and only there")
-    b = [_tokens(dy, "dy", f), _tokens(df, "df", f), _tokens(dz, "dz", f), None if do is None else _tokens(do, "do", f)]
+    b = [_tokens(dy, "dy", shape, dtype), _tokens(df, "df", shape, dtype), _tokens(dz, "dz", shape, dtype),
+         None if do is None else _tokens(do, "do", shape, dtype)]
     lib = _lib()
     d = _device(f, z, o, dy, saved, offsets, state, dfinal, dstate, df, dz, do)
-    ws = _workspace(workspace, _recurrence_workspace(cfg), f.device)
+    ws, size = _recurrence_workspace(cfg, workspace, f.device)
     _call(d, lib.asteroid_recurrence_backward, cfg, b[0], a[0], a[1], a[2], _ptr(state), saved.data_ptr(), _ptr(dfinal), b[1], b[2],
-          b[3], _ptr(dstate), ws.data_ptr(), ws.numel())
+          b[3], _ptr(dstate), ws, size)
     return df, dz, do, dstate
 
 

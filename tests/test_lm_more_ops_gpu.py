@@ -87,12 +87,16 @@ def test_rms_norm_forward(ops, rows, width, dt, st):
     inside(y, want, bound(want))
     n = rows * ((width + 31) // 32) * 33
     assert torch.equal(kept.data[:n], ops.stash8_pack(y).data[:n])
-    # in place, and without keeping: the same bits
-    y2, s2, none = ops.rms_norm_forward(x, gain, residual=res, eps=1e-5, out=x, sum_out=res)
-    assert none is None and y2 is x and s2 is res and torch.equal(y2, y) and torch.equal(s2, s)
+    # Without keeping, and in place.  (Rows whose length is no multiple of eight are then read in the tensor's groups, and the squares
+    # added up in that order: the bound is the same, the bits need not be.)
+    y2, s2, none = ops.rms_norm_forward(x, gain, residual=res, eps=1e-5)
+    assert none is None and torch.equal(s2, s) and (width % 8 or torch.equal(y2, y))
+    inside(y2, want, bound(want))
+    y3, s3, _ = ops.rms_norm_forward(x, gain, residual=res, eps=1e-5, out=x, sum_out=res)
+    assert y3 is x and s3 is res and torch.equal(y3, y2) and torch.equal(s3, s)
     if dt == st:   # nothing added
-        y3, s3, _ = ops.rms_norm_forward(s, gain, eps=1e-5)
-        assert s3 is s and torch.equal(y3, y)
+        y4, s4, _ = ops.rms_norm_forward(s, gain, eps=1e-5)
+        assert s4 is s and torch.equal(y4, y2)
 
 
 @pytest.mark.parametrize("dt,st", TYPES)
