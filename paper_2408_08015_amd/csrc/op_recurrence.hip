@@ -691,7 +691,7 @@ struct Layout { size_t maps, heads, counters, seq, end; int64_t words; int chunk
 Layout layout_of(const ast_recurrence_cfg& c, int per) {
   Layout l = {};
   l.chunks = (int)((c.tokens + per - 1) / per);
-  l.pairs = c.dtype != AST_F32 && c.channels > 1 && (int64_t)l.chunks * ((c.channels + 127) / 128) >= 256;
+  l.pairs = c.dtype != AST_F32 && c.channels > 1 && (int64_t)l.chunks * ((c.channels + 127) / 128) >= 1024;
   const int width = l.pairs ? 128 : 64;  // channels of a block
   l.columns = (int)((c.channels + width - 1) / width);
   // (chunks that each begin with a sequence's first token need nothing from each other)
