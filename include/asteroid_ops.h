@@ -248,10 +248,12 @@ ast_status asteroid_distill_backward(const ast_distill_cfg* cfg, const float* dl
                                      const int32_t* ids_dev, const void* teacher_dev, const float* stats_dev, void* dlogits_dev,
                                      int64_t dlogits_stride, void* hip_stream);
 
-/* Both at once, where dloss is known beforehand (1 / tokens, a mask): the logits are read from memory once. */
+/* Both at once, where dloss is known beforehand (1 / tokens, a mask): the logits are read from memory once.  The workspace may
+ * be of 0 bytes (it serves few long rows). */
+ast_status asteroid_distill_step_workspace(const ast_distill_cfg* cfg, size_t* bytes);
 ast_status asteroid_distill_step(const ast_distill_cfg* cfg, const float* dloss_dev, const void* logits_dev, const int32_t* ids_dev,
                                  const void* teacher_dev, float* loss_dev, void* dlogits_dev, int64_t dlogits_stride,
-                                 void* hip_stream);
+                                 void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -25,7 +25,8 @@ struct DistillArgs {
   const void* t;
   const float *dloss, *stats_in;
   float *loss, *stats;
-  int vocab, entries, teacher_bf16;
+  float *parts, *places_z;   // few rows, loss and gradient: sums of a row's slices [rows][slices][3]; logits at the entries' places [rows][entries + 1]
+  int vocab, entries, teacher_bf16, slices;
   float scale, inv_tau;      // log2(e) / tau; 1 / tau
   float kl, rate, mix;       // (1 - l) tau^2, (1 - l) tau, l
 };
@@ -60,11 +61,16 @@ __device__ __forceinline__ void merge(Sums& s, float m, float a, float b, float 
   s.m = top;
 }
 
-template <int THREADS, Exps E>
-__device__ __forceinline__ Sums block_sums(Sums s, float scale, float (*sh)[16]) {
+template <Exps E>
+__device__ __forceinline__ Sums wave_sums(Sums s, float scale) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2)
     merge<E>(s, __shfl_xor(s.m, d, 64), __shfl_xor(s.a, d, 64), E != ONE ? __shfl_xor(s.b, d, 64) : 0.f, scale);
+  return s;
+}
+template <int THREADS, Exps E>
+__device__ __forceinline__ Sums block_sums(Sums s, float scale, float (*sh)[16]) {
+  s = wave_sums<E>(s, scale);
   const int wave = threadIdx.x >> 6;
   if ((threadIdx.x & 63) == 0) {
     sh[0][wave] = s.m;
@@ -86,9 +92,10 @@ struct Entries {
   float z_label;
 };
 struct Places { uint32_t seen[kSeen / 32], twice[kSeen / 32]; };  // of the ids' lowest bits: stand in the row, stand more than once
-// every one of THREADS threads its entries; returns whether it has one that counts
+// Every one of THREADS threads its entries; returns whether it has one that counts.  Logits are read from z where they lie in
+// [lo, hi), or all of them from saved (a row's places_z).
 template <typename T, int THREADS>
-__device__ __forceinline__ bool gather(const DistillArgs& g, int64_t row, const T* z, int label, Entries& e) {
+__device__ __forceinline__ bool gather(const DistillArgs& g, int64_t row, const T* z, const float* saved, int lo, int hi, int label, Entries& e) {
   bool any = false;
   for (int k = threadIdx.x; k < g.entries; k += THREADS) {
     const int64_t at = row * g.entries + k;
@@ -98,13 +105,17 @@ __device__ __forceinline__ bool gather(const DistillArgs& g, int64_t row, const 
     e.id[k] = id;
     e.logp[k] = t;
     if (id >= 0) {
-      e.z[k] = load1(z + id);
+      if (saved) e.z[k] = saved[k];
+      else if (id >= lo && id < hi) e.z[k] = load1(z + id);
       any = true;
     }
   }
   if (threadIdx.x < 3)  // (what a group of four reads behind the last entry)
     if (g.entries + (int)threadIdx.x < kMostEntries) e.id[g.entries + threadIdx.x] = -1;
-  if (threadIdx.x == THREADS - 1 && label >= 0) e.z_label = load1(z + label);
+  if (threadIdx.x == THREADS - 1 && label >= 0) {
+    if (saved) e.z_label = saved[g.entries];
+    else if (label >= lo && label < hi) e.z_label = load1(z + label);
+  }
   return any;
 }
 // p and log p, by one wavefront, once all entries are there; and which ids may stand several times
@@ -200,50 +211,84 @@ __device__ __forceinline__ float row_loss(const DistillArgs& g, const Entries& e
   return loss;
 }
 
-// MODE 0: loss and statistics; 1: the gradient from them; 2: loss and gradient.  With MODE 2 a thread keeps the first KEEP groups that
-// it reads in registers; what a row has more is read again (from the caches, where it stayed there).
-template <typename T, int THREADS, int KEEP, Exps E, int MODE>
+// What a launch does.  A row is a block's, or, where there are few rows, cut into slices: PART sums a slice (and the first slice
+// saves the logits at the entries' places: others may be writing the gradient in place of them later), JOIN_STEP adds the slices up.
+enum Mode : int {
+  LOSS = 0,           // loss and statistics
+  GRADIENT = 1,       // the gradient from them (a slice)
+  STEP = 2,           // loss and gradient
+  PART = 3,
+  JOIN_STEP = 4       // STEP from the sums of the slices
+};
+// KEEP: with STEP a thread keeps the first KEEP groups that it reads in registers; what a row has more is read again (from the caches,
+// where it stayed there).
+template <typename T, int THREADS, int KEEP, Exps E, Mode MODE>
 __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g) {
+  constexpr bool SUMS = MODE == LOSS || MODE == STEP || MODE == PART, JOIN = MODE == JOIN_STEP;
+  constexpr bool GRAD = MODE == GRADIENT || MODE == STEP || MODE == JOIN_STEP;
+  constexpr bool CUT = MODE != LOSS && MODE != STEP;  // blockIdx.y: a slice
   constexpr int U = 4, K = KEEP ? KEEP : 1;  // U: groups that are asked for together
   __shared__ Entries e;
   __shared__ float sh[3][16];
   const int64_t row = blockIdx.x;
   const T* const z = static_cast<const T*>(g.z) + row * g.z_stride;
   const int tid = threadIdx.x, lane = tid & 63;
-  const Split sp = split_row(z, g.vocab);
-  const T* const zg = z + sp.head;
+  Split sp = split_row(z, g.vocab);
+  const int slice = CUT ? blockIdx.y : 0, slices = CUT ? gridDim.y : 1;
+  const int per = CUT ? (sp.groups + slices - 1) / slices : sp.groups, g0 = min(slice * per, sp.groups);
+  const bool lowest = slice == 0, highest = slice == slices - 1;
+  const int lo = lowest ? 0 : sp.head + g0 * 8, hi = highest ? g.vocab : sp.head + min(g0 + per, sp.groups) * 8;
+  const T* const zg = z + sp.head + g0 * 8;
   // the value in front of or behind the groups that falls to this thread
-  const int odd = tid < sp.head ? tid : tid - sp.head < sp.tail ? sp.groups * 8 + tid : -1;
+  const int behind = tid - (lowest ? sp.head : 0);
+  const int odd = lowest && tid < sp.head ? tid : highest && behind >= 0 && behind < sp.tail ? sp.head + sp.groups * 8 + behind : -1;
+  sp.groups = min(per, sp.groups - g0);
 
   int label = g.labels && g.mix != 0.f ? g.labels[row] : -1;
   if (label < 0 || label >= g.vocab) label = -1;
-  const float w = MODE ? g.dloss[row] : 1.f;
+  const float w = GRAD ? g.dloss[row] : 1.f;
   Eight<T, true> kept[K];
 #pragma unroll
   for (int u = 0; u < KEEP; ++u)
     if (u * THREADS < sp.groups) load_group(kept[u], zg, tid + u * THREADS, sp.groups, (u + 1) * THREADS <= sp.groups);
   const float zodd = odd >= 0 ? load1(z + odd) : -INFINITY;
   bool any = false;  // an entry of the teacher's counts
+  const float* const saved = JOIN ? g.places_z + row * (g.entries + 1) : nullptr;
   Places* places = nullptr;
-  if constexpr (MODE != 0) {
+  if constexpr (GRAD) {  // (what may be written in place of the logits waits for their values at the entries' places)
     __shared__ Places store;
     places = &store;
-  }
-  if (MODE == 0) {  // (the others go on to the row)
-    if (tid < 64) {
-      gather<T, 64>(g, row, z, label, e);
-      teacher(g, e, lane, nullptr);
-    }
-  } else {  // (what may be written in place of the logits waits for their values at the entries' places)
     for (int i = tid; i < kSeen / 32; i += THREADS) places->seen[i] = places->twice[i] = 0;
-    any = __syncthreads_or(gather<T, THREADS>(g, row, z, label, e));
+    any = __syncthreads_or(gather<T, THREADS>(g, row, z, saved, lo, hi, label, e));
     if (tid < 64) teacher(g, e, lane, places);
+  } else if constexpr (MODE == PART) {
+    if (lowest) {
+      float* const to = g.places_z + row * (g.entries + 1);
+      for (int k = tid; k <= g.entries; k += THREADS) {
+        const int id = k < g.entries ? g.ids[row * g.entries + k] : label;
+        to[k] = id >= 0 && id < g.vocab ? load1(z + id) : 0.f;
+      }
+    }
+  } else {  // (the others go on to the row; many entries are gathered by all: 8192 x 2000 with 512 47 us from 65, 2001 x 50021 with
+            // 100 would take 53.7 from 51.8)
+    if (g.entries > 128) {
+      gather<T, THREADS>(g, row, z, saved, lo, hi, label, e);
+      __syncthreads();
+    } else if (tid < 64) {
+      gather<T, 64>(g, row, z, saved, lo, hi, label, e);
+    }
+    if (tid < 64) teacher(g, e, lane, nullptr);
   }
 
   Sums s = {kLowest, 0.f, 0.f};
-  if (MODE == 1) {
-    s = {g.stats_in[row * 3], g.stats_in[row * 3 + 1], g.stats_in[row * 3 + 2]};
-  } else {
+  if constexpr (MODE == GRADIENT) s = {g.stats_in[row * 3], g.stats_in[row * 3 + 1], g.stats_in[row * 3 + 2]};
+  if constexpr (JOIN) {
+    const float* const p = g.parts + (row * g.slices + lane) * 3;
+    if (lane < g.slices) s = {p[0], p[1], p[2]};
+    s = wave_sums<E>(s, g.scale);
+    if (E == ONE) s.b = s.a;
+  }
+  if constexpr (SUMS) {
     for (int at = tid + KEEP * THREADS; at - tid < sp.groups; at += U * THREADS) {
       Eight<T, true> r[U];
       const bool all = at - tid + U * THREADS <= sp.groups;
@@ -264,22 +309,26 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
     exps<E>(zodd - fmaxf(zodd, kLowest), g.scale, oa, ob);
     merge<E>(s, fmaxf(zodd, kLowest), oa, ob, g.scale);
     s = block_sums<THREADS, E>(s, g.scale, sh);
-    if (tid < 64) {
-      const float loss = row_loss(g, e, s, label >= 0, lane);
-      if (lane == 0) {
-        g.loss[row] = loss;
-        if (MODE == 0) {
-          g.stats[row * 3] = s.m;
-          g.stats[row * 3 + 1] = s.a;
-          g.stats[row * 3 + 2] = g.labels && g.mix != 0.f ? s.b : 0.f;
-        }
+  }
+  if constexpr (MODE == PART) {
+    if (tid < 3) g.parts[(row * g.slices + slice) * 3 + tid] = tid == 0 ? s.m : tid == 1 ? s.a : s.b;
+    return;
+  }
+  if (MODE != GRADIENT && lowest && tid < 64) {
+    const float loss = row_loss(g, e, s, label >= 0, lane);
+    if (lane == 0) {
+      g.loss[row] = loss;
+      if (!GRAD) {
+        g.stats[row * 3] = s.m;
+        g.stats[row * 3 + 1] = s.a;
+        g.stats[row * 3 + 2] = g.labels && g.mix != 0.f ? s.b : 0.f;
       }
     }
   }
-  if (MODE == 0) return;
+  if constexpr (GRAD) {
 
   T* const dz = static_cast<T*>(g.dz) + row * g.dz_stride;
-  T* const dg = dz + sp.head;
+  T* const dg = dz + (zg - z);
   const float rate = any && g.rate != 0.f ? w * g.rate : 0.f, mix = label >= 0 ? w * g.mix : 0.f;
   const float ca = rate != 0.f ? rate / s.a : 0.f, cb = mix != 0.f ? mix / s.b : 0.f;
   auto slope = [&](float v) __attribute__((always_inline)) {  // dloss (rate q + mix q1)
@@ -318,7 +367,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
   // with another: only those look through the row for equal ones.
   for (int k = tid; k <= g.entries; k += THREADS) {
     const int id = k < g.entries ? e.id[k] : label;
-    if (id < 0) continue;
+    if (id < 0 || id < lo || id >= hi) continue;
     float p = k < g.entries ? e.p[k] : 0.f;
     bool first = true;
     const uint32_t at = (uint32_t)id % kSeen;
@@ -340,33 +389,50 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
     if (mix != 0.f) x += mix * (b / s.b - (id == label ? 1.f : 0.f));
     store1(dz + id, x);
   }
+  }
 }
 
-template <int MODE, typename T, int THREADS, int KEEP>
-void go(hipStream_t st, int64_t rows, const DistillArgs& g, Exps e) {
-  const char* const name = MODE == 0 ? "distill_kernel" : MODE == 1 ? "distill_bwd_kernel" : "distill_step_kernel";
-  auto run = [&](auto kernel) { KLAUNCH_NAMED(name, kernel, dim3((unsigned)rows), dim3(THREADS), 0, st, g); };
+// Slices of a row: of 8192 values or more where rows alone would leave compute units without a block (16 bf16 rows of 131072: gradient
+// 7.7 us from 13.7, loss and gradient in two launches 13.9 from 22; the loss alone would take 15.6 in two launches, 11.5 in one).
+int slices_of(int64_t rows, int64_t vocab) {
+  if (rows > 64) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({64, vocab / 8192, 512 / std::max<int64_t>(rows, 1)}));
+}
+
+template <Mode MODE, typename T, int THREADS, int KEEP>
+void go(hipStream_t st, int64_t rows, int slices, const DistillArgs& g, Exps e) {
+  const char* const name = MODE == GRADIENT ? "distill_bwd_kernel" : MODE == STEP || MODE == JOIN_STEP ? "distill_step_kernel" : "distill_kernel";
+  auto run = [&](auto kernel) { KLAUNCH_NAMED(name, kernel, dim3((unsigned)rows, (unsigned)slices), dim3(THREADS), 0, st, g); };
   if (e == ONE) run(distill_kernel<T, THREADS, KEEP, ONE, MODE>);
   else if (e == SQUARE) run(distill_kernel<T, THREADS, KEEP, SQUARE, MODE>);
   else if (e == FOURTH) run(distill_kernel<T, THREADS, KEEP, FOURTH, MODE>);
   else run(distill_kernel<T, THREADS, KEEP, BOTH, MODE>);
 }
-template <int MODE, typename T>
+template <Mode MODE, typename T>
 void pick(hipStream_t st, const ast_distill_cfg& c, const DistillArgs& g, Exps e) {
   const int64_t r = c.rows, v = c.vocab;
-  if constexpr (MODE == 2) {
-    if (v <= 8192) go<MODE, T, 256, 4>(st, r, g, e);
-    else if (v <= 16384) go<MODE, T, 256, 8>(st, r, g, e);
-    else go<MODE, T, 512, sizeof(T) == 2 ? 16 : 8>(st, r, g, e);
+  if constexpr (MODE == GRADIENT) {
+    if (v <= 8192) go<MODE, T, 256, 0>(st, r, 1, g, e);
+    else go<MODE, T, 512, 0>(st, r, g.slices, g, e);
+  } else if constexpr (MODE == STEP) {
+    if (g.slices > 1) {
+      go<PART, T, 512, 0>(st, r, g.slices, g, e);
+      go<JOIN_STEP, T, 512, 0>(st, r, g.slices, g, e);
+    } else if (v <= 8192) go<MODE, T, 256, 4>(st, r, 1, g, e);
+    else if (v <= 16384) go<MODE, T, 256, 8>(st, r, 1, g, e);
+    else go<MODE, T, 512, sizeof(T) == 2 ? 16 : 8>(st, r, 1, g, e);
   } else {
-    if (v <= 8192) go<MODE, T, 256, 0>(st, r, g, e);
-    else go<MODE, T, 512, 0>(st, r, g, e);
+    if (v <= 8192) go<MODE, T, 256, 0>(st, r, 1, g, e);
+    else go<MODE, T, 512, 0>(st, r, 1, g, e);
   }
 }
-template <int MODE>
-void launch(hipStream_t st, const ast_distill_cfg& c, DistillArgs g) {
+template <Mode MODE>
+void launch(hipStream_t st, const ast_distill_cfg& c, DistillArgs g, void* ws) {
   const float tau = c.temperature;
   const Exps e = !g.labels || g.mix == 0.f || tau == 1.f ? ONE : tau == 2.f ? SQUARE : tau == 4.f ? FOURTH : BOTH;
+  g.slices = slices_of(c.rows, c.vocab);
+  g.parts = static_cast<float*>(ws);
+  g.places_z = g.parts + c.rows * g.slices * 3;
   if (c.dtype == AST_F32) pick<MODE, float>(st, c, g, e);
   else pick<MODE, bf16_t>(st, c, g, e);
 }
@@ -391,11 +457,16 @@ DistillArgs args_of(const ast_distill_cfg& c, const void* z, const int32_t* ids,
 
 }  // namespace
 
+size_t distill_step_ws_bytes(const ast_distill_cfg& c) {
+  const int slices = slices_of(c.rows, c.vocab);
+  return slices > 1 ? (size_t)c.rows * (size_t)(slices * 3 + c.entries + 1) * sizeof(float) : 0;
+}
+
 void distill_fwd(hipStream_t st, const ast_distill_cfg& c, const void* z, const int32_t* ids, const void* t, float* loss, float* stats) {
   DistillArgs g = args_of(c, z, ids, t);
   g.loss = loss;
   g.stats = stats;
-  launch<0>(st, c, g);
+  launch<LOSS>(st, c, g, nullptr);
 }
 
 void distill_bwd(hipStream_t st, const ast_distill_cfg& c, const float* dloss, const void* z, const int32_t* ids, const void* t,
@@ -405,17 +476,17 @@ void distill_bwd(hipStream_t st, const ast_distill_cfg& c, const float* dloss, c
   g.stats_in = stats;
   g.dz = dz;
   g.dz_stride = dz_stride;
-  launch<1>(st, c, g);
+  launch<GRADIENT>(st, c, g, nullptr);
 }
 
 void distill_step(hipStream_t st, const ast_distill_cfg& c, const float* dloss, const void* z, const int32_t* ids, const void* t,
-                  float* loss, void* dz, int64_t dz_stride) {
+                  float* loss, void* dz, int64_t dz_stride, void* ws) {
   DistillArgs g = args_of(c, z, ids, t);
   g.dloss = dloss;
   g.loss = loss;
   g.dz = dz;
   g.dz_stride = dz_stride;
-  launch<2>(st, c, g);
+  launch<STEP>(st, c, g, ws);
 }
 
 }  // namespace ast

@@ -41,11 +41,12 @@ void recurrence_bwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows&
                     const ast_rows& dz, const ast_rows* dgo, float* dstate, void* ws);
 
 // ---- distillation from a teacher's top logits (op_distill.hip)
+size_t distill_step_ws_bytes(const ast_distill_cfg& c);
 void distill_fwd(hipStream_t st, const ast_distill_cfg& c, const void* z, const int32_t* ids, const void* t, float* loss, float* stats);
 void distill_bwd(hipStream_t st, const ast_distill_cfg& c, const float* dloss, const void* z, const int32_t* ids, const void* t,
                  const float* stats, void* dz, int64_t dz_stride);
 void distill_step(hipStream_t st, const ast_distill_cfg& c, const float* dloss, const void* z, const int32_t* ids, const void* t,
-                  float* loss, void* dz, int64_t dz_stride);
+                  float* loss, void* dz, int64_t dz_stride, void* ws);
 
 // ---- activations kept in 8 bits (op_stash8.hip, op_stash8_wgrad.hip)
 constexpr int kStash8Block = 32;  // values that share a scale

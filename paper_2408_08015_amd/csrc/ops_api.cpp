@@ -384,8 +384,17 @@ ast_status asteroid_distill_backward(const ast_distill_cfg* cfg, const float* dl
   return launched(fn);
 }
 
+ast_status asteroid_distill_step_workspace(const ast_distill_cfg* cfg, size_t* bytes) {
+  const char* const fn = "distill_step_workspace";
+  if (!bytes) return fail(fn, "NULL argument");
+  if (const char* e = distill_cfg(cfg)) return fail(fn, e);
+  *bytes = ast::distill_step_ws_bytes(*cfg);
+  return AST_OK;
+}
+
 ast_status asteroid_distill_step(const ast_distill_cfg* cfg, const float* dloss_dev, const void* logits_dev, const int32_t* ids_dev,
-                                 const void* teacher_dev, float* loss_dev, void* dlogits_dev, int64_t dlogits_stride, void* hip_stream) {
+                                 const void* teacher_dev, float* loss_dev, void* dlogits_dev, int64_t dlogits_stride, void* workspace_dev,
+                                 size_t workspace_bytes, void* hip_stream) {
   const char* const fn = "distill_step";
   if (const char* e = distill_cfg(cfg)) return fail(fn, e);
   if (cfg->rows == 0) return AST_OK;
@@ -394,7 +403,11 @@ ast_status asteroid_distill_step(const ast_distill_cfg* cfg, const float* dloss_
   if (!loss_dev || !aligned(loss_dev, 4)) return fail(fn, "loss_dev must be non-NULL and 4-byte aligned");
   const size_t nd = ((size_t)(cfg->rows - 1) * (size_t)dlogits_stride + (size_t)cfg->vocab) * esize(cfg->dtype);
   if (overlap(loss_dev, 4 * (size_t)cfg->rows, dlogits_dev, nd)) return fail(fn, "outputs overlap");
-  ast::distill_step(stream_of(hip_stream), *cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, loss_dev, dlogits_dev, dlogits_stride);
+  const size_t need = ast::distill_step_ws_bytes(*cfg);
+  if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
+    return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  ast::distill_step(stream_of(hip_stream), *cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, loss_dev, dlogits_dev, dlogits_stride,
+                    workspace_dev);
   return launched(fn);
 }
 

@@ -76,7 +76,8 @@ def _lib():
             "recurrence_backward": [rp, sp, sp, sp, sp, vp, vp, vp, sp, sp, sp, vp, vp, sz, vp],
             "distill_forward": [dp, vp, vp, vp, vp, vp, vp],
             "distill_backward": [dp, vp, vp, vp, vp, vp, vp, i64, vp],
-            "distill_step": [dp, vp, vp, vp, vp, vp, vp, i64, vp],
+            "distill_step_workspace": [dp, szp],
+            "distill_step": [dp, vp, vp, vp, vp, vp, vp, i64, vp, sz, vp],
         }.items():
             getattr(lib, "asteroid_" + name).argtypes = types
         _LIB = lib
@@ -486,13 +487,12 @@ def _states(t, name, n, f):
     return torch.empty(shape, dtype=torch.float32, device=f.device) if t is True else _is(t, name, _F32, shape)
 
 
-def _recurrence_workspace(cfg, given, device):
-    """The workspace and its size; none where the call takes none."""
+def _workspace_of(fn, cfg, given, device):
+    """The workspace and its size, which `fn` says; none where the call takes none."""
     n = C.c_size_t()
-    lib = _lib()
-    st = lib.asteroid_recurrence_workspace(cfg, n)
+    st = fn(cfg, n)
     if st:
-        _check(lib, st)
+        _check(_LIB, st)
     if not n.value:
         return None, 0
     ws = _workspace(given, n.value, device)
@@ -523,7 +523,7 @@ def recurrence_forward(f, z, o=None, offsets=None, period=0, state=None, final=N
         _is(out, "out", (f.dtype,), f.shape)
     lib = _lib()
     d = _device(f, z, o, offsets, state, final, saved, out)
-    ws, size = _recurrence_workspace(cfg, workspace, f.device)
+    ws, size = _workspace_of(lib.asteroid_recurrence_workspace, cfg, workspace, f.device)
     _call(d, lib.asteroid_recurrence_forward, cfg, a[0], a[1], a[2], _ptr(state), out.data_ptr(), _ptr(final), _ptr(saved), ws, size)
     return out, final, saved
 
@@ -548,7 +548,7 @@ def recurrence_backward(dy, f, z, saved, o=None, offsets=None, period=0, state=N
          None if do is None else _tokens(do, "do", shape, dtype)]
     lib = _lib()
     d = _device(f, z, o, dy, saved, offsets, state, dfinal, dstate, df, dz, do)
-    ws, size = _recurrence_workspace(cfg, workspace, f.device)
+    ws, size = _workspace_of(lib.asteroid_recurrence_workspace, cfg, workspace, f.device)
     _call(d, lib.asteroid_recurrence_backward, cfg, b[0], a[0], a[1], a[2], _ptr(state), saved.data_ptr(), _ptr(dfinal), b[1], b[2],
           b[3], _ptr(dstate), ws, size)
     return df, dz, do, dstate
@@ -620,7 +620,15 @@ def distill_backward(dloss, logits, ids, teacher, stats, temperature=1.0, labels
     return out
 
 
-def distill_step(dloss, logits, ids, teacher, temperature=1.0, labels=None, label_weight=0.0, out=None, loss_out=None):
+def distill_step_workspace(rows, vocab, entries):
+    """Bytes of workspace that distill_step takes."""
+    n = C.c_size_t()
+    lib = _lib()
+    _check(lib, lib.asteroid_distill_step_workspace(ast_distill_cfg(rows, vocab, vocab, 0, entries, 0, 1.0, 0.0, None), n))
+    return n.value
+
+
+def distill_step(dloss, logits, ids, teacher, temperature=1.0, labels=None, label_weight=0.0, out=None, loss_out=None, workspace=None):
     """(loss, the logits' gradient) at once, where dloss is known beforehand.  out may be logits."""
     cfg = _distill_cfg(logits, ids, teacher, temperature, labels, label_weight)
     out, stride = _gradient_of(logits, out, dloss)
@@ -628,6 +636,8 @@ def distill_step(dloss, logits, ids, teacher, temperature=1.0, labels=None, labe
         loss_out = torch.empty((logits.shape[0],), dtype=torch.float32, device=logits.device)
     _is(loss_out, "loss_out", _F32, (logits.shape[0],))
     lib = _lib()
-    _call(_device(logits, ids, teacher, labels, dloss, loss_out, out), lib.asteroid_distill_step, cfg, dloss.data_ptr(),
-          logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(), loss_out.data_ptr(), out.data_ptr(), stride)
+    d = _device(logits, ids, teacher, labels, dloss, loss_out, out)
+    ws, size = _workspace_of(lib.asteroid_distill_step_workspace, cfg, workspace, logits.device)
+    _call(d, lib.asteroid_distill_step, cfg, dloss.data_ptr(), logits.data_ptr(), ids.data_ptr(), teacher.data_ptr(), loss_out.data_ptr(),
+          out.data_ptr(), stride, ws, size)
     return loss_out, out

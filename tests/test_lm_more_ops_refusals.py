@@ -134,22 +134,31 @@ BAD_DIST = [None] + [dist(**k) for k in (dict(rows=-1), dict(rows=1 << 31), dict
 
 
 def test_distill_refusals(lib):
-    z, ids, t, loss, st, w, dz = FAR[:7]
+    z, ids, t, loss, st, w, dz, ws = FAR[:8]
+    n = C.c_size_t()
+    for c in BAD_DIST:
+        refused(lib, "distill_step_workspace", c, C.byref(n))
+    refused(lib, "distill_step_workspace", dist(), None)
+    assert lib.asteroid_distill_step_workspace(dist(), C.byref(n)) == 0 and n.value == 0
+    few = dist(vocab=40000, logits_stride=40000)      # few long rows are cut into slices
+    assert lib.asteroid_distill_step_workspace(few, C.byref(n)) == 0 and n.value > 0
     ok = [dist(), z, ids, t, loss, st, None]
     for a in each(ok, {0: BAD_DIST, 1: [None, z + 1], 2: [None, ids + 2], 3: [None, t + 2], 4: [None, loss + 2, st, st + 44], 5: [None, st + 2]}):
         refused(lib, "distill_forward", *a)
+    for a in each([few, w, z, ids, t, loss, dz, 40000, ws, n.value, None], {8: [None, ws + 8], 9: [n.value - 1]}):
+        refused(lib, "distill_step", *a)
     ok = [dist(), w, z, ids, t, st, dz, 50, None]
     for a in each(ok, {0: BAD_DIST, 1: [None, w + 2], 2: [None, z + 1], 3: [None, ids + 2], 4: [None, t + 2], 5: [None, st + 2], 6: [None, dz + 1, z],
                        7: [49, (1 << 31) + 1]}):
         refused(lib, "distill_backward", *a)
-    ok = [dist(), w, z, ids, t, loss, dz, 50, None]
+    ok = [dist(), w, z, ids, t, loss, dz, 50, None, 0, None]
     for a in each(ok, {0: BAD_DIST, 1: [None, w + 2], 2: [None, z + 1], 3: [None, ids + 2], 4: [None, t + 2], 5: [None, loss + 2, dz, dz + 64],
                        6: [None, dz + 1, z], 7: [49, (1 << 31) + 1]}):
         refused(lib, "distill_step", *a)
     c = dist(rows=0)
     assert lib.asteroid_distill_forward(c, None, None, None, None, None, None) == 0
     assert lib.asteroid_distill_backward(c, None, None, None, None, None, None, 0, None) == 0
-    assert lib.asteroid_distill_step(c, None, None, None, None, None, None, 0, None) == 0
+    assert lib.asteroid_distill_step(c, None, None, None, None, None, None, 0, None, 0, None) == 0
 
 
 def test_tensors_are_checked():
