@@ -184,7 +184,8 @@ ast_status asteroid_rms_norm_backward(const ast_norm_cfg* cfg, const void* dy_de
  * fp32 throughout, and nothing of a sequence, infinities and NaN included, reaches another.
  * saved_dev (NULL: no backward pass follows): fp32 [tokens / AST_RECURRENCE_CHUNK rounded up][channels], for the backward
  * pass: the state in front of every AST_RECURRENCE_CHUNK-th token.
- * tokens < 2^31, channels in [1, 2^20], tokens * channels < 2^40, sequences in [0, 2^31 - 2], period in [1, 2^31). */
+ * tokens < 2^31, channels in [1, 2^20], tokens (rounded up to 512) * channels (rounded up to 64) <= 2^34, sequences in
+ * [0, 2^31 - 2], period in [1, 2^31). */
 #define AST_RECURRENCE_CHUNK 64
 
 typedef struct {

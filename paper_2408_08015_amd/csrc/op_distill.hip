@@ -26,6 +26,7 @@ struct DistillArgs {
   const float *dloss, *stats_in;
   float *loss, *stats;
   float *parts, *places_z;   // few rows, loss and gradient: sums of a row's slices [rows][slices][3]; logits at the entries' places [rows][entries + 1]
+  int64_t row0;              // of the launch
   int vocab, entries, teacher_bf16, slices;
   float scale, inv_tau;      // log2(e) / tau; 1 / tau
   float kl, rate, mix;       // (1 - l) tau^2, (1 - l) tau, l
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
   constexpr int U = 4, K = KEEP ? KEEP : 1;  // U: groups that are asked for together
   __shared__ Entries e;
   __shared__ float sh[3][16];
-  const int64_t row = blockIdx.x;
+  const int64_t row = g.row0 + blockIdx.x;
   const T* const z = static_cast<const T*>(g.z) + row * g.z_stride;
   const int tid = threadIdx.x, lane = tid & 63;
   Split sp = split_row(z, g.vocab);
@@ -399,10 +400,14 @@ int slices_of(int64_t rows, int64_t vocab) {
   return (int)std::max<int64_t>(1, std::min<int64_t>({64, vocab / 8192, 512 / std::max<int64_t>(rows, 1)}));
 }
 
+constexpr int64_t kRowsAtOnce = 1 << 22;  // (a launch has fewer than 2^32 threads)
 template <Mode MODE, typename T, int THREADS, int KEEP>
-void go(hipStream_t st, int64_t rows, int slices, const DistillArgs& g, Exps e) {
+void go(hipStream_t st, int64_t rows, int slices, DistillArgs g, Exps e) {
   const char* const name = MODE == GRADIENT ? "distill_bwd_kernel" : MODE == STEP || MODE == JOIN_STEP ? "distill_step_kernel" : "distill_kernel";
-  auto run = [&](auto kernel) { KLAUNCH_NAMED(name, kernel, dim3((unsigned)rows, (unsigned)slices), dim3(THREADS), 0, st, g); };
+  auto run = [&](auto kernel) {
+    for (g.row0 = 0; g.row0 < rows; g.row0 += kRowsAtOnce)
+      KLAUNCH_NAMED(name, kernel, dim3((unsigned)std::min<int64_t>(rows - g.row0, kRowsAtOnce), (unsigned)slices), dim3(THREADS), 0, st, g);
+  };
   if (e == ONE) run(distill_kernel<T, THREADS, KEEP, ONE, MODE>);
   else if (e == SQUARE) run(distill_kernel<T, THREADS, KEEP, SQUARE, MODE>);
   else if (e == FOURTH) run(distill_kernel<T, THREADS, KEEP, FOURTH, MODE>);

@@ -100,7 +100,8 @@ const char* recurrence_cfg(const ast_recurrence_cfg* c) {
   if (!dtype_ok(c->dtype)) return "unknown dtype";
   if (c->tokens < 0 || c->tokens > kMostRows) return "tokens must lie in [0, 2^31)";
   if (c->channels < 1 || c->channels > kMostWidth) return "channels must lie in [1, 2^20]";
-  if (c->tokens * c->channels >= (int64_t)1 << 40) return "tokens * channels must stay below 2^40";
+  // (a launch has fewer than 2^32 threads)
+  if ((c->tokens + 511) / 512 * 512 * ((c->channels + 63) / 64 * 64) > (int64_t)1 << 34) return "tokens * channels must not exceed 2^34";
   if (c->offsets_dev) {
     if (!aligned(c->offsets_dev, 4)) return "offsets_dev must be 4-byte aligned";
     if (c->sequences < 0 || c->sequences > kMostRows - 1) return "sequences must lie in [0, 2^31 - 2]";

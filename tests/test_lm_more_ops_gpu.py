@@ -523,6 +523,24 @@ def test_distill_of_no_rows(ops):
     assert ops.distill_backward(w, e, ids, t, stats).shape == (0, 40) and ops.distill_step(w, e, ids, t)[1].shape == (0, 40)
 
 
+def test_distill_of_more_rows_than_a_launch_takes(ops):
+    """The rows behind the 2^22nd are a launch of their own."""
+    g = torch.Generator(device="cuda").manual_seed(12)
+    T, V = (1 << 22) + 37, 9
+    z = torch.randn(T, V, generator=g, device="cuda")
+    ids = torch.randint(-1, V, (T, 3), generator=g, device="cuda", dtype=torch.int32)
+    t, w = torch.randn(T, 3, generator=g, device="cuda"), torch.rand(T, generator=g, device="cuda")
+    loss, dz = ops.distill_step(w, z, ids, t)
+    stats = ops.distill_forward(z, ids, t)[1]
+    for a, b in ((0, 50), ((1 << 22) - 20, T)):
+        s = slice(a, b)
+        want = ops.distill_step(w[s], z[s].clone(), ids[s], t[s])
+        assert torch.equal(loss[s], want[0]) and torch.equal(dz[s], want[1])
+    # two ways to the same gradient, |dloss| <= 1 and softmax values at most 1: each is off by at most the exponential (4 (|z - max|) + 6,
+    # here below 60), its sum and the teacher's p (64 and 2 x (4 x 12 + 8) + 3) in steps of u
+    assert (ops.distill_backward(w, z, ids, t, stats) - dz).abs().max() <= 2 * (60 + 64 + 115) * u and bool(loss.isfinite().all())
+
+
 # ------------------------------------------------------------------------------------------------ together
 
 def stage(ops, D, V, K, g):

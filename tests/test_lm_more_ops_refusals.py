@@ -77,7 +77,7 @@ def rec(**kw):
 
 
 BAD_REC = [None] + [rec(**k) for k in (dict(tokens=-1), dict(tokens=1 << 31), dict(channels=0), dict(channels=(1 << 20) + 1), dict(dtype=2),
-                                       dict(tokens=1 << 30, channels=1 << 10), dict(offsets_dev=P + 2), dict(sequences=-1),
+                                       dict(tokens=1 << 30, channels=17), dict(tokens=(1 << 28) + 1, channels=64), dict(offsets_dev=P + 2), dict(sequences=-1),
                                        dict(sequences=(1 << 31) - 1), dict(offsets_dev=None), dict(offsets_dev=None, period=-1),
                                        dict(offsets_dev=None, period=1 << 31))]
 BAD_ROWS = [None, rows(None), rows(P + 1), rows(stride=-1), rows(stride=(1 << 40) + 1)]
