@@ -221,9 +221,9 @@ enum Mode : int {
   PART = 3,
   JOIN_STEP = 4       // STEP from the sums of the slices
 };
-// KEEP: with STEP a thread keeps the first KEEP groups that it reads in registers; what a row has more is read again (from the caches,
-// where it stayed there).
-template <typename T, int THREADS, int KEEP, Exps E, Mode MODE>
+// KEEP: with STEP a thread keeps the first KEEP groups that it reads in registers, and the next four in shared memory (STORE); what a
+// row has more is read again (from the caches, where it stayed there).
+template <typename T, int THREADS, int KEEP, bool STORE, Exps E, Mode MODE>
 __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g) {
   constexpr bool SUMS = MODE == LOSS || MODE == STEP || MODE == PART, JOIN = MODE == JOIN_STEP;
   constexpr bool GRAD = MODE == GRADIENT || MODE == STEP || MODE == JOIN_STEP;
@@ -248,6 +248,8 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
   int label = g.labels && g.mix != 0.f ? g.labels[row] : -1;
   if (label < 0 || label >= g.vocab) label = -1;
   const float w = GRAD ? g.dloss[row] : 1.f;
+  static_assert(!STORE || sizeof(T) == 2, "a group is 16 bytes");
+  __shared__ uint4 stored[STORE ? U : 1][STORE ? THREADS : 1];  // (a thread reads what it wrote)
   Eight<T, true> kept[K];
 #pragma unroll
   for (int u = 0; u < KEEP; ++u)
@@ -295,6 +297,10 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
       const bool all = at - tid + U * THREADS <= sp.groups;
 #pragma unroll
       for (int u = 0; u < U; ++u) load_group(r[u], zg, at + u * THREADS, sp.groups, all);
+      if (STORE && at == tid + KEEP * THREADS) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) stored[u][tid] = *reinterpret_cast<const uint4*>(r[u].v);
+      }
       add_groups<T, E>(s, r, g.scale);
     }
 #pragma unroll
@@ -335,7 +341,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
   auto slope = [&](float v) __attribute__((always_inline)) {  // dloss (rate q + mix q1)
     float a, b;
     exps<E>(v - s.m, g.scale, a, b);
-    return E == ONE ? (ca + cb) * a : ca * a + cb * b;
+    return E == ONE ? (ca + cb) * a : E == SQUARE ? a * fmaf(cb, a, ca) : ca * a + cb * b;
   };
   auto write = [&](const Eight<T, true>& r, int at) __attribute__((always_inline)) {
     float v[8];
@@ -353,7 +359,16 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
 #pragma unroll
   for (int u = 0; u < KEEP; ++u)
     if (tid + u * THREADS < sp.groups) write(kept[u], tid + u * THREADS);
-  for (int at = tid + KEEP * THREADS; at < sp.groups; at += U * THREADS) {
+  if (STORE) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (tid + (KEEP + u) * THREADS < sp.groups) {
+        Eight<T, true> r;
+        *reinterpret_cast<uint4*>(r.v) = stored[u][tid];
+        write(r, tid + (KEEP + u) * THREADS);
+      }
+  }
+  for (int at = tid + (KEEP + (STORE ? U : 0)) * THREADS; at < sp.groups; at += U * THREADS) {
     Eight<T, true> r[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -401,17 +416,17 @@ int slices_of(int64_t rows, int64_t vocab) {
 }
 
 constexpr int64_t kRowsAtOnce = 1 << 22;  // (a launch has fewer than 2^32 threads)
-template <Mode MODE, typename T, int THREADS, int KEEP>
+template <Mode MODE, typename T, int THREADS, int KEEP, bool STORE = false>
 void go(hipStream_t st, int64_t rows, int slices, DistillArgs g, Exps e) {
   const char* const name = MODE == GRADIENT ? "distill_bwd_kernel" : MODE == STEP || MODE == JOIN_STEP ? "distill_step_kernel" : "distill_kernel";
   auto run = [&](auto kernel) {
     for (g.row0 = 0; g.row0 < rows; g.row0 += kRowsAtOnce)
       KLAUNCH_NAMED(name, kernel, dim3((unsigned)std::min<int64_t>(rows - g.row0, kRowsAtOnce), (unsigned)slices), dim3(THREADS), 0, st, g);
   };
-  if (e == ONE) run(distill_kernel<T, THREADS, KEEP, ONE, MODE>);
-  else if (e == SQUARE) run(distill_kernel<T, THREADS, KEEP, SQUARE, MODE>);
-  else if (e == FOURTH) run(distill_kernel<T, THREADS, KEEP, FOURTH, MODE>);
-  else run(distill_kernel<T, THREADS, KEEP, BOTH, MODE>);
+  if (e == ONE) run(distill_kernel<T, THREADS, KEEP, STORE, ONE, MODE>);
+  else if (e == SQUARE) run(distill_kernel<T, THREADS, KEEP, STORE, SQUARE, MODE>);
+  else if (e == FOURTH) run(distill_kernel<T, THREADS, KEEP, STORE, FOURTH, MODE>);
+  else run(distill_kernel<T, THREADS, KEEP, STORE, BOTH, MODE>);
 }
 template <Mode MODE, typename T>
 void pick(hipStream_t st, const ast_distill_cfg& c, const DistillArgs& g, Exps e) {
@@ -425,7 +440,9 @@ void pick(hipStream_t st, const ast_distill_cfg& c, const DistillArgs& g, Exps e
       go<JOIN_STEP, T, 512, 0>(st, r, g.slices, g, e);
     } else if (v <= 8192) go<MODE, T, 256, 4>(st, r, 1, g, e);
     else if (v <= 16384) go<MODE, T, 256, 8>(st, r, 1, g, e);
-    else go<MODE, T, 512, sizeof(T) == 2 ? 16 : 8>(st, r, 1, g, e);
+    else if constexpr (sizeof(T) == 4) go<MODE, T, 512, 8>(st, r, 1, g, e);
+    else if (v <= 16 * 512 * 8) go<MODE, T, 512, 16>(st, r, 1, g, e);
+    else go<MODE, T, 512, 16, true>(st, r, 1, g, e);  // (4096 bf16 rows of 131072 at a temperature of 2: 472 us, without shared memory 485)
   } else {
     if (v <= 8192) go<MODE, T, 256, 0>(st, r, 1, g, e);
     else go<MODE, T, 512, 0>(st, r, 1, g, e);
