@@ -145,7 +145,7 @@ ast_status asteroid_gelu_backward_stash8(const void* dy_dev, int32_t dtype, cons
  * residual_dev == NULL: s is x, sum_dtype == dtype, nothing is written to sum_dev (NULL).
  * stash_dev (NULL: none) receives y, as it is written, in 8 bits: the bytes of asteroid_stash8_pack(y_dev).  (s is the same with and
  * without it; y too, bit for bit, where width is a multiple of 8, otherwise the squares may be added up in another order.)
- * rows < 2^31, width in [1, 16384], eps > 0.  sum_dev may be residual_dev, y_dev may be x_dev, and where the types
+ * rows < 2^31, width in [1, 16384], eps >= 2^-126.  sum_dev may be residual_dev, y_dev may be x_dev, and where the types
  * are the same sum_dev may be x_dev and y_dev residual_dev. */
 typedef struct {
   int64_t rows;
@@ -226,7 +226,8 @@ ast_status asteroid_recurrence_backward(const ast_recurrence_cfg* cfg, const ast
  * counts with the sum of its p.  A row without a valid entry has no first term, a row whose label lies outside [0, vocab) no
  * second one.  labels_dev int32[rows], or NULL: l is 0.
  * logits: [rows][vocab] in rows of logits_stride >= vocab elements; ids_dev int32[rows][entries], teacher_dev
- * [rows][entries]; loss_dev fp32[rows].  rows < 2^31, vocab in [1, 2^30], entries in [1, 1024], T > 0, l in [0, 1].
+ * [rows][entries]; loss_dev fp32[rows].  rows < 2^31, vocab in [1, 2^30], entries in [1, 1024], T in [2^-30, 2^30],
+ * l in [0, 1].
  * stats_dev fp32[rows][3], for the backward pass: max z, sum exp((z - max) / T), sum exp(z - max) (0 without labels or with l == 0). */
 typedef struct {
   int64_t rows;

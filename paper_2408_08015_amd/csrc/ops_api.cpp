@@ -91,7 +91,7 @@ const char* norm_cfg(const ast_norm_cfg* c) {
   if (c->sum_dtype != c->dtype && c->sum_dtype != AST_F32) return "sum_dtype must be dtype or AST_F32";
   if (c->rows < 0 || c->rows > kMostRows) return "rows must lie in [0, 2^31)";
   if (c->width < 1 || c->width > 16384) return "width must lie in [1, 16384]";
-  if (!(c->eps > 0.f) || !std::isfinite(c->eps)) return "eps must be positive";
+  if (!(c->eps >= 0x1p-126f) || !std::isfinite(c->eps)) return "eps must be positive, and no subnormal number";
   return nullptr;
 }
 
@@ -138,7 +138,7 @@ const char* distill_cfg(const ast_distill_cfg* c) {
   if (c->vocab < 1 || c->vocab > (int64_t)1 << 30) return "vocab must lie in [1, 2^30]";
   if (c->logits_stride < c->vocab || c->logits_stride > (int64_t)1 << 31) return "logits_stride must lie in [vocab, 2^31]";
   if (c->entries < 1 || c->entries > 1024) return "entries must lie in [1, 1024]";
-  if (!(c->temperature > 0.f) || !std::isfinite(c->temperature)) return "temperature must be positive";
+  if (!(c->temperature >= 0x1p-30f && c->temperature <= 0x1p30f)) return "temperature must lie in [2^-30, 2^30]";  // (T^2 and log2(e) / T)
   if (!(c->label_weight >= 0.f && c->label_weight <= 1.f)) return "label_weight must lie in [0, 1]";
   if (!c->labels_dev && c->label_weight != 0.f) return "a label_weight needs labels";
   if (!aligned(c->labels_dev, 4)) return "labels_dev must be 4-byte aligned";

@@ -389,6 +389,8 @@ DISTILL = [  # rows, vocab, entries, temperature, label weight, room behind a ro
     (2, 131077, 9, 2.0, 0.5, 3), (2, 250001, 50, 1.0, 0.0, 7), (40, 16391, 33, 4.0, 0.4, 0),
     # (more rows than are cut into slices: kept in registers whole, or the first part of them)
     (80, 9001, 8, 1.0, 0.0, 0), (65, 20000, 30, 4.0, 0.5, 1), (70, 33000, 12, 1.5, 0.2, 0), (66, 131077, 40, 2.0, 0.5, 3),
+    # (bf16: a part of the rows in shared memory; a little more than fits there)
+    (66, 69633, 30, 4.0, 0.5, 0), (65, 98313, 16, 1.5, 0.2, 0),
 ]
 
 
@@ -642,6 +644,53 @@ def test_operators_on_another_stream_and_in_replayed_graphs(ops):
         torch.cuda.synchronize()
         for _, res in graphs:
             assert same(res, want), n
+
+
+def test_in_place_and_with_a_workspace_of_the_callers(ops):
+    """Outputs on every input that the interface allows, and a workspace that is larger than needed, full of other calls' words and
+    taken by several of them: the bits of outputs of their own."""
+    g = torch.Generator(device="cuda").manual_seed(13)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    ws = torch.full((1 << 22,), 0xAB, dtype=torch.uint8, device="cuda")
+    for rows, width in ((70, 1000), (41, 1501), (37, 5000)):
+        x, r, dsum, gain = rnd(rows, width), rnd(rows, width), rnd(rows, width), torch.rand(width, generator=g, device="cuda")
+        y, s, _ = ops.rms_norm_forward(x, gain, residual=r)
+        for into in ("x", "r"):
+            a, b = x.clone(), r.clone()
+            got = ops.rms_norm_forward(a, gain, residual=b, **(dict(out=b, sum_out=a) if into == "x" else dict(out=a, sum_out=b)))
+            assert torch.equal(got[0], y) and torch.equal(got[1], s)
+        want = ops.rms_norm_backward(x, s, gain, dsum=dsum)
+        for n in range(3):
+            three = [x.clone(), s.clone(), dsum.clone()]
+            got = ops.rms_norm_backward(three[0], three[1], gain, dsum=three[2], out=three[n], workspace=ws)
+            assert got[0] is three[n] and same(got, want)
+        s32, d32 = s.float(), dsum.float()
+        want = ops.rms_norm_backward(x, s32, gain, dsum=d32)
+        for n in range(2):
+            two = [s32.clone(), d32.clone()]
+            got = ops.rms_norm_backward(x, two[0], gain, dsum=two[1], sum_out=two[n], workspace=ws)
+            assert got[1] is two[n] and same(got, want)
+    for T, C, kw in ((1700, 130, dict(period=1700)), (300, 66, dict(period=100)), (129, 31, dict(period=1)),
+                     (900, 65, dict(offsets=torch.tensor([0, 5, 400, 400, 900], dtype=torch.int32, device="cuda")))):
+        n = 4 if "offsets" in kw else -(-T // kw["period"])
+        data, dy = [rnd(T, C) for _ in range(3)], rnd(T, C)
+        h0 = torch.randn(n, C, generator=g, device="cuda")
+        f, z, o = data
+        want = ops.recurrence_forward(f, z, o=o, state=h0, final=True, saved=True, **kw)
+        for k in range(3):
+            d = [t.clone() for t in data]
+            got = ops.recurrence_forward(d[0], d[1], o=d[2], state=h0, final=True, saved=True, out=d[k], workspace=ws, **kw)
+            assert got[0] is d[k] and same(got, want)
+        back = ops.recurrence_backward(dy, f, z, want[2], o=o, state=h0, dfinal=want[1], dstate=True, **kw)
+        for k in range(3):
+            d, e = [t.clone() for t in data], dy.clone()
+            out = d[:k] + [e] + d[k + 1:]        # one of the gradients in place of dy, the others of their inputs
+            assert same(ops.recurrence_backward(e, d[0], d[1], want[2], o=d[2], state=h0, dfinal=want[1], dstate=True, out=out, workspace=ws, **kw), back)
+    z, ids = 2 * rnd(5, 40000), torch.randint(0, 40000, (5, 9), generator=g, device="cuda", dtype=torch.int32)
+    t, w = torch.randn(5, 9, generator=g, device="cuda"), torch.rand(5, generator=g, device="cuda")
+    want = ops.distill_step(w, z, ids, t)
+    got = ops.distill_step(w, z, ids, t, out=z, workspace=ws)
+    assert got[1] is z and same(got, want)
 
 
 def test_two_recurrences_at_once(ops):

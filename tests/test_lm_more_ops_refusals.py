@@ -39,7 +39,7 @@ def norm(**kw):
 
 
 BAD_NORM = [None] + [norm(**k) for k in (dict(rows=-1), dict(rows=1 << 31), dict(width=0), dict(width=16385), dict(dtype=2), dict(sum_dtype=3),
-                                         dict(dtype=0, sum_dtype=1), dict(eps=0.0), dict(eps=NAN), dict(eps=INF), dict(eps=-1.0))]
+                                         dict(dtype=0, sum_dtype=1), dict(eps=0.0), dict(eps=1e-40), dict(eps=NAN), dict(eps=INF), dict(eps=-1.0))]
 
 
 def test_rms_norm_refusals(lib):
@@ -128,7 +128,7 @@ def dist(**kw):
 
 BAD_DIST = [None] + [dist(**k) for k in (dict(rows=-1), dict(rows=1 << 31), dict(vocab=0), dict(vocab=(1 << 30) + 1, logits_stride=1 << 31),
                                          dict(logits_stride=49), dict(logits_stride=(1 << 31) + 1), dict(dtype=2), dict(entries=0), dict(entries=1025),
-                                         dict(teacher_dtype=5), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=NAN),
+                                         dict(teacher_dtype=5), dict(temperature=0.0), dict(temperature=1e-30), dict(temperature=1e20), dict(temperature=-1.0), dict(temperature=NAN),
                                          dict(temperature=INF), dict(label_weight=-0.1), dict(label_weight=1.1), dict(label_weight=NAN),
                                          dict(labels_dev=None), dict(labels_dev=P + 1))]
 
