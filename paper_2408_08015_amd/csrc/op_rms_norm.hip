@@ -56,10 +56,18 @@ struct Part {  // eight values of a row from place c on (GROUPS: c may lie in fr
     e.load(p, c, cols);
   }
   __device__ __forceinline__ void values(float (&f)[8], int, int) const { e.values(f); }
+  __device__ __forceinline__ void pin() {
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) asm volatile("" : "+v"(e.e.v[i]));
+  }
 };
 template <typename T>
 struct Part<T, GROUPS> {
   uint32_t v[2 * sizeof(T)];
+  __device__ __forceinline__ void pin() {
+#pragma unroll
+    for (int i = 0; i < 2 * (int)sizeof(T); ++i) asm volatile("" : "+v"(v[i]));
+  }
   __device__ __forceinline__ void load(const void* base, int64_t row, int c, int cols, int64_t all) {
     const int64_t at = row * cols + c;  // (a multiple of eight; the tensor's last 16 bytes are read again where nothing follows them)
 #pragma unroll
@@ -92,10 +100,6 @@ __device__ __forceinline__ void store_part(void* base, int64_t row, int c, int c
 __device__ __forceinline__ void gains(const NormArgs& g, int c, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) v[e] = (unsigned)(c + e) < (unsigned)g.cols ? g.gain[c + e] : 0.f;
-}
-__device__ __forceinline__ void copy8(const float (&a)[8], float (&b)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) b[e] = a[e];
 }
 
 // Sums over the lanes of a row: inside a wavefront, or (THREADS > 0) over a block; two at once, valid in every lane.  sh: two
@@ -153,10 +157,9 @@ __global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_kernel(con
   __shared__ float sh[2][32];
   Rows<W, BLOCK> at(g);
   const int64_t all = g.rows * g.cols;
-  constexpr bool AHEAD = BLOCK < 1024;  // the next row is asked for before this one is worked on, and gains stay in registers
-  float kept[AHEAD ? IT : 1][8];
+  float gain[IT][8];
 #pragma unroll
-  for (int i = 0; i < (AHEAD ? IT : 0); ++i) gains(g, at.place(i), kept[i]);
+  for (int i = 0; i < IT; ++i) gains(g, at.place(i), gain[i]);
   struct Row {
     Part<T, W> x[IT];
     Part<S, W> r[IT];
@@ -172,12 +175,11 @@ __global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_kernel(con
     }
   };
   Row cur;
-  if (AHEAD) fetch(at.row, cur);
+  fetch(at.row, cur);
   int turn = 0;
   for (int64_t row = at.row; row < g.rows; row += at.step, turn ^= 1) {
-    Row next;
-    if (AHEAD) fetch(row + at.step, next);
-    else fetch(row, cur);
+    Row next;  // (asked for before this one is worked on)
+    fetch(row + at.step, next);
     float v[IT][8], ss = 0.f, none = 0.f;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
@@ -204,11 +206,8 @@ __global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_kernel(con
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const int c = at.place(i);
-      float gain[8];
-      if (AHEAD) copy8(kept[AHEAD ? i : 0], gain);
-      else gains(g, c, gain);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * rho * gain[e];
+      for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * rho * gain[i][e];
       if (c < g.cols) store_part<T, W>(g.y, row, c, g.cols, v[i]);
       if (W != GROUPS && g.q && c < g.pitch) {  // (a block of 32 values is four lanes' groups, all inside the pitch or none)
         if (W != EVEN) {
@@ -222,7 +221,7 @@ __global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_kernel(con
         if ((at.lane & 3) == 0) g.scales[row * (g.pitch / kStash8Block) + c / kStash8Block] = scale;
       }
     }
-    if (AHEAD) cur = next;
+    cur = next;
   }
 }
 
@@ -231,11 +230,13 @@ __global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_bwd_kernel
   __shared__ float sh[2][32];
   Rows<W, BLOCK> at(g);
   const int64_t all = g.rows * g.cols;
-  constexpr bool AHEAD = BLOCK < 1024;
-  float kept[AHEAD ? IT : 1][8], acc[IT][8];
+  // Four groups a lane: the next row is not asked for early, and values are formed from the loaded words again behind the sums, or
+  // the rows do not fit the registers.
+  constexpr bool AHEAD = IT < 4, AGAIN = IT == 4;
+  float gain[IT][8], acc[IT][8];
 #pragma unroll
   for (int i = 0; i < IT; ++i) {
-    if (AHEAD) gains(g, at.place(i), kept[AHEAD ? i : 0]);
+    gains(g, at.place(i), gain[i]);
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[i][e] = 0.f;
   }
@@ -272,13 +273,10 @@ __global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_bwd_kernel
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[i][e] = d[i][e] = 0.f;
       }
-      float gain[8];
-      if (AHEAD) copy8(kept[AHEAD ? i : 0], gain);
-      else gains(g, c, gain);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         ss += s[i][e] * s[i][e];
-        dot += d[i][e] * gain[e] * s[i][e];
+        dot += d[i][e] * gain[i][e] * s[i][e];
       }
     }
     row_sums<BLOCK>(ss, dot, true, g.ls, sh, turn);
@@ -288,14 +286,18 @@ __global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_bwd_kernel
     for (int i = 0; i < IT; ++i) {
       const int c = at.place(i);
       if (c >= g.cols) continue;
-      float r[8] = {}, gain[8];
-      if (AHEAD) copy8(kept[AHEAD ? i : 0], gain);
-      else gains(g, c, gain);
+      float r[8] = {};
+      if (AGAIN) {  // (pinned, or the compiler keeps the values of before)
+        cur.s[i].pin();
+        cur.d[i].pin();
+        cur.s[i].values(s[i], c, g.cols);
+        cur.d[i].values(d[i], c, g.cols);
+      }
       if (g.r) cur.r[i].values(r, c, g.cols);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         acc[i][e] += d[i][e] * (s[i][e] * rho);
-        s[i][e] = rho * (d[i][e] * gain[e] - s[i][e] * m) + r[e];
+        s[i][e] = rho * (d[i][e] * gain[i][e] - s[i][e] * m) + r[e];
       }
       if (g.y) store_part<T, W>(g.y, row, c, g.cols, s[i]);
       if (g.sum) store_part<S, W>(g.sum, row, c, g.cols, s[i]);
@@ -355,8 +357,9 @@ __global__ __launch_bounds__(1024) void rms_norm_gain_sum_kernel(const float* __
 
 struct Shape { int it, block, ls; };
 
-// Lanes of a row: one group of eight values a lane up to 512 values, two up to 1024; then a block's of 256, 512, 1024 threads, two
-// groups a lane.
+// Lanes of a row: one group of eight values a lane up to 512 values, two up to 1024; then a block's of 256, 512 threads, two groups a
+// lane, and four in 512 threads: their registers hold 2048 groups where those of 1024 threads spill (us of 2048 rows of 16384 in bf16
+// and of 4096 of 10001: forward 88, 85, backward 74, 84; with 1024 threads 96, 119, 152, 209).
 Shape shape_of(int cols, bool keep, Way way) {
   const int groups = (cols + (way == GROUPS ? 14 : 7)) / 8;
   Shape s = {1, 0, keep ? 2 : 0};  // (8 bits: four lanes a block of 32 values)
@@ -365,18 +368,19 @@ Shape shape_of(int cols, bool keep, Way way) {
     while ((s.it << s.ls) < groups) ++s.ls;
     return s;
   }
-  s.block = groups <= 512 ? 256 : groups <= 1024 ? 512 : 1024;
-  s.it = groups <= s.block ? 1 : 2;
+  s.block = groups <= 512 ? 256 : 512;
+  s.it = groups <= s.block ? 1 : groups <= 2 * s.block ? 2 : 4;
   return s;
 }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
-Way way_of(int cols, bool aligned, bool keep) {
+Way way_of(int cols, bool aligned, bool keep, bool wide) {  // wide: backward on an fp32 stream
   if (!aligned) return ANY;
   if (cols % 8 == 0) return EVEN;
-  // (8 bits lie in groups of a row's own; and where the one group more, that of a row which begins inside one, would take twice the
-  // threads, nothing is gained: 4096 bf16 rows of 8191 backward 184 us in 1024 threads, 104 shifted into place in 512)
-  const bool over = (cols + 14) / 8 > 1024 && cols <= 8192;
+  // (8 bits lie in groups of a row's own; and where the one group more, that of a row which begins inside one, takes four groups a lane
+  // instead of two, the backward pass on an fp32 stream loses: 4096 rows of 8191, bf16 on fp32: 153 us, 117 shifted into place; bf16:
+  // 71 and 103; forward 96 and 104, 73 and 97)
+  const bool over = wide && (cols + 14) / 8 > 1024 && cols <= 8192;
   return keep || over || cols > 16376 ? ANY : GROUPS;
 }
 
@@ -406,10 +410,10 @@ void pick(hipStream_t st, int64_t blocks, const Shape& s, const NormArgs& g) {
   } else if (s.block == 256) {
     if (s.it == 1) go<BWD, T, S, W, 1, 256>(st, blocks, g);
     else go<BWD, T, S, W, 2, 256>(st, blocks, g);
-  } else if (s.block == 512) {
+  } else if (s.it == 2) {
     go<BWD, T, S, W, 2, 512>(st, blocks, g);
   } else {
-    go<BWD, T, S, W, 2, 1024>(st, blocks, g);
+    go<BWD, T, S, W, 4, 512>(st, blocks, g);
   }
 }
 template <bool BWD>
@@ -441,7 +445,8 @@ void rms_norm_fwd(hipStream_t st, const ast_norm_cfg& c, const void* x, const vo
                   void* sum, void* stash) {
   if (c.rows <= 0) return;
   const int cols = (int)c.width;
-  const Way way = way_of(cols, aligned16(x) && aligned16(residual) && aligned16(y) && aligned16(sum), stash != nullptr);
+  const Way way = way_of(cols, aligned16(x) && aligned16(residual) && aligned16(y) && aligned16(sum), stash != nullptr,
+                         false);
   const Shape s = shape_of(cols, stash != nullptr, way);
   NormArgs g = args_of(c, s, gain);
   g.x = x;
@@ -465,7 +470,8 @@ size_t rms_norm_bwd_ws_bytes(int64_t rows, int64_t width) {  // (whatever the te
 void rms_norm_bwd(hipStream_t st, const ast_norm_cfg& c, const void* dy, const void* sum, const float* gain, const void* dsum,
                   void* dx, void* ds, float* dgain, bool accumulate, void* ws) {
   const int cols = (int)c.width;
-  const Way way = way_of(cols, aligned16(dy) && aligned16(sum) && aligned16(dsum) && aligned16(dx) && aligned16(ds), false);
+  const Way way = way_of(cols, aligned16(dy) && aligned16(sum) && aligned16(dsum) && aligned16(dx) && aligned16(ds), false,
+                         c.sum_dtype == AST_F32);
   const Shape s = shape_of(cols, false, way);
   const int64_t blocks = c.rows > 0 ? blocks_of(c.rows, s, way, true) : 0;
   NormArgs g = args_of(c, s, gain);

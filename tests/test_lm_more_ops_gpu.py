@@ -166,6 +166,29 @@ def test_rms_norm_of_no_rows_and_unaligned_rows(ops):
         assert same(ops.rms_norm_backward(a, a, gain, dsum=a)[:2], ops.rms_norm_backward(a.clone(), a.clone(), gain, dsum=a.clone())[:2])
 
 
+@pytest.mark.parametrize("dt,st", TYPES)
+@pytest.mark.parametrize("rows,width,off", [(530, 8191, 0), (600, 9001, 0), (2100, 8200, 0), (300, 16384, 1), (290, 9001, 3), (270, 16383, 0)])
+def test_rms_norm_of_long_rows(ops, rows, width, off, dt, st):
+    """Several rows a block, in every way that rows are read."""
+    _, x, res, gain, g = norm_data(rows, width, dt, st, 3)
+    if off:
+        x, res = (torch.cat([t.new_zeros(off), t.view(-1)])[off:].view(rows, width) for t in (x, res))
+    eps = float(np.float32(1e-5))
+    y, s, _ = ops.rms_norm_forward(x, gain, residual=res, eps=1e-5)
+    total = host(x) + host(res)
+    inside(s, total, abs(total) * (HALF[st] + u) * 1.001)
+    want = O.rms_norm_forward(host(s), g, eps)
+    inside(y, want, abs(want) * ((width / 2 + 8) * u * 1.01 + HALF[dt]) + TINY)
+    dx, ds, dg = ops.rms_norm_backward(x, res, gain, dsum=s, eps=1e-5)
+    m = host(s)
+    want, wg, wa, wga = O.rms_norm_backward(host(x), host(res), g, m, eps)
+    near = (wa * (2 * width + 24) * u + abs(m) * u) * 1.01 + TINY
+    inside(dx, want, near + (abs(want) + near) * HALF[dt])
+    inside(ds, want, near + (abs(want) + near) * HALF[st])
+    inside(dg, wg, wga * (rows + width / 2 + 16) * u * 1.01 + TINY)
+    assert same(ops.rms_norm_backward(x, res, gain, dsum=s, eps=1e-5), (dx, ds, dg))
+
+
 # ------------------------------------------------------------------------------------------------ gated recurrence
 
 def period(T, n):
