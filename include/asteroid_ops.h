@@ -145,8 +145,8 @@ ast_status asteroid_gelu_backward_stash8(const void* dy_dev, int32_t dtype, cons
  * residual_dev == NULL: s is x, sum_dtype == dtype, nothing is written to sum_dev (NULL).
  * stash_dev (NULL: none) receives y, as it is written, in 8 bits: the bytes of asteroid_stash8_pack(y_dev).  (s is the same with and
  * without it; y too, bit for bit, where width is a multiple of 8, otherwise the squares may be added up in another order.)
- * rows < 2^31, width in [1, 16384], eps >= 2^-126.  sum_dev may be residual_dev, y_dev may be x_dev, and where the types
- * are the same sum_dev may be x_dev and y_dev residual_dev. */
+ * rows < 2^31, width in [1, 16384], eps >= 2^-126; squares are added up in fp32 (a row whose sum that does not hold: y is 0).
+ * sum_dev may be residual_dev, y_dev may be x_dev, and where the types are the same sum_dev may be x_dev and y_dev residual_dev. */
 typedef struct {
   int64_t rows;
   int64_t width;

@@ -350,7 +350,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
     for (int i = 0; i < 8; ++i) v[i] = slope(v[i]);
     store8(dg + at * 8, v);
   };
-  if (ca == 0.f && cb == 0.f) {  // (a token that does not count: zeros, whatever its logits are)
+  if (rate == 0.f && mix == 0.f) {  // (a token that does not count: zeros, whatever its logits are)
     const float zero[8] = {};
     for (int at = tid; at < sp.groups; at += THREADS) store8(dg + at * 8, zero);
     if (odd >= 0) store1(dz + odd, 0.f);

@@ -209,11 +209,8 @@ __global__ __launch_bounds__((Rows<W, BLOCK>::THREADS)) void rms_norm_kernel(con
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[i][e] = v[i][e] * rho * gain[i][e];
       if (c < g.cols) store_part<T, W>(g.y, row, c, g.cols, v[i]);
-      if (W != GROUPS && g.q && c < g.pitch) {  // (a block of 32 values is four lanes' groups, all inside the pitch or none)
-        if (W != EVEN) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[i][e] = c + e < g.cols ? v[i][e] : 0.f;  // (0 times an infinite rho is no zero)
-        }
+      if (W != GROUPS && g.q && c < g.pitch) {  // (a block of 32 values is four lanes' groups, all inside the pitch or none; values behind
+                                                // the row are 0 times a finite rho, or their block has a NaN anyway)
         round_to(v[i], static_cast<const T*>(nullptr));
         uint2 w;
         const uint8_t scale = stash8_block(v[i], w);

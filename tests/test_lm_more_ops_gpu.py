@@ -540,6 +540,15 @@ def test_distill_of_logits_at_the_ends_of_the_range(ops, dt):
         assert np.isnan(host(loss)[[4, 5, 6, 7]]).all()
 
 
+def test_distill_of_a_gradient_that_only_the_entries_have(ops):
+    """Softmax values times dloss that round to 0: the entries' places still get dloss (q - p), here -dloss."""
+    z = torch.zeros(1, 64, device="cuda")
+    ids, t = torch.tensor([[5]], dtype=torch.int32, device="cuda"), torch.zeros(1, 1, device="cuda")
+    w = torch.full((1,), 2e-37, device="cuda")
+    dz = ops.distill_backward(w, z, ids, t, torch.tensor([[0.0, 2.0 ** 30, 0.0]], device="cuda"))   # (the sum of 2^30 equal logits)
+    assert dz[0, 5] == -w[0] and dz.abs().sum() == w[0]
+
+
 def test_distill_of_no_rows(ops):
     e = torch.zeros(0, 40, device="cuda")
     ids, t, w = torch.zeros(0, 3, dtype=torch.int32, device="cuda"), torch.zeros(0, 3, device="cuda"), torch.zeros(0, device="cuda")
