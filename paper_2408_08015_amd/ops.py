@@ -86,6 +86,7 @@ def _lib():
 
 # the handle of a device's current stream (without a Stream object around it, where torch offers that)
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+_current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _device(t, *others):
@@ -101,7 +102,7 @@ def _device(t, *others):
 
 def _call(d, fn, *args):
     """fn(*args, stream) with device d current (the calls launch on the current one) and its current stream."""
-    if torch.cuda.current_device() == d:
+    if _current() == d:
         st = fn(*args, _stream(d))
     else:
         with torch.cuda.device(d):
@@ -384,12 +385,14 @@ def rms_norm_forward(x, gain, residual=None, eps=1e-6, keep8=False, out=None, su
         _is(residual, "residual", (x.dtype, torch.float32), x.shape)
         if sum_out is None:
             sum_out = torch.empty_like(residual)
-        _is(sum_out, "sum_out", (residual.dtype,), x.shape)
+        else:
+            _is(sum_out, "sum_out", (residual.dtype,), x.shape)
     elif sum_out is not None:
         raise ValueError("without a residual there is no sum to write")
     if out is None:
         out = torch.empty_like(x)
-    _is(out, "out", (x.dtype,), x.shape)
+    else:
+        _is(out, "out", (x.dtype,), x.shape)
     kept = None
     if keep8 or kept_out is not None:
         kept = Stash8(x.shape[0], x.shape[1], x.device) if kept_out is None else _stash(kept_out)
@@ -427,19 +430,24 @@ def rms_norm_backward(dy, s, gain, dsum=None, eps=1e-6, out=None, sum_out=None, 
     one = s.dtype == dy.dtype
     if one and out is not None and sum_out is not None and out is not sum_out:
         raise ValueError("out and sum_out are one tensor where the types are the same")
+    if one and out is None:
+        out = sum_out
     if out is None:
-        out = sum_out if one and sum_out is not None else torch.empty_like(dy)
-    _is(out, "out", (dy.dtype,), dy.shape)
+        out = torch.empty_like(dy)
+    else:
+        _is(out, "out", (dy.dtype,), dy.shape)
     if one:
         sum_out = out
     elif sum_out is None:
         sum_out = torch.empty_like(s)
-    _is(sum_out, "sum_out", (s.dtype,), dy.shape)
+    else:
+        _is(sum_out, "sum_out", (s.dtype,), dy.shape)
     if gain_out is None:
         if accumulate:
             raise ValueError("accumulate needs the tensor to add to")
         gain_out = torch.empty_like(gain)
-    _is(gain_out, "gain_out", _F32, gain.shape)
+    else:
+        _is(gain_out, "gain_out", _F32, gain.shape)
     cfg = ast_norm_cfg(dy.shape[0], dy.shape[1], _DT[dy.dtype], _DT[s.dtype], eps)
     lib = _lib()
     d = _device(dy, s, gain, dsum, out, sum_out, gain_out)
@@ -479,10 +487,17 @@ def _recurrence_inputs(f, z, o, offsets, period):
     return ast_recurrence_cfg(T, D, _DT[dtype], None, 0, period), -(-T // period), rows
 
 
-def _states(t, name, n, f):
-    """None, a tensor [sequences, channels], or (True) one that is made here."""
+def _state(t, name, n, f):
+    """None or a tensor [sequences, channels] to read from."""
+    return None if t is None else _is(t, name, _F32, (n, f.shape[1]))
+
+
+def _states(t, name, n, f, like=None):
+    """None, a tensor [sequences, channels], or (True) one that is made here (as `like`, which has been checked, where there is one)."""
     if t is None or t is False:
         return None
+    if t is True and like is not None:
+        return torch.empty_like(like)
     shape = (n, f.shape[1])
     return torch.empty(shape, dtype=torch.float32, device=f.device) if t is True else _is(t, name, _F32, shape)
 
@@ -514,11 +529,11 @@ def recurrence_forward(f, z, o=None, offsets=None, period=0, state=None, final=N
     final: True or a tensor (state itself allowed) to receive the states behind them.  saved: True or a float32 tensor
     [tokens / 64 rounded up, channels] for recurrence_backward.  y is dense; rows of no sequence are not written."""
     cfg, n, a = _recurrence_inputs(f, z, o, offsets, period)
-    state = _states(state, "state", n, f)
-    final = _states(final, "final", n, f)
+    state = _state(state, "state", n, f)
+    final = _states(final, "final", n, f, state)
     saved = _states(saved, "saved", -(-f.shape[0] // RECURRENCE_CHUNK), f)
     if out is None:
-        out = torch.empty(f.shape, dtype=f.dtype, device=f.device)
+        out = torch.empty_like(f, memory_format=torch.contiguous_format)
     else:
         _is(out, "out", (f.dtype,), f.shape)
     lib = _lib()
@@ -535,17 +550,21 @@ def recurrence_backward(dy, f, z, saved, o=None, offsets=None, period=0, state=N
     out: (df, dz, do), rows with any stride; (f, z, o) themselves allowed.  do is None where o is."""
     cfg, n, a = _recurrence_inputs(f, z, o, offsets, period)
     _is(saved, "saved", _F32, (-(-f.shape[0] // RECURRENCE_CHUNK), f.shape[1]))
-    state = _states(state, "state", n, f)
-    dfinal = _states(dfinal, "dfinal", n, f)
-    dstate = _states(dstate, "dstate", n, f)
+    state = _state(state, "state", n, f)
+    dfinal = _state(dfinal, "dfinal", n, f)
+    dstate = _states(dstate, "dstate", n, f, state)
     shape, dtype = f.shape, f.dtype
+    b = [_tokens(dy, "dy", shape, dtype)]
     if out is None:
         out = torch.empty((2 if o is None else 3,) + tuple(shape), dtype=dtype, device=f.device).unbind(0)
+        b += [ast_rows(g.data_ptr(), shape[1]) for g in out]
     df, dz, do = (tuple(out) + (None,))[:3]
     if (do is None) != (o is None):
         raise ValueError("out holds the gradient of o where o is given, and only there")
-    b = [_tokens(dy, "dy", shape, dtype), _tokens(df, "df", shape, dtype), _tokens(dz, "dz", shape, dtype),
-         None if do is None else _tokens(do, "do", shape, dtype)]
+    if len(b) == 1:
+        b += [_tokens(g, name, shape, dtype) for g, name in ((df, "df"), (dz, "dz"), (do, "do")) if g is not None]
+    if do is None:
+        b.append(None)
     lib = _lib()
     d = _device(f, z, o, dy, saved, offsets, state, dfinal, dstate, df, dz, do)
     ws, size = _workspace_of(lib.asteroid_recurrence_workspace, cfg, workspace, f.device)
@@ -581,9 +600,9 @@ def _gradient_of(logits, out, dloss):
     if out is None:
         T, V = logits.shape
         step = logits.stride(0) if T > 1 and 0 < logits.stride(0) - V < 64 else V   # rows padded a little stay so
-        out = torch.empty((T, step), dtype=logits.dtype, device=logits.device)
-        if step != V:
-            out = out[:, :V]
+        if step == V:
+            return torch.empty_like(logits, memory_format=torch.contiguous_format), V
+        out = torch.empty((T, step), dtype=logits.dtype, device=logits.device)[:, :V]
     if not isinstance(out, torch.Tensor) or out.shape != logits.shape or out.dtype != logits.dtype:
         raise ValueError("out must be a %s tensor %s" % (logits.dtype, tuple(logits.shape)))
     return out, _vocab_rows(out, "out")
@@ -598,10 +617,12 @@ def distill_forward(logits, ids, teacher, temperature=1.0, labels=None, label_we
     T = logits.shape[0]
     if out is None:
         out = torch.empty((T,), dtype=torch.float32, device=logits.device)
+    else:
+        _is(out, "out", _F32, (T,))
     if stats_out is None:
         stats_out = torch.empty((T, 3), dtype=torch.float32, device=logits.device)
-    _is(out, "out", _F32, (T,))
-    _is(stats_out, "stats_out", _F32, (T, 3))
+    else:
+        _is(stats_out, "stats_out", _F32, (T, 3))
     lib = _lib()
     _call(_device(logits, ids, teacher, labels, out, stats_out), lib.asteroid_distill_forward, cfg, logits.data_ptr(), ids.data_ptr(),
           teacher.data_ptr(), out.data_ptr(), stats_out.data_ptr())
@@ -633,8 +654,9 @@ def distill_step(dloss, logits, ids, teacher, temperature=1.0, labels=None, labe
     cfg = _distill_cfg(logits, ids, teacher, temperature, labels, label_weight)
     out, stride = _gradient_of(logits, out, dloss)
     if loss_out is None:
-        loss_out = torch.empty((logits.shape[0],), dtype=torch.float32, device=logits.device)
-    _is(loss_out, "loss_out", _F32, (logits.shape[0],))
+        loss_out = torch.empty_like(dloss)
+    else:
+        _is(loss_out, "loss_out", _F32, (logits.shape[0],))
     lib = _lib()
     d = _device(logits, ids, teacher, labels, dloss, loss_out, out)
     ws, size = _workspace_of(lib.asteroid_distill_step_workspace, cfg, workspace, logits.device)

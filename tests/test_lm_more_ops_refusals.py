@@ -205,3 +205,13 @@ def test_tensors_are_checked():
         ops.distill_step(f(4), z, ids, t, out=f(4, 50, dtype=h))
     with pytest.raises(ValueError, match="stats"):
         ops.distill_backward(f(4), z, ids, t, f(4, 2))
+
+
+def test_states_that_are_read_are_tensors():
+    """True asks for a tensor to be made; that is for results only."""
+    a, s = torch.zeros(5, 8), torch.zeros(1, 8)
+    with pytest.raises(ValueError, match="state must be a tensor"):
+        ops.recurrence_forward(a, a, period=5, state=True)
+    for kw in (dict(state=True), dict(dfinal=True)):
+        with pytest.raises(ValueError, match="must be a tensor"):
+            ops.recurrence_backward(a, a, a, s, period=5, **kw)
