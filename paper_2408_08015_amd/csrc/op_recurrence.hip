@@ -47,7 +47,9 @@ struct RecArgs {
   const float *state, *dfinal;  // [sequences][channels] or nullptr
   float *final, *dstate;
   float* saved;                 // state in front of every AST_RECURRENCE_CHUNK-th token
-  const int32_t* seq;           // a token's sequence, -1: none; nullptr: t / period
+  const int32_t* seq;           // a token's sequence, -1: none; nullptr: by offsets or t / period
+  const int32_t* offsets;       // of a call of one chunk and fewer than 64 sequences, which prepares nothing; or nullptr
+  int sequences;                // (where offsets is given)
   int64_t tokens, period;
   unsigned long long *maps, *heads;  // the chain: [chunk][channels], [group][channels]; nullptr: chunks on their own
   unsigned* counters;           // [columns], COUNTER apart
@@ -188,17 +190,25 @@ __device__ __forceinline__ unsigned long long look(unsigned long long* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 // What a wavefront's tokens are (the same in all its lanes): bit i stands for token i.
-template <int TOK>
+template <int TOK, bool FEW>  // FEW: g.offsets may be given
 struct Tokens {
   unsigned live, start, last;  // belongs to a sequence; is its first; its last
   int32_t at;                  // lane i: the sequence of token i (0: with the token in front) or, by period, of token 0
   bool listed;
-  __device__ __forceinline__ Tokens(const RecArgs& g, int64_t t0, int lane) : live(0), start(0), last(0), at(0), listed(g.seq != nullptr) {
+  __device__ __forceinline__ Tokens(const RecArgs& g, int64_t t0, int lane)
+      : live(0), start(0), last(0), at(0), listed(g.seq != nullptr || (FEW && g.offsets != nullptr)) {
     if (t0 >= g.tokens) return;
     const int n = (int)min((int64_t)TOK, g.tokens - t0);
     if (listed) {
       const int64_t t = t0 - 1 + lane;  // (lanes 0 .. TOK + 1 count)
-      at = t >= 0 && t < g.tokens && lane <= TOK + 1 ? g.seq[t] : -1;
+      if (FEW && g.offsets) {  // (lane i holds offsets[i]; counted: the sequences that begin at the token or in front of it)
+        const int32_t o = g.offsets[min(lane, g.sequences)];
+        for (int s = 0; s < g.sequences; ++s) at += __builtin_amdgcn_readlane(o, s) <= t ? 1 : 0;
+        const bool in = t >= __builtin_amdgcn_readlane(o, 0) && t < __builtin_amdgcn_readlane(o, g.sequences);
+        at = in && t < g.tokens && lane <= TOK + 1 ? at - 1 : -1;
+      } else {
+        at = t >= 0 && t < g.tokens && lane <= TOK + 1 ? g.seq[t] : -1;
+      }
       const int32_t next = __builtin_amdgcn_update_dpp(-1, at, DPP_WAVE_SHL1, 0xF, 0xF, false);
       const bool differ = at != next;
       const unsigned long long all = (1ull << n) - 1, change = __ballot(differ);  // bit i: tokens i - 1 and i differ
@@ -219,6 +229,18 @@ struct Tokens {
     return (int64_t)__builtin_amdgcn_readlane(at, listed ? i + 1 : 0) + (listed ? 0 : __popc(start & ((2u << i) - 2)));
   }
 };
+
+// What comes out of sequences without tokens (copied, or 0 where nothing is passed in), by the wavefront of the call's one block
+// of these channels.
+template <int V>
+__device__ __forceinline__ void pass_on(const RecArgs& g, const float* in, float* out, int c) {
+  for (int s = 0; s < g.sequences; ++s) {
+    if (g.offsets[s] != g.offsets[s + 1]) continue;
+    float x[V] = {};
+    if (in) load_state(in, s, c, g.channels, x);
+    store_state(out, s, c, g.channels, x);
+  }
+}
 
 // The chain.  Lane i takes the block's channels i, i + 64 here (words side by side), whichever it computes with.
 // A block leaves its map: that of its wavefronts' maps in the order of the scan (`back`: from the last).
@@ -341,7 +363,8 @@ __global__ __launch_bounds__(64 * FWD_WAVES, 4) void recurrence_kernel(const Rec
       if (GATE) ro[GATE ? i : 0] = at.load(o.next());
     }
   }
-  const Tokens<TOK> tk(g, t0, lane);
+  const Tokens<TOK, V == 1> tk(g, t0, lane);
+  if (V == 1 && g.offsets && g.final && wave == FWD_WAVES - 1) pass_on<V>(g, g.state, g.final, c);
   // the gates, and the wavefront's map
   float s[TOK][V], A[V], U[V];
 #pragma unroll
@@ -464,7 +487,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void recurrence_bwd_kernel(const Rec
   }
   float h[V];  // the state in front of the block
   load_state(g.saved, (int64_t)chunk * (WAVES / BWD_WAVES), c, g.channels, h);
-  const Tokens<TOK> tk(g, t0, lane);
+  const Tokens<TOK, V == 1> tk(g, t0, lane);
+  if (V == 1 && g.offsets && g.dstate && wave == WAVES - 1) pass_on<V>(g, g.dfinal, g.dstate, c);
 
   // the gates, and the gradients at the tokens
   float a[TOK][V], b[TOK][V], d[TOK][V], q[GATE ? TOK : 1][V], A[V], U[V], K[V];
@@ -721,8 +745,15 @@ void prepare(hipStream_t st, const ast_recurrence_cfg& c, const Layout& l, void*
     g.heads = reinterpret_cast<unsigned long long*>(w + l.heads);
     g.counters = reinterpret_cast<unsigned*>(w + l.counters);
   }
-  if (c.offsets_dev) g.seq = reinterpret_cast<int32_t*>(w + l.seq);
   if (!l.chained && !c.offsets_dev) return;
+  // Nothing to prepare: the wavefronts of a block look their tokens' sequences up among fewer than 64 (64 x 512 bf16 in five: 10.5 us
+  // forward, 12 backward, after a launch that prepares 14.2 and 14.8).
+  if (l.chunks == 1 && !l.pairs && c.sequences < 64) {
+    g.offsets = c.offsets_dev;
+    g.sequences = (int)c.sequences;
+    return;
+  }
+  if (c.offsets_dev) g.seq = reinterpret_cast<int32_t*>(w + l.seq);
   const int64_t most = std::max<int64_t>({l.words / 4, c.offsets_dev ? c.tokens : 0, c.offsets_dev && out ? 64 * c.sequences : 0, 1});
   KLAUNCH(recurrence_prepare_kernel, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 2048)), dim3(256), 0, st, g.maps, l.words,
           g.counters, l.columns, c.offsets_dev, c.sequences, c.tokens, reinterpret_cast<int32_t*>(w + l.seq), in, out, (int)c.channels);
