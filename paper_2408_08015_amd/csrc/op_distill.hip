@@ -221,9 +221,9 @@ enum Mode : int {
   PART = 3,
   JOIN_STEP = 4       // STEP from the sums of the slices
 };
-// KEEP: with STEP a thread keeps the first KEEP groups that it reads in registers, and the next four in shared memory (STORE); what a
-// row has more is read again (from the caches, where it stayed there).
-template <typename T, int THREADS, int KEEP, bool STORE, Exps E, Mode MODE>
+// KEEP: with STEP a thread keeps the first KEEP groups that it reads in registers, and the next STORE in shared memory; what a row has
+// more is read again (from the caches, where it stayed there).
+template <typename T, int THREADS, int KEEP, int STORE, Exps E, Mode MODE>
 __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g) {
   constexpr bool SUMS = MODE == LOSS || MODE == STEP || MODE == PART, JOIN = MODE == JOIN_STEP;
   constexpr bool GRAD = MODE == GRADIENT || MODE == STEP || MODE == JOIN_STEP;
@@ -248,8 +248,8 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
   int label = g.labels && g.mix != 0.f ? g.labels[row] : -1;
   if (label < 0 || label >= g.vocab) label = -1;
   const float w = GRAD ? g.dloss[row] : 1.f;
-  static_assert(!STORE || sizeof(T) == 2, "a group is 16 bytes");
-  __shared__ uint4 stored[STORE ? U : 1][STORE ? THREADS : 1];  // (a thread reads what it wrote)
+  constexpr int W = sizeof(T) / 2;  // 16 bytes each of a group
+  __shared__ uint4 stored[STORE ? STORE * W : 1][STORE ? THREADS : 1];  // (a thread reads what it wrote)
   Eight<T, true> kept[K];
 #pragma unroll
   for (int u = 0; u < KEEP; ++u)
@@ -297,9 +297,14 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
       const bool all = at - tid + U * THREADS <= sp.groups;
 #pragma unroll
       for (int u = 0; u < U; ++u) load_group(r[u], zg, at + u * THREADS, sp.groups, all);
-      if (STORE && at == tid + KEEP * THREADS) {
+      if (STORE) {
+        const int n = (at - tid) / THREADS - KEEP;  // (the same in all threads)
 #pragma unroll
-        for (int u = 0; u < U; ++u) stored[u][tid] = *reinterpret_cast<const uint4*>(r[u].v);
+        for (int u = 0; u < U; ++u)
+          if (n + u < STORE) {
+#pragma unroll
+            for (int w = 0; w < W; ++w) stored[(n + u) * W + w][tid] = reinterpret_cast<const uint4*>(r[u].v)[w];
+          }
       }
       add_groups<T, E>(s, r, g.scale);
     }
@@ -361,14 +366,15 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
     if (tid + u * THREADS < sp.groups) write(kept[u], tid + u * THREADS);
   if (STORE) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < STORE; ++u)
       if (tid + (KEEP + u) * THREADS < sp.groups) {
         Eight<T, true> r;
-        *reinterpret_cast<uint4*>(r.v) = stored[u][tid];
+#pragma unroll
+        for (int w = 0; w < W; ++w) reinterpret_cast<uint4*>(r.v)[w] = stored[u * W + w][tid];
         write(r, tid + (KEEP + u) * THREADS);
       }
   }
-  for (int at = tid + (KEEP + (STORE ? U : 0)) * THREADS; at < sp.groups; at += U * THREADS) {
+  for (int at = tid + (KEEP + STORE) * THREADS; at < sp.groups; at += U * THREADS) {
     Eight<T, true> r[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -416,7 +422,7 @@ int slices_of(int64_t rows, int64_t vocab) {
 }
 
 constexpr int64_t kRowsAtOnce = 1 << 22;  // (a launch has fewer than 2^32 threads)
-template <Mode MODE, typename T, int THREADS, int KEEP, bool STORE = false>
+template <Mode MODE, typename T, int THREADS, int KEEP, int STORE = 0>
 void go(hipStream_t st, int64_t rows, int slices, DistillArgs g, Exps e) {
   const char* const name = MODE == GRADIENT ? "distill_bwd_kernel" : MODE == STEP || MODE == JOIN_STEP ? "distill_step_kernel" : "distill_kernel";
   auto run = [&](auto kernel) {
@@ -440,9 +446,12 @@ void pick(hipStream_t st, const ast_distill_cfg& c, const DistillArgs& g, Exps e
       go<JOIN_STEP, T, 512, 0>(st, r, g.slices, g, e);
     } else if (v <= 8192) go<MODE, T, 256, 4>(st, r, 1, g, e);
     else if (v <= 16384) go<MODE, T, 256, 8>(st, r, 1, g, e);
-    else if constexpr (sizeof(T) == 4) go<MODE, T, 512, 8>(st, r, 1, g, e);
-    else if (v <= 16 * 512 * 8) go<MODE, T, 512, 16>(st, r, 1, g, e);
-    else go<MODE, T, 512, 16, true>(st, r, 1, g, e);  // (4096 bf16 rows of 131072 at a temperature of 2: 472 us, without shared memory 485)
+    // (what a row has more than 512 threads keep beside their work is read again; with shared memory for a part of it two blocks share
+    // a unit as without.  us of 4096 rows, 131072 bf16 at temperatures of 2 and 1: 16 groups a thread 485, 481, and 4 in shared memory 472,
+    // 467, 20 and 6 462, 452, 22 and 6 466, 446, but 100021 392 for 374; spilled from there on.  fp32, 40000 and 65536: 8 286, 467, 10 and 3
+    // 268, 459)
+    else if (v <= (sizeof(T) == 4 ? 8 : 16) * 512 * 8) go<MODE, T, 512, sizeof(T) == 4 ? 8 : 16>(st, r, 1, g, e);
+    else go<MODE, T, 512, sizeof(T) == 4 ? 10 : 20, sizeof(T) == 4 ? 3 : 6>(st, r, 1, g, e);
   } else {
     if (v <= 8192) go<MODE, T, 256, 0>(st, r, 1, g, e);
     else go<MODE, T, 512, 0>(st, r, 1, g, e);

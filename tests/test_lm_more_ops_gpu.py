@@ -414,8 +414,9 @@ DISTILL = [  # rows, vocab, entries, temperature, label weight, room behind a ro
     (2, 131077, 9, 2.0, 0.5, 3), (2, 250001, 50, 1.0, 0.0, 7), (40, 16391, 33, 4.0, 0.4, 0),
     # (more rows than are cut into slices: kept in registers whole, or the first part of them)
     (80, 9001, 8, 1.0, 0.0, 0), (65, 20000, 30, 4.0, 0.5, 1), (70, 33000, 12, 1.5, 0.2, 0), (66, 131077, 40, 2.0, 0.5, 3),
-    # (bf16: a part of the rows in shared memory; a little more than fits there)
-    (66, 69633, 30, 4.0, 0.5, 0), (65, 98313, 16, 1.5, 0.2, 0),
+    # (a part of the rows in shared memory, less and a little more than fits there; fp32, then bf16)
+    (65, 36001, 11, 2.0, 0.5, 0), (65, 45007, 30, 1.5, 0.2, 0), (65, 53256, 16, 1.0, 0.0, 0),
+    (66, 69633, 30, 4.0, 0.5, 0), (65, 98313, 16, 1.5, 0.2, 0), (65, 106505, 9, 2.0, 0.3, 2),
 ]
 
 
