@@ -352,14 +352,14 @@ __global__ __launch_bounds__(1024) void rms_norm_gain_sum_kernel(const float* __
   if (y == 0 && c < cols) out[c] = (accumulate ? out[c] : 0.f) + (float)sh[0][x];
 }
 
-struct Shape { int it, block, ls; };
+struct Shape { int it, block, ls, groups; };
 
 // Lanes of a row: one group of eight values a lane up to 512 values, two up to 1024; then a block's of 256, 512 threads, two groups a
 // lane, and four in 512 threads: their registers hold 2048 groups where those of 1024 threads spill (us of 2048 rows of 16384 in bf16
 // and of 4096 of 10001: forward 88, 85, backward 74, 84; with 1024 threads 96, 119, 152, 209).
 Shape shape_of(int cols, bool keep, Way way) {
   const int groups = (cols + (way == GROUPS ? 14 : 7)) / 8;
-  Shape s = {1, 0, keep ? 2 : 0};  // (8 bits: four lanes a block of 32 values)
+  Shape s = {1, 0, keep ? 2 : 0, groups};  // (8 bits: four lanes a block of 32 values)
   if (groups <= 128) {
     if (groups > 64) s.it = 2;
     while ((s.it << s.ls) < groups) ++s.ls;
@@ -383,11 +383,15 @@ Way way_of(int cols, bool aligned, bool keep, bool wide) {  // wide: backward on
 
 // Blocks of a call: as many as rows need, at most 2048 forward.  Backward every block leaves partial sums; us of 12288 rows of 1504,
 // bf16 on an fp32 stream, of 32768 of 1024, and of 4096 of 8192 in bf16: 1024 blocks 63.6, 61.0, 84.5; 512 57.9, 56.2, 68.2;
-// 256 74.1, 65.7, 60.7.  Rows that are shifted into place keep more of them busy (12289 of 1501 so: 68.7, 74.4, 127).
+// 256 74.1, 65.7, 60.7.  On a bf16 stream 512 leave too little under way where a row leaves lanes without a group: so many more (32 M values
+// in rows of 24, 40, 200, 1025, 1201, 1600: 53, 57, 54, 63, 65, 54 us, with 512 63, 71, 64, 93, 82, 64; not where rows are full, 2048 57
+// for 55.5 with 768, nor for two groups a lane, 700 74 for 68).  Rows that are shifted into place keep more of them busy (12289 of 1501 so: 68.7, 74.4, 127).
 constexpr int kMostPartials = 1024;
-int64_t blocks_of(int64_t rows, const Shape& s, Way way, bool bwd) {
+int64_t blocks_of(int64_t rows, const Shape& s, Way way, bool bwd, bool wide) {
   const int64_t at_once = s.block ? 1 : (way == GROUPS ? 512 : 256) >> s.ls;
-  const int64_t most = !bwd ? 2048 : way == ANY && s.block < 512 ? kMostPartials : s.block < 512 ? 512 : 256;
+  int64_t most = !bwd ? 2048 : way == ANY && s.block < 512 ? kMostPartials : s.block < 512 ? 512 : 256;
+  if (bwd && !wide && s.it == 1 && (way == EVEN || (way == GROUPS && s.block)))
+    most = (512 * (s.block ? s.block : 1 << s.ls) / s.groups + 128) / 256 * 256;
   int64_t n = std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, most));
   if (bwd && s.block) n = std::min(n, std::max<int64_t>(256, rows / 4));  // (1024 bf16 rows of 4096: 512 blocks 20.1 us, 256 16.7)
   return s.block && way == GROUPS ? (n + 7) / 8 * 8 : n;  // (a block's rows begin at one place of a group)
@@ -455,12 +459,12 @@ void rms_norm_fwd(hipStream_t st, const ast_norm_cfg& c, const void* x, const vo
     g.q = static_cast<uint8_t*>(stash);
     g.scales = g.q + c.rows * g.pitch;
   }
-  launch<false>(st, c, way, s, blocks_of(c.rows, s, way, false), g);
+  launch<false>(st, c, way, s, blocks_of(c.rows, s, way, false, false), g);
 }
 
-size_t rms_norm_bwd_ws_bytes(int64_t rows, int64_t width) {  // (whatever the tensors' addresses)
+size_t rms_norm_bwd_ws_bytes(int64_t rows, int64_t width) {  // (whatever the tensors' addresses and types: fp32 streams take no more)
   int64_t most = 0;
-  for (const Way way : {ANY, EVEN, GROUPS}) most = std::max(most, blocks_of(rows, shape_of((int)width, false, way), way, true));
+  for (const Way way : {ANY, EVEN, GROUPS}) most = std::max(most, blocks_of(rows, shape_of((int)width, false, way), way, true, false));
   return (size_t)most * (size_t)width * sizeof(float);
 }
 
@@ -470,7 +474,7 @@ void rms_norm_bwd(hipStream_t st, const ast_norm_cfg& c, const void* dy, const v
   const Way way = way_of(cols, aligned16(dy) && aligned16(sum) && aligned16(dsum) && aligned16(dx) && aligned16(ds), false,
                          c.sum_dtype == AST_F32);
   const Shape s = shape_of(cols, false, way);
-  const int64_t blocks = c.rows > 0 ? blocks_of(c.rows, s, way, true) : 0;
+  const int64_t blocks = c.rows > 0 ? blocks_of(c.rows, s, way, true, c.sum_dtype == AST_F32) : 0;
   NormArgs g = args_of(c, s, gain);
   g.x = dy;
   g.s = sum;
