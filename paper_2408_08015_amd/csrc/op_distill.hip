@@ -34,8 +34,8 @@ struct DistillArgs {
 
 constexpr float kLog2e = 1.44269504f;
 constexpr float kLowest = -3.402823466e38f;  // where a running maximum starts (an infinity would give NaN for -inf - -inf)
-constexpr int kMostEntries = 1024;
-constexpr int kSeen = 32768;  // places that an id's lowest bits tell apart
+// A row of few values is a wavefront's: several times as many rows are under way, and none waits for another wavefront of its own.
+constexpr int kFewValues = 4096, kFewEntries = 256;
 
 __device__ __forceinline__ float exp_scaled(float x, float s) { return __builtin_amdgcn_exp2f(x * s); }
 
@@ -87,16 +87,22 @@ __device__ __forceinline__ Sums block_sums(Sums s, float scale, float (*sh)[16])
 }
 
 // The teacher's side of a row, and the student's logits at its places.
+template <int THREADS>
 struct Entries {
-  __attribute__((aligned(16))) int id[kMostEntries];  // -1: does not count
-  float p[kMostEntries], logp[kMostEntries], z[kMostEntries];
+  static constexpr int MOST = THREADS == 64 ? kFewEntries : 1024;
+  __attribute__((aligned(16))) int id[MOST];  // -1: does not count
+  float p[MOST], logp[MOST], z[MOST];
   float z_label;
 };
-struct Places { uint32_t seen[kSeen / 32], twice[kSeen / 32]; };  // of the ids' lowest bits: stand in the row, stand more than once
+template <int THREADS>
+struct Places {  // of the ids' lowest bits: stand in the row, stand more than once
+  static constexpr int SEEN = THREADS == 64 ? kFewValues : 32768;  // places that these bits tell apart
+  uint32_t seen[SEEN / 32], twice[SEEN / 32];
+};
 // Every one of THREADS threads its entries; returns whether it has one that counts.  Logits are read from z where they lie in
 // [lo, hi), or all of them from saved (a row's places_z).
-template <typename T, int THREADS>
-__device__ __forceinline__ bool gather(const DistillArgs& g, int64_t row, const T* z, const float* saved, int lo, int hi, int label, Entries& e) {
+template <int THREADS, typename T, typename E>
+__device__ __forceinline__ bool gather(const DistillArgs& g, int64_t row, const T* z, const float* saved, int lo, int hi, int label, E& e) {
   bool any = false;
   for (int k = threadIdx.x; k < g.entries; k += THREADS) {
     const int64_t at = row * g.entries + k;
@@ -112,7 +118,7 @@ __device__ __forceinline__ bool gather(const DistillArgs& g, int64_t row, const 
     }
   }
   if (threadIdx.x < 3)  // (what a group of four reads behind the last entry)
-    if (g.entries + (int)threadIdx.x < kMostEntries) e.id[g.entries + threadIdx.x] = -1;
+    if (g.entries + (int)threadIdx.x < E::MOST) e.id[g.entries + threadIdx.x] = -1;
   if (threadIdx.x == THREADS - 1 && label >= 0) {
     if (saved) e.z_label = saved[g.entries];
     else if (label >= lo && label < hi) e.z_label = load1(z + label);
@@ -120,7 +126,8 @@ __device__ __forceinline__ bool gather(const DistillArgs& g, int64_t row, const 
   return any;
 }
 // p and log p, by one wavefront, once all entries are there; and which ids may stand several times
-__device__ __forceinline__ void teacher(const DistillArgs& g, Entries& e, int lane, Places* places) {
+template <int THREADS>
+__device__ __forceinline__ void teacher(const DistillArgs& g, Entries<THREADS>& e, int lane, Places<THREADS>* places) {
   float top = -INFINITY;
   for (int k = lane; k < g.entries; k += 64) {
     const float t = e.logp[k];
@@ -147,7 +154,7 @@ __device__ __forceinline__ void teacher(const DistillArgs& g, Entries& e, int la
     e.p[k] *= inv;
     e.logp[k] -= ls;
     if (!places) continue;
-    const uint32_t at = (uint32_t)id % kSeen, bit = 1u << (at & 31);
+    const uint32_t at = (uint32_t)id % Places<THREADS>::SEEN, bit = 1u << (at & 31);
     if (atomicOr(&places->seen[at / 32], bit) & bit) atomicOr(&places->twice[at / 32], bit);
   }
 }
@@ -198,7 +205,8 @@ __device__ __forceinline__ void load_group(Eight<T, true>& e, const T* z, int at
 }
 
 // the loss of a row, by one wavefront
-__device__ __forceinline__ float row_loss(const DistillArgs& g, const Entries& e, const Sums& s, bool label, int lane) {
+template <int THREADS>
+__device__ __forceinline__ float row_loss(const DistillArgs& g, const Entries<THREADS>& e, const Sums& s, bool label, int lane) {
   float loss = 0.f;
   if (g.kl != 0.f) {
     const float ls = logf(s.a);
@@ -229,7 +237,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
   constexpr bool GRAD = MODE == GRADIENT || MODE == STEP || MODE == JOIN_STEP;
   constexpr bool CUT = MODE != LOSS && MODE != STEP;  // blockIdx.y: a slice
   constexpr int U = 4, K = KEEP ? KEEP : 1;  // U: groups that are asked for together
-  __shared__ Entries e;
+  __shared__ Entries<THREADS> e;
   __shared__ float sh[3][16];
   const int64_t row = g.row0 + blockIdx.x;
   const T* const z = static_cast<const T*>(g.z) + row * g.z_stride;
@@ -257,13 +265,14 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
   const float zodd = odd >= 0 ? load1(z + odd) : -INFINITY;
   bool any = false;  // an entry of the teacher's counts
   const float* const saved = JOIN ? g.places_z + row * (g.entries + 1) : nullptr;
-  Places* places = nullptr;
+  typedef Places<THREADS> Seen;
+  Seen* places = nullptr;
   if constexpr (GRAD) {  // (what may be written in place of the logits waits for their values at the entries' places)
-    __shared__ Places store;
+    __shared__ Seen store;
     places = &store;
-    for (int i = tid; i < kSeen / 32; i += THREADS) places->seen[i] = places->twice[i] = 0;
-    any = __syncthreads_or(gather<T, THREADS>(g, row, z, saved, lo, hi, label, e));
-    if (tid < 64) teacher(g, e, lane, places);
+    for (int i = tid; i < Seen::SEEN / 32; i += THREADS) places->seen[i] = places->twice[i] = 0;
+    any = __syncthreads_or(gather<THREADS>(g, row, z, saved, lo, hi, label, e));
+    if (tid < 64) teacher<THREADS>(g, e, lane, places);
   } else if constexpr (MODE == PART) {
     if (lowest) {
       float* const to = g.places_z + row * (g.entries + 1);
@@ -275,12 +284,12 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
   } else {  // (the others go on to the row; many entries are gathered by all: 8192 x 2000 with 512 47 us from 65, 2001 x 50021 with
             // 100 would take 53.7 from 51.8)
     if (g.entries > 128) {
-      gather<T, THREADS>(g, row, z, saved, lo, hi, label, e);
+      gather<THREADS>(g, row, z, saved, lo, hi, label, e);
       __syncthreads();
     } else if (tid < 64) {
-      gather<T, 64>(g, row, z, saved, lo, hi, label, e);
+      gather<64>(g, row, z, saved, lo, hi, label, e);
     }
-    if (tid < 64) teacher(g, e, lane, nullptr);
+    if (tid < 64) teacher<THREADS>(g, e, lane, nullptr);
   }
 
   Sums s = {kLowest, 0.f, 0.f};
@@ -392,7 +401,7 @@ __global__ __launch_bounds__(THREADS, 4) void distill_kernel(const DistillArgs g
     if (id < 0 || id < lo || id >= hi) continue;
     float p = k < g.entries ? e.p[k] : 0.f;
     bool first = true;
-    const uint32_t at = (uint32_t)id % kSeen;
+    const uint32_t at = (uint32_t)id % Seen::SEEN;
     if ((k < g.entries ? places->twice : places->seen)[at / 32] >> (at & 31) & 1) {
       p = 0.f;
       for (int j = 0; j < g.entries; j += 4) {
@@ -437,6 +446,12 @@ void go(hipStream_t st, int64_t rows, int slices, DistillArgs g, Exps e) {
 template <Mode MODE, typename T>
 void pick(hipStream_t st, const ast_distill_cfg& c, const DistillArgs& g, Exps e) {
   const int64_t r = c.rows, v = c.vocab;
+  // (us of 8192 rows with 32 entries, loss, gradient, both: 1000 bf16 13, 13, 17, in blocks of 256 threads 25, 27, 33; 4096 bf16 19, 34, 37
+  // and 32, 39, 43; fp32 of 2048 17, 35, 34 and 32, 39, 39, of 4096 28, 65, 64 and 36, 57, 63)
+  if (v <= (sizeof(T) == 2 || MODE == LOSS ? kFewValues : kFewValues / 2) && c.entries <= kFewEntries) {
+    if constexpr (MODE != PART && MODE != JOIN_STEP) go<MODE, T, 64, MODE == STEP ? 8 : 0>(st, r, 1, g, e);
+    return;
+  }
   if constexpr (MODE == GRADIENT) {
     if (v <= 8192) go<MODE, T, 256, 0>(st, r, 1, g, e);
     else go<MODE, T, 512, 0>(st, r, g.slices, g, e);

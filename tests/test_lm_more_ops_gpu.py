@@ -412,6 +412,8 @@ DISTILL = [  # rows, vocab, entries, temperature, label weight, room behind a ro
     (1, 1, 1, 1.0, 0.0, 0), (2, 7, 3, 2.0, 0.5, 0), (3, 8, 8, 0.5, 0.0, 3), (5, 33, 40, 1.0, 0.3, 0), (9, 100, 1, 3.0, 1.0, 0), (4, 511, 17, 1.5, 0.0, 1),
     (6, 512, 64, 2.0, 0.1, 0), (3, 4096, 65, 1.0, 0.0, 0), (2, 4097, 200, 4.0, 0.5, 7), (2, 30011, 1024, 0.7, 0.2, 5), (3, 65536, 128, 1.0, 0.5, 0), (2, 131072, 64, 2.0, 0.5, 0),
     (2, 131077, 9, 2.0, 0.5, 3), (2, 250001, 50, 1.0, 0.0, 7), (40, 16391, 33, 4.0, 0.4, 0),
+    # (rows of a wavefront each, with as many entries as those take and one more; and rows that are just too long)
+    (11, 1999, 256, 1.5, 0.3, 1), (11, 1999, 257, 1.0, 0.0, 1), (7, 2049, 256, 2.0, 0.5, 0), (6, 4096, 255, 4.0, 0.2, 0), (300, 130, 20, 1.0, 0.4, 6),
     # (more rows than are cut into slices: kept in registers whole, or the first part of them)
     (80, 9001, 8, 1.0, 0.0, 0), (65, 20000, 30, 4.0, 0.5, 1), (70, 33000, 12, 1.5, 0.2, 0), (66, 131077, 40, 2.0, 0.5, 3),
     # (a part of the rows in shared memory, less and a little more than fits there; fp32, then bf16)
