@@ -208,7 +208,7 @@ REC = [  # tokens, channels, sequences
     (300, 63, ("ragged", 7, 20, 9)), (1500, 66, ("ragged", 4, 0, 0)), (1500, 20, ("ragged", 200, 300, 130)), (4200, 48, ("ragged", 3, 1, 0)),
     (260, 16, ("ragged", 600, 0, 0)), (2304, 34, ("ragged", 2, 2000, 0)),
     (60, 65, ("ragged", 63, 3, 2)), (60, 33, ("ragged", 64, 5, 0)), (128, 40, ("ragged", 200, 10, 10)), (128, 9, ("ragged", 20, 0, 100)),
-    (9, 5, ("ragged", 3, 4, 5)), (100, 200, ("ragged", 12, 0, 1)),
+    (4200, 1000, ("period", 1)), (9, 5, ("ragged", 3, 4, 5)), (100, 200, ("ragged", 12, 0, 1)),
 ]
 
 
