@@ -1,4 +1,5 @@
 // C ABI of the single operators (include/asteroid_ops.h): argument checks, then the launches of ops.h.
+#include <algorithm>
 #include <cmath>
 #include <string>
 
@@ -78,11 +79,41 @@ const char* heads_apart(const ast_qk_cfg& c, const ast_heads& h) {
   return head_inner || token_inner ? nullptr : "the heads of an output overlap";
 }
 
-
 // ranges of bytes that lie on each other (NULL lies on nothing)
 bool overlap(const void* p, size_t n, const void* q, size_t m) {
   const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
   return a && b && a < b + m && b < a + n;
+}
+
+// The memory of a tensor: rows of `wide` bytes, `step` bytes from one to the next, all of them in [lo, hi).  (In 128 bits: the products
+// of the sizes and strides that the calls take do not fit 64.)
+typedef unsigned __int128 Place;
+struct Area {
+  Place lo = 0, hi = 0;  // (equal: nothing, a tensor that is not there or has no rows)
+  Place step = 0, wide = 0;
+  int64_t rows = 0;
+  Area() {}
+  Area(const void* p, int64_t rows_, int64_t step_, int64_t wide_) {
+    if (!p || rows_ <= 0 || wide_ <= 0) return;
+    lo = reinterpret_cast<uintptr_t>(p);
+    rows = rows_, step = (Place)step_, wide = (Place)wide_;
+    hi = lo + (Place)(rows - 1) * step + wide;
+    if (step <= wide) wide = hi - lo, rows = 1;  // (no gaps)
+  }
+};
+// A byte belongs to both.  Exact, except that rows with gaps and different steps count as all that lies between their first and last.
+bool meet(const Area& a, const Area& b) {
+  if (a.lo >= b.hi || b.lo >= a.hi) return false;
+  if (a.rows == 1 && b.rows == 1) return true;
+  if (a.rows == 1 || b.rows == 1) {
+    const Area &one = a.rows == 1 ? a : b, &many = a.rows == 1 ? b : a;
+    const Place row = std::min((one.hi - 1 - many.lo) / many.step, (Place)(many.rows - 1));  // the last that begins in front of its end
+    return many.lo + row * many.step + many.wide > one.lo;
+  }
+  if (a.step != b.step) return true;
+  const Area &p = a.lo <= b.lo ? a : b, &q = a.lo <= b.lo ? b : a;  // q's first row: behind p's row k, by r bytes
+  const Place k = (q.lo - p.lo) / p.step, r = (q.lo - p.lo) % p.step;
+  return (k < (Place)p.rows && r < p.wide) || (k + 1 < (Place)p.rows && p.step - r < q.wide);
 }
 
 const char* norm_cfg(const ast_norm_cfg* c) {
@@ -118,17 +149,9 @@ const char* rows_ok(const ast_recurrence_cfg& c, const ast_rows* r, bool out) {
   if (out && c.tokens > 1 && r->stride < c.channels) return "the rows of an output overlap";
   return nullptr;
 }
-// two outputs of which rows lie on each other (with different strides: of which the ranges do)
-bool rows_meet(const ast_recurrence_cfg& c, const ast_rows& p, const ast_rows& q) {
-  if (c.tokens == 0) return false;
+Area rows_of(const ast_recurrence_cfg& c, const ast_rows* r) {
   const int64_t e = (int64_t)esize(c.dtype);
-  auto span = [&](const ast_rows& r) { return (size_t)(((c.tokens - 1) * r.stride + c.channels) * e); };
-  if (!overlap(p.dev, span(p), q.dev, span(q))) return false;
-  if (p.stride != q.stride || c.tokens == 1) return true;
-  const int64_t step = p.stride * e, wide = c.channels * e;
-  int64_t apart = (int64_t)(reinterpret_cast<uintptr_t>(q.dev) - reinterpret_cast<uintptr_t>(p.dev)) % step;
-  if (apart < 0) apart += step;
-  return apart < wide || step - apart < wide;
+  return r ? Area(r->dev, c.tokens, r->stride * e, c.channels * e) : Area();
 }
 
 const char* distill_cfg(const ast_distill_cfg* c) {
@@ -348,7 +371,8 @@ ast_status asteroid_recurrence_backward(const ast_recurrence_cfg* cfg, const ast
     if (const char* e = rows_ok(*cfg, r, false)) return fail(fn, e);
   for (const ast_rows* r : {df, dz, dgo ? dgo : dz})
     if (const char* e = rows_ok(*cfg, r, true)) return fail(fn, e);
-  if (rows_meet(*cfg, *df, *dz) || (dgo && (rows_meet(*cfg, *df, *dgo) || rows_meet(*cfg, *dz, *dgo)))) return fail(fn, "outputs overlap");
+  const Area gf = rows_of(*cfg, df), gz = rows_of(*cfg, dz), go = rows_of(*cfg, dgo);
+  if (meet(gf, gz) || meet(gf, go) || meet(gz, go)) return fail(fn, "outputs overlap");
   if (cfg->tokens > 0 && !saved_dev) return fail(fn, "saved_dev is NULL");
   if (!aligned(state_dev, 4) || !aligned(saved_dev, 4) || !aligned(dfinal_dev, 4) || !aligned(dstate_dev, 4))
     return fail(fn, "states must be 4-byte aligned");

@@ -1,0 +1,61 @@
+"""CPU: tensors of one call of the norm with the residual, the gated recurrence and the distillation loss that lie on each other
+are refused, before anything is launched, except where the interface allows it."""
+import ctypes as C
+
+import pytest
+
+import paper_2408_08015_amd as A
+from paper_2408_08015_amd import ops
+
+EINVAL = -1
+FAR = [(1 << 40) + (i << 32) for i in range(16)]   # addresses that are never read: every call below is refused
+
+
+@pytest.fixture(scope="module")
+def lib():
+    A.load_library()
+    return ops._lib()
+
+
+def refused(lib, name, *args):
+    st = getattr(lib, "asteroid_" + name)(*args)
+    msg = lib.asteroid_last_error().decode()
+    assert st == EINVAL and name in msg, (name, args, st, msg)
+    return msg
+
+
+# ------------------------------------------------------------------------------------------------ recurrence
+
+R = ops.ast_rows
+
+
+def rec(tokens=300, channels=40, dtype=1, offsets=FAR[15], sequences=3, period=0):
+    return ops.ast_recurrence_cfg(tokens, channels, dtype, offsets, sequences, period)
+
+
+def recurrence_backward(lib, cfg, **at):
+    """The message of the refused call; what `at` does not give lies apart.  (Without its workspace it would be refused last.)"""
+    c = cfg.channels
+    a = {n: R(FAR[i], c) for i, n in enumerate(("dy", "f", "z", "o", "df", "dz", "do"))}
+    a.update(state=FAR[7], saved=FAR[8], dfinal=FAR[9], dstate=FAR[10], ws=None, size=0)
+    a.update(at)
+    return refused(lib, "recurrence_backward", cfg, a["dy"], a["f"], a["z"], a["o"], a["state"], a["saved"], a["dfinal"], a["df"], a["dz"], a["do"],
+                   a["dstate"], a["ws"], a["size"], None)
+
+
+def test_gradients_of_the_recurrence_whose_extent_passes_64_bits(lib):
+    """The rows of dz begin at df's second row; (tokens - 1) * stride * 2 bytes is 2^64."""
+    big = rec(tokens=(1 << 23) + 1)
+    for other in ("dz", "do"):
+        assert "outputs overlap" in recurrence_backward(lib, big, df=R(FAR[4], 1 << 40), **{other: R(FAR[4] + (2 << 40), 1 << 40)})
+
+
+def test_gradients_of_the_recurrence_beside_each_other(lib):
+    """Parts of one packed tensor, and rows behind another's last one, are no overlap; one value on another is."""
+    e, c, T = 2, 40, 300
+    p = FAR[4]
+    for dz, fine in ((R(p + 80 * e, 120), True), (R(p + 39 * e, 120), False), (R(p - 40 * e, 120), True), (R(p - 39 * e, 120), False),
+                     (R(p + T * 120 * e, 120), True), (R(p + (T - 1) * 120 * e, 120), False), (R(p + ((T - 1) * 120 + 40) * e, 120), True),
+                     (R(p - T * 120 * e, 120), True), (R(p - (T - 1) * 120 * e, 120), False), (R(p - (T * 120 - 81) * e, 120), False),
+                     (R(p + ((T - 1) * 120 + 40) * e, 40), True), (R(p + ((T - 1) * 120 + 39) * e, 40), False)):
+        assert ("workspace" if fine else "outputs overlap") in recurrence_backward(lib, rec(tokens=T, channels=c), df=R(p, 120), dz=dz), (dz.dev - p, dz.stride)
