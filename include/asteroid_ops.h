@@ -211,7 +211,8 @@ ast_status asteroid_recurrence_forward(const ast_recurrence_cfg* cfg, const ast_
 /* Gradients of all inputs from dy, dfinal_dev (NULL: none; fp32 [sequences][channels]), and saved_dev of the
  * forward pass of the same inputs.  df, dz, dgo (NULL iff o is) are rows of any stride >= channels, and may be the
  * tensors of f, z, o (same pointer and stride), or dy; they may not overlap each other.  dstate_dev (or NULL): fp32
- * [sequences][channels], the gradient of state_dev (of a sequence without tokens: its dfinal, or 0); it may be dfinal_dev. */
+ * [sequences][channels], the gradient of state_dev (of a sequence without tokens: its dfinal, or 0); it may be dfinal_dev or
+ * state_dev. */
 ast_status asteroid_recurrence_backward(const ast_recurrence_cfg* cfg, const ast_rows* dy, const ast_rows* f, const ast_rows* z,
                                         const ast_rows* o, const float* state_dev, const float* saved_dev,
                                         const float* dfinal_dev, const ast_rows* df, const ast_rows* dz, const ast_rows* dgo,

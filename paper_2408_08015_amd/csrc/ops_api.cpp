@@ -1,6 +1,7 @@
 // C ABI of the single operators (include/asteroid_ops.h): argument checks, then the launches of ops.h.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <string>
 
 #include "ops.h"
@@ -116,6 +117,25 @@ bool meet(const Area& a, const Area& b) {
   return (k < (Place)p.rows && r < p.wide) || (k + 1 < (Place)p.rows && p.step - r < q.wide);
 }
 
+// the same rows at the same place
+bool same(const Area& a, const Area& b) { return a.lo == b.lo && a.hi == b.hi && a.rows == b.rows && (a.rows == 1 || (a.step == b.step && a.wide == b.wide)); }
+typedef std::initializer_list<Area> Areas;
+bool any_meet(Areas outputs) {
+  for (const Area* a = outputs.begin(); a != outputs.end(); ++a)
+    for (const Area* b = outputs.begin(); b != a; ++b)
+      if (meet(*a, *b)) return true;
+  return false;
+}
+// ... one of each; in_place: not counting an output that is the input
+bool any_meet(Areas outputs, Areas inputs, bool in_place = false) {
+  for (const Area& a : outputs)
+    for (const Area& b : inputs)
+      if (meet(a, b) && !(in_place && same(a, b))) return true;
+  return false;
+}
+const char* const kOnInput = "an output and an input overlap, and are not the same rows where that is allowed";
+const char* const kOnWorkspace = "the workspace overlaps a tensor";
+
 const char* norm_cfg(const ast_norm_cfg* c) {
   if (!c) return "cfg is NULL";
   if (!dtype_ok(c->dtype) || !dtype_ok(c->sum_dtype)) return "unknown dtype";
@@ -153,6 +173,15 @@ Area rows_of(const ast_recurrence_cfg& c, const ast_rows* r) {
   const int64_t e = (int64_t)esize(c.dtype);
   return r ? Area(r->dev, c.tokens, r->stride * e, c.channels * e) : Area();
 }
+Area states_of(const ast_recurrence_cfg& c, const float* p) {
+  const int64_t n = c.offsets_dev ? c.sequences : (c.tokens + c.period - 1) / c.period;
+  return Area(p, n, c.channels * 4, c.channels * 4);
+}
+Area saved_of(const ast_recurrence_cfg& c, const float* p) {
+  return Area(p, (c.tokens + AST_RECURRENCE_CHUNK - 1) / AST_RECURRENCE_CHUNK, c.channels * 4, c.channels * 4);
+}
+Area offsets_of(const ast_recurrence_cfg& c) { return Area(c.offsets_dev, c.sequences + 1, 4, 4); }
+Area block_of(const void* p, size_t bytes) { return Area(p, 1, (int64_t)bytes, (int64_t)bytes); }
 
 const char* distill_cfg(const ast_distill_cfg* c) {
   if (!c) return "cfg is NULL";
@@ -371,14 +400,20 @@ ast_status asteroid_recurrence_backward(const ast_recurrence_cfg* cfg, const ast
     if (const char* e = rows_ok(*cfg, r, false)) return fail(fn, e);
   for (const ast_rows* r : {df, dz, dgo ? dgo : dz})
     if (const char* e = rows_ok(*cfg, r, true)) return fail(fn, e);
-  const Area gf = rows_of(*cfg, df), gz = rows_of(*cfg, dz), go = rows_of(*cfg, dgo);
-  if (meet(gf, gz) || meet(gf, go) || meet(gz, go)) return fail(fn, "outputs overlap");
+  const Area gf = rows_of(*cfg, df), gz = rows_of(*cfg, dz), go = rows_of(*cfg, dgo), gs = states_of(*cfg, dstate_dev);
+  if (any_meet({gf, gz, go, gs})) return fail(fn, "outputs overlap");
+  const Area ydy = rows_of(*cfg, dy), xf = rows_of(*cfg, f), xz = rows_of(*cfg, z), xo = rows_of(*cfg, o), off = offsets_of(*cfg);
+  const Area xs = states_of(*cfg, state_dev), xd = states_of(*cfg, dfinal_dev), kept = saved_of(*cfg, saved_dev);
+  if (any_meet({gf, gz, go}, {ydy, xf, xz, xo}, true) || any_meet({gf, gz, go}, {xs, xd, kept, off}) || any_meet({gs}, {xs, xd}, true) ||
+      any_meet({gs}, {ydy, xf, xz, xo, kept, off}))
+    return fail(fn, kOnInput);
   if (cfg->tokens > 0 && !saved_dev) return fail(fn, "saved_dev is NULL");
   if (!aligned(state_dev, 4) || !aligned(saved_dev, 4) || !aligned(dfinal_dev, 4) || !aligned(dstate_dev, 4))
     return fail(fn, "states must be 4-byte aligned");
   const size_t need = ast::recurrence_ws_bytes(*cfg);
   if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
     return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  if (any_meet({block_of(workspace_dev, need)}, {gf, gz, go, gs, ydy, xf, xz, xo, xs, xd, kept, off})) return fail(fn, kOnWorkspace);
   ast::recurrence_bwd(stream_of(hip_stream), *cfg, *dy, *f, *z, o, state_dev, saved_dev, dfinal_dev, *df, *dz, dgo, dstate_dev,
                       workspace_dev);
   return launched(fn);

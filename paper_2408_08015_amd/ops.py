@@ -546,7 +546,8 @@ def recurrence_forward(f, z, o=None, offsets=None, period=0, state=None, final=N
 def recurrence_backward(dy, f, z, saved, o=None, offsets=None, period=0, state=None, dfinal=None, dstate=None, out=None,
                         workspace=None):
     """(df, dz, do, dstate) of recurrence_forward with the same arguments; saved is what it left.  dfinal float32
-    [sequences, channels]: the gradient of final (0 if not given).  dstate: True or a tensor to receive the gradient of state.
+    [sequences, channels]: the gradient of final (0 if not given).  dstate: True or a tensor (dfinal or state allowed) to receive the gradient
+    of state.
     out: (df, dz, do), rows with any stride; (f, z, o) themselves allowed.  do is None where o is."""
     cfg, n, a = _recurrence_inputs(f, z, o, offsets, period)
     _is(saved, "saved", _F32, (-(-f.shape[0] // RECURRENCE_CHUNK), f.shape[1]))

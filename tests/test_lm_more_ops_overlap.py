@@ -59,3 +59,27 @@ def test_gradients_of_the_recurrence_beside_each_other(lib):
                      (R(p - T * 120 * e, 120), True), (R(p - (T - 1) * 120 * e, 120), False), (R(p - (T * 120 - 81) * e, 120), False),
                      (R(p + ((T - 1) * 120 + 40) * e, 40), True), (R(p + ((T - 1) * 120 + 39) * e, 40), False)):
         assert ("workspace" if fine else "outputs overlap") in recurrence_backward(lib, rec(tokens=T, channels=c), df=R(p, 120), dz=dz), (dz.dev - p, dz.stride)
+
+
+def test_gradients_of_the_recurrence_on_other_tensors(lib):
+    """Blocks read the inputs, states and offsets of their own tokens while others write: only the same rows may be shared."""
+    e, c, T, n = 2, 40, 300, 3
+    packed = {k: R(FAR[1] + i * c * e, 3 * c) for i, k in enumerate(("f", "z", "o"))}
+    need = C.c_size_t()
+    assert lib.asteroid_recurrence_workspace(rec(), need) == 0 and need.value > 0
+    ok = [{}, dict(df=R(FAR[1], c), dz=R(FAR[2], c), do=R(FAR[3], c)), dict(df=R(FAR[0], c)), dict(df=R(FAR[2], c), dz=R(FAR[1], c)),
+          dict(packed, df=packed["f"], dz=packed["z"], do=packed["o"]), dict(packed, df=packed["o"]), dict(packed, df=R(FAR[1] + T * 3 * c * e, 3 * c)),
+          dict(dstate=FAR[9]), dict(dstate=FAR[7]), dict(dstate=FAR[9] + n * c * 4), dict(state=None, dfinal=None, dstate=None)]
+    for a in ok:
+        assert "workspace is missing" in recurrence_backward(lib, rec(), **a), a
+    for a in (dict(dstate=FAR[4]), dict(dstate=FAR[5] + T * c * e - 4), dict(dstate=FAR[6] - n * c * 4 + 4)):
+        assert "outputs overlap" in recurrence_backward(lib, rec(), **a), a
+    for a in (dict(dstate=FAR[0]), dict(dstate=FAR[1]), dict(dstate=FAR[2]), dict(dstate=FAR[3] + T * c * e - 4), dict(dstate=FAR[8]), dict(dstate=FAR[9] + 4),
+              dict(dstate=FAR[9] + c * 4), dict(dstate=FAR[7] - c * 4), dict(dstate=FAR[15]), dict(dstate=FAR[15] + 4 * n),
+              dict(df=R(FAR[0] + e, c)), dict(dz=R(FAR[1] + c * e, c)), dict(do=R(FAR[3] + e, c)), dict(df=R(FAR[1], c + 1)), dict(f=R(FAR[4], 0)),
+              dict(packed, df=R(FAR[1] + e, 3 * c)), dict(packed, df=R(FAR[1] + 3 * c * e, 3 * c)), dict(packed, df=R(FAR[1], c)),
+              dict(df=R(FAR[7], c)), dict(dz=R(FAR[8], c)), dict(do=R(FAR[9], c)), dict(df=R(FAR[15], c))):
+        assert "an output and an input" in recurrence_backward(lib, rec(), **a), a
+    for at in range(11):
+        a = dict(ws=FAR[at], size=need.value)
+        assert "workspace overlaps" in recurrence_backward(lib, rec(), **a), at

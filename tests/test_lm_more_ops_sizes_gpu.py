@@ -1,0 +1,31 @@
+"""The norm with the residual, the gated recurrence and the distillation loss (paper_2408_08015_amd.ops) at sizes where a block has
+more than one run of rows, where a lane has two channels, and with outputs in place of further inputs."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2408_08015_amd import ops
+    return ops
+
+
+# tokens, channels, lengths (0: by period), period: alone, by a few offsets, by many, as a chain, in wide blocks
+@pytest.mark.parametrize("T,C,off,period", [(90, 33, [0, 7, 7, 60, 90], 0), (300, 65, list(range(0, 290, 4)) + [290, 290], 0), (700, 40, None, 700),
+                                            (700, 40, None, 128), (129, 8, None, 1)])
+def test_gradient_of_the_states_in_place_of_them(ops, T, C, off, period):
+    g = torch.Generator(device="cuda").manual_seed(T)
+    f, z, o, dy = (torch.randn(T, C, generator=g, device="cuda") for _ in range(4))
+    kw = dict(offsets=torch.tensor(off, dtype=torch.int32, device="cuda")) if off else dict(period=period)
+    n = len(off) - 1 if off else -(-T // period)
+    h0, dfin = (torch.randn(n, C, generator=g, device="cuda") for _ in range(2))
+    _, _, saved = ops.recurrence_forward(f, z, o=o, state=h0, saved=True, **kw)
+    out = lambda: [torch.zeros(T, C, device="cuda") for _ in range(3)]   # (rows of no sequence are not written)
+    for d in (dfin, None):
+        want = ops.recurrence_backward(dy, f, z, saved, o=o, state=h0, dfinal=d, dstate=True, out=out(), **kw)
+        moved = h0.clone()
+        got = ops.recurrence_backward(dy, f, z, saved, o=o, state=moved, dfinal=d, dstate=moved, out=out(), **kw)
+        assert got[3] is moved and all(torch.equal(a, b) for a, b in zip(got, want))
