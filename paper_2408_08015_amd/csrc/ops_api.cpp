@@ -375,16 +375,18 @@ ast_status asteroid_recurrence_forward(const ast_recurrence_cfg* cfg, const ast_
   for (const ast_rows* r : {f, z, o ? o : z})
     if (const char* e = rows_ok(*cfg, r, false)) return fail(fn, e);
   if (!aligned(state_dev, 4) || !aligned(final_dev, 4) || !aligned(saved_dev, 4)) return fail(fn, "states must be 4-byte aligned");
-  if (cfg->tokens > 0) {
-    if (!y_dev || !aligned(y_dev, esize(cfg->dtype))) return fail(fn, "y_dev must be non-NULL and aligned to its element size");
-    const int64_t sequences = cfg->offsets_dev ? cfg->sequences : (cfg->tokens + cfg->period - 1) / cfg->period;
-    const size_t ny = (size_t)(cfg->tokens * cfg->channels) * esize(cfg->dtype), nf = 4 * (size_t)sequences * (size_t)cfg->channels;
-    const size_t ns = 4 * (size_t)((cfg->tokens + AST_RECURRENCE_CHUNK - 1) / AST_RECURRENCE_CHUNK) * (size_t)cfg->channels;
-    if (overlap(y_dev, ny, final_dev, nf) || overlap(y_dev, ny, saved_dev, ns) || overlap(final_dev, nf, saved_dev, ns)) return fail(fn, "outputs overlap");
-  }
+  if (cfg->tokens > 0 && (!y_dev || !aligned(y_dev, esize(cfg->dtype)))) return fail(fn, "y_dev must be non-NULL and aligned to its element size");
+  const ast_rows dense = {y_dev, cfg->channels};
+  const Area y = rows_of(*cfg, &dense), fin = states_of(*cfg, final_dev), kept = saved_of(*cfg, saved_dev);
+  if (any_meet({y, fin, kept})) return fail(fn, "outputs overlap");
+  const Area xf = rows_of(*cfg, f), xz = rows_of(*cfg, z), xo = rows_of(*cfg, o), xs = states_of(*cfg, state_dev), off = offsets_of(*cfg);
+  if (any_meet({y}, {xf, xz, xo}, true) || any_meet({y}, {xs, off}) || any_meet({fin}, {xs}, true) || any_meet({fin}, {xf, xz, xo, off}) ||
+      any_meet({kept}, {xf, xz, xo, xs, off}))
+    return fail(fn, kOnInput);
   const size_t need = ast::recurrence_ws_bytes(*cfg);
   if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
     return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  if (any_meet({block_of(workspace_dev, need)}, {y, fin, kept, xf, xz, xo, xs, off})) return fail(fn, kOnWorkspace);
   ast::recurrence_fwd(stream_of(hip_stream), *cfg, *f, *z, o, state_dev, y_dev, final_dev, saved_dev, workspace_dev);
   return launched(fn);
 }

@@ -83,3 +83,29 @@ def test_gradients_of_the_recurrence_on_other_tensors(lib):
     for at in range(11):
         a = dict(ws=FAR[at], size=need.value)
         assert "workspace overlaps" in recurrence_backward(lib, rec(), **a), at
+
+
+def recurrence_forward(lib, cfg, **at):
+    c = cfg.channels
+    a = {n: R(FAR[i], c) for i, n in enumerate(("f", "z", "o"))}
+    a.update(state=FAR[3], y=FAR[4], final=FAR[5], saved=FAR[6], ws=None, size=0)
+    a.update(at)
+    return refused(lib, "recurrence_forward", cfg, a["f"], a["z"], a["o"], a["state"], a["y"], a["final"], a["saved"], a["ws"], a["size"], None)
+
+
+def test_results_of_the_recurrence_on_other_tensors(lib):
+    e, c, T, n = 2, 40, 300, 3
+    need = C.c_size_t()
+    assert lib.asteroid_recurrence_workspace(rec(), need) == 0 and need.value > 0
+    wide = R(FAR[0], 3 * c)
+    for a in ({}, dict(y=FAR[0]), dict(y=FAR[2]), dict(final=FAR[3]), dict(final=FAR[3] + n * c * 4), dict(state=None, final=None, saved=None, o=None),
+              dict(f=wide, z=R(FAR[0] + c * e, 3 * c), y=FAR[0] + T * 3 * c * e)):
+        assert "workspace is missing" in recurrence_forward(lib, rec(), **a), a
+    for a in (dict(y=FAR[0] + e), dict(y=FAR[1] - T * c * e + e), dict(f=wide, y=FAR[0]), dict(f=R(FAR[0], 0), y=FAR[0]), dict(f=wide, y=FAR[0] + (T - 1) * 3 * c * e),
+              dict(y=FAR[3]), dict(y=FAR[15]), dict(final=FAR[3] + 4), dict(final=FAR[3] + c * 4), dict(final=FAR[1]), dict(final=FAR[15]),
+              dict(saved=FAR[0]), dict(saved=FAR[1]), dict(saved=FAR[2] + T * c * e - 4), dict(saved=FAR[3]), dict(saved=FAR[15] + 4 * n)):
+        assert "an output and an input" in recurrence_forward(lib, rec(), **a), a
+    # of no tokens, states are passed on
+    assert "an output and an input" in recurrence_forward(lib, rec(tokens=0), final=FAR[3] + 4)
+    for at in range(7):
+        assert "workspace overlaps" in recurrence_forward(lib, rec(), ws=FAR[at], size=need.value), at
