@@ -201,11 +201,24 @@ const char* distill_inputs(const ast_distill_cfg& c, const void* z, const int32_
   if (!aligned(z, esize(c.dtype)) || !aligned(ids, 4) || !aligned(t, esize(c.teacher_dtype))) return "buffers must be aligned to their element size";
   return nullptr;
 }
-const char* distill_gradient(const ast_distill_cfg& c, const float* dloss, const void* z, const void* dz, int64_t stride) {
+Area vocab_rows(const ast_distill_cfg& c, const void* p, int64_t stride) {
+  const int64_t e = (int64_t)esize(c.dtype);
+  return Area(p, c.rows, stride * e, c.vocab * e);
+}
+Area entries_of(const ast_distill_cfg& c, const void* p, size_t e) {
+  const int64_t wide = c.entries * (int64_t)e;
+  return Area(p, c.rows, wide, wide);
+}
+Area a_row(const ast_distill_cfg& c, const void* p, int64_t values = 1) { return Area(p, c.rows, 4 * values, 4 * values); }
+const char* distill_gradient(const ast_distill_cfg& c, const float* dloss, const void* z, const int32_t* ids, const void* t, const void* dz,
+                             int64_t stride) {
   if (!dloss || !dz) return "NULL argument";
   if (!aligned(dloss, 4) || !aligned(dz, esize(c.dtype))) return "buffers must be aligned to their element size";
   if (stride < c.vocab || stride > (int64_t)1 << 31) return "dlogits_stride must lie in [vocab, 2^31]";
   if (z == dz && stride != c.logits_stride) return "a gradient in place of the logits needs their stride";
+  const Area g = vocab_rows(c, dz, stride);
+  const Area id = entries_of(c, ids, 4), top = entries_of(c, t, esize(c.teacher_dtype));
+  if (any_meet({g}, {vocab_rows(c, z, c.logits_stride)}, true) || any_meet({g}, {id, top, a_row(c, dloss), a_row(c, c.labels_dev)})) return kOnInput;
   return nullptr;
 }
 
@@ -440,8 +453,9 @@ ast_status asteroid_distill_backward(const ast_distill_cfg* cfg, const float* dl
   if (const char* e = distill_cfg(cfg)) return fail(fn, e);
   if (cfg->rows == 0) return AST_OK;
   if (const char* e = distill_inputs(*cfg, logits_dev, ids_dev, teacher_dev)) return fail(fn, e);
-  if (const char* e = distill_gradient(*cfg, dloss_dev, logits_dev, dlogits_dev, dlogits_stride)) return fail(fn, e);
+  if (const char* e = distill_gradient(*cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, dlogits_dev, dlogits_stride)) return fail(fn, e);
   if (!stats_dev || !aligned(stats_dev, 4)) return fail(fn, "stats_dev must be non-NULL and 4-byte aligned");
+  if (any_meet({vocab_rows(*cfg, dlogits_dev, dlogits_stride)}, {a_row(*cfg, stats_dev, 3)})) return fail(fn, kOnInput);
   ast::distill_bwd(stream_of(hip_stream), *cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, stats_dev, dlogits_dev, dlogits_stride);
   return launched(fn);
 }
@@ -461,7 +475,7 @@ ast_status asteroid_distill_step(const ast_distill_cfg* cfg, const float* dloss_
   if (const char* e = distill_cfg(cfg)) return fail(fn, e);
   if (cfg->rows == 0) return AST_OK;
   if (const char* e = distill_inputs(*cfg, logits_dev, ids_dev, teacher_dev)) return fail(fn, e);
-  if (const char* e = distill_gradient(*cfg, dloss_dev, logits_dev, dlogits_dev, dlogits_stride)) return fail(fn, e);
+  if (const char* e = distill_gradient(*cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, dlogits_dev, dlogits_stride)) return fail(fn, e);
   if (!loss_dev || !aligned(loss_dev, 4)) return fail(fn, "loss_dev must be non-NULL and 4-byte aligned");
   const size_t nd = ((size_t)(cfg->rows - 1) * (size_t)dlogits_stride + (size_t)cfg->vocab) * esize(cfg->dtype);
   if (overlap(loss_dev, 4 * (size_t)cfg->rows, dlogits_dev, nd)) return fail(fn, "outputs overlap");

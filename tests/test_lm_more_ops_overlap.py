@@ -109,3 +109,33 @@ def test_results_of_the_recurrence_on_other_tensors(lib):
     assert "an output and an input" in recurrence_forward(lib, rec(tokens=0), final=FAR[3] + 4)
     for at in range(7):
         assert "workspace overlaps" in recurrence_forward(lib, rec(), ws=FAR[at], size=need.value), at
+
+
+# ------------------------------------------------------------------------------------------------ distillation
+
+def dist(rows=4, vocab=40000, stride=40000, dtype=1, entries=7, teacher=0, labels=FAR[15]):
+    return ops.ast_distill_cfg(rows, vocab, stride, dtype, entries, teacher, 2.0, 0.5 if labels else 0.0, labels)
+
+
+def distill_step(lib, cfg, **at):
+    a = dict(dloss=FAR[0], z=FAR[1], ids=FAR[2], t=FAR[3], loss=FAR[4], dz=FAR[5], stride=cfg.logits_stride, ws=None, size=0)
+    a.update(at)
+    return refused(lib, "distill_step", cfg, a["dloss"], a["z"], a["ids"], a["t"], a["loss"], a["dz"], a["stride"], a["ws"], a["size"], None)
+
+
+def test_gradient_of_the_logits_on_other_tensors(lib):
+    """Few rows are cut into slices, whose blocks read logits while others write: only the same rows may be shared."""
+    e, T, V = 2, 4, 40000
+    side = dict(cfg=dist(stride=2 * V), dz=FAR[1] + V * e)        # the gradient beside the logits in the same rows
+    for a in ({}, dict(dz=FAR[1]), side, dict(side, dz=FAR[1] - V * e), dict(dz=FAR[1] + T * V * e), dict(cfg=dist(labels=None))):
+        a = dict(dict(cfg=dist()), **a)
+        assert "workspace is missing" in distill_step(lib, **a), a
+    on = [dict(dz=FAR[1] + e), dict(dz=FAR[1] - e), dict(dz=FAR[1] + V * e), dict(side, dz=FAR[1] + (V - 1) * e), dict(dz=FAR[1] + 2 * e, stride=V + 8),
+          dict(dz=FAR[0]), dict(dz=FAR[2]), dict(dz=FAR[3] + 4 * 7 * T - e), dict(dz=FAR[15]), dict(dz=FAR[15] - T * V * e + e)]
+    for a in on:
+        a = dict(dict(cfg=dist()), **a)
+        assert "an output and an input" in distill_step(lib, **a), a
+        cfg, dz, stride = a["cfg"], a["dz"], a.get("stride", a["cfg"].logits_stride)
+        assert "an output and an input" in refused(lib, "distill_backward", cfg, FAR[0], FAR[1], FAR[2], FAR[3], FAR[6], dz, stride, None), a
+    assert "an output and an input" in refused(lib, "distill_backward", dist(), FAR[0], FAR[1], FAR[2], FAR[3], FAR[6], FAR[6] + 12 * T - e, V, None)
+    assert "an output and an input" in distill_step(lib, dist(rows=(1 << 31) - 1, vocab=1 << 30, stride=1 << 31, dtype=0), dz=FAR[1] + 4, stride=1 << 31)
