@@ -441,7 +441,11 @@ ast_status asteroid_distill_forward(const ast_distill_cfg* cfg, const void* logi
   if (cfg->rows == 0) return AST_OK;
   if (const char* e = distill_inputs(*cfg, logits_dev, ids_dev, teacher_dev)) return fail(fn, e);
   if (!loss_dev || !stats_dev || !aligned(loss_dev, 4) || !aligned(stats_dev, 4)) return fail(fn, "loss_dev and stats_dev must be non-NULL and 4-byte aligned");
-  if (overlap(loss_dev, 4 * (size_t)cfg->rows, stats_dev, 12 * (size_t)cfg->rows)) return fail(fn, "outputs overlap");
+  const Area loss = a_row(*cfg, loss_dev), stats = a_row(*cfg, stats_dev, 3);
+  if (any_meet({loss, stats})) return fail(fn, "outputs overlap");
+  if (any_meet({loss, stats}, {vocab_rows(*cfg, logits_dev, cfg->logits_stride), entries_of(*cfg, ids_dev, 4),
+                               entries_of(*cfg, teacher_dev, esize(cfg->teacher_dtype)), a_row(*cfg, cfg->labels_dev)}))
+    return fail(fn, kOnInput);
   ast::distill_fwd(stream_of(hip_stream), *cfg, logits_dev, ids_dev, teacher_dev, loss_dev, stats_dev);
   return launched(fn);
 }
@@ -477,11 +481,16 @@ ast_status asteroid_distill_step(const ast_distill_cfg* cfg, const float* dloss_
   if (const char* e = distill_inputs(*cfg, logits_dev, ids_dev, teacher_dev)) return fail(fn, e);
   if (const char* e = distill_gradient(*cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, dlogits_dev, dlogits_stride)) return fail(fn, e);
   if (!loss_dev || !aligned(loss_dev, 4)) return fail(fn, "loss_dev must be non-NULL and 4-byte aligned");
-  const size_t nd = ((size_t)(cfg->rows - 1) * (size_t)dlogits_stride + (size_t)cfg->vocab) * esize(cfg->dtype);
-  if (overlap(loss_dev, 4 * (size_t)cfg->rows, dlogits_dev, nd)) return fail(fn, "outputs overlap");
+  const Area loss = a_row(*cfg, loss_dev), g = vocab_rows(*cfg, dlogits_dev, dlogits_stride), z = vocab_rows(*cfg, logits_dev, cfg->logits_stride);
+  if (any_meet({loss, g})) return fail(fn, "outputs overlap");
+  // (dloss too: of a row in slices one writes the loss while others may still have to read dloss)
+  const Area id = entries_of(*cfg, ids_dev, 4), top = entries_of(*cfg, teacher_dev, esize(cfg->teacher_dtype));
+  const Area w = a_row(*cfg, dloss_dev), lab = a_row(*cfg, cfg->labels_dev);
+  if (any_meet({loss}, {z, id, top, w, lab})) return fail(fn, kOnInput);
   const size_t need = ast::distill_step_ws_bytes(*cfg);
   if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
     return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  if (any_meet({block_of(workspace_dev, need)}, {loss, g, z, id, top, w, lab})) return fail(fn, kOnWorkspace);
   ast::distill_step(stream_of(hip_stream), *cfg, dloss_dev, logits_dev, ids_dev, teacher_dev, loss_dev, dlogits_dev, dlogits_stride,
                     workspace_dev);
   return launched(fn);

@@ -139,3 +139,18 @@ def test_gradient_of_the_logits_on_other_tensors(lib):
         assert "an output and an input" in refused(lib, "distill_backward", cfg, FAR[0], FAR[1], FAR[2], FAR[3], FAR[6], dz, stride, None), a
     assert "an output and an input" in refused(lib, "distill_backward", dist(), FAR[0], FAR[1], FAR[2], FAR[3], FAR[6], FAR[6] + 12 * T - e, V, None)
     assert "an output and an input" in distill_step(lib, dist(rows=(1 << 31) - 1, vocab=1 << 30, stride=1 << 31, dtype=0), dz=FAR[1] + 4, stride=1 << 31)
+
+
+def test_loss_on_other_tensors(lib):
+    """One that lies on dloss, for instance: of a row in slices, the first writes it while others still read dloss."""
+    e, T, V = 2, 4, 40000
+    need = C.c_size_t()
+    assert lib.asteroid_distill_step_workspace(dist(), need) == 0 and need.value > 0
+    assert "workspace is missing" in distill_step(lib, dist(), loss=FAR[0] + 4 * T)
+    for a in (FAR[0], FAR[0] + 4, FAR[0] - 4 * T + 4, FAR[1], FAR[1] + T * V * e - 4, FAR[2], FAR[3] + 4 * 7 * T - 4, FAR[15]):
+        assert "an output and an input" in distill_step(lib, dist(), loss=a), a - FAR[0]
+        if a not in (FAR[0], FAR[0] + 4, FAR[0] - 4 * T + 4):
+            for loss, stats in ((a, FAR[6]), (FAR[6], a)):
+                assert "an output and an input" in refused(lib, "distill_forward", dist(), FAR[1], FAR[2], FAR[3], loss, stats, None), a - FAR[0]
+    for at in (0, 1, 2, 3, 4, 5, 15):
+        assert "workspace overlaps" in distill_step(lib, dist(), ws=FAR[at], size=need.value), at
