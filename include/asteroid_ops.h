@@ -162,8 +162,8 @@ ast_status asteroid_rms_norm_forward(const ast_norm_cfg* cfg, const void* x_dev,
  *   ds = dsum + rho (dy gain - n mean(dy gain n)),  n = s rho,  rho = 1 / sqrt(mean(s^2) + eps);   dgain (+)= sum over the rows of dy n
  * dsum_dev (NULL: none): the gradient that reaches the sum from further on, of sum_dtype.  ds is the gradient of x and of
  * the residual: dx_dev receives it in dtype, ds_dev in sum_dtype; either may be NULL, not both.  dgain_dev fp32[width], written
- * (accumulate == 0) or added to.  dx_dev may be dy_dev, ds_dev may be dsum_dev or sum_dev; where the types are the same either output
- * may be any of the three inputs. */
+ * (accumulate == 0) or added to; it may be gain_dev.  dx_dev may be dy_dev, ds_dev may be dsum_dev or sum_dev; where the types are the
+ * same either output may be any of the three inputs. */
 ast_status asteroid_rms_norm_backward_workspace(const ast_norm_cfg* cfg, size_t* bytes);
 ast_status asteroid_rms_norm_backward(const ast_norm_cfg* cfg, const void* dy_dev, const void* sum_dev, const float* gain_dev,
                                       const void* dsum_dev, void* dx_dev, void* ds_dev, float* dgain_dev, int32_t accumulate,

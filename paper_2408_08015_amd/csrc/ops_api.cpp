@@ -80,12 +80,6 @@ const char* heads_apart(const ast_qk_cfg& c, const ast_heads& h) {
   return head_inner || token_inner ? nullptr : "the heads of an output overlap";
 }
 
-// ranges of bytes that lie on each other (NULL lies on nothing)
-bool overlap(const void* p, size_t n, const void* q, size_t m) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return a && b && a < b + m && b < a + n;
-}
-
 // The memory of a tensor: rows of `wide` bytes, `step` bytes from one to the next, all of them in [lo, hi).  (In 128 bits: the products
 // of the sizes and strides that the calls take do not fit 64.)
 typedef unsigned __int128 Place;
@@ -117,8 +111,11 @@ bool meet(const Area& a, const Area& b) {
   return (k < (Place)p.rows && r < p.wide) || (k + 1 < (Place)p.rows && p.step - r < q.wide);
 }
 
+Area block_of(const void* p, size_t bytes) { return Area(p, 1, (int64_t)bytes, (int64_t)bytes); }
 // the same rows at the same place
-bool same(const Area& a, const Area& b) { return a.lo == b.lo && a.hi == b.hi && a.rows == b.rows && (a.rows == 1 || (a.step == b.step && a.wide == b.wide)); }
+bool same(const Area& a, const Area& b) {
+  return a.lo == b.lo && a.hi == b.hi && a.rows == b.rows && (a.rows == 1 || (a.step == b.step && a.wide == b.wide));
+}
 typedef std::initializer_list<Area> Areas;
 bool any_meet(Areas outputs) {
   for (const Area* a = outputs.begin(); a != outputs.end(); ++a)
@@ -145,6 +142,8 @@ const char* norm_cfg(const ast_norm_cfg* c) {
   if (!(c->eps >= 0x1p-126f) || !std::isfinite(c->eps)) return "eps must be positive, and no subnormal number";
   return nullptr;
 }
+
+size_t norm_bytes(const ast_norm_cfg& c, int32_t dtype) { return (size_t)c.rows * (size_t)c.width * esize(dtype); }
 
 const char* recurrence_cfg(const ast_recurrence_cfg* c) {
   if (!c) return "cfg is NULL";
@@ -181,7 +180,6 @@ Area saved_of(const ast_recurrence_cfg& c, const float* p) {
   return Area(p, (c.tokens + AST_RECURRENCE_CHUNK - 1) / AST_RECURRENCE_CHUNK, c.channels * 4, c.channels * 4);
 }
 Area offsets_of(const ast_recurrence_cfg& c) { return Area(c.offsets_dev, c.sequences + 1, 4, 4); }
-Area block_of(const void* p, size_t bytes) { return Area(p, 1, (int64_t)bytes, (int64_t)bytes); }
 
 const char* distill_cfg(const ast_distill_cfg* c) {
   if (!c) return "cfg is NULL";
@@ -330,9 +328,12 @@ ast_status asteroid_rms_norm_forward(const ast_norm_cfg* cfg, const void* x_dev,
   if (!aligned(x_dev, esize(cfg->dtype)) || !aligned(y_dev, esize(cfg->dtype)) || !aligned(residual_dev, esize(cfg->sum_dtype)) ||
       !aligned(sum_dev, esize(cfg->sum_dtype)) || !aligned(gain_dev, 4) || !aligned(stash_dev, 16))
     return fail(fn, "buffers must be aligned to their element size, the stash to 16 bytes");
-  const size_t n = (size_t)cfg->rows * (size_t)cfg->width, ny = n * esize(cfg->dtype), ns = n * esize(cfg->sum_dtype);
-  const size_t nk = ast::stash8_bytes(cfg->rows, cfg->width);
-  if (overlap(y_dev, ny, sum_dev, ns) || overlap(y_dev, ny, stash_dev, nk) || overlap(sum_dev, ns, stash_dev, nk)) return fail(fn, "outputs overlap");
+  const Area x = block_of(x_dev, norm_bytes(*cfg, cfg->dtype)), r = block_of(residual_dev, norm_bytes(*cfg, cfg->sum_dtype));
+  const Area y = block_of(y_dev, norm_bytes(*cfg, cfg->dtype)), sum = block_of(sum_dev, norm_bytes(*cfg, cfg->sum_dtype));
+  const Area kept = block_of(stash_dev, ast::stash8_bytes(cfg->rows, cfg->width)), gain = block_of(gain_dev, 4 * (size_t)cfg->width);
+  if (any_meet({y, sum, kept})) return fail(fn, "outputs overlap");
+  // (rows of another type lie elsewhere: a block's would be another block's)
+  if (any_meet({y, sum}, {x, r}, true) || any_meet({kept}, {x, r}) || any_meet({y, sum, kept}, {gain})) return fail(fn, kOnInput);
   ast::rms_norm_fwd(stream_of(hip_stream), *cfg, x_dev, residual_dev, gain_dev, y_dev, sum_dev, stash_dev);
   return launched(fn);
 }
@@ -358,15 +359,19 @@ ast_status asteroid_rms_norm_backward(const ast_norm_cfg* cfg, const void* dy_de
     if (!aligned(dy_dev, esize(cfg->dtype)) || !aligned(dx_dev, esize(cfg->dtype)) || !aligned(sum_dev, esize(cfg->sum_dtype)) ||
         !aligned(dsum_dev, esize(cfg->sum_dtype)) || !aligned(ds_dev, esize(cfg->sum_dtype)))
       return fail(fn, "buffers must be aligned to their element size");
-    const size_t n = (size_t)cfg->rows * (size_t)cfg->width;
-    if (overlap(dx_dev, n * esize(cfg->dtype), ds_dev, n * esize(cfg->sum_dtype)) ||
-        overlap(dgain_dev, 4 * (size_t)cfg->width, dx_dev, n * esize(cfg->dtype)) ||
-        overlap(dgain_dev, 4 * (size_t)cfg->width, ds_dev, n * esize(cfg->sum_dtype)))
-      return fail(fn, "outputs overlap");
   }
+  const Area dy = block_of(dy_dev, norm_bytes(*cfg, cfg->dtype)), sum = block_of(sum_dev, norm_bytes(*cfg, cfg->sum_dtype));
+  const Area dsum = block_of(dsum_dev, norm_bytes(*cfg, cfg->sum_dtype)), gain = block_of(gain_dev, 4 * (size_t)cfg->width);
+  const Area dx = block_of(dx_dev, norm_bytes(*cfg, cfg->dtype)), ds = block_of(ds_dev, norm_bytes(*cfg, cfg->sum_dtype));
+  const Area dgain = block_of(dgain_dev, 4 * (size_t)cfg->width);
+  if (any_meet({dx, ds, dgain})) return fail(fn, "outputs overlap");
+  if (any_meet({dx, ds}, {dy, sum, dsum}, true) || any_meet({dx, ds}, {gain}) || any_meet({dgain}, {gain}, true) ||
+      any_meet({dgain}, {dy, sum, dsum}))
+    return fail(fn, kOnInput);
   const size_t need = ast::rms_norm_bwd_ws_bytes(cfg->rows, cfg->width);
   if (need && (!workspace_dev || workspace_bytes < need || !aligned(workspace_dev, 16)))
     return fail(fn, "the workspace is missing, too small or not 16-byte aligned");
+  if (any_meet({block_of(workspace_dev, need)}, {dx, ds, dgain, dy, sum, dsum, gain})) return fail(fn, kOnWorkspace);
   ast::rms_norm_bwd(stream_of(hip_stream), *cfg, dy_dev, sum_dev, gain_dev, dsum_dev, dx_dev, ds_dev, dgain_dev, accumulate != 0,
                     workspace_dev);
   return launched(fn);

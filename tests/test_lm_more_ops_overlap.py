@@ -154,3 +154,41 @@ def test_loss_on_other_tensors(lib):
                 assert "an output and an input" in refused(lib, "distill_forward", dist(), FAR[1], FAR[2], FAR[3], loss, stats, None), a - FAR[0]
     for at in (0, 1, 2, 3, 4, 5, 15):
         assert "workspace overlaps" in distill_step(lib, dist(), ws=FAR[at], size=need.value), at
+
+
+# ------------------------------------------------------------------------------------------------ norm and residual
+
+def norm(dtype=1, sum_dtype=0):
+    return ops.ast_norm_cfg(8, 40, dtype, sum_dtype, 1e-6)
+
+
+def test_gradients_of_the_norm_on_other_tensors(lib):
+    """A block's rows of another type, or shifted, are other blocks' rows."""
+    n, need = 8 * 40, C.c_size_t()
+    assert lib.asteroid_rms_norm_backward_workspace(norm(), need) == 0 and need.value > 0
+
+    def call(cfg, ws=None, size=0, **at):
+        a = dict(dy=FAR[0], s=FAR[1], gain=FAR[2], dsum=FAR[3], dx=FAR[4], ds=FAR[5], dgain=FAR[6])
+        a.update(at)
+        return refused(lib, "rms_norm_backward", cfg, a["dy"], a["s"], a["gain"], a["dsum"], a["dx"], a["ds"], a["dgain"], 0, ws, size, None)
+    for cfg, a in ((norm(), {}), (norm(), dict(dx=FAR[0], ds=FAR[1])), (norm(), dict(ds=FAR[3])), (norm(), dict(dgain=FAR[2])), (norm(1, 1), dict(dx=FAR[1], ds=FAR[0])),
+                   (norm(0, 0), dict(dx=FAR[3], ds=None)), (norm(), dict(dx=FAR[0] + 2 * n)), (norm(), dict(dsum=None, dx=None))):
+        assert "workspace is missing" in call(cfg, **a), a
+    for cfg, a in ((norm(), dict(dx=FAR[1])), (norm(), dict(dx=FAR[3])), (norm(), dict(ds=FAR[0])), (norm(1, 1), dict(dx=FAR[0] + 2)), (norm(0, 0), dict(ds=FAR[3] - 4 * n + 4)),
+                   (norm(), dict(dx=FAR[2])), (norm(), dict(ds=FAR[2] + 4 * 39)), (norm(), dict(dgain=FAR[2] + 4)), (norm(), dict(dgain=FAR[0])), (norm(), dict(dgain=FAR[1])),
+                   (norm(), dict(dgain=FAR[3] + 4 * n - 4))):
+        assert "an output and an input" in call(cfg, **a), a
+    for at in range(7):
+        assert "workspace overlaps" in call(norm(), ws=FAR[at], size=need.value), at
+
+
+def test_results_of_the_norm_on_other_tensors(lib):
+    n = 8 * 40
+
+    def call(cfg, **at):
+        a = dict(x=FAR[0], r=FAR[1], gain=FAR[2], y=FAR[3], s=FAR[4], kept=FAR[5])
+        a.update(at)
+        return refused(lib, "rms_norm_forward", cfg, a["x"], a["r"], a["gain"], a["y"], a["s"], a["kept"], None)
+    for cfg, a in ((norm(), dict(y=FAR[1])), (norm(), dict(s=FAR[0])), (norm(1, 1), dict(y=FAR[1] + 2)), (norm(0, 0), dict(s=FAR[0] + 4 * n - 4)), (norm(), dict(y=FAR[0] - 2)),
+                   (norm(), dict(y=FAR[2])), (norm(), dict(s=FAR[2])), (norm(), dict(kept=FAR[2])), (norm(), dict(kept=FAR[0])), (norm(), dict(kept=FAR[1] + 16))):
+        assert "an output and an input" in call(cfg, **a), a

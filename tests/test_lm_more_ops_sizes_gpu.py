@@ -29,3 +29,13 @@ def test_gradient_of_the_states_in_place_of_them(ops, T, C, off, period):
         moved = h0.clone()
         got = ops.recurrence_backward(dy, f, z, saved, o=o, state=moved, dfinal=d, dstate=moved, out=out(), **kw)
         assert got[3] is moved and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_the_gain_in_place_of_it(ops, accumulate):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    dy, s = (torch.randn(500, 257, generator=g, device="cuda").bfloat16() for _ in range(2))
+    gain = torch.rand(257, generator=g, device="cuda")
+    want = ops.rms_norm_backward(dy, s, gain, gain_out=gain.clone(), accumulate=accumulate)
+    got = ops.rms_norm_backward(dy, s, gain, gain_out=gain, accumulate=accumulate)
+    assert got[2] is gain and torch.equal(got[2], want[2]) and torch.equal(got[0], want[0])
