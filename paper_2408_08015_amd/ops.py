@@ -586,8 +586,14 @@ def _distill_cfg(logits, ids, teacher, temperature, labels, label_weight):
     _is(teacher, "teacher", tuple(_DT), ids.shape)
     if labels is not None:
         _vector_i32(labels, "labels", T)
-    return ast_distill_cfg(T, V, _vocab_rows(logits, "logits"), _DT[logits.dtype], ids.shape[1], _DT[teacher.dtype], temperature,
+    return ast_distill_cfg(T, V, _vocab_rows(logits, "logits"), _DT[logits.dtype], _entries(ids.shape[1]), _DT[teacher.dtype], temperature,
                            label_weight, None if labels is None else labels.data_ptr())
+
+
+def _entries(n):
+    if not -1 << 31 <= n < 1 << 31:   # (ctypes would cut it off)
+        raise ValueError("entries must lie in [1, 1024], got %d" % n)
+    return n
 
 
 def _vocab_rows(t, name):
@@ -646,7 +652,7 @@ def distill_step_workspace(rows, vocab, entries):
     """Bytes of workspace that distill_step takes."""
     n = C.c_size_t()
     lib = _lib()
-    _check(lib, lib.asteroid_distill_step_workspace(ast_distill_cfg(rows, vocab, vocab, 0, entries, 0, 1.0, 0.0, None), n))
+    _check(lib, lib.asteroid_distill_step_workspace(ast_distill_cfg(rows, vocab, vocab, 0, _entries(entries), 0, 1.0, 0.0, None), n))
     return n.value
 
 

@@ -1,8 +1,9 @@
 """CPU: tensors of one call of the norm with the residual, the gated recurrence and the distillation loss that lie on each other
-are refused, before anything is launched, except where the interface allows it."""
+are refused, before anything is launched, except where the interface allows it; and numbers that it has no room for."""
 import ctypes as C
 
 import pytest
+import torch
 
 import paper_2408_08015_amd as A
 from paper_2408_08015_amd import ops
@@ -192,3 +193,16 @@ def test_results_of_the_norm_on_other_tensors(lib):
     for cfg, a in ((norm(), dict(y=FAR[1])), (norm(), dict(s=FAR[0])), (norm(1, 1), dict(y=FAR[1] + 2)), (norm(0, 0), dict(s=FAR[0] + 4 * n - 4)), (norm(), dict(y=FAR[0] - 2)),
                    (norm(), dict(y=FAR[2])), (norm(), dict(s=FAR[2])), (norm(), dict(kept=FAR[2])), (norm(), dict(kept=FAR[0])), (norm(), dict(kept=FAR[1] + 16))):
         assert "an output and an input" in call(cfg, **a), a
+
+
+# ------------------------------------------------------------------------------------------------ numbers without room
+
+def test_entries_that_the_interface_has_no_room_for(lib):
+    n = (1 << 32) + 7
+    with pytest.raises(ValueError, match="entries"):
+        ops.distill_step_workspace(4, 40000, n)
+    ids, t, z = torch.zeros(0, n, dtype=torch.int32), torch.zeros(0, n), torch.zeros(0, 50)
+    for call in (lambda: ops.distill_forward(z, ids, t), lambda: ops.distill_step(torch.zeros(0), z, ids, t),
+                 lambda: ops.distill_backward(torch.zeros(0), z, ids, t, torch.zeros(0, 3))):
+        with pytest.raises(ValueError, match="entries"):
+            call()
