@@ -3,6 +3,8 @@ more than one run of rows, where a lane has two channels, and with outputs in pl
 import pytest
 import torch
 
+import test_lm_more_ops_gpu as G   # (the comparisons with the definition in 64 bits, and their bounds)
+
 pytestmark = pytest.mark.gpu
 
 
@@ -39,3 +41,36 @@ def test_gradient_of_the_gain_in_place_of_it(ops, accumulate):
     want = ops.rms_norm_backward(dy, s, gain, gain_out=gain.clone(), accumulate=accumulate)
     got = ops.rms_norm_backward(dy, s, gain, gain_out=gain, accumulate=accumulate)
     assert got[2] is gain and torch.equal(got[2], want[2]) and torch.equal(got[0], want[0])
+
+
+# ------------------------------------------------------------------------------------------------ several rows a group of lanes
+
+# A launch has at most 2048 blocks forward (1024 backward) of 256 threads, or of 512 where rows are read in the tensor's groups, and a row of up to
+# 512 values takes the power of two of lanes that holds a group of eight each, one of up to 1024 values 64 lanes, a longer one the block.
+LOOPS = [(70000, 40), (140000, 41), (9000, 512), (17000, 513), (9000, 1024), (2500, 1504), (2500, 1501), (2300, 3001), (4096, 512), (40000, 100)]
+
+
+def rows_at_once(width, blocks):
+    lanes = 1 if width <= 8 else 1 << ((min(width, 512) + 14) // 8 - 1).bit_length()
+    return blocks * (1 if width > 1024 else 512 // min(lanes, 64) if width % 8 else 256 // min(lanes, 64))
+
+
+@pytest.mark.parametrize("dt,st", G.TYPES)
+@pytest.mark.parametrize("rows,width", LOOPS[:8])
+def test_norm_of_more_rows_than_a_launch_takes_at_once(ops, rows, width, dt, st):
+    assert rows > rows_at_once(width, 2048)
+    G.test_rms_norm_forward(ops, rows, width, dt, st)
+
+
+@pytest.mark.parametrize("dt,st", G.TYPES)
+@pytest.mark.parametrize("rows,width", LOOPS)
+def test_gradient_of_the_norm_of_more_rows_than_a_launch_takes_at_once(ops, rows, width, dt, st):
+    """The gain's gradient is a sum over a lane's own rows, then over the others'; also in place, and added to what is there."""
+    assert rows > (rows_at_once(width, 512 if width <= 1024 else 1024))
+    G.test_rms_norm_backward(ops, rows, width, dt, st)
+
+
+@pytest.mark.parametrize("dt,st", G.TYPES)
+@pytest.mark.parametrize("rows,width,off", [(70000, 40, 1), (9000, 512, 3), (9000, 1024, 1), (2500, 1501, 5), (9000, 700, 1)])
+def test_norm_of_many_rows_from_odd_addresses(ops, rows, width, off, dt, st):
+    G.test_rms_norm_of_long_rows(ops, rows, width, off, dt, st)
