@@ -74,3 +74,59 @@ def test_gradient_of_the_norm_of_more_rows_than_a_launch_takes_at_once(ops, rows
 @pytest.mark.parametrize("rows,width,off", [(70000, 40, 1), (9000, 512, 3), (9000, 1024, 1), (2500, 1501, 5), (9000, 700, 1)])
 def test_norm_of_many_rows_from_odd_addresses(ops, rows, width, off, dt, st):
     G.test_rms_norm_of_long_rows(ops, rows, width, off, dt, st)
+
+
+# ------------------------------------------------------------------------------------------------ two channels a lane
+
+# bf16 calls of at least 1024 blocks of 128 tokens and channels: the last block column of one channel, of two, of some, full; a lane's pair
+# that is half a row; one chain, uneven sequences with empty ones and rows of none, sequences that need no chain
+PAIRS = [(65600, 129, ("period", 65600), True, True, "packed"), (65600, 129, ("ragged", 90, 70, 300), True, True, "apart"),
+         (131100, 2, ("period", 50000), False, True, "apart"), (131100, 3, ("ragged", 2000, 5, 1), True, False, "packed"),
+         (43700, 258, ("period", 64), True, True, "apart"), (43700, 300, ("period", 128), False, False, "packed"),
+         (22000, 641, ("ragged", 61, 0, 0), True, True, "packed"), (33000, 512, ("ragged", 7, 129, 0), False, True, "packed")]
+
+
+def takes_pairs(T, C):
+    return -(-T // 128) * -(-C // 128) >= 1024
+
+
+@pytest.mark.parametrize("T,C,how,gate,state,layout", PAIRS)
+def test_recurrence_of_two_channels_a_lane(ops, T, C, how, gate, state, layout):
+    assert takes_pairs(T, C)
+    G.test_recurrence(ops, T, C, how, "bf16", gate, state, layout)
+
+
+@pytest.mark.parametrize("how", ["period", "ragged"])
+def test_recurrence_of_two_channels_a_lane_keeps_what_is_not_finite(ops, how):
+    """NaN and infinities in one sequence, in its states, its gates and its gradients, in a lane's first and second channel: no other
+    sequence's results change by a bit, nor do the other channels' in that one."""
+    T, C = 65600, 129
+    assert takes_pairs(T, C)
+    g = torch.Generator(device="cuda").manual_seed(15)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    f, z, o, dy = (rnd(T, C).bfloat16() for _ in range(4))
+    off = [0, 20000, 20000, 20100, 36001, 36003, 65600] if how == "ragged" else [0, 20000, 40000, 60000, 65600]
+    n = len(off) - 1
+    kw = dict(offsets=torch.tensor(off, dtype=torch.int32, device="cuda")) if how == "ragged" else dict(period=20000)
+    h0, dfin = rnd(n, C), rnd(n, C)
+
+    def both():
+        y, fin, saved = ops.recurrence_forward(f, z, o=o, state=h0, final=True, saved=True, **kw)
+        return (y, fin) + ops.recurrence_backward(dy, f, z, saved, o=o, state=h0, dfinal=dfin, dstate=True, **kw)
+    clean = both()
+    assert all(torch.isfinite(t).all() for t in clean)
+    s = 3 if how == "ragged" else 1
+    a, b = off[s], off[s + 1]
+    nan, inf = float("nan"), float("inf")
+    f[a, 2], f[a + 5000, 5], f[b - 1, 128], z[a + 1, 8], o[b - 2, 11], dy[a + 9, 14] = [nan] * 6
+    z[a + 130, 17], h0[s, 20], dfin[s, 23], f[a + 7, 26], f[a + 8, 29] = inf, -inf, nan, inf, -inf
+    touched = torch.tensor([2, 5, 128, 8, 11, 14, 17, 20, 23, 26, 29], device="cuda")
+    got = both()
+    for p, q in zip(got, clean):
+        rows = torch.arange(p.shape[0], device="cuda")
+        own = ((rows >= a) & (rows < b) if p.shape[0] == T else rows == s)[:, None]
+        cols = torch.zeros(C, dtype=torch.bool, device="cuda").index_fill(0, touched, True)[None]
+        assert torch.equal(torch.where(own & cols, 0.0, p), torch.where(own & cols, 0.0, q))
+    assert got[0][a:a + 5000, 5].isfinite().all() and got[0][a + 5000:b, 5].isnan().all() and got[1][s, 5].isnan()
+    assert got[0][a:b, 26].isfinite().all() and got[0][a:b, 29].isfinite().all()
+    assert got[2][a:b, 23].isnan().any() and got[5][s, 23].isnan()
