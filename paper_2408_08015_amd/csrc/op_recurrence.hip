@@ -832,7 +832,7 @@ void recurrence_bwd(hipStream_t st, const ast_recurrence_cfg& c, const ast_rows&
 #define PICK(L) (o ? go(recurrence_bwd_kernel<L, true, BWD_WAVES>) : go(recurrence_bwd_kernel<L, false, BWD_WAVES>))
 #define PICK_WIDE(L) (o ? go(recurrence_bwd_kernel<L, true, 2 * BWD_WAVES>) : go(recurrence_bwd_kernel<L, false, 2 * BWD_WAVES>))
   if (c.dtype == AST_F32) wide ? PICK_WIDE(Lane32) : PICK(Lane32);
-  else if (l.pairs) wide ? PICK_WIDE(Lane16) : PICK(Lane16);
+  else if (l.pairs) PICK(Lane16);  // (wide calls, of more than 64 tokens and at most 1024 blocks of 64 tokens and channels, have fewer than 1024 of 128)
   else wide ? PICK_WIDE(Lane16One) : PICK(Lane16One);
 #undef PICK
 #undef PICK_WIDE
