@@ -449,7 +449,7 @@ void pick(hipStream_t st, const ast_distill_cfg& c, const DistillArgs& g, Exps e
   // (us of 8192 rows with 32 entries, loss, gradient, both: 1000 bf16 13, 13, 17, in blocks of 256 threads 25, 27, 33; 4096 bf16 19, 34, 37
   // and 32, 39, 43; fp32 of 2048 17, 35, 34 and 32, 39, 39, of 4096 28, 65, 64 and 36, 57, 63)
   if (v <= (sizeof(T) == 2 || MODE == LOSS ? kFewValues : kFewValues / 2) && c.entries <= kFewEntries) {
-    if constexpr (MODE != PART && MODE != JOIN_STEP) go<MODE, T, 64, MODE == STEP ? 8 : 0>(st, r, 1, g, e);
+    go<MODE, T, 64, MODE == STEP ? 8 : 0>(st, r, 1, g, e);
     return;
   }
   if constexpr (MODE == GRADIENT) {
