@@ -80,54 +80,57 @@ const char* heads_apart(const ast_qk_cfg& c, const ast_heads& h) {
   return head_inner || token_inner ? nullptr : "the heads of an output overlap";
 }
 
-// The memory of a tensor: rows of `wide` bytes, `step` bytes from one to the next, all of them in [lo, hi).  (In 128 bits: the products
-// of the sizes and strides that the calls take do not fit 64.)
-typedef unsigned __int128 Place;
+// The memory of a tensor: rows of `wide` bytes, `step` bytes from one to the next, all of them in [lo, hi).  (Products of the sizes and
+// strides that the calls take do not fit 64 bits: they are formed in 128, and hi ends with the address space.)
+typedef unsigned __int128 Wide;
 struct Area {
-  Place lo = 0, hi = 0;  // (equal: nothing, a tensor that is not there or has no rows)
-  Place step = 0, wide = 0;
-  int64_t rows = 0;
+  uint64_t lo = 0, hi = 0;  // (equal: nothing, a tensor that is not there or has no rows)
+  uint64_t rows = 0, step = 0, wide = 0;
   Area() {}
   Area(const void* p, int64_t rows_, int64_t step_, int64_t wide_) {
     if (!p || rows_ <= 0 || wide_ <= 0) return;
     lo = reinterpret_cast<uintptr_t>(p);
-    rows = rows_, step = (Place)step_, wide = (Place)wide_;
-    hi = lo + (Place)(rows - 1) * step + wide;
+    rows = (uint64_t)rows_, step = (uint64_t)step_, wide = (uint64_t)wide_;
+    hi = (uint64_t)std::min(lo + (Wide)(rows - 1) * step + wide, (Wide)UINT64_MAX);
     if (step <= wide) wide = hi - lo, rows = 1;  // (no gaps)
   }
 };
-// A byte belongs to both.  Exact, except that rows with gaps and different steps count as all that lies between their first and last.
-bool meet(const Area& a, const Area& b) {
-  if (a.lo >= b.hi || b.lo >= a.hi) return false;
+Area block_of(const void* p, size_t bytes) { return Area(p, 1, (int64_t)bytes, (int64_t)bytes); }
+// A byte belongs to both, whose ranges lie on each other.  Exact, except that rows with gaps and different steps count as all that lies
+// between their first and last.
+bool rows_meet(const Area& a, const Area& b) {
   if (a.rows == 1 && b.rows == 1) return true;
   if (a.rows == 1 || b.rows == 1) {
     const Area &one = a.rows == 1 ? a : b, &many = a.rows == 1 ? b : a;
-    const Place row = std::min((one.hi - 1 - many.lo) / many.step, (Place)(many.rows - 1));  // the last that begins in front of its end
-    return many.lo + row * many.step + many.wide > one.lo;
+    const uint64_t row = std::min((one.hi - 1 - many.lo) / many.step, many.rows - 1);  // the last that begins in front of its end
+    return many.lo + (Wide)row * many.step + many.wide > one.lo;
   }
   if (a.step != b.step) return true;
   const Area &p = a.lo <= b.lo ? a : b, &q = a.lo <= b.lo ? b : a;  // q's first row: behind p's row k, by r bytes
-  const Place k = (q.lo - p.lo) / p.step, r = (q.lo - p.lo) % p.step;
-  return (k < (Place)p.rows && r < p.wide) || (k + 1 < (Place)p.rows && p.step - r < q.wide);
+  const uint64_t k = (q.lo - p.lo) / p.step, r = (q.lo - p.lo) % p.step;
+  return (k < p.rows && r < p.wide) || (k + 1 < p.rows && p.step - r < q.wide);
 }
-
-Area block_of(const void* p, size_t bytes) { return Area(p, 1, (int64_t)bytes, (int64_t)bytes); }
+bool meet(const Area& a, const Area& b) { return a.lo < b.hi && b.lo < a.hi && rows_meet(a, b); }
 // the same rows at the same place
 bool same(const Area& a, const Area& b) {
   return a.lo == b.lo && a.hi == b.hi && a.rows == b.rows && (a.rows == 1 || (a.step == b.step && a.wide == b.wide));
 }
-typedef std::initializer_list<Area> Areas;
+struct Some {  // (a list of areas holds no copies)
+  const Area* area;
+  Some(const Area& a) : area(&a) {}
+};
+typedef std::initializer_list<Some> Areas;
 bool any_meet(Areas outputs) {
-  for (const Area* a = outputs.begin(); a != outputs.end(); ++a)
-    for (const Area* b = outputs.begin(); b != a; ++b)
-      if (meet(*a, *b)) return true;
+  for (auto a = outputs.begin(); a != outputs.end(); ++a)
+    for (auto b = outputs.begin(); b != a; ++b)
+      if (meet(*a->area, *b->area)) return true;
   return false;
 }
 // ... one of each; in_place: not counting an output that is the input
 bool any_meet(Areas outputs, Areas inputs, bool in_place = false) {
-  for (const Area& a : outputs)
-    for (const Area& b : inputs)
-      if (meet(a, b) && !(in_place && same(a, b))) return true;
+  for (const Some& a : outputs)
+    for (const Some& b : inputs)
+      if (meet(*a.area, *b.area) && !(in_place && same(*a.area, *b.area))) return true;
   return false;
 }
 const char* const kOnInput = "an output and an input overlap, and are not the same rows where that is allowed";
