@@ -128,8 +128,10 @@ __device__ __forceinline__ void store_state(float* rows, int64_t row, int c, int
     if (c + i < channels) p[(uint32_t)(c + i)] = v[i];
 }
 
-// exp(-|x|), within about 2^-22 of it for fp32 results (the rest of the product with log2 e is added behind the exponential:
-// 2^-24 of an argument of 20 would be 1e-6 of the result), with a product alone for bf16 results
+// exp(-|x|), within about 2^-22 of it for fp32 tensors (the rest of the product with log2 e is added behind the exponential:
+// 2^-24 of an argument of 20 would be 1e-6 of the result), with a product alone for bf16 ones: off by up to 1.3 |x| steps of 2^-24, 1e-6 at 12.
+// That is far below a step of their results and reaches the fp32 states only; the rest would cost 65536 x 1024 in sequences of 64 115 us
+// forward instead of 108, as one sequence 144 to 147 instead of 132 to 140, backward 232 instead of 223.
 template <bool EXACT>
 __device__ __forceinline__ float exp_neg(float x) {
   const float n = -fabsf(x), t = n * 1.44269504f;
@@ -138,7 +140,7 @@ __device__ __forceinline__ float exp_neg(float x) {
   const float rest = fmaf(n, 1.44269504f, -t) + n * 1.925963033e-8f;  // (log2 e in two parts)
   return n < -100.f ? 0.f : fmaf(e, rest * 0.69314718f, e);
 }
-// sigmoid(x) and 1 - sigmoid(x), each to its own relative precision; 0 and 1 at the infinities
+// sigmoid(x) and 1 - sigmoid(x), each to the relative precision of the exponential; 0 and 1 at the infinities
 template <bool EXACT>
 __device__ __forceinline__ void gates(float x, float& a, float& b) {
   const float e = exp_neg<EXACT>(x);
