@@ -23,8 +23,8 @@
  * call may be recorded into a HIP graph.  `workspace_dev` is the call's alone until the stream has
  * passed it: calls that may overlap in time (two streams, two graphs replayed side by side) take one
  * each.  Its contents before the call do not matter.  Outputs may not overlap each other, nor inputs or
- * the workspace except where a call allows it; rms_norm, recurrence and distill refuse it (rows of the
- * recurrence or the logits that lie between another tensor's rows overlap only if their strides differ).
+ * the workspace except where a call allows it; rms_norm, recurrence and distill refuse it (rows
+ * that lie between those of another tensor, as parts of one packed tensor do, are taken where the strides are equal).
  * Element types are AST_F32 and AST_BF16_F32ACC (bf16) of ast_dtype; sums, norms and angles are formed
  * in 32 bits or more and every result is rounded once.  Results do not depend on the order in which
  * blocks run: equal calls give equal bits.
